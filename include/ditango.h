@@ -335,7 +335,110 @@ dt_status dt_selftest_wait_timeout(dt_ctx *ctx, uint32_t limit_us, void *stream)
 dt_status dt_poll(dt_ctx *ctx);
 
 const char *dt_status_str(dt_status s);
-const char *dt_last_error(dt_ctx *ctx); /* text of the last error on this context ("" if none) */
+const char *dt_last_error(dt_ctx *ctx); /* text of the last error on this context ("" if none); NULL: of the calling
+                                           thread's last call of an operator below that failed */
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Operators around the self-attention of a transformer block: rotary positions on Q and K before it, the norm with the
+ * residual's addition that follows it and feeds the next projection in 8 bits, and the cross attention to an encoder's
+ * states (the prompt).  The paper has no counterpart; its models' blocks (Table 1) are made of them.
+ *   - No context: shapes come with the call.  The current device must be the one that owns `stream` and the buffers, and
+ *     an sm_100.  The first call on a device looks up a few facts about it; every call is ONE kernel launch, stream-ordered,
+ *     and may be captured into a graph.  Nothing is allocated, there is no workspace, and calls on different streams or
+ *     from different threads are independent.
+ *   - Results do not depend on the order in which anything ran (no atomics): the same inputs give the same bits.
+ *   - Argument errors are found before any launch; their text is dt_last_error(NULL).  A bounded device-side wait that ran
+ *     out is recorded in a status word per device that dt_poll_ops reads.
+ *   - Strides are in elements: D's is 1, those of B, L, H are positive multiples of 8 (a stride of a dimension of one entry
+ *     is not looked at, an input's batch stride may be 0); bases are 16-byte aligned.  Outputs must not overlap inputs except
+ *     where a call says so.  Values of another dtype or shape than the config's are not found out. */
+enum { DT_VALUE_BF16 = 0, DT_VALUE_FP16 = 1, DT_VALUE_FP32 = 2 };   /* the first two as DT_INPUT_* */
+
+/* Rotary positions: pair i of the first rotary_dim values of every head turns by angle_i = sum_a pos[a] * freqs[a][i],
+ *     (x, y) -> attn_factor * (x cos - y sin, y cos + x sin);
+ * pairs are (2i, 2i + 1) with DT_ROPE_INTERLEAVED and (i, i + rotary_dim / 2) with DT_ROPE_HALF; values from rotary_dim on
+ * are copied.  Several axes serve a video's grid: a pair that belongs to the height has 0 in the other axes' rows.  Angles
+ * are taken in fp64 and reduced there (positions of 10^8 are exact), the rotation is fp32, rounded once.
+ *   q, k            device [B, L, H, D] and [B, L, H_k, D]; H_k = 0: no k.  An output may be its input (same strides).
+ *   freqs_dev       device, double [axes][rotary_dim / 2], radians per position (see dt_rope_freqs)
+ *   positions_dev   device, int32, [B, L, axes] with position_strides (any, 0 included); NULL: the token's index l (one axis)
+ *   transpose       1: by the negative angle -- the gradient's rotation, and with attn_factor 1 the inverse
+ * Limits: D a multiple of 8, at most 256; rotary_dim even; 1 to 4 axes. */
+enum { DT_ROPE_INTERLEAVED = 0, DT_ROPE_HALF = 1 };
+typedef struct {
+    int32_t dtype;                     /* DT_VALUE_BF16 or DT_VALUE_FP16 */
+    int32_t B, L, H, H_k, D;
+    int32_t rotary_dim, layout, axes;
+    int32_t transpose;
+    float attn_factor;
+} dt_rope_config;
+dt_status dt_rope(const dt_rope_config *cfg, const void *q_dev, const int64_t q_strides_blhd[4], void *q_out_dev,
+                  const int64_t q_out_strides_blhd[4], const void *k_dev, const int64_t k_strides_blhd[4], void *k_out_dev,
+                  const int64_t k_out_strides_blhd[4], const double *freqs_dev, const int32_t *positions_dev,
+                  const int64_t position_strides[3], void *stream);
+
+/* Frequencies of one axis, base^(-2 i / rotary_dim) for i < rotary_dim / 2, scaled for sequences beyond the trained
+ * length, written to HOST memory; *attn_factor is what dt_rope_config wants beside them.
+ *   DT_ROPE_NONE
+ *   DT_ROPE_LINEAR  positions divided by `factor` (position interpolation)
+ *   DT_ROPE_BASE    the base raised so that the slowest pair turns `factor` times slower and the fastest as before
+ *   DT_ROPE_PARTS   YaRN: pairs that make turns_fast or more turns over trained_length positions stay, those with turns_slow
+ *                   or fewer are divided by `factor`, linear in between; attn_factor = 0.1 ln(factor) + 1 */
+enum { DT_ROPE_NONE = 0, DT_ROPE_LINEAR = 1, DT_ROPE_BASE = 2, DT_ROPE_PARTS = 3 };
+typedef struct {
+    int32_t kind;
+    double base, factor;
+    int32_t trained_length;           /* DT_ROPE_PARTS */
+    double turns_fast, turns_slow;    /* DT_ROPE_PARTS: 32 and 1 in the published form */
+} dt_rope_scaling;
+dt_status dt_rope_freqs(const dt_rope_scaling *scaling, int32_t rotary_dim, double *freqs_host, float *attn_factor);
+
+/* Norm with the residual's addition.  Per row of `width` values
+ *     h = x + residual (x alone without one),  residual_out = h,  y = h / sqrt(mean(h^2) + eps) * weight
+ * in fp32; y is made from the unrounded h.  DT_NORM_OUT_E4M3: per row, or per scale_group neighbouring values of it,
+ *     scale = max(max |y|, 2^-100) / 448,  value = e4m3(y / scale) (to nearest even, saturated)
+ * so that value * scale stands for y.
+ *   x, y            device, n0 x n1 rows, row (i, j) at i * strides[0] + j * strides[1] (multiples of 8 elements)
+ *   weight_dev      device [width], x's type or fp32; NULL: 1
+ *   residual_dev, residual_out_dev   device, as x, of x's type or fp32; both NULL: no residual.  residual_out may be
+ *                   residual or (in x's type) x, y may be x: same base and strides
+ *   scales_dev      device, fp32 [n0][n1][width / scale_group] ([n0][n1][1] for scale_group 0); unused with DT_NORM_OUT_SAME
+ * Limits: width a multiple of 8 (and of scale_group), at most 16384; y in 8 bits 8-byte aligned. */
+enum { DT_NORM_OUT_SAME = 0, DT_NORM_OUT_E4M3 = 1 };
+typedef struct {
+    int32_t dtype, weight_dtype, residual_dtype, out_kind;   /* DT_VALUE_* (x: bf16 or fp16), DT_NORM_OUT_* */
+    int64_t n0, n1;
+    int32_t width;
+    int32_t scale_group;              /* 0 (one scale per row), 32, 64 or 128 */
+    int64_t x_strides[2], residual_strides[2], residual_out_strides[2], y_strides[2];
+    float eps;
+} dt_norm_config;
+dt_status dt_add_rmsnorm(const dt_norm_config *cfg, const void *x_dev, const void *weight_dev, const void *residual_dev,
+                         void *residual_out_dev, void *y_dev, float *scales_dev, void *stream);
+
+/* Cross attention: every query row against the keys that count, j < key_lens[b] and key_mask[b][j] != 0:
+ *     LSE = log sum_j exp(softmax_scale * q.k_j),  OUT = sum_j exp(softmax_scale * q.k_j - LSE) v_j
+ * -- a state (Eq. 1), so it composes with others by Eq. 2.  A row without keys has OUT = 0 and LSE = -inf.  What stands in
+ * K and V at keys that do not count (NaN and infinities too) has no effect.
+ *   q, out          device [B, Lq, H, D]; out may be q (same strides)
+ *   k, v            device [B, Lk, H_kv, D], strides of their own; query head h reads key head h / (H / H_kv)
+ *   key_lens_dev    device, int32 [B] (values outside [0, Lk] are clamped), or NULL: Lk
+ *   key_mask_dev    device, uint8 rows of Lk, key_mask_stride bytes apart (0: one row for all), or NULL
+ *   lse_out_dev     device, fp32 [B, H, Lq], or NULL
+ * Limits: D in {64, 128}; B * H <= 65535; Lq, Lk from 0 (Lq = 0: nothing to do; Lk = 0: rows without keys). */
+typedef struct {
+    int32_t dtype;                    /* DT_VALUE_BF16 or DT_VALUE_FP16 */
+    int32_t B, Lq, Lk, H, H_kv, D;
+    float softmax_scale;
+} dt_cross_config;
+dt_status dt_cross_attn(const dt_cross_config *cfg, const void *q_dev, const int64_t q_strides_blhd[4], const void *k_dev,
+                        const int64_t k_strides_blhd[4], const void *v_dev, const int64_t v_strides_blhd[4],
+                        const int32_t *key_lens_dev, const uint8_t *key_mask_dev, int64_t key_mask_stride, void *out_dev,
+                        const int64_t out_strides_blhd[4], float *lse_out_dev, void *stream);
+
+/* Read (and clear) the current device's status word of the operators above; synchronises the device.  DT_OK or
+ * DT_ERR_TIMEOUT. */
+dt_status dt_poll_ops(void);
 
 #ifdef __cplusplus
 }

@@ -18,6 +18,10 @@ DT_OK, DT_ERR_INVALID_ARG, DT_ERR_UNSUPPORTED, DT_ERR_STATE, DT_ERR_CUDA, DT_ERR
 DT_STATE_FP32, DT_STATE_BF16 = 0, 1
 DT_INPUT_BF16, DT_INPUT_FP16 = 0, 1
 DT_MAX_P = 32
+DT_VALUE_BF16, DT_VALUE_FP16, DT_VALUE_FP32 = 0, 1, 2
+DT_ROPE_INTERLEAVED, DT_ROPE_HALF = 0, 1
+DT_ROPE_NONE, DT_ROPE_LINEAR, DT_ROPE_BASE, DT_ROPE_PARTS = range(4)
+DT_NORM_OUT_SAME, DT_NORM_OUT_E4M3 = 0, 1
 
 EXPORTS = [
     "dt_create", "dt_destroy", "dt_cache_bytes", "dt_bind_cache", "dt_attn_states", "dt_attn_local", "dt_state_merge",
@@ -26,6 +30,7 @@ EXPORTS = [
     "dt_launch_count", "dt_selftest_wait_timeout", "dt_poll", "dt_status_str", "dt_last_error",
     "dt_attn_fused", "dt_num_slots", "dt_slot_ranges", "dt_group_compose", "dt_group_fit", "dt_group_reset",
     "dt_plan_sums", "dt_plan_from_sums",
+    "dt_rope", "dt_rope_freqs", "dt_add_rmsnorm", "dt_cross_attn", "dt_poll_ops",
 ]
 
 
@@ -39,6 +44,27 @@ class dt_config(C.Structure):
 class dt_planner_config(C.Structure):
     _fields_ = [("group_size", C.c_int32), ("eps_initial", C.c_double), ("eps_local", C.c_double),
                 ("cache_ratio", C.c_double)]
+
+
+class dt_rope_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "B", "L", "H", "H_k", "D", "rotary_dim", "layout", "axes", "transpose")] + [
+        ("attn_factor", C.c_float)]
+
+
+class dt_rope_scaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("base", C.c_double), ("factor", C.c_double), ("trained_length", C.c_int32),
+                ("turns_fast", C.c_double), ("turns_slow", C.c_double)]
+
+
+class dt_norm_config(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("weight_dtype", C.c_int32), ("residual_dtype", C.c_int32), ("out_kind", C.c_int32),
+                ("n0", C.c_int64), ("n1", C.c_int64), ("width", C.c_int32), ("scale_group", C.c_int32),
+                ("x_strides", C.c_int64 * 2), ("residual_strides", C.c_int64 * 2), ("residual_out_strides", C.c_int64 * 2),
+                ("y_strides", C.c_int64 * 2), ("eps", C.c_float)]
+
+
+class dt_cross_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "B", "Lq", "Lk", "H", "H_kv", "D")] + [("softmax_scale", C.c_float)]
 
 
 class DitangoError(RuntimeError):
@@ -95,6 +121,11 @@ def lib():
         "dt_group_compose": (C.c_int, [vp, vp]),
         "dt_group_fit": (C.c_int, [vp, C.c_size_t, i32p, vp]),
         "dt_group_reset": (C.c_int, [vp, vp]),
+        "dt_rope": (C.c_int, [C.POINTER(dt_rope_config), vp, i64p, vp, i64p, vp, i64p, vp, i64p, vp, vp, i64p, vp]),
+        "dt_rope_freqs": (C.c_int, [C.POINTER(dt_rope_scaling), C.c_int32, vp, C.POINTER(C.c_float)]),
+        "dt_add_rmsnorm": (C.c_int, [C.POINTER(dt_norm_config), vp, vp, vp, vp, vp, vp, vp]),
+        "dt_cross_attn": (C.c_int, [C.POINTER(dt_cross_config), vp, i64p, vp, i64p, vp, i64p, vp, vp, C.c_int64, vp, i64p, vp, vp]),
+        "dt_poll_ops": (C.c_int, []),
         "dt_status_str": (C.c_char_p, [C.c_int]),
         "dt_last_error": (C.c_char_p, [vp]),
     }
@@ -166,6 +197,170 @@ def dt_plan_static(lse_state, offsets, B, H, L, mask_dev, eps=0.0, target_fracti
         detail = ("problem exceeds the built-in scratch of %d partial sums" % STATIC_PLAN_MAX_PARTIALS
                   if s == DT_ERR_UNSUPPORTED else "dt_plan_static")
         raise DitangoError(s, status_str(s), detail)
+
+
+# ---------------------------------------------------------------- operators around the self-attention (no context)
+_VALUE = {torch.bfloat16: DT_VALUE_BF16, torch.float16: DT_VALUE_FP16, torch.float32: DT_VALUE_FP32}
+_STRIDES4 = C.c_int64 * 4
+
+
+def _op_call(fn, device, stream, *args):
+    """One call on `device` (made current for it): the stream's pointer goes last, a status other than DT_OK raises."""
+    if torch.cuda.current_device() != device.index:
+        with torch.cuda.device(device):
+            s = fn(*args, (stream or torch.cuda.current_stream()).cuda_stream)
+    else:
+        s = fn(*args, (stream or torch.cuda.current_stream()).cuda_stream)
+    if s != DT_OK:
+        raise DitangoError(s, status_str(s), lib().dt_last_error(None).decode())
+
+
+def dt_rope(q, k, q_out, k_out, freqs, positions=None, layout=DT_ROPE_INTERLEAVED, attn_factor=1.0, transpose=False, stream=None):
+    """Rotary positions on q [B, L, H, D] and k [B, L, H_k, D] (k may be None) into q_out, k_out (which may be q, k).
+    `freqs` is float64 [axes, rotary_dim / 2] on the device, `positions` int32 [B, L, axes] ([B, L] for one axis; any
+    strides, expanded batches too) or None for the token's index."""
+    B, L, H, D = q.shape
+    dev = q.device
+    assert q.is_cuda and q_out.shape == q.shape and q_out.dtype == q.dtype and q_out.device == dev
+    assert freqs.dtype == torch.float64 and freqs.dim() == 2 and freqs.is_contiguous() and freqs.device == dev
+    Hk, ks, kos, kp, kop = 0, None, None, None, None
+    if k is not None:
+        Hk = k.shape[2]
+        assert k.shape == (B, L, Hk, D) and k_out.shape == k.shape and k.dtype == k_out.dtype == q.dtype
+        assert k.device == dev and k_out.device == dev
+        ks, kos, kp, kop = _STRIDES4(*k.stride()), _STRIDES4(*k_out.stride()), k.data_ptr(), k_out.data_ptr()
+    axes, pairs = freqs.shape
+    pp = ps = None
+    if positions is not None:
+        assert positions.dtype == torch.int32 and positions.device == dev
+        assert positions.shape == (B, L, axes) or (axes == 1 and positions.shape == (B, L))
+        pp, ps = positions.data_ptr(), (C.c_int64 * 3)(*positions.stride()) if positions.dim() == 3 else (C.c_int64 * 3)(*positions.stride(), 0)
+    cfg = dt_rope_config(_VALUE[q.dtype], B, L, H, Hk, D, 2 * pairs, layout, axes, 1 if transpose else 0, attn_factor)
+    _op_call(lib().dt_rope, dev, stream, cfg, q.data_ptr(), _STRIDES4(*q.stride()), q_out.data_ptr(), _STRIDES4(*q_out.stride()),
+             kp, ks, kop, kos, freqs.data_ptr(), pp, ps)
+
+
+def dt_rope_freqs(rotary_dim, base=10000.0, kind=DT_ROPE_NONE, factor=1.0, trained_length=0, turns_fast=32.0, turns_slow=1.0):
+    """(float64 [rotary_dim / 2] on the host, attn_factor): the frequencies of one axis, scaled for long contexts."""
+    f = torch.empty(max(rotary_dim, 2) // 2, dtype=torch.float64)
+    m = C.c_float()
+    sc = dt_rope_scaling(kind, base, factor, trained_length, turns_fast, turns_slow)
+    s = lib().dt_rope_freqs(C.byref(sc), rotary_dim, f.data_ptr(), C.byref(m))
+    if s != DT_OK:
+        raise DitangoError(s, status_str(s), lib().dt_last_error(None).decode())
+    return f, m.value
+
+
+def dt_rope_grid_freqs(dims, base=10000.0):
+    """float64 [axes, sum(dims) / 2] on the host: a grid's axes share out a head's pairs, dims[a] values each (e.g. time,
+    height and width: 44, 42, 42 of 128)."""
+    table = torch.zeros((len(dims), sum(dims) // 2), dtype=torch.float64)
+    at = 0
+    for a, d in enumerate(dims):
+        table[a, at:at + d // 2] = dt_rope_freqs(d, base)[0]
+        at += d // 2
+    return table
+
+
+def _rows(t):
+    """(n0, n1, (stride0, stride1)) of the rows of t [..., width], whose leading dimensions have to collapse into two."""
+    dims = [(n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n != 1]
+    out = []
+    for n, s in dims:
+        if out and out[-1][1] == n * s:
+            out[-1] = (out[-1][0] * n, s)
+        else:
+            out.append((n, s))
+    assert len(out) <= 2 and (t.stride(-1) == 1 or t.shape[-1] == 1), "rows must have two strides at most, values stride 1"
+    out = [(1, 0)] * (2 - len(out)) + out
+    return out
+
+
+def _norm_rows(tensors):
+    """The rows of several tensors of one shape as one n0 x n1 and strides for each."""
+    if all(t.is_contiguous() for t in tensors):
+        w = tensors[0].shape[-1]
+        n = tensors[0].numel() // w if w else 0
+        return 1, n, [(0, w)] * len(tensors)
+    rows = [_rows(t) for t in tensors]
+    # a tensor whose rows collapse further than another's is split the same way
+    n0, n1 = next(((a[0], b[0]) for a, b in rows if a[0] != 1), (rows[0][0][0], rows[0][1][0]))
+    strides = []
+    for a, b in rows:
+        if (a[0], b[0]) == (n0, n1):
+            strides.append((a[1], b[1]))
+        else:
+            assert a[0] == 1 and b[0] == n0 * n1, "the tensors' rows do not have common strides"
+            strides.append((n1 * b[1], b[1]))
+    return n0, n1, strides
+
+
+def dt_add_rmsnorm(x, weight, y, eps, residual=None, residual_out=None, scales=None, stream=None):
+    """Norm of x (+ residual) over the last dimension into y: x's type, or float8_e4m3fn with `scales` fp32
+    [..., width / group] (group: 32, 64, 128 or the whole row).  residual_out takes the sum; it may be residual or x."""
+    w = x.shape[-1]
+    dev = x.device
+    q8 = y.dtype == torch.float8_e4m3fn
+    assert x.is_cuda and y.shape == x.shape and (q8 or y.dtype == x.dtype) and y.device == dev
+    assert (residual is None) == (residual_out is None)
+    tensors = [x, y]
+    rt = x.dtype
+    if residual is not None:
+        rt = residual.dtype
+        assert residual.shape == x.shape and residual_out.shape == x.shape and residual_out.dtype == rt
+        assert residual.device == dev and residual_out.device == dev
+        tensors += [residual, residual_out]
+    wt = x.dtype
+    if weight is not None:
+        wt = weight.dtype
+        assert weight.shape == (w,) and weight.device == dev and weight.is_contiguous()
+    group = 0
+    if q8:
+        per_row = scales.shape[-1]
+        assert scales.dtype == torch.float32 and scales.is_contiguous() and scales.device == dev
+        assert scales.shape[:-1] == x.shape[:-1] and per_row > 0 and w % per_row == 0
+        group = 0 if per_row == 1 else w // per_row
+    n0, n1, st = _norm_rows(tensors)
+    st += [(0, 0)] * (4 - len(st))
+    pair = C.c_int64 * 2
+    cfg = dt_norm_config(_VALUE[x.dtype], _VALUE[wt], _VALUE[rt], DT_NORM_OUT_E4M3 if q8 else DT_NORM_OUT_SAME, n0, n1, w, group,
+                         pair(*st[0]), pair(*st[2]), pair(*st[3]), pair(*st[1]), eps)
+    _op_call(lib().dt_add_rmsnorm, dev, stream, cfg, x.data_ptr(), None if weight is None else weight.data_ptr(),
+             None if residual is None else residual.data_ptr(), None if residual is None else residual_out.data_ptr(),
+             y.data_ptr(), scales.data_ptr() if q8 else None)
+
+
+def dt_cross_attn(q, k, v, out, softmax_scale, key_lens=None, key_mask=None, lse_out=None, stream=None):
+    """Attention of q [B, Lq, H, D] to an encoder's k, v [B, Lk, H_kv, D]; key_lens int32 [B], key_mask uint8 or bool
+    [B, Lk] (expanded batches too), lse_out fp32 [B, H, Lq]."""
+    B, Lq, H, D = q.shape
+    Lk, Hkv = k.shape[1], k.shape[2]
+    dev = q.device
+    assert q.is_cuda and k.shape == v.shape == (B, Lk, Hkv, D) and out.shape == q.shape
+    assert k.dtype == v.dtype == out.dtype == q.dtype and k.device == v.device == out.device == dev
+    lp = mp = op = None
+    ms = 0
+    if key_lens is not None:
+        assert key_lens.dtype == torch.int32 and key_lens.shape == (B,) and key_lens.is_contiguous() and key_lens.device == dev
+        lp = key_lens.data_ptr()
+    if key_mask is not None:
+        assert key_mask.dtype in (torch.uint8, torch.bool) and key_mask.shape == (B, Lk) and key_mask.device == dev
+        assert Lk <= 1 or key_mask.stride(1) == 1
+        mp, ms = key_mask.data_ptr(), key_mask.stride(0)
+    if lse_out is not None:
+        assert lse_out.dtype == torch.float32 and lse_out.shape == (B, H, Lq) and lse_out.is_contiguous() and lse_out.device == dev
+        op = lse_out.data_ptr()
+    cfg = dt_cross_config(_VALUE[q.dtype], B, Lq, Lk, H, Hkv, D, softmax_scale)
+    _op_call(lib().dt_cross_attn, dev, stream, cfg, q.data_ptr(), _STRIDES4(*q.stride()), k.data_ptr(), _STRIDES4(*k.stride()),
+             v.data_ptr(), _STRIDES4(*v.stride()), lp, mp, ms, out.data_ptr(), _STRIDES4(*out.stride()), op)
+
+
+def dt_poll_ops(device=None):
+    """Raises DitangoError if an operator recorded a condition on the (current) device; synchronises it."""
+    with torch.cuda.device(device):
+        s = lib().dt_poll_ops()
+    if s != DT_OK:
+        raise DitangoError(s, status_str(s), lib().dt_last_error(None).decode())
 
 
 class Context:

@@ -15,8 +15,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libditango.so")
-SOURCES = ["api.cu", "attn_states.cu", "state_merge.cu", "plan.cu", "planner.cu"]
-HEADERS = ["dt_internal.h", "ptx_sm100.cuh", os.path.join("..", "..", "include", "ditango.h")]
+SOURCES = ["api.cu", "attn_states.cu", "state_merge.cu", "plan.cu", "planner.cu", "ops_api.cu", "rope.cu", "add_rmsnorm.cu",
+           "cross_attn.cu"]
+HEADERS = ["dt_internal.h", "ops.h", "ptx_sm100.cuh", os.path.join("..", "..", "include", "ditango.h")]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 
@@ -33,7 +34,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [NVCC, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
            "-shared", "-Xcompiler", "-fPIC", 
-           "--threads", "4", "-o", tmp]
+           "--threads", "8", "-o", tmp]
     if verbose:
         cmd += ["-Xptxas", "-v"]
     cmd += [os.path.join(CSRC, f) for f in SOURCES]

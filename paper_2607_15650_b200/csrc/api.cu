@@ -8,6 +8,7 @@
 #include <new>
 
 #include "dt_internal.h"
+#include "ops.h"
 
 namespace {
 
@@ -139,7 +140,7 @@ const char *dt_status_str(dt_status s) {
     return "DT_ERR_UNKNOWN";
 }
 
-const char *dt_last_error(dt_ctx *ctx) { return ctx ? ctx->err.c_str() : ""; }
+const char *dt_last_error(dt_ctx *ctx) { return ctx ? ctx->err.c_str() : dt::ops_last_error(); }
 
 dt_status dt_cache_bytes(const dt_config *cfg, size_t *o_bytes, size_t *lse_bytes) {
     const char *why;

@@ -1,0 +1,28 @@
+// Internal declarations of the operators around the self-attention (rotary positions, norm, cross attention): they take
+// no context, so what they share -- error text, per-device facts, argument checks -- is here.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/ditango.h"
+
+namespace dt {
+
+// What the operators need to know of the current device, looked up on the first call on it.
+struct OpsDevice {
+    int sms;
+    int32_t *status;      // device status word of the operators (dt_poll_ops)
+    void *encode_tiled;   // cuTensorMapEncodeTiled
+};
+
+dt_status ops_fail(dt_status s, const char *what);                 // keeps the text for dt_last_error(NULL)
+dt_status ops_fail_cuda(cudaError_t e, const char *where);
+dt_status ops_device(const OpsDevice **out);
+const char *ops_last_error();
+
+// B, L, H, D strides in elements: D's is 1, the others are multiples of 8 (a stride of a dimension of one entry is not
+// looked at), the base is 16-byte aligned.  Inputs may repeat (stride 0) along the batch; outputs may not.
+dt_status check_blhd(const char *name, const void *base, const int64_t *s, int B, int L, int H, bool output);
+
+}  // namespace dt

@@ -1,0 +1,91 @@
+// What the context-free operators share: error text, facts about the current device, argument checks.
+#include <atomic>
+#include <cstdio>
+#include <cstring>
+
+#include "dt_internal.h"
+#include "ops.h"
+
+namespace dt {
+namespace {
+
+thread_local char g_error[192] = "";
+__device__ int32_t g_status;   // conditions only the device can see; zero at load time, cleared by dt_poll_ops
+
+constexpr int MAX_DEVICES = 64;
+OpsDevice g_devices[MAX_DEVICES];
+std::atomic<int> g_ready[MAX_DEVICES];
+
+}  // namespace
+
+dt_status ops_fail(dt_status s, const char *what) {
+    snprintf(g_error, sizeof g_error, "%s", what);
+    return s;
+}
+
+dt_status ops_fail_cuda(cudaError_t e, const char *where) {
+    snprintf(g_error, sizeof g_error, "%s: %s", where, cudaGetErrorString(e));
+    return DT_ERR_CUDA;
+}
+
+const char *ops_last_error() { return g_error; }
+
+dt_status ops_device(const OpsDevice **out) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return ops_fail_cuda(e, "cudaGetDevice");
+    if (dev < 0 || dev >= MAX_DEVICES) return ops_fail(DT_ERR_UNSUPPORTED, "device ordinal beyond 63");
+    if (!g_ready[dev].load(std::memory_order_acquire)) {
+        OpsDevice d = {};
+        int major = 0;
+        if ((e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev)) != cudaSuccess ||
+            (e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess)
+            return ops_fail_cuda(e, "device attributes");
+        if (major != 10) return ops_fail(DT_ERR_UNSUPPORTED, "the kernels are built for sm_100 only");
+        void *word = nullptr;
+        if ((e = cudaGetSymbolAddress(&word, g_status)) != cudaSuccess) return ops_fail_cuda(e, "status word");
+        d.status = static_cast<int32_t *>(word);
+        cudaDriverEntryPointQueryResult qres;
+        e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &d.encode_tiled, cudaEnableDefault, &qres);
+        if (e != cudaSuccess) return ops_fail_cuda(e, "cuTensorMapEncodeTiled");
+        if (qres != cudaDriverEntryPointSuccess || !d.encode_tiled) return ops_fail(DT_ERR_CUDA, "cuTensorMapEncodeTiled not found");
+        // two threads may get here at once: both write the same facts
+        g_devices[dev] = d;
+        g_ready[dev].store(1, std::memory_order_release);
+    }
+    *out = &g_devices[dev];
+    return DT_OK;
+}
+
+dt_status check_blhd(const char *name, const void *base, const int64_t *s, int B, int L, int H, bool output) {
+    char text[128];
+    const char *why = nullptr;
+    const int n[3] = {B, L, H};
+    if (!base || !s) why = "null pointer or strides";
+    else if (s[3] != 1) why = "stride of D must be 1";
+    else if ((reinterpret_cast<uintptr_t>(base) & 15u) != 0) why = "base must be 16-byte aligned";
+    else
+        for (int d = 0; d < 3 && !why; ++d) {
+            if (n[d] <= 1) continue;
+            const bool repeats = d == 0 && s[d] == 0 && !output;
+            if (!repeats && (s[d] <= 0 || s[d] % 8 != 0)) why = "strides of B, L, H must be positive multiples of 8 elements";
+        }
+    if (!why) return DT_OK;
+    snprintf(text, sizeof text, "%s: %s", name, why);
+    return ops_fail(DT_ERR_INVALID_ARG, text);
+}
+
+}  // namespace dt
+
+extern "C" dt_status dt_poll_ops(void) {
+    const dt::OpsDevice *dev;
+    dt_status s = dt::ops_device(&dev);
+    if (s != DT_OK) return s;
+    int32_t word = 0;
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpy(&word, dev->status, sizeof word, cudaMemcpyDeviceToHost);
+    if (e == cudaSuccess && word) e = cudaMemset(dev->status, 0, sizeof word);
+    if (e != cudaSuccess) return dt::ops_fail_cuda(e, "dt_poll_ops");
+    if (word & dt::STATUS_WAIT_TIMEOUT) return dt::ops_fail(DT_ERR_TIMEOUT, "a bounded device-side wait expired");
+    return DT_OK;
+}
