@@ -16,8 +16,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libditango.so")
 SOURCES = ["api.cu", "attn_states.cu", "state_merge.cu", "plan.cu", "planner.cu", "ops_api.cu", "rope.cu", "add_rmsnorm.cu",
-           "cross_attn.cu"]
-HEADERS = ["dt_internal.h", "ops.h", "ptx_sm100.cuh", os.path.join("..", "..", "include", "ditango.h")]
+           "cross_attn.cu", "cross_tiles.cu"]
+HEADERS = ["dt_internal.h", "ops.h", "cross_attn.h", "ptx_sm100.cuh", os.path.join("..", "..", "include", "ditango.h")]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 

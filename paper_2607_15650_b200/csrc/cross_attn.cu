@@ -16,31 +16,10 @@
 
 #include <cmath>
 
-#include "dt_internal.h"
-#include "ops.h"
-#include "ptx_sm100.cuh"
+#include "cross_attn.h"
 
 namespace dt {
 namespace {
-
-constexpr float LN2 = 0.69314718055994530942f, LOG2E = 1.44269504088896340736f;
-
-struct CrossParams {
-    const uint16_t *q, *k, *v;
-    uint16_t *out;
-    float *lse;                      // [B][H][Lq] or null
-    const int32_t *key_lens;         // [B] or null
-    const uint8_t *key_mask;         // [B] rows of Lk bytes, mask_stride apart, or null
-    long long mask_stride;
-    long long qs[3], ks[3], vs[3], os[3];   // B, L, H strides in elements
-    int B, Lq, Lk, H, Hkv, rep;
-    float scale_log2;
-    int32_t *status;
-};
-
-__device__ __forceinline__ int keys_of(const CrossParams &p, int b) {
-    return p.key_lens ? min(max(__ldg(p.key_lens + b), 0), p.Lk) : p.Lk;
-}
 
 // ------------------------------------------------------------------------------------------------ few rows
 constexpr int FEW_WARPS = 4, FEW_THREADS = FEW_WARPS * 32, FEW_ROWS = 16, FEW_KEYS = 16;
@@ -368,7 +347,10 @@ extern "C" dt_status dt_cross_attn(const dt_cross_config *cfg, const void *q_dev
     p.status = dev->status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool fp16 = c.dtype == DT_VALUE_FP16;
-    cudaError_t e = c.D == 64 ? (fp16 ? launch_few<64, true>(p, dev->sms, st) : launch_few<64, false>(p, dev->sms, st))
-                              : (fp16 ? launch_few<128, true>(p, dev->sms, st) : launch_few<128, false>(p, dev->sms, st));
+    // few rows per key head: K and V are read once whatever the rows; many: the tensor-memory tiles
+    cudaError_t e;
+    if (c.Lk > 0 && (long long)c.Lq * p.rep > 64) e = launch_cross_tiles(p, c.D, fp16, *dev, st);
+    else e = c.D == 64 ? (fp16 ? launch_few<64, true>(p, dev->sms, st) : launch_few<64, false>(p, dev->sms, st))
+                       : (fp16 ? launch_few<128, true>(p, dev->sms, st) : launch_few<128, false>(p, dev->sms, st));
     return e == cudaSuccess ? DT_OK : ops_fail_cuda(e, "cross-attention launch");
 }
