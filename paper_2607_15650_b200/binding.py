@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 import torch
@@ -121,10 +122,10 @@ def lib():
         "dt_group_compose": (C.c_int, [vp, vp]),
         "dt_group_fit": (C.c_int, [vp, C.c_size_t, i32p, vp]),
         "dt_group_reset": (C.c_int, [vp, vp]),
-        "dt_rope": (C.c_int, [C.POINTER(dt_rope_config), vp, i64p, vp, i64p, vp, i64p, vp, i64p, vp, vp, i64p, vp]),
+        "dt_rope": (C.c_int, [vp] * 13),
         "dt_rope_freqs": (C.c_int, [C.POINTER(dt_rope_scaling), C.c_int32, vp, C.POINTER(C.c_float)]),
-        "dt_add_rmsnorm": (C.c_int, [C.POINTER(dt_norm_config), vp, vp, vp, vp, vp, vp, vp]),
-        "dt_cross_attn": (C.c_int, [C.POINTER(dt_cross_config), vp, i64p, vp, i64p, vp, i64p, vp, vp, C.c_int64, vp, i64p, vp, vp]),
+        "dt_add_rmsnorm": (C.c_int, [vp] * 8),
+        "dt_cross_attn": (C.c_int, [vp] * 9 + [C.c_int64] + [vp] * 4),
         "dt_poll_ops": (C.c_int, []),
         "dt_status_str": (C.c_char_p, [C.c_int]),
         "dt_last_error": (C.c_char_p, [vp]),
@@ -200,17 +201,24 @@ def dt_plan_static(lse_state, offsets, B, H, L, mask_dev, eps=0.0, target_fracti
 
 
 # ---------------------------------------------------------------- operators around the self-attention (no context)
+# A call on small tensors takes as long as its marshalling: configs and strides are packed as the C structs' bytes in one
+# call each (struct.pack; the layouts are the structures' above) and a tensor's device is compared by its index.
 _VALUE = {torch.bfloat16: DT_VALUE_BF16, torch.float16: DT_VALUE_FP16, torch.float32: DT_VALUE_FP32}
-_STRIDES4 = C.c_int64 * 4
+_S3, _S4 = struct.Struct("3q").pack, struct.Struct("4q").pack
+_ROPE_CFG, _NORM_CFG, _CROSS_CFG = struct.Struct("10if").pack, struct.Struct("4i2q2i8qf4x").pack, struct.Struct("7if").pack
 
 
-def _op_call(fn, device, stream, *args):
-    """One call on `device` (made current for it): the stream's pointer goes last, a status other than DT_OK raises."""
-    if torch.cuda.current_device() != device.index:
-        with torch.cuda.device(device):
-            s = fn(*args, (stream or torch.cuda.current_stream()).cuda_stream)
+def _on_device(index, fn, args, stream):
+    """One call with the tensors' device current: the stream's pointer goes last, a status other than DT_OK raises."""
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(index)
     else:
-        s = fn(*args, (stream or torch.cuda.current_stream()).cuda_stream)
+        stream = stream.cuda_stream
+    if torch._C._cuda_getDevice() == index:
+        s = fn(*args, stream)
+    else:
+        with torch.cuda.device(index):
+            s = fn(*args, stream)
     if s != DT_OK:
         raise DitangoError(s, status_str(s), lib().dt_last_error(None).decode())
 
@@ -219,25 +227,30 @@ def dt_rope(q, k, q_out, k_out, freqs, positions=None, layout=DT_ROPE_INTERLEAVE
     """Rotary positions on q [B, L, H, D] and k [B, L, H_k, D] (k may be None) into q_out, k_out (which may be q, k).
     `freqs` is float64 [axes, rotary_dim / 2] on the device, `positions` int32 [B, L, axes] ([B, L] for one axis; any
     strides, expanded batches too) or None for the token's index."""
-    B, L, H, D = q.shape
-    dev = q.device
-    assert q.is_cuda and q_out.shape == q.shape and q_out.dtype == q.dtype and q_out.device == dev
-    assert freqs.dtype == torch.float64 and freqs.dim() == 2 and freqs.is_contiguous() and freqs.device == dev
+    shape, dtype, dev = q.shape, q.dtype, q.get_device()
+    B, L, H, D = shape
+    axes, pairs = freqs.shape
+    assert dev >= 0 and q_out.shape == shape and q_out.dtype is dtype and q_out.get_device() == dev
+    assert freqs.dtype is torch.float64 and freqs.is_contiguous() and freqs.get_device() == dev
     Hk, ks, kos, kp, kop = 0, None, None, None, None
     if k is not None:
         Hk = k.shape[2]
-        assert k.shape == (B, L, Hk, D) and k_out.shape == k.shape and k.dtype == k_out.dtype == q.dtype
-        assert k.device == dev and k_out.device == dev
-        ks, kos, kp, kop = _STRIDES4(*k.stride()), _STRIDES4(*k_out.stride()), k.data_ptr(), k_out.data_ptr()
-    axes, pairs = freqs.shape
+        assert k.shape == (B, L, Hk, D) and k_out.shape == k.shape and k.dtype is dtype and k_out.dtype is dtype
+        assert k.get_device() == dev and k_out.get_device() == dev
+        ks, kos, kp, kop = _S4(*k.stride()), _S4(*k_out.stride()), k.data_ptr(), k_out.data_ptr()
     pp = ps = None
     if positions is not None:
-        assert positions.dtype == torch.int32 and positions.device == dev
-        assert positions.shape == (B, L, axes) or (axes == 1 and positions.shape == (B, L))
-        pp, ps = positions.data_ptr(), (C.c_int64 * 3)(*positions.stride()) if positions.dim() == 3 else (C.c_int64 * 3)(*positions.stride(), 0)
-    cfg = dt_rope_config(_VALUE[q.dtype], B, L, H, Hk, D, 2 * pairs, layout, axes, 1 if transpose else 0, attn_factor)
-    _op_call(lib().dt_rope, dev, stream, cfg, q.data_ptr(), _STRIDES4(*q.stride()), q_out.data_ptr(), _STRIDES4(*q_out.stride()),
-             kp, ks, kop, kos, freqs.data_ptr(), pp, ps)
+        assert positions.dtype is torch.int32 and positions.get_device() == dev
+        if positions.dim() == 3:
+            assert positions.shape == (B, L, axes)
+            ps = _S3(*positions.stride())
+        else:
+            assert axes == 1 and positions.shape == (B, L)
+            ps = _S3(*positions.stride(), 0)
+        pp = positions.data_ptr()
+    cfg = _ROPE_CFG(_VALUE[dtype], B, L, H, Hk, D, 2 * pairs, layout, axes, 1 if transpose else 0, attn_factor)
+    _on_device(dev, (_lib or lib()).dt_rope, (cfg, q.data_ptr(), _S4(*q.stride()), q_out.data_ptr(), _S4(*q_out.stride()), kp, ks, kop, kos,
+                                    freqs.data_ptr(), pp, ps), stream)
 
 
 def dt_rope_freqs(rotary_dim, base=10000.0, kind=DT_ROPE_NONE, factor=1.0, trained_length=0, turns_fast=32.0, turns_slow=1.0):
@@ -298,61 +311,62 @@ def _norm_rows(tensors):
 def dt_add_rmsnorm(x, weight, y, eps, residual=None, residual_out=None, scales=None, stream=None):
     """Norm of x (+ residual) over the last dimension into y: x's type, or float8_e4m3fn with `scales` fp32
     [..., width / group] (group: 32, 64, 128 or the whole row).  residual_out takes the sum; it may be residual or x."""
-    w = x.shape[-1]
-    dev = x.device
-    q8 = y.dtype == torch.float8_e4m3fn
-    assert x.is_cuda and y.shape == x.shape and (q8 or y.dtype == x.dtype) and y.device == dev
-    assert (residual is None) == (residual_out is None)
-    tensors = [x, y]
-    rt = x.dtype
+    shape, dtype, dev = x.shape, x.dtype, x.get_device()
+    w = shape[-1]
+    q8 = y.dtype is torch.float8_e4m3fn
+    assert dev >= 0 and y.shape == shape and (q8 or y.dtype is dtype) and y.get_device() == dev
+    rt, rp, rop = dtype, None, None
+    tensors = (x, y)
     if residual is not None:
         rt = residual.dtype
-        assert residual.shape == x.shape and residual_out.shape == x.shape and residual_out.dtype == rt
-        assert residual.device == dev and residual_out.device == dev
-        tensors += [residual, residual_out]
-    wt = x.dtype
+        assert residual.shape == shape and residual_out.shape == shape and residual_out.dtype is rt
+        assert residual.get_device() == dev and residual_out.get_device() == dev
+        tensors = (x, y, residual, residual_out)
+        rp, rop = residual.data_ptr(), residual_out.data_ptr()
+    else:
+        assert residual_out is None
+    wt, wp = dtype, None
     if weight is not None:
-        wt = weight.dtype
-        assert weight.shape == (w,) and weight.device == dev and weight.is_contiguous()
-    group = 0
+        wt, wp = weight.dtype, weight.data_ptr()
+        assert weight.shape == (w,) and weight.get_device() == dev and weight.is_contiguous()
+    group, sp = 0, None
     if q8:
         per_row = scales.shape[-1]
-        assert scales.dtype == torch.float32 and scales.is_contiguous() and scales.device == dev
-        assert scales.shape[:-1] == x.shape[:-1] and per_row > 0 and w % per_row == 0
+        assert scales.dtype is torch.float32 and scales.is_contiguous() and scales.get_device() == dev
+        assert scales.shape[:-1] == shape[:-1] and per_row > 0 and w % per_row == 0
         group = 0 if per_row == 1 else w // per_row
+        sp = scales.data_ptr()
     n0, n1, st = _norm_rows(tensors)
-    st += [(0, 0)] * (4 - len(st))
-    pair = C.c_int64 * 2
-    cfg = dt_norm_config(_VALUE[x.dtype], _VALUE[wt], _VALUE[rt], DT_NORM_OUT_E4M3 if q8 else DT_NORM_OUT_SAME, n0, n1, w, group,
-                         pair(*st[0]), pair(*st[2]), pair(*st[3]), pair(*st[1]), eps)
-    _op_call(lib().dt_add_rmsnorm, dev, stream, cfg, x.data_ptr(), None if weight is None else weight.data_ptr(),
-             None if residual is None else residual.data_ptr(), None if residual is None else residual_out.data_ptr(),
-             y.data_ptr(), scales.data_ptr() if q8 else None)
+    xs, ys, rs, ros = st if len(st) == 4 else (*st, (0, 0), (0, 0))
+    cfg = _NORM_CFG(_VALUE[dtype], _VALUE[wt], _VALUE[rt], DT_NORM_OUT_E4M3 if q8 else DT_NORM_OUT_SAME, n0, n1, w, group,
+                    *xs, *rs, *ros, *ys, eps)
+    _on_device(dev, (_lib or lib()).dt_add_rmsnorm, (cfg, x.data_ptr(), wp, rp, rop, y.data_ptr(), sp), stream)
 
 
 def dt_cross_attn(q, k, v, out, softmax_scale, key_lens=None, key_mask=None, lse_out=None, stream=None):
     """Attention of q [B, Lq, H, D] to an encoder's k, v [B, Lk, H_kv, D]; key_lens int32 [B], key_mask uint8 or bool
     [B, Lk] (expanded batches too), lse_out fp32 [B, H, Lq]."""
-    B, Lq, H, D = q.shape
-    Lk, Hkv = k.shape[1], k.shape[2]
-    dev = q.device
-    assert q.is_cuda and k.shape == v.shape == (B, Lk, Hkv, D) and out.shape == q.shape
-    assert k.dtype == v.dtype == out.dtype == q.dtype and k.device == v.device == out.device == dev
+    shape, kshape, dtype, dev = q.shape, k.shape, q.dtype, q.get_device()
+    B, Lq, H, D = shape
+    Bk, Lk, Hkv, Dk = kshape
+    assert dev >= 0 and Bk == B and Dk == D and v.shape == kshape and out.shape == shape
+    assert k.dtype is dtype and v.dtype is dtype and out.dtype is dtype
+    assert k.get_device() == dev and v.get_device() == dev and out.get_device() == dev
     lp = mp = op = None
     ms = 0
     if key_lens is not None:
-        assert key_lens.dtype == torch.int32 and key_lens.shape == (B,) and key_lens.is_contiguous() and key_lens.device == dev
+        assert key_lens.dtype is torch.int32 and key_lens.shape == (B,) and key_lens.is_contiguous() and key_lens.get_device() == dev
         lp = key_lens.data_ptr()
     if key_mask is not None:
-        assert key_mask.dtype in (torch.uint8, torch.bool) and key_mask.shape == (B, Lk) and key_mask.device == dev
+        assert key_mask.dtype in (torch.uint8, torch.bool) and key_mask.shape == (B, Lk) and key_mask.get_device() == dev
         assert Lk <= 1 or key_mask.stride(1) == 1
         mp, ms = key_mask.data_ptr(), key_mask.stride(0)
     if lse_out is not None:
-        assert lse_out.dtype == torch.float32 and lse_out.shape == (B, H, Lq) and lse_out.is_contiguous() and lse_out.device == dev
+        assert lse_out.dtype is torch.float32 and lse_out.shape == (B, H, Lq) and lse_out.is_contiguous() and lse_out.get_device() == dev
         op = lse_out.data_ptr()
-    cfg = dt_cross_config(_VALUE[q.dtype], B, Lq, Lk, H, Hkv, D, softmax_scale)
-    _op_call(lib().dt_cross_attn, dev, stream, cfg, q.data_ptr(), _STRIDES4(*q.stride()), k.data_ptr(), _STRIDES4(*k.stride()),
-             v.data_ptr(), _STRIDES4(*v.stride()), lp, mp, ms, out.data_ptr(), _STRIDES4(*out.stride()), op)
+    _on_device(dev, (_lib or lib()).dt_cross_attn,
+               (_CROSS_CFG(_VALUE[dtype], B, Lq, Lk, H, Hkv, D, softmax_scale), q.data_ptr(), _S4(*q.stride()), k.data_ptr(), _S4(*k.stride()),
+                v.data_ptr(), _S4(*v.stride()), lp, mp, ms, out.data_ptr(), _S4(*out.stride()), op), stream)
 
 
 def dt_poll_ops(device=None):

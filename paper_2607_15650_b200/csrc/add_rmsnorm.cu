@@ -75,24 +75,33 @@ __device__ __forceinline__ void load8_f32(const float *p, float (&v)[8]) {
 
 enum : int { RES_NONE = 0, RES_SAME = 1, RES_FP32 = 2 };
 
-// h of one vector, and its store to residual_out.  Plain loads and stores: the outputs may be the inputs' own buffers.
-template <bool FP16, int RES>
-__device__ __forceinline__ void load_h(const NormParams &p, long long xo, long long ro, int vec, float (&h)[8]) {
-    const uint4 xr = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.x) + xo + vec * 8);
+// One vector of x and of the residual as it stands in memory.  Plain (coherent) loads and stores: the outputs may be the
+// inputs' own buffers.
+template <int RES>
+struct Raw { uint4 x, r[RES == RES_FP32 ? 2 : 1]; };
+template <int RES>
+__device__ __forceinline__ void load_raw(const NormParams &p, long long xo, long long ro, int vec, Raw<RES> &v) {
+    v.x = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.x) + xo + vec * 8);
     if constexpr (RES == RES_FP32) {
-        const float4 *r = reinterpret_cast<const float4 *>(static_cast<const float *>(p.residual) + ro + vec * 8);
-        const float4 a = r[0], b = r[1];
-        unpack8<FP16>(xr, h);
-        h[0] += a.x; h[1] += a.y; h[2] += a.z; h[3] += a.w; h[4] += b.x; h[5] += b.y; h[6] += b.z; h[7] += b.w;
+        const uint4 *r = reinterpret_cast<const uint4 *>(static_cast<const float *>(p.residual) + ro + vec * 8);
+        v.r[0] = r[0];
+        v.r[1] = r[1];
     } else if constexpr (RES == RES_SAME) {
-        const uint4 rr = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.residual) + ro + vec * 8);
+        v.r[0] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.residual) + ro + vec * 8);
+    }
+}
+template <bool FP16, int RES>
+__device__ __forceinline__ void sum_raw(const Raw<RES> &v, float (&h)[8]) {
+    unpack8<FP16>(v.x, h);
+    if constexpr (RES == RES_FP32) {
+        const uint32_t w[8] = {v.r[0].x, v.r[0].y, v.r[0].z, v.r[0].w, v.r[1].x, v.r[1].y, v.r[1].z, v.r[1].w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] += __uint_as_float(w[e]);
+    } else if constexpr (RES == RES_SAME) {
         float r[8];
-        unpack8<FP16>(xr, h);
-        unpack8<FP16>(rr, r);
+        unpack8<FP16>(v.r[0], r);
 #pragma unroll
         for (int e = 0; e < 8; ++e) h[e] += r[e];
-    } else {
-        unpack8<FP16>(xr, h);
     }
 }
 template <bool FP16, int RES>
@@ -130,26 +139,36 @@ __device__ __forceinline__ float amax8(const float (&y)[8]) {
     return m;
 }
 
-// One row per block, NV vectors of 8 values per thread (vector i * blockDim + thread).
+// Offsets of a row's x, residual, residual_out and y.
+struct RowAt { long long x, r, ro, y; };
+__device__ __forceinline__ RowAt row_at(const NormParams &p, uint32_t row) {
+    const uint32_t i0 = p.n0 == 1 ? 0u : row / (uint32_t)p.n1, i1 = row - i0 * (uint32_t)p.n1;
+    return {i0 * p.xs[0] + i1 * p.xs[1], i0 * p.rs[0] + i1 * p.rs[1], i0 * p.ros[0] + i1 * p.ros[1], i0 * p.ys[0] + i1 * p.ys[1]};
+}
+
+// One row at a time per block, NV vectors of 8 values per thread (vector i * blockDim + thread).  Blocks stay and walk the
+// rows; the next row's loads go out before this row's reductions, so that bytes are in flight throughout.
 template <int NV, bool FP16, int RES, bool Q8>
-__global__ void __launch_bounds__(512) norm_row_kernel(const NormParams p) {
-    __shared__ float red[2][16];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-    const long long row = blockIdx.x;
-    const long long i0 = row / p.n1, i1 = row - i0 * p.n1;
-    const long long xo = i0 * p.xs[0] + i1 * p.xs[1], ro = i0 * p.rs[0] + i1 * p.rs[1];
-    const long long roo = i0 * p.ros[0] + i1 * p.ros[1], yo = i0 * p.ys[0] + i1 * p.ys[1];
+__global__ void __launch_bounds__(512) norm_row_kernel(const NormParams p, const uint32_t rows) {
+  __shared__ float red[2][2][16];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  Raw<RES> raw[NV] = {};
+  RowAt at = row_at(p, blockIdx.x);
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+      if (i * (int)blockDim.x + tid < p.vecs) load_raw<RES>(p, at.x, at.r, i * blockDim.x + tid, raw[i]);
+  int turn = 0;
+  for (uint32_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
+    const long long roo = at.ro, yo = at.y;
     float h[NV][8];
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int vec = i * blockDim.x + tid;
-        if (vec < p.vecs) {
-            load_h<FP16, RES>(p, xo, ro, vec, h[i]);
-        } else {
+    for (int i = 0; i < NV; ++i) sum_raw<FP16, RES>(raw[i], h[i]);   // (vectors behind the row's end are zeros)
+    if (row + gridDim.x < rows) {
+        at = row_at(p, row + gridDim.x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) h[i][e] = 0.f;
-        }
+        for (int i = 0; i < NV; ++i)
+            if (i * (int)blockDim.x + tid < p.vecs) load_raw<RES>(p, at.x, at.r, i * blockDim.x + tid, raw[i]);
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -159,10 +178,10 @@ __global__ void __launch_bounds__(512) norm_row_kernel(const NormParams p) {
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    if (lane == 0) red[0][warp] = s;
+    if (lane == 0) red[turn][0][warp] = s;   // (two sets in turn: a warp may be a row ahead of another that still reads)
     __syncthreads();
     s = 0.f;
-    for (int w = 0; w < warps; ++w) s += red[0][w];
+    for (int w = 0; w < warps; ++w) s += red[turn][0][w];
     const float r = rsqrtf(s + p.eps);
     float row_amax = 0.f;
 #pragma unroll
@@ -184,12 +203,12 @@ __global__ void __launch_bounds__(512) norm_row_kernel(const NormParams p) {
     } else if (p.group_vecs == 0) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) row_amax = fmaxf(row_amax, __shfl_xor_sync(0xFFFFFFFFu, row_amax, o));
-        if (lane == 0) red[1][warp] = row_amax;
+        if (lane == 0) red[turn][1][warp] = row_amax;
         __syncthreads();
-        for (int w = 0; w < warps; ++w) row_amax = fmaxf(row_amax, red[1][w]);
+        for (int w = 0; w < warps; ++w) row_amax = fmaxf(row_amax, red[turn][1][w]);
         row_amax = fmaxf(row_amax, AMAX_FLOOR);
-        if (tid == 0) p.scales[row] = row_amax / E4M3_MAX;
-        const float mul = E4M3_MAX / row_amax;
+        if (tid == 0) p.scales[row] = row_amax * (1.0f / E4M3_MAX);
+        const float mul = __fdividef(E4M3_MAX, row_amax);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int vec = i * blockDim.x + tid;
@@ -206,78 +225,86 @@ __global__ void __launch_bounds__(512) norm_row_kernel(const NormParams p) {
             for (int o = p.group_vecs >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
             m = fmaxf(m, AMAX_FLOOR);
             if (vec < p.vecs) {
-                if (vec % p.group_vecs == 0) p.scales[row * groups + vec / p.group_vecs] = m / E4M3_MAX;
-                *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.y) + yo + vec * 8) = pack8_e4m3(h[i], E4M3_MAX / m);
+                if ((vec & (p.group_vecs - 1)) == 0) p.scales[(long long)row * groups + vec / p.group_vecs] = m * (1.0f / E4M3_MAX);
+                *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.y) + yo + vec * 8) = pack8_e4m3(h[i], __fdividef(E4M3_MAX, m));
+            }
+        }
+    }
+  }
+}
+
+// Short rows (width <= 256): 8, 16 or 32 lanes of a warp per row, one vector per lane, SHORT_ROWS rows one after the other of
+// which all loads go out first.
+constexpr int SHORT_ROWS = 4;
+template <bool FP16, int RES, bool Q8>
+__global__ void __launch_bounds__(256) norm_short_kernel(const NormParams p, const int lanes, const uint32_t rows) {
+    const int vec = threadIdx.x & (lanes - 1), per_pass = 256 / lanes;
+    const uint32_t row0 = blockIdx.x * (uint32_t)(per_pass * SHORT_ROWS) + threadIdx.x / lanes;
+    Raw<RES> raw[SHORT_ROWS] = {};
+#pragma unroll
+    for (int i = 0; i < SHORT_ROWS; ++i) {
+        const uint32_t row = row0 + i * per_pass;
+        if (row < rows && vec < p.vecs) {
+            const RowAt at = row_at(p, row);
+            load_raw<RES>(p, at.x, at.r, vec, raw[i]);
+        }
+    }
+    float w[8] = {};
+    if (vec < p.vecs) load_weight<FP16>(p, vec, w);
+    const int groups = p.group_vecs ? p.vecs / p.group_vecs : 1, g = p.group_vecs ? p.group_vecs : lanes;
+#pragma unroll
+    for (int i = 0; i < SHORT_ROWS; ++i) {
+        const uint32_t row = row0 + i * per_pass;
+        const bool here = row < rows && vec < p.vecs;
+        const RowAt at = row_at(p, here ? row : 0);
+        float h[8];
+        sum_raw<FP16, RES>(raw[i], h);
+        if (RES != RES_NONE && here) store_h<FP16, RES>(p, at.ro, vec, h);
+        float s = meansq8(h, p.inv_width);
+        for (int o = lanes >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        const float r = rsqrtf(s + p.eps);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] = here ? h[e] * r * w[e] : 0.f;
+        if constexpr (!Q8) {
+            if (here) *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.y) + at.y + vec * 8) = pack8<FP16>(h);
+        } else {
+            float m = amax8(h);
+            for (int o = g >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+            m = fmaxf(m, AMAX_FLOOR);
+            if (here) {
+                if ((vec & (g - 1)) == 0) p.scales[(long long)row * groups + vec / g] = m * (1.0f / E4M3_MAX);
+                *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.y) + at.y + vec * 8) = pack8_e4m3(h, __fdividef(E4M3_MAX, m));
             }
         }
     }
 }
 
-// Short rows (width <= 256): 8, 16 or 32 lanes of a warp per row, one vector per lane.
 template <bool FP16, int RES, bool Q8>
-__global__ void __launch_bounds__(256) norm_short_kernel(const NormParams p, const int lanes, const long long rows) {
-    const int vec = threadIdx.x & (lanes - 1);
-    const long long row = (long long)blockIdx.x * (blockDim.x / lanes) + threadIdx.x / lanes;
-    const bool here = row < rows && vec < p.vecs;
-    long long xo = 0, ro = 0, roo = 0, yo = 0;
-    float h[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = 0.f;
-    if (here) {
-        const long long i0 = row / p.n1, i1 = row - i0 * p.n1;
-        xo = i0 * p.xs[0] + i1 * p.xs[1]; ro = i0 * p.rs[0] + i1 * p.rs[1];
-        roo = i0 * p.ros[0] + i1 * p.ros[1]; yo = i0 * p.ys[0] + i1 * p.ys[1];
-        load_h<FP16, RES>(p, xo, ro, vec, h);
-        if (RES != RES_NONE) store_h<FP16, RES>(p, roo, vec, h);
-    }
-    float s = meansq8(h, p.inv_width);
-    for (int o = lanes >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    const float r = rsqrtf(s + p.eps);
-    if (here) {
-        float w[8];
-        load_weight<FP16>(p, vec, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = h[e] * r * w[e];
-    }
-    if constexpr (!Q8) {
-        if (here) *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.y) + yo + vec * 8) = pack8<FP16>(h);
-    } else {
-        float m = here ? amax8(h) : 0.f;
-        const int g = p.group_vecs ? p.group_vecs : lanes;
-        for (int o = g >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-        m = fmaxf(m, AMAX_FLOOR);
-        if (here) {
-            const int groups = p.group_vecs ? p.vecs / p.group_vecs : 1;
-            if (vec % g == 0) p.scales[row * groups + vec / g] = m / E4M3_MAX;
-            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.y) + yo + vec * 8) = pack8_e4m3(h, E4M3_MAX / m);
-        }
-    }
-}
-
-template <bool FP16, int RES, bool Q8>
-cudaError_t launch_norm(const NormParams &p, cudaStream_t st) {
-    const long long rows = p.n0 * p.n1;
+cudaError_t launch_norm(const NormParams &p, uint32_t sms, cudaStream_t st) {
+    const uint32_t rows = (uint32_t)(p.n0 * p.n1);
     if (p.vecs <= 32) {
-        const int lanes = p.vecs <= 8 ? 8 : p.vecs <= 16 ? 16 : 32, per_block = 256 / lanes;
-        norm_short_kernel<FP16, RES, Q8><<<(unsigned)((rows + per_block - 1) / per_block), 256, 0, st>>>(p, lanes, rows);
+        const int lanes = p.vecs <= 8 ? 8 : p.vecs <= 16 ? 16 : 32;
+        const uint32_t per_block = (256 / lanes) * SHORT_ROWS;
+        norm_short_kernel<FP16, RES, Q8><<<(rows - 1) / per_block + 1, 256, 0, st>>>(p, lanes, rows);
     } else {
-        const int nv = p.vecs <= 256 ? 1 : p.vecs <= 512 ? 2 : 4;
+        const int nv = p.vecs <= 256 ? 1 : p.vecs <= 1024 ? 2 : 4;
         const int threads = ((p.vecs + nv - 1) / nv + 31) / 32 * 32;
-        if (nv == 1) norm_row_kernel<1, FP16, RES, Q8><<<(unsigned)rows, threads, 0, st>>>(p);
-        else if (nv == 2) norm_row_kernel<2, FP16, RES, Q8><<<(unsigned)rows, threads, 0, st>>>(p);
-        else norm_row_kernel<4, FP16, RES, Q8><<<(unsigned)rows, threads, 0, st>>>(p);
+        const uint32_t most = sms * 32u, grid = rows < most ? rows : most;
+        if (nv == 1) norm_row_kernel<1, FP16, RES, Q8><<<grid, threads, 0, st>>>(p, rows);
+        else if (nv == 2) norm_row_kernel<2, FP16, RES, Q8><<<grid, threads, 0, st>>>(p, rows);
+        else norm_row_kernel<4, FP16, RES, Q8><<<grid, threads, 0, st>>>(p, rows);
     }
     return cudaGetLastError();
 }
 
 template <bool FP16, int RES>
-cudaError_t launch_out(const NormParams &p, bool q8, cudaStream_t st) {
-    return q8 ? launch_norm<FP16, RES, true>(p, st) : launch_norm<FP16, RES, false>(p, st);
+cudaError_t launch_out(const NormParams &p, bool q8, uint32_t sms, cudaStream_t st) {
+    return q8 ? launch_norm<FP16, RES, true>(p, sms, st) : launch_norm<FP16, RES, false>(p, sms, st);
 }
 template <bool FP16>
-cudaError_t launch_res(const NormParams &p, int res, bool q8, cudaStream_t st) {
-    if (res == RES_NONE) return launch_out<FP16, RES_NONE>(p, q8, st);
-    return res == RES_SAME ? launch_out<FP16, RES_SAME>(p, q8, st) : launch_out<FP16, RES_FP32>(p, q8, st);
+cudaError_t launch_res(const NormParams &p, int res, bool q8, uint32_t sms, cudaStream_t st) {
+    if (res == RES_NONE) return launch_out<FP16, RES_NONE>(p, q8, sms, st);
+    return res == RES_SAME ? launch_out<FP16, RES_SAME>(p, q8, sms, st) : launch_out<FP16, RES_FP32>(p, q8, sms, st);
 }
 
 // Row strides: multiples of 8 values, no negative ones; a stride of a dimension of one entry is not looked at.
@@ -337,6 +364,6 @@ extern "C" dt_status dt_add_rmsnorm(const dt_norm_config *cfg, const void *x_dev
     p.eps = c.eps; p.inv_width = 1.0f / (float)c.width;
     const int res = !residual_dev ? RES_NONE : c.residual_dtype == DT_VALUE_FP32 ? RES_FP32 : RES_SAME;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    cudaError_t e = c.dtype == DT_VALUE_FP16 ? launch_res<true>(p, res, q8, st) : launch_res<false>(p, res, q8, st);
+    cudaError_t e = c.dtype == DT_VALUE_FP16 ? launch_res<true>(p, res, q8, (uint32_t)dev->sms, st) : launch_res<false>(p, res, q8, (uint32_t)dev->sms, st);
     return e == cudaSuccess ? DT_OK : ops_fail_cuda(e, "norm launch");
 }

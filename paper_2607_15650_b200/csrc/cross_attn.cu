@@ -6,12 +6,12 @@
 // negative number, and their V rows are replaced by zeros, so whatever stands in masked places has no effect.  A row
 // without keys has OUT = 0, LSE = -inf.
 //
-// cross_few_kernel: few query rows.  Bound by reading K and V once.  The rows that share a key head (query heads of the
-// group x tokens) fill the 16 rows of an mma.sync tile; the keys are split over the warps of a block and over the blocks of
-// a cluster, whose states are joined in shared memory and then across the cluster (no workspace, no atomics, one launch).
-// K and V go from global memory straight into the fragments, 16 bytes per load: the contraction over d may take d in any
-// order, so lane t of a row takes 8 neighbouring values as its share of two k-steps, and the columns of P V are permuted
-// the same way.
+// cross_few_kernel: few query rows.  Bound by reading K and V once.  The products are taken the other way round, S^T = K Q^T
+// and O^T = V^T P^T, so that the keys (and the head's values) fill the 16 rows of mma.sync and the few query rows its 8 columns:
+// 8 or 16 rows that share a key head (query heads of the group x tokens) per block.  The keys are split over the warps of a
+// block and over the blocks of a cluster, whose states are joined in shared memory and then across the cluster (no
+// workspace, no atomics, one launch).  Every warp streams chunks of 16 keys through a ring of its own in shared memory
+// (cp.async, no barrier between warps), so that two thirds of the ring are in flight while it computes.
 #include <cuda_bf16.h>
 
 #include <cmath>
@@ -22,7 +22,8 @@ namespace dt {
 namespace {
 
 // ------------------------------------------------------------------------------------------------ few rows
-constexpr int FEW_WARPS = 4, FEW_THREADS = FEW_WARPS * 32, FEW_ROWS = 16, FEW_KEYS = 16;
+constexpr int FEW_KEYS = 16, FEW_WARPS = 4, FEW_THREADS = FEW_WARPS * 32;
+constexpr float RESCALE_AT = 8.0f;   // binades that a logit may exceed the running reference by (P <= 2^8, exact in both types)
 
 template <bool FP16>
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -57,200 +58,242 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t smem_addr, uint32_t rank)
 // weight of a partial state with maximum m in a state with maximum top (m = -inf: no keys)
 __device__ __forceinline__ float state_weight(float m, float top) { return m == -INFINITY ? 0.f : ex2_approx(m - top); }
 
-template <int D>
-struct FewSmem {
-    float o[FEW_WARPS][FEW_ROWS][D + 4];
-    float m[FEW_WARPS][FEW_ROWS], l[FEW_WARPS][FEW_ROWS];
-    float cta_m[FEW_ROWS], cta_l[FEW_ROWS];   // this block's joined state (O in o[0])
+// Shared memory: the warps' rings, and after the last chunk, in the same place, the states to be joined.
+template <int D, int ROWS>
+struct FewCfg {
+    static constexpr int ROW = D * 2, TILE = FEW_KEYS * ROW, STAGE = 2 * TILE;   // bytes: a key's row, K of a chunk, K and V
+    static constexpr int MAX_STAGES = D == 128 ? 3 : 6;
+    static constexpr int PITCH = D + 4;                                           // floats of a row of O
+    static constexpr int STATES = FEW_WARPS * ROWS * (PITCH + 2) * 4 + ROWS * 8;
+    static int smem(int stages) { return FEW_WARPS * stages * STAGE > STATES ? FEW_WARPS * stages * STAGE : STATES; }
 };
 
-template <int D, bool FP16>
-__global__ void __launch_bounds__(FEW_THREADS, 3) cross_few_kernel(const CrossParams p, const int splits) {
-    extern __shared__ __align__(16) uint8_t smem_raw[];
-    FewSmem<D> &sm = *reinterpret_cast<FewSmem<D> *>(smem_raw);
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool here) {   // zeros where there is nothing to read
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(here ? 16 : 0) : "memory");
+}
+template <bool TRANS>
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
+    if constexpr (TRANS)
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+    else
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+
+// NT: columns of 8 query rows.
+template <int D, bool FP16, int NT>
+__global__ void __launch_bounds__(FEW_THREADS, 2) cross_few_kernel(const CrossParams p, const int splits, const int stages) {
+    constexpr int FEW_ROWS = 8 * NT;
+    using C = FewCfg<D, FEW_ROWS>;
+    extern __shared__ __align__(128) uint8_t smem_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int split = splits > 1 ? (int)cluster_rank() : 0;
     const int b = blockIdx.y / p.Hkv, hk = blockIdx.y - b * p.Hkv;
-    const int rows = p.Lq * p.rep, row0 = (blockIdx.x / splits) * FEW_ROWS;
+    const int rows = p.Lq * p.rep, row0 = (blockIdx.x / splits) * FEW_ROWS, live = min(rows - row0, FEW_ROWS);
     const int len = keys_of(p, b);
-    const uint16_t *kb = p.k + b * p.ks[0] + hk * p.ks[2], *vb = p.v + b * p.vs[0] + hk * p.vs[2];
     const uint8_t *mb = p.key_mask ? p.key_mask + b * p.mask_stride : nullptr;
+    const int step = splits * FEW_WARPS * FEW_KEYS, first = (split * FEW_WARPS + warp) * FEW_KEYS;
+    const uint32_t ring = smem_u32(smem_raw) + warp * stages * C::STAGE;
 
-    // Q: rows g and g + 8, of every 32 values the 8 at 8 t
-    uint4 qf[2][D / 32];
+    // Chunk of keys -> ring stage.  16-byte piece c of row r lies at c ^ (r & 7): the fragments' reads meet no bank twice.
+    // One group per chunk, an empty one behind the last.  Rows behind the last key are zeros.
+    constexpr int PIECES = D / 8, PER_PASS = 32 / PIECES;   // pieces of a row; rows a pass of the warp takes
+    const int fr = lane / PIECES, fc = lane % PIECES;
+    const uint16_t *kp = p.k + b * p.ks[0] + hk * p.ks[2] + (first + fr) * p.ks[1] + 8 * fc;   // this lane's piece of the next chunk
+    const uint16_t *vp = p.v + b * p.vs[0] + hk * p.vs[2] + (first + fr) * p.vs[1] + 8 * fc;
+    auto fetch = [&](int key0, int st) {
+        const uint32_t at = ring + st * C::STAGE + fr * C::ROW;
+        if (key0 + FEW_KEYS <= len) {
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        const int row = row0 + g + 8 * r;
-        const int l = row / p.rep, h = hk * p.rep + (row - l * p.rep);
-        const uint16_t *src = p.q + b * p.qs[0] + l * p.qs[1] + h * p.qs[2] + 8 * t;
+            for (int i = 0; i < FEW_KEYS / PER_PASS; ++i)
+                copy16(at + i * PER_PASS * C::ROW + ((fc ^ ((i * PER_PASS + fr) & 7)) << 4), kp + i * PER_PASS * p.ks[1], true);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) qf[r][i] = row < rows ? __ldg(reinterpret_cast<const uint4 *>(src + 32 * i)) : make_uint4(0, 0, 0, 0);
-    }
-    float o[D / 8][4];
+            for (int i = 0; i < FEW_KEYS / PER_PASS; ++i)
+                copy16(at + C::TILE + i * PER_PASS * C::ROW + ((fc ^ ((i * PER_PASS + fr) & 7)) << 4), vp + i * PER_PASS * p.vs[1], true);
+        } else if (key0 < len) {
 #pragma unroll
-    for (int j = 0; j < D / 8; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-
-    uint4 kf[2][D / 32], vf[4][D / 64];
-    auto load_k = [&](int key0) {
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const int key = key0 + 8 * n + g;
-            const uint16_t *src = kb + key * p.ks[1] + 8 * t;
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) kf[n][i] = key < len ? __ldg(reinterpret_cast<const uint4 *>(src + 32 * i)) : make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < FEW_KEYS / PER_PASS; ++i) {
+                const bool here = key0 + i * PER_PASS + fr < len;
+                copy16(at + i * PER_PASS * C::ROW + ((fc ^ ((i * PER_PASS + fr) & 7)) << 4), here ? kp + i * PER_PASS * p.ks[1] : p.k, here);
+                copy16(at + C::TILE + i * PER_PASS * C::ROW + ((fc ^ ((i * PER_PASS + fr) & 7)) << 4), here ? vp + i * PER_PASS * p.vs[1] : p.v, here);
+            }
         }
+        kp += step * p.ks[1];
+        vp += step * p.vs[1];
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    // key of this lane's place e (0..3) in a chunk: the columns of its S fragments, and the V rows it multiplies
-    auto key_at = [&](int key0, int e) { return key0 + 2 * t + (e & 1) + 8 * (e >> 1); };
+    for (int i = 0; i < stages - 1; ++i) fetch(first + i * step, i);
+    // which of this lane's two keys of a chunk count: g and g + 8, the rows of its S^T fragments
     auto keys_on = [&](int key0) {
-        uint32_t on = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int key = key_at(key0, e);
-            if (key < len && (mb == nullptr || __ldg(mb + key) != 0)) on |= 1u << e;
-        }
-        return on;
+        const int k0 = key0 + g, k1 = k0 + 8;
+        return (uint32_t)(k0 < len && (mb == nullptr || __ldg(mb + k0) != 0)) | (uint32_t)(k1 < len && (mb == nullptr || __ldg(mb + k1) != 0)) << 1;
     };
-    auto load_v = [&](int key0) {
+    uint32_t on = keys_on(first);
+
+    uint32_t qf[NT][D / 16][2];   // Q^T: column g, values 2 t, 2 t + 1 and 8 on of every 16
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int key = key_at(key0, e);
-            const uint16_t *src = vb + key * p.vs[1] + 8 * g;
+    for (int n = 0; n < NT; ++n) {
+        const int row = row0 + 8 * n + g, l = row / p.rep, h = hk * p.rep + (row - l * p.rep);
+        const uint16_t *src = p.q + b * p.qs[0] + l * p.qs[1] + h * p.qs[2] + 2 * t;
 #pragma unroll
-            for (int j = 0; j < D / 64; ++j) vf[e][j] = key < len ? __ldg(reinterpret_cast<const uint4 *>(src + 64 * j)) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < D / 16; ++i) {
+            qf[n][i][0] = row < rows ? __ldg(reinterpret_cast<const uint32_t *>(src + 16 * i)) : 0u;
+            qf[n][i][1] = row < rows ? __ldg(reinterpret_cast<const uint32_t *>(src + 16 * i + 8)) : 0u;
         }
-    };
-    const int step = splits * FEW_WARPS * FEW_KEYS;
-    int key0 = (split * FEW_WARPS + warp) * FEW_KEYS;
-    uint32_t on = 0;
-    if (key0 < len) {
-        on = keys_on(key0);
-        load_k(key0);
-        load_v(key0);
     }
-    for (; key0 < len; key0 += step) {
-        float s[2][4] = {};
+    // O^T: rows g, g + 8 of every 16 values, columns (query rows) 2 t, 2 t + 1; maximum and sum of those columns
+    float o[NT][D / 16][4], m[NT][2], l[NT][2];
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i)
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                mma_16816<FP16>(s[n], qf[0][i].x, qf[1][i].x, qf[0][i].y, qf[1][i].y, kf[n][i].x, kf[n][i].y);
-                mma_16816<FP16>(s[n], qf[0][i].z, qf[1][i].z, qf[0][i].w, qf[1][i].w, kf[n][i].z, kf[n][i].w);
-            }
+        for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[n][j][e] = 0.f;
+        m[n][0] = m[n][1] = -INFINITY;
+        l[n][0] = l[n][1] = 0.f;
+    }
+    // rows and pieces that this lane points ldmatrix at
+    const int kr = (lane & 7) + ((lane >> 3) & 1) * 8, kc = lane >> 4;
+    const int vr = (lane & 7) + (lane >> 4) * 8, vc = (lane >> 3) & 1;
+
+    int st = 0;
+    for (int key0 = first; key0 < len; key0 += step) {
+        // the chunk has landed when at most stages - 2 younger groups are outstanding
+        if (stages == 2) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        else if (stages == 3) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 4;" ::: "memory");
+        __syncwarp();
+        const uint32_t at = ring + st * C::STAGE;
+        // the stage before this one was read by all lanes ahead of the __syncwarp above: it takes the next chunk
+        fetch(key0 + (stages - 1) * step, st == 0 ? stages - 1 : st - 1);
         const uint32_t now = on;
-        if (key0 + step < len) {   // K's registers are free: the next chunk's go out before this one's softmax
-            on = keys_on(key0 + step);
-            load_k(key0 + step);
+        on = keys_on(key0 + step);
+        float s[NT][2][4] = {};   // two accumulators: chains of half the length
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            uint32_t a[4];
+            ldmatrix4<false>(a, at + kr * C::ROW + (((2 * i + kc) ^ (kr & 7)) << 4));
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma_16816<FP16>(s[n][i & 1], a[0], a[1], a[2], a[3], qf[n][i][0], qf[n][i][1]);
         }
-        float pr[2][4];
+        if (mb != nullptr && !__all_sync(0xFFFFFFFFu, now == 3u)) {
+            // V rows of masked keys: zeros, whatever they hold; lane r or 16 + r zeroes half of row r
+            const uint32_t lo = __ballot_sync(0xFFFFFFFFu, now & 1u), hi = __ballot_sync(0xFFFFFFFFu, now & 2u);
+            const int r = lane & 15;
+            if (!((r < 8 ? lo : hi) >> (4 * (r & 7)) & 1u))
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            float x[4], top = -INFINITY;
+                for (int c = 0; c < PIECES / 2; ++c)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + C::TILE + r * C::ROW + (lane >> 4) * (C::ROW / 2) + c * 16), "r"(0) : "memory");
+            __syncwarp();
+        }
+        uint32_t pf[NT][2];   // P^T: column g, keys 2 t, 2 t + 1 and 8 on
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float x[4];   // (key g, key g + 8) x (row 2 t, row 2 t + 1)
+            bool over = false;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                x[e] = (now >> e & 1u) ? s[e >> 1][2 * r + (e & 1)] * p.scale_log2 : -INFINITY;
-                top = fmaxf(top, x[e]);
+                x[e] = (now >> (e >> 1) & 1u) ? (s[n][0][e] + s[n][1][e]) * p.scale_log2 : -INFINITY;
+                over |= x[e] > m[n][e & 1] + RESCALE_AT;
             }
-            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-            const float mn = fmaxf(m[r], top), ref = mn == -INFINITY ? 0.f : mn;
-            const float alpha = ex2_approx(m[r] - ref);   // m = -inf: 0
-            m[r] = mn;
-            float sum = 0.f;
+            if (__any_sync(0xFFFFFFFFu, over)) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                pr[r][e] = ex2_approx(x[e] - ref);
-                sum += pr[r][e];
-            }
-            l[r] = l[r] * alpha + sum;
-            if (__any_sync(0xFFFFFFFFu, alpha != 1.f)) {
+                for (int c = 0; c < 2; ++c) {
+                    float top = fmaxf(x[c], x[2 + c]);
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
+                    const float mn = fmaxf(m[n][c], top);
+                    const float alpha = mn == -INFINITY ? 1.f : ex2_approx(m[n][c] - mn);   // m = -inf: 0
+                    m[n][c] = mn;
+                    l[n][c] *= alpha;
 #pragma unroll
-                for (int j = 0; j < D / 8; ++j) {
-                    o[j][2 * r] *= alpha;
-                    o[j][2 * r + 1] *= alpha;
+                    for (int j = 0; j < D / 16; ++j) {
+                        o[n][j][c] *= alpha;
+                        o[n][j][2 + c] *= alpha;
+                    }
                 }
             }
+            float pr[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                pr[e] = ex2_approx(x[e] - (m[n][e & 1] == -INFINITY ? 0.f : m[n][e & 1]));
+                l[n][e & 1] += pr[e];
+            }
+            pf[n][0] = transpose8x8(pack_half2<FP16>(pr[0], pr[1]));
+            pf[n][1] = transpose8x8(pack_half2<FP16>(pr[2], pr[3]));
         }
-        const uint32_t a0 = pack_half2<FP16>(pr[0][0], pr[0][1]), a1 = pack_half2<FP16>(pr[1][0], pr[1][1]);
-        const uint32_t a2 = pack_half2<FP16>(pr[0][2], pr[0][3]), a3 = pack_half2<FP16>(pr[1][2], pr[1][3]);
-        if (now != 0xFu) {   // V rows of keys that do not count: zeros, whatever they hold
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (!(now >> e & 1u))
+        for (int j = 0; j < D / 16; ++j) {
+            uint32_t a[4];
+            ldmatrix4<true>(a, at + C::TILE + vr * C::ROW + (((2 * j + vc) ^ (vr & 7)) << 4));
 #pragma unroll
-                    for (int j = 0; j < D / 64; ++j) vf[e][j] = make_uint4(0, 0, 0, 0);
+            for (int n = 0; n < NT; ++n) mma_16816<FP16>(o[n][j], a[0], a[1], a[2], a[3], pf[n][0], pf[n][1]);
         }
+        if (++st == stages) st = 0;
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();   // the rings are done with: the states take their place
+    float *const so = reinterpret_cast<float *>(smem_raw);                       // [warp][row][PITCH]
+    float *const sm = so + FEW_WARPS * FEW_ROWS * C::PITCH, *const sl = sm + FEW_WARPS * FEW_ROWS;   // [warp][row]
+    float *const cm = sl + FEW_WARPS * FEW_ROWS, *const cl = cm + FEW_ROWS;      // the block's joined state (O in so's first)
+    // this warp's state
 #pragma unroll
-        for (int j = 0; j < D / 64; ++j) {
-            const uint32_t w0[4] = {vf[0][j].x, vf[0][j].y, vf[0][j].z, vf[0][j].w}, w1[4] = {vf[1][j].x, vf[1][j].y, vf[1][j].z, vf[1][j].w};
-            const uint32_t w2[4] = {vf[2][j].x, vf[2][j].y, vf[2][j].z, vf[2][j].w}, w3[4] = {vf[3][j].x, vf[3][j].y, vf[3][j].z, vf[3][j].w};
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {   // value 2c (low halves) and 2c + 1 (high halves) of the lane's 8
-                mma_16816<FP16>(o[8 * j + 2 * c], a0, a1, a2, a3, __byte_perm(w0[c], w1[c], 0x5410), __byte_perm(w2[c], w3[c], 0x5410));
-                mma_16816<FP16>(o[8 * j + 2 * c + 1], a0, a1, a2, a3, __byte_perm(w0[c], w1[c], 0x7632), __byte_perm(w2[c], w3[c], 0x7632));
+        for (int c = 0; c < 2; ++c) {
+            float sum = l[n][c];
+            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 4);
+            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 8);
+            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 16);
+            const int row = 8 * n + 2 * t + c;
+            if (row >= live) continue;
+            if (g == 0) {
+                sm[warp * FEW_ROWS + row] = m[n][c];
+                sl[warp * FEW_ROWS + row] = sum;
+            }
+            float *dst = so + (warp * FEW_ROWS + row) * C::PITCH + g;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) {
+                dst[16 * j] = o[n][j][c];
+                dst[16 * j + 8] = o[n][j][2 + c];
             }
         }
-        if (key0 + step < len) load_v(key0 + step);
-    }
-    // this warp's state: rows g, g + 8; the fragment column n of tile 8 j + e is d = 64 j + 8 n + e
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        l[r] += __shfl_xor_sync(0xFFFFFFFFu, l[r], 1);
-        l[r] += __shfl_xor_sync(0xFFFFFFFFu, l[r], 2);
-        if (t == 0) {
-            sm.m[warp][g + 8 * r] = m[r];
-            sm.l[warp][g + 8 * r] = l[r];
-        }
-#pragma unroll
-        for (int j = 0; j < D / 64; ++j)
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {   // column 2 t + n
-                float *dst = &sm.o[warp][g + 8 * r][64 * j + 8 * (2 * t + n)];
-                *reinterpret_cast<float4 *>(dst) = make_float4(o[8 * j][2 * r + n], o[8 * j + 1][2 * r + n], o[8 * j + 2][2 * r + n], o[8 * j + 3][2 * r + n]);
-                *reinterpret_cast<float4 *>(dst + 4) = make_float4(o[8 * j + 4][2 * r + n], o[8 * j + 5][2 * r + n], o[8 * j + 6][2 * r + n], o[8 * j + 7][2 * r + n]);
-            }
-    }
     __syncthreads();
-    // join the block's warps: 8 threads per row, D / 8 values each (threads of a row are in one warp)
-    const int live = min(rows - row0, FEW_ROWS);
-    const int row = threadIdx.x >> 3, part = threadIdx.x & 7;
-    {
+    // join the block's warps, 4 values of a row at a time, into the first warp's place
+    for (int i = threadIdx.x; i < live * (D / 4); i += FEW_THREADS) {
+        const int r = i / (D / 4), c = i - r * (D / 4);
         float top = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < FEW_WARPS; ++w) top = fmaxf(top, sm.m[w][row]);
-        float sum = 0.f, wt[FEW_WARPS];
+        for (int w = 0; w < FEW_WARPS; ++w) top = fmaxf(top, sm[w * FEW_ROWS + r]);
+        float sum = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < FEW_WARPS; ++w) {
-            wt[w] = state_weight(sm.m[w][row], top);
-            sum += wt[w] * sm.l[w][row];
+            const float wt = state_weight(sm[w * FEW_ROWS + r], top);
+            const float4 x = *reinterpret_cast<const float4 *>(so + (w * FEW_ROWS + r) * C::PITCH + 4 * c);
+            sum = fmaf(wt, sl[w * FEW_ROWS + r], sum);
+            acc.x = fmaf(wt, x.x, acc.x); acc.y = fmaf(wt, x.y, acc.y);
+            acc.z = fmaf(wt, x.z, acc.z); acc.w = fmaf(wt, x.w, acc.w);
         }
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) {   // 4 values at 4 (part + 8 c)
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < FEW_WARPS; ++w) {
-                const float4 x = *reinterpret_cast<const float4 *>(&sm.o[w][row][4 * (part + 8 * c)]);
-                acc.x = fmaf(wt[w], x.x, acc.x); acc.y = fmaf(wt[w], x.y, acc.y);
-                acc.z = fmaf(wt[w], x.z, acc.z); acc.w = fmaf(wt[w], x.w, acc.w);
-            }
-            *reinterpret_cast<float4 *>(&sm.o[0][row][4 * (part + 8 * c)]) = acc;
-        }
-        if (part == 0) {
-            sm.cta_m[row] = top;
-            sm.cta_l[row] = sum;
+        *reinterpret_cast<float4 *>(so + r * C::PITCH + 4 * c) = acc;
+        if (c == 0) {
+            cm[r] = top;
+            cl[r] = sum;
         }
     }
     if (splits > 1) cluster_arrive_wait();
     else __syncthreads();
     // join the cluster's blocks: groups of 4 values (row, 4 values) shared out over the blocks
-    const uint32_t m_addr = smem_u32(sm.cta_m), l_addr = smem_u32(sm.cta_l), o_addr = smem_u32(&sm.o[0][0][0]);
+    const uint32_t m_addr = smem_u32(cm), l_addr = smem_u32(cl), o_addr = smem_u32(so);
     for (int i = split * FEW_THREADS + threadIdx.x; i < live * (D / 4); i += splits * FEW_THREADS) {
         const int r = i / (D / 4), c = i - r * (D / 4);
         float top = -INFINITY;
-        for (int s = 0; s < splits; ++s) top = fmaxf(top, splits > 1 ? ld_cluster(m_addr + 4 * r, s) : sm.cta_m[r]);
+        for (int s = 0; s < splits; ++s) top = fmaxf(top, splits > 1 ? ld_cluster(m_addr + 4 * r, s) : cm[r]);
         float sum = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int s = 0; s < splits; ++s) {
@@ -259,10 +302,10 @@ __global__ void __launch_bounds__(FEW_THREADS, 3) cross_few_kernel(const CrossPa
             if (splits > 1) {
                 ms = ld_cluster(m_addr + 4 * r, s);
                 ls = ld_cluster(l_addr + 4 * r, s);
-                x = ld_cluster4(o_addr + (r * (D + 4) + 4 * c) * 4, s);
+                x = ld_cluster4(o_addr + (r * C::PITCH + 4 * c) * 4, s);
             } else {
-                ms = sm.cta_m[r]; ls = sm.cta_l[r];
-                x = *reinterpret_cast<const float4 *>(&sm.o[0][r][4 * c]);
+                ms = cm[r]; ls = cl[r];
+                x = *reinterpret_cast<const float4 *>(so + r * C::PITCH + 4 * c);
             }
             const float wt = state_weight(ms, top);
             sum = fmaf(wt, ls, sum);
@@ -279,30 +322,56 @@ __global__ void __launch_bounds__(FEW_THREADS, 3) cross_few_kernel(const CrossPa
     if (splits > 1) cluster_arrive_wait();   // no block leaves while another still reads its shared memory
 }
 
-template <int D, bool FP16>
+template <int D, bool FP16, int NT>
 cudaError_t launch_few(const CrossParams &p, int sms, cudaStream_t st) {
-    const long long rows = (long long)p.Lq * p.rep, row_blocks = (rows + FEW_ROWS - 1) / FEW_ROWS;
+    using C = FewCfg<D, 8 * NT>;
+    const long long rows = (long long)p.Lq * p.rep, row_blocks = (rows + 8 * NT - 1) / (8 * NT);
     const long long groups = row_blocks * p.B * p.Hkv;
-    // split the keys while that still gives every warp a chunk of its own and the GPU has room for the blocks (3 per SM)
+    // Split the keys while that still gives every warp a chunk of its own and the blocks fit the GPU at once (2 per SM).
+    // Clusters of 8 at most: with 16 blocks they do not all find a place at once (2 x 8 key heads, 32760 keys: 57 us with 16,
+    // 45 with 8, 63 with 4).
     int splits = 1;
-    while (splits < 8 && groups * splits * 2 <= 3LL * sms && splits * 2 * FEW_WARPS * FEW_KEYS <= p.Lk + FEW_WARPS * FEW_KEYS - 1) splits *= 2;
-    auto kernel = cross_few_kernel<D, FP16>;
-    constexpr int smem = sizeof(FewSmem<D>);
-    static_assert(smem <= 48 * 1024, "within the shared memory every block may have");
+    while (splits < 8 && groups * splits * 2 <= 2LL * sms && splits * FEW_WARPS * FEW_KEYS < p.Lk) splits *= 2;
+    const int chunks = (p.Lk + splits * FEW_WARPS * FEW_KEYS - 1) / (splits * FEW_WARPS * FEW_KEYS);   // of a warp
+    const int stages = chunks >= C::MAX_STAGES ? C::MAX_STAGES : chunks >= 3 ? 3 : 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(row_blocks * splits), (unsigned)(p.B * p.Hkv));
     cfg.blockDim = dim3(FEW_THREADS);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = C::smem(stages);
     cfg.stream = st;
     cudaLaunchAttribute attr = {};
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = (unsigned)splits; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = splits > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kernel, p, splits);
+    return cudaLaunchKernelEx(&cfg, cross_few_kernel<D, FP16, NT>, p, splits, stages);
+}
+template <int D, bool FP16>
+cudaError_t launch_few(const CrossParams &p, int sms, cudaStream_t st) {
+    return (long long)p.Lq * p.rep <= 8 ? launch_few<D, FP16, 1>(p, sms, st) : launch_few<D, FP16, 2>(p, sms, st);
+}
+
+template <int D, bool FP16, int NT>
+cudaError_t configure_few() {
+    return cudaFuncSetAttribute(cross_few_kernel<D, FP16, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                FewCfg<D, 8 * NT>::smem(FewCfg<D, 8 * NT>::MAX_STAGES));
+}
+template <int D, bool FP16>
+cudaError_t configure_few() {
+    cudaError_t e = configure_few<D, FP16, 1>();
+    return e == cudaSuccess ? configure_few<D, FP16, 2>() : e;
 }
 
 }  // namespace
+
+cudaError_t cross_few_configure() {
+    cudaError_t e;
+    if ((e = configure_few<64, false>()) != cudaSuccess) return e;
+    if ((e = configure_few<64, true>()) != cudaSuccess) return e;
+    if ((e = configure_few<128, false>()) != cudaSuccess) return e;
+    return configure_few<128, true>();
+}
+
 }  // namespace dt
 
 extern "C" dt_status dt_cross_attn(const dt_cross_config *cfg, const void *q_dev, const int64_t q_strides_blhd[4], const void *k_dev,

@@ -27,6 +27,7 @@ __device__ __forceinline__ int keys_of(const CrossParams &p, int b) {
 
 // Many query rows (Lk > 0): tensor-memory tiles.
 cudaError_t launch_cross_tiles(const CrossParams &p, int D, bool fp16, const OpsDevice &dev, cudaStream_t st);
-cudaError_t cross_tiles_configure();   // per device, once
+cudaError_t cross_tiles_configure();   // both per device, once
+cudaError_t cross_few_configure();
 
 }  // namespace dt

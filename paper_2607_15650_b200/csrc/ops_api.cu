@@ -48,7 +48,7 @@ dt_status ops_device(const OpsDevice **out) {
         e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &d.encode_tiled, cudaEnableDefault, &qres);
         if (e != cudaSuccess) return ops_fail_cuda(e, "cuTensorMapEncodeTiled");
         if (qres != cudaDriverEntryPointSuccess || !d.encode_tiled) return ops_fail(DT_ERR_CUDA, "cuTensorMapEncodeTiled not found");
-        if ((e = cross_tiles_configure()) != cudaSuccess) return ops_fail_cuda(e, "cross-attention kernels");
+        if ((e = cross_tiles_configure()) != cudaSuccess || (e = cross_few_configure()) != cudaSuccess) return ops_fail_cuda(e, "cross-attention kernels");
         // two threads may get here at once: both write the same facts
         g_devices[dev] = d;
         g_ready[dev].store(1, std::memory_order_release);

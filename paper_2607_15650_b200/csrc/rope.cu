@@ -4,7 +4,8 @@
 //     (x, y) -> m (x cos - y sin, y cos + x sin).
 // The angle is summed in fp64 and reduced to (-1/2, 1/2] turns there, so that a position of 10^8 is as exact as one of 10;
 // sine and cosine are then taken in fp32 (sincospif), the rotation is fp32 with one rounding to the tensors' type.
-// A token's angles are the same for all its heads: a block takes them once into shared memory and walks the heads.
+// A token's angles are the same for all its heads: the lanes that share a token take them once, between them, into
+// registers and walk the heads.
 //
 // Bound: HBM (each value read and written once; the angles are D/2 per token against D * heads values).
 #include <cuda_bf16.h>
@@ -18,8 +19,7 @@
 namespace dt {
 namespace {
 
-constexpr int ROPE_THREADS = 256;
-constexpr int ROPE_TABLE = 2048;   // cosines (and as many sines) a block holds
+constexpr int ROPE_THREADS = 256, ROPE_WARPS = ROPE_THREADS / 32;
 constexpr double INV_2PI = 0.15915494309189533577;
 
 enum : int { UNIT_INTERLEAVED = 0, UNIT_HALF = 1, UNIT_HALF_ODD = 2 };
@@ -32,9 +32,11 @@ struct RopeParams {
     const int32_t *pos;         // null: the token's index
     long long ps[3];            // B, L, axis
     int B, L, Hq, Ht, D;        // Ht = query heads + key heads
-    int pairs, pitch, axes;     // pitch: pairs rounded up to a multiple of 8
-    int tokens;                 // tokens per block
+    int pairs, axes;
     int units, lanes;           // 16-byte units of work per head, and lanes (a power of two) that walk them
+    int heads;                  // 1, 2 or 4: heads that a warp takes side by side (lanes * heads <= 32)
+    int per_warp;               // tokens side by side in a warp: 32 / (lanes * heads)
+    int chunk, chunks;          // heads a warp walks, and warps per token that way
     float factor, sin_sign;
 };
 
@@ -67,118 +69,182 @@ __device__ __forceinline__ float widen(uint16_t v) {
     if constexpr (FP16) return __half2float(__ushort_as_half(v));
     return __uint_as_float((uint32_t)v << 16);
 }
-__device__ __forceinline__ void load8(const float *p, float (&v)[8]) {
-    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+
+// A unit is 8 values of a head, 16 bytes.  Interleaved: 4 pairs.  Half layout: one side of 8 pairs, whose other side is
+// another lane's unit (UNIT_HALF), or lies across two of them (UNIT_HALF_ODD: halves that do not meet 16-byte borders).
+template <int UNIT>
+__device__ __forceinline__ int pair_of(int u, int i, int pairs) {
+    if constexpr (UNIT == UNIT_INTERLEAVED) return u * 4 + i;
+    const int v = u * 8 + i;
+    return v < pairs ? v : v - pairs;   // (past 2 * pairs: a pair that does not exist, not turned)
 }
 
 template <bool FP16, int UNIT>
-__global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const RopeParams p) {
-    __shared__ __align__(16) float cos_tab[ROPE_TABLE], sin_tab[ROPE_TABLE];
+__global__ void __launch_bounds__(ROPE_THREADS, UNIT == UNIT_INTERLEAVED ? 4 : 3) rope_kernel(const RopeParams p) {
+    constexpr int ANGLES = UNIT == UNIT_INTERLEAVED ? 4 : 8;
+    constexpr int U = 4;   // units loaded before the first is turned: 64 bytes in flight per lane
     __shared__ __align__(16) uint16_t stage[UNIT == UNIT_HALF_ODD ? ROPE_THREADS * 8 : 8];
-    const long long n0 = (long long)blockIdx.x * p.tokens, all = (long long)p.B * p.L;
-    const int count = (int)min((long long)p.tokens, all - n0);
-    for (int i = threadIdx.x; i < count * p.pairs; i += ROPE_THREADS) {
-        const int t = i / p.pairs, pair = i - t * p.pairs;
-        const long long n = n0 + t, b = n / p.L, l = n - b * p.L;
-        double angle = 0.0;
-        if (p.pos == nullptr) angle = (double)l * p.freqs[pair];
-        else
-            for (int a = 0; a < p.axes; ++a)
-                angle = fma((double)p.pos[b * p.ps[0] + l * p.ps[1] + a * p.ps[2]], p.freqs[a * p.pairs + pair], angle);
-        const double turns = angle * INV_2PI;
-        float s, c;
-        sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-        cos_tab[t * p.pitch + pair] = c * p.factor;
-        sin_tab[t * p.pitch + pair] = s * p.factor * p.sin_sign;
-    }
-    __syncthreads();
-    const int u = threadIdx.x & (p.lanes - 1), row_step = ROPE_THREADS / p.lanes;
-    const int rows = count * p.Ht;
-    // (whole warps stay in the loop: a row's lanes exchange values in the odd form)
-    for (int row0 = 0; row0 < rows; row0 += row_step) {
-        const int row = row0 + threadIdx.x / p.lanes;
-        const bool here = row < rows && u < p.units;
-        const int t = row < rows ? row / p.Ht : 0, ht = row < rows ? row - t * p.Ht : 0;
-        const long long n = n0 + t, b = n / p.L, l = n - b * p.L;
-        const int which = ht >= p.Hq, h = which ? ht - p.Hq : ht;
-        const uint16_t *src = p.in[which] + b * p.is[which][0] + l * p.is[which][1] + h * p.is[which][2];
-        uint16_t *dst = p.out[which] + b * p.os[which][0] + l * p.os[which][1] + h * p.os[which][2];
-        const float *ct = cos_tab + t * p.pitch, *st = sin_tab + t * p.pitch;
-        if constexpr (UNIT == UNIT_INTERLEAVED) {
-            if (!here) continue;
-            const uint4 raw = *reinterpret_cast<const uint4 *>(src + u * 8);
-            float x[8];
-            unpack<FP16>(raw, x);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t wg = blockIdx.x * (uint32_t)ROPE_WARPS + warp, group = wg / (uint32_t)p.chunks;
+    const uint32_t all = (uint32_t)p.B * (uint32_t)p.L;
+    if ((unsigned long long)group * p.per_warp >= all) return;   // (whole warps)
+    const int u = lane & (p.lanes - 1), hslot = (lane / p.lanes) & (p.heads - 1), slot = lane / (p.lanes * p.heads);
+    const unsigned long long n64 = (unsigned long long)group * p.per_warp + slot;
+    const bool here = n64 < all && u < p.units;
+    const uint32_t n = n64 < all ? (uint32_t)n64 : all - 1, b = n / (uint32_t)p.L, l = n - b * (uint32_t)p.L;
+    const int h0 = (int)(wg - group * (uint32_t)p.chunks) * p.chunk, h1 = min(h0 + p.chunk, p.Ht);
+    // UNIT_HALF: the lane with the other side of this unit's pairs (itself where nothing turns), and its sine's sign
+    const int side = p.pairs / 8;
+    const int other = u < side ? lane + side : u < 2 * side ? lane - side : lane;
+    const float other_sign = u < side ? -1.f : 1.f;
+
+    // the warp's heads: those of q, then those of k
+    int h, hi;
+    const uint16_t *src;
+    uint16_t *dst;
+    long long s_step, d_step;
+    auto enter = [&](bool k) {
+        const long long off_s = k ? b * p.is[1][0] + l * p.is[1][1] : b * p.is[0][0] + l * p.is[0][1];
+        const long long off_d = k ? b * p.os[1][0] + l * p.os[1][1] : b * p.os[0][0] + l * p.os[0][1];
+        src = (k ? p.in[1] : p.in[0]) + off_s + u * 8;
+        dst = (k ? p.out[1] : p.out[0]) + off_d + u * 8;
+        s_step = k ? p.is[1][2] : p.is[0][2];
+        d_step = k ? p.os[1][2] : p.os[0][2];
+        h = k ? max(h0 - p.Hq, 0) : h0;
+        hi = k ? h1 - p.Hq : min(h1, p.Hq);
+    };
+    enter(h0 >= p.Hq);
+    bool more_k = h0 < p.Hq && h1 > p.Hq;
+    uint4 raw[U] = {};
+    auto load = [&]() {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int pair = min(u * 4 + i, p.pairs - 1);
-                const float c = ct[pair], s = st[pair], a = x[2 * i], d = x[2 * i + 1];
-                x[2 * i] = a * c - d * s;
-                x[2 * i + 1] = d * c + a * s;
-            }
-            uint4 got = pack<FP16>(x);
-            // pairs that do not turn keep their bits (a NaN's too)
-            if (u * 4 + 0 >= p.pairs) got.x = raw.x;
-            if (u * 4 + 1 >= p.pairs) got.y = raw.y;
-            if (u * 4 + 2 >= p.pairs) got.z = raw.z;
-            if (u * 4 + 3 >= p.pairs) got.w = raw.w;
-            *reinterpret_cast<uint4 *>(dst + u * 8) = got;
-        } else if constexpr (UNIT == UNIT_HALF) {
-            if (!here) continue;
-            const int turning = p.pairs / 8;   // units of 8 pairs; the units behind them copy 8 values each
-            if (u < turning) {
-                float x[8], y[8], c[8], s[8], o[8];
-                const uint4 rx = *reinterpret_cast<const uint4 *>(src + u * 8);
-                const uint4 ry = *reinterpret_cast<const uint4 *>(src + p.pairs + u * 8);
-                load8(ct + u * 8, c);
-                load8(st + u * 8, s);
-                unpack<FP16>(rx, x);
-                unpack<FP16>(ry, y);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = x[e] * c[e] - y[e] * s[e];
-                *reinterpret_cast<uint4 *>(dst + u * 8) = pack<FP16>(o);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = y[e] * c[e] + x[e] * s[e];
-                *reinterpret_cast<uint4 *>(dst + p.pairs + u * 8) = pack<FP16>(o);
-            } else if (src != dst) {
-                const int at = 2 * p.pairs + (u - turning) * 8;
-                *reinterpret_cast<uint4 *>(dst + at) = *reinterpret_cast<const uint4 *>(src + at);
-            }
-        } else {
-            // the halves do not meet 16-byte borders: a row goes through shared memory, every lane makes its own 8 values
-            uint16_t *line = stage + (threadIdx.x / p.lanes) * p.lanes * 8;
-            float x[8];
-            uint4 raw = make_uint4(0, 0, 0, 0);
-            if (here) {
-                raw = *reinterpret_cast<const uint4 *>(src + u * 8);
-                *reinterpret_cast<uint4 *>(line + u * 8) = raw;
-                unpack<FP16>(raw, x);
-            }
-            __syncwarp();
-            if (here) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int at = u * 8 + e;
-                    if (at < p.pairs) x[e] = x[e] * ct[at] - widen<FP16>(line[at + p.pairs]) * st[at];
-                    else if (at < 2 * p.pairs) x[e] = x[e] * ct[at - p.pairs] + widen<FP16>(line[at - p.pairs]) * st[at - p.pairs];
-                }
-                const uint4 made = pack<FP16>(x);
-                uint32_t got[4] = {made.x, made.y, made.z, made.w};
-                const uint32_t was[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-                for (int w = 0; w < 4; ++w)   // values that do not turn keep their bits; rotary_dim is even, so by the pair
-                    if (u * 8 + 2 * w >= 2 * p.pairs) got[w] = was[w];
-                *reinterpret_cast<uint4 *>(dst + u * 8) = make_uint4(got[0], got[1], got[2], got[3]);
-            }
-            __syncwarp();
+        for (int i = 0; i < U; ++i) {
+            const int at = h + i * p.heads + hslot;
+            if (here && at < hi) raw[i] = *reinterpret_cast<const uint4 *>(src + at * s_step);
         }
+    };
+    load();
+    float c[ANGLES], s[ANGLES];
+    {   // every lane takes ANGLES / heads of its unit's angles, then the lanes of the unit's other heads hand theirs over
+        const int mine = ANGLES / p.heads;
+        float cm[ANGLES], sm[ANGLES];
+#pragma unroll
+        for (int i = 0; i < ANGLES; ++i) {
+            cm[i] = 1.f;
+            sm[i] = 0.f;
+            if (i >= mine) continue;
+            const int pair = pair_of<UNIT>(u, hslot * mine + i, p.pairs);
+            if (pair < p.pairs) {
+                double angle = 0.0;
+                if (p.pos == nullptr) angle = (double)l * p.freqs[pair];
+                else
+                    for (int a = 0; a < p.axes; ++a)
+                        angle = fma((double)p.pos[b * p.ps[0] + l * p.ps[1] + a * p.ps[2]], p.freqs[a * p.pairs + pair], angle);
+                const double turns = angle * INV_2PI;
+                sincospif(2.0f * (float)(turns - rint(turns)), &sm[i], &cm[i]);
+                cm[i] *= p.factor;
+                sm[i] *= p.factor * p.sin_sign;
+            }
+        }
+        if constexpr (UNIT == UNIT_HALF)
+#pragma unroll
+            for (int i = 0; i < ANGLES; ++i) sm[i] *= other_sign;
+        const int base = lane & ~(p.lanes * (p.heads - 1));   // this unit's lane in head slot 0
+#pragma unroll
+        for (int i = 0; i < ANGLES; ++i) {
+            c[i] = cm[i];
+            s[i] = sm[i];
+            if (p.heads == 2) {
+                const int from = base + (i / (ANGLES / 2)) * p.lanes;
+                c[i] = __shfl_sync(0xFFFFFFFFu, cm[i % (ANGLES / 2)], from);
+                s[i] = __shfl_sync(0xFFFFFFFFu, sm[i % (ANGLES / 2)], from);
+            } else if (p.heads == 4) {
+                const int from = base + (i / (ANGLES / 4)) * p.lanes;
+                c[i] = __shfl_sync(0xFFFFFFFFu, cm[i % (ANGLES / 4)], from);
+                s[i] = __shfl_sync(0xFFFFFFFFu, sm[i % (ANGLES / 4)], from);
+            }
+        }
+    }
+    while (true) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int at = h + i * p.heads + hslot;
+            const bool on = here && at < hi;
+            uint16_t *to = dst + at * d_step;
+            if constexpr (UNIT == UNIT_INTERLEAVED) {
+                if (!on) continue;
+                float x[8];
+                unpack<FP16>(raw[i], x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x0 = x[2 * e], x1 = x[2 * e + 1];
+                    x[2 * e] = x0 * c[e] - x1 * s[e];
+                    x[2 * e + 1] = x1 * c[e] + x0 * s[e];
+                }
+                uint4 got = pack<FP16>(x);
+                if (u * 4 + 3 >= p.pairs) {   // pairs that do not turn keep their bits (a NaN's too)
+                    got.w = raw[i].w;
+                    if (u * 4 + 2 >= p.pairs) got.z = raw[i].z;
+                    if (u * 4 + 1 >= p.pairs) got.y = raw[i].y;
+                    if (u * 4 + 0 >= p.pairs) got.x = raw[i].x;
+                }
+                *reinterpret_cast<uint4 *>(to) = got;
+            } else if constexpr (UNIT == UNIT_HALF) {
+                uint4 far;
+                far.x = __shfl_sync(0xFFFFFFFFu, raw[i].x, other);
+                far.y = __shfl_sync(0xFFFFFFFFu, raw[i].y, other);
+                far.z = __shfl_sync(0xFFFFFFFFu, raw[i].z, other);
+                far.w = __shfl_sync(0xFFFFFFFFu, raw[i].w, other);
+                if (!on) continue;
+                if (other != lane) {
+                    float x[8], y[8];
+                    unpack<FP16>(raw[i], x);
+                    unpack<FP16>(far, y);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = x[e] * c[e] + y[e] * s[e];
+                    *reinterpret_cast<uint4 *>(to) = pack<FP16>(x);
+                } else {
+                    *reinterpret_cast<uint4 *>(to) = raw[i];
+                }
+            } else {
+                // a head goes through shared memory (its lanes are in one warp), every lane makes its own 8 values
+                uint16_t *line = stage + (threadIdx.x / p.lanes) * p.lanes * 8;
+                if (on) *reinterpret_cast<uint4 *>(line + u * 8) = raw[i];
+                __syncwarp();
+                if (on) {
+                    float x[8];
+                    unpack<FP16>(raw[i], x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int v = u * 8 + e;
+                        if (v < p.pairs) x[e] = x[e] * c[e] - widen<FP16>(line[v + p.pairs]) * s[e];
+                        else if (v < 2 * p.pairs) x[e] = x[e] * c[e] + widen<FP16>(line[v - p.pairs]) * s[e];
+                    }
+                    const uint4 made = pack<FP16>(x);
+                    uint32_t got[4] = {made.x, made.y, made.z, made.w};
+                    const uint32_t was[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+                    for (int w = 0; w < 4; ++w)   // values that do not turn keep their bits; rotary_dim is even, so by the pair
+                        if (u * 8 + 2 * w >= 2 * p.pairs) got[w] = was[w];
+                    *reinterpret_cast<uint4 *>(to) = make_uint4(got[0], got[1], got[2], got[3]);
+                }
+                __syncwarp();
+            }
+        }
+        h += U * p.heads;
+        if (h >= hi) {
+            if (!more_k) break;
+            more_k = false;
+            enter(true);
+        }
+        load();
     }
 }
 
 template <bool FP16>
 cudaError_t launch_rope(const RopeParams &p, int unit, cudaStream_t st) {
-    const unsigned grid = (unsigned)(((long long)p.B * p.L + p.tokens - 1) / p.tokens);
+    const long long warps = ((long long)p.B * p.L + p.per_warp - 1) / p.per_warp * p.chunks;
+    const unsigned grid = (unsigned)((warps + ROPE_WARPS - 1) / ROPE_WARPS);
     if (unit == UNIT_INTERLEAVED) rope_kernel<FP16, UNIT_INTERLEAVED><<<grid, ROPE_THREADS, 0, st>>>(p);
     else if (unit == UNIT_HALF) rope_kernel<FP16, UNIT_HALF><<<grid, ROPE_THREADS, 0, st>>>(p);
     else rope_kernel<FP16, UNIT_HALF_ODD><<<grid, ROPE_THREADS, 0, st>>>(p);
@@ -238,18 +304,21 @@ extern "C" dt_status dt_rope(const dt_rope_config *cfg, const void *q_dev, const
     p.pos = positions_dev;
     p.B = c.B; p.L = c.L; p.Hq = c.H; p.Ht = c.H + c.H_k; p.D = c.D;
     p.pairs = c.rotary_dim / 2;
-    p.pitch = (p.pairs + 7) / 8 * 8;
     p.axes = c.axes;
     const int unit = c.layout == DT_ROPE_INTERLEAVED ? UNIT_INTERLEAVED : c.rotary_dim % 16 == 0 ? UNIT_HALF : UNIT_HALF_ODD;
-    p.units = unit == UNIT_HALF ? c.rotary_dim / 16 + (c.D - c.rotary_dim) / 8 : c.D / 8;
+    p.units = c.D / 8;
     p.lanes = 1;
     while (p.lanes < p.units) p.lanes *= 2;
-    // tokens per block: about 2048 units of work, no more than the tables hold, no fewer blocks than fill the GPU
-    const long long all = (long long)c.B * c.L;
-    long long tb = 2048 / ((long long)p.Ht * p.units);
-    if (tb > all / (2 * dev->sms)) tb = all / (2 * dev->sms);
-    if (tb > ROPE_TABLE / p.pitch) tb = ROPE_TABLE / p.pitch;
-    p.tokens = tb < 1 ? 1 : (int)tb;
+    p.heads = 1;
+    while (p.heads < 4 && p.heads * 2 * p.lanes <= 32 && p.heads < p.Ht) p.heads *= 2;
+    p.per_warp = 32 / (p.lanes * p.heads);
+    // a warp walks all heads of its tokens, fewer when there are too few tokens to fill the GPU
+    const long long groups = ((long long)c.B * c.L + p.per_warp - 1) / p.per_warp;
+    p.chunk = p.Ht;
+    while (p.chunk > p.heads && groups * ((p.Ht + p.chunk - 1) / p.chunk) < 32LL * dev->sms) p.chunk = (p.chunk + 1) / 2;
+    if (p.chunk < p.heads) p.chunk = p.heads;
+    p.chunks = (p.Ht + p.chunk - 1) / p.chunk;
+    if (groups * p.chunks > 0xFFFFFFF0LL) return ops_fail(DT_ERR_UNSUPPORTED, "more tokens and heads than one launch takes");
     p.factor = c.attn_factor;
     p.sin_sign = c.transpose ? -1.0f : 1.0f;
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -136,6 +136,15 @@ def test_frequency_refusals(lib, kw):
         dt.dt_rope_freqs(**kw)
 
 
+def test_packed_configs_have_the_layout_of_the_structures(lib):
+    pair = C.c_int64 * 2
+    for packed, st in ((dt._ROPE_CFG(*range(10), 1.5), dt.dt_rope_config(*range(10), 1.5)),
+                       (dt._CROSS_CFG(*range(7), 0.5), dt.dt_cross_config(*range(7), 0.5)),
+                       (dt._NORM_CFG(*range(8), 10, 11, 12, 13, 14, 15, 16, 17, 2.5),
+                        dt.dt_norm_config(*range(8), pair(10, 11), pair(12, 13), pair(14, 15), pair(16, 17), 2.5))):
+        assert packed == bytes(st)
+
+
 def test_rows_of_views_collapse_to_two_strides():
     x = torch.empty(2, 5, 9, 64)
     assert dt._norm_rows([x])[:2] == (1, 90)
