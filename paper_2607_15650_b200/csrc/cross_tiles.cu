@@ -1,19 +1,26 @@
 // dt_cross_attn for many query rows: flash attention in tensor-memory tiles, 256 query rows of one head per work item,
 // against all keys of the request.
 //
-// The split is that of the self-attention kernel: one persistent CTA per SM, 12 warps --
-//   warps 0-3 / 4-7  softmax of query tile 0 / 1 (128 rows each, one row per thread), and its epilogue
-//   warp 8           TMA producer: Q once per item, K and V tiles through a ring in the order the MMAs consume them
+// One persistent CTA per SM, 16 warps --
+//   warps 0-3 / 4-7  softmax of query tile 0 / 1 (128 rows each, one row per thread)
+//   warp 8           TMA producer: Q of an item, K and V tiles through a ring in the order the MMAs consume them
 //   warps 9, 10      MMA issuers of query tile 0 / 1
-//   warp 11          zeroes V rows of keys that do not count before the MMAs read them
-// -- and TMEM holds S | P0 | P1 | O0 | O1, with one place for S that the two tiles use in turn.
-// What differs: an item has few K/V tiles (4 for a prompt of 512), so the first tile's maximum and the epilogue weigh more;
-// the output goes straight to the caller's tensor; and the running maximum is exact: every tile's row maximum is taken, and
-// when it exceeds the reference by more than RESCALE_AT binades, O and l are rescaled (P <= 2^RESCALE_AT in between, which
-// bf16 and fp16 hold at full precision), so no logit is out of range.
+//   warp 11          masks: in tiles that hold keys that do not count, it zeroes their K and V rows in shared memory and
+//                    writes the tile's column of -inf / 0
+//   warps 12-15      epilogue of both query tiles: O from TMEM, divided by the sum, to the caller's tensor
+// -- and TMEM holds S | P0 | P1 | O0 | O1, with one place for S that the two tiles use in turn, as in the self-attention
+// kernel.  What differs: an item has few K/V tiles (4 for a prompt of 512), so nothing may wait at its end.  The tiles of
+// all items of a CTA are one stream (the next item's first Q K^T is issued like any other, ahead of this item's last P V), and
+// the epilogue has warps of its own: with the softmax warps doing it, their turn at S held up the other tile for the whole of
+// it, 14100 cycles per item of 256 rows x 512 keys against 8192 of exponentials and as many of MMA.
+// The running maximum is exact: every tile's row maximum is taken, and when it exceeds the reference by more than RESCALE_AT
+// binades, O and l are rescaled (P <= 2^RESCALE_AT in between, which bf16 and fp16 hold at full precision), so no logit is out
+// of range.
 //
-// Keys that do not count: their logits are replaced by -inf (selected, so a NaN in K does not matter) and their V rows by
-// zeros in shared memory (0 * NaN would be NaN).  Tiles behind the last key that counts are never loaded.
+// Keys that do not count are masked by the MMA itself: Q K^T of such a tile gets one more k-step, a column of ones times a
+// column of -inf / 0, which leaves -inf in S for every one of them; their K and V rows are zeroed, so that what stands there
+// (NaN, infinities) has no effect.  The softmax does nothing for a mask (selecting 128 logits by bits took 800 cycles a tile).
+// Tiles behind the last key that counts are never loaded, and the last tile's P V stops at its last 16 keys that may.
 //
 // Every wait on an mbarrier is bounded; on expiry the CTA records STATUS_WAIT_TIMEOUT, leaves its loops, frees TMEM and
 // returns.
@@ -26,12 +33,12 @@ namespace {
 
 constexpr int NQ = 2, TILE = 128;                // query tiles in flight; rows of a query tile, keys of a K/V tile
 constexpr int SOFTMAX_THREADS = NQ * 128;
-constexpr int TMA_WARP = SOFTMAX_THREADS / 32, MMA_WARP = TMA_WARP + 1, ZERO_WARP = TMA_WARP + 3;
-constexpr int THREADS = SOFTMAX_THREADS + 128;
+constexpr int TMA_WARP = SOFTMAX_THREADS / 32, MMA_WARP = TMA_WARP + 1, ZERO_WARP = TMA_WARP + 3, OUT_WARP = TMA_WARP + 4;
+constexpr int THREADS = SOFTMAX_THREADS + 256;
 // setmaxnreg.inc only takes registers that a setmaxnreg.dec of the same CTA has released; LAUNCH_REGS is what ptxas
-// assigns under __launch_bounds__(384, 1), checked by cross_tiles_configure().
-constexpr int LAUNCH_REGS = 168, REGS_SOFTMAX = 208, REGS_OTHER = 88;
-static_assert((REGS_SOFTMAX - LAUNCH_REGS) * SOFTMAX_THREADS <= (LAUNCH_REGS - REGS_OTHER) * 128,
+// assigns under __launch_bounds__(512, 1), checked by cross_tiles_configure().
+constexpr int LAUNCH_REGS = 128, REGS_SOFTMAX = 184, REGS_OTHER = 64, REGS_OUT = 80;
+static_assert((REGS_SOFTMAX - LAUNCH_REGS) * SOFTMAX_THREADS <= (LAUNCH_REGS - REGS_OTHER) * 128 + (LAUNCH_REGS - REGS_OUT) * 128,
               "softmax warps would wait forever for registers nobody releases");
 constexpr long long WAIT_LIMIT_CYCLES = 4000000000ll;   // SM clock cycles: about 2 s
 constexpr float RESCALE_AT = 8.0f;
@@ -44,17 +51,22 @@ struct Cfg {
     static constexpr int STAGES = (D == 128) ? 4 : 8;
     static constexpr int Q_BYTES = NQ * TILE_BYTES;
     static constexpr int KV_BYTES = STAGES * TILE_BYTES;
-    static constexpr int OUT_BYTES = NQ * TILE * 128;         // epilogue staging: 8 warps x [32 rows x 128 bytes]
-    static constexpr int NBARS = 2 + 3 * STAGES + 7 * NQ;
-    static constexpr int SMEM_BYTES = 1024 /*alignment slack*/ + Q_BYTES + KV_BYTES + OUT_BYTES + NBARS * 8 + 64;
+    static constexpr int OUT_BYTES = TILE * 128;              // epilogue staging: 4 warps x [32 rows x 128 bytes]
+    static constexpr int ML_BYTES = NQ * TILE * 8;            // (maximum, sum) of every row
+    // 16-byte pieces of 128 rows: a ring stage's column of -inf / 0, then ones, then zeros (the second pieces of both)
+    static constexpr int COL_BYTES = TILE * 16, MASK_BYTES = (STAGES + 2) * COL_BYTES;
+    static constexpr int NBARS = 3 * STAGES + 10 * NQ;
+    static constexpr int SMEM_BYTES = 1024 /*alignment slack*/ + Q_BYTES + KV_BYTES + OUT_BYTES + MASK_BYTES + ML_BYTES + NBARS * 8 + 64;
+    static_assert(SMEM_BYTES + 64 <= 227 * 1024, "beyond the shared memory of a CTA");
     static constexpr int S_COL = 0, P_COL = 128, P_STRIDE = 64, O_COL = 256;
     static_assert(O_COL + NQ * D <= 512, "beyond the tensor memory of an SM");
 };
 
 struct Bars {
-    uint32_t q_full, q_empty;
     uint32_t kv_full, kv_empty, kv_raw;                                // + 8*stage; raw: landed, rows still to be zeroed
-    uint32_t s_full, p_full, o_full, o_free, pv_done, s_free, s_req;   // + 8*q
+    uint32_t q_full, q_empty;                                          // + 8*q
+    uint32_t s_full, p_full, o_full, o_free, pv_done, ml_full, s_req;  // + 8*q
+    uint32_t s_free;
 };
 
 // Tensor maps' coordinates: a dimension of one entry, or one that repeats (stride 0), has one entry in the map too.
@@ -63,44 +75,60 @@ struct TileParams {
     CrossParams c;
     MapCoord mq, mk, mv;
     int qblocks;             // ceil(Lq / 256)
-    long long items;         // B * H * qblocks
+    int items;               // B * H * qblocks
+    int dq, dh, db;          // gridDim.x items on, in blocks, heads and requests
 };
 
-struct Item {
-    int b, h, hk, row0, tiles, len;
-};
-__device__ __forceinline__ Item decode(const TileParams &p, long long w) {
-    Item it;
-    const int bh = (int)(w / p.qblocks);
-    it.row0 = (int)(w - (long long)bh * p.qblocks) * (NQ * TILE);
-    it.b = bh / p.c.H;
-    it.h = bh - it.b * p.c.H;
-    it.hk = it.h / p.c.rep;
-    it.len = keys_of(p.c, it.b);
-    it.tiles = (it.len + TILE - 1) / TILE;
-    return it;
-}
-
-// Places of an item's K/V tiles in load order: K_0, K_1, V_0, K_2, V_1, ..., K_{n-1}, V_{n-2}, V_{n-1}
-__device__ __forceinline__ uint32_t k_place(int t) { return t == 0 ? 0u : (uint32_t)(2 * t - 1); }
-__device__ __forceinline__ uint32_t v_place(int t, int tiles) { return t + 1 == tiles ? (uint32_t)(2 * tiles - 1) : (uint32_t)(2 * t + 2); }
-__device__ __forceinline__ void place_of(int n, int tiles, bool &is_k, int &t) {
-    is_k = (n == 0) || ((n & 1) && n + 1 < 2 * tiles);
-    t = is_k ? (n + 1) / 2 : (n + 1 == 2 * tiles ? tiles - 1 : (n - 2) / 2);
-}
-// V rows of tile t may have to be zeroed: a mask may have holes anywhere, a length ends inside one tile (rows behind Lk are
-// zeros already: the tensor map ends there)
-__device__ __forceinline__ bool v_needs_zeroing(const CrossParams &p, const Item &it, int t) {
-    return p.key_mask != nullptr || (it.len < p.Lk && it.len < (t + 1) * TILE);
-}
-// Which of a tile's 128 keys count: one bit each, 32 in every word, the same in all lanes of the warp.
-__device__ __forceinline__ void tile_bits(const CrossParams &p, const Item &it, int t, int lane, uint32_t (&bits)[4]) {
-    const uint8_t *m = p.key_mask ? p.key_mask + it.b * p.mask_stride : nullptr;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const int key = t * TILE + 32 * w + lane;
-        bits[w] = __ballot_sync(0xFFFFFFFFu, key < it.len && (m == nullptr || __ldg(m + key) != 0));
+// The stream of a CTA's tiles: item after item, the items without keys left out.  K and V are loaded (and consumed) in the
+// order K_0, K_1, V_0, K_2, V_1, ..., K_n, V_{n-1}, ..., V_last, across items.  Stepping costs additions only: divisions here
+// were on the way to the next Q K^T (1400 cycles per item).
+struct Cursor {
+    int w, qb, h, b;         // item: block of 256 rows, head, request
+    int len, tiles, t;       // its keys and tiles; the current tile
+    bool valid;
+    __device__ __forceinline__ void first_item(const TileParams &p) {
+        w = blockIdx.x;
+        const int bh = w / p.qblocks;
+        qb = w - bh * p.qblocks;
+        b = bh / p.c.H;
+        h = bh - b * p.c.H;
+        look(p);
     }
+    __device__ __forceinline__ void next_item(const TileParams &p) {
+        w += gridDim.x;
+        qb += p.dq;
+        h += p.dh;
+        b += p.db;
+        if (qb >= p.qblocks) { qb -= p.qblocks; ++h; }
+        if (h >= p.c.H) { h -= p.c.H; ++b; }
+        look(p);
+    }
+    __device__ __forceinline__ void look(const TileParams &p) {
+        t = 0;
+        valid = w < p.items;
+        len = valid ? keys_of(p.c, b) : 0;
+        tiles = (len + TILE - 1) / TILE;
+    }
+    __device__ __forceinline__ void first(const TileParams &p) {
+        first_item(p);
+        while (valid && tiles == 0) next_item(p);
+    }
+    __device__ __forceinline__ void advance(const TileParams &p) {
+        if (++t < tiles) return;
+        do next_item(p);
+        while (valid && tiles == 0);
+    }
+    __device__ __forceinline__ bool last() const { return t + 1 == tiles; }
+    __device__ __forceinline__ int row0() const { return qb * (NQ * TILE); }
+    // keys in the tile that do not count: a mask may have holes anywhere, the last tile may be ragged
+    __device__ __forceinline__ bool masked(const CrossParams &c) const { return c.key_mask != nullptr || len < (t + 1) * TILE; }
+};
+
+// Shared-memory matrix descriptor without swizzle: core matrices of 8 rows x 16 bytes; `lbo`: to the next 16 bytes of a row,
+// `sbo`: to the next 8 rows.
+__device__ __forceinline__ uint64_t make_smem_desc_plain(uint32_t smem_addr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
+    return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | (uint64_t)((lbo_bytes >> 4) & 0x3FFFu) << 16 |
+           (uint64_t)((sbo_bytes >> 4) & 0x3FFFu) << 32 | (uint64_t)1 << 46;
 }
 
 // O (this thread's row, D fp32 columns) times alpha, in place.  Out of line: it runs once in many tiles.
@@ -118,7 +146,8 @@ __device__ __noinline__ void scale_o(uint32_t o_tmem, float alpha) {
     tmem_wait_st();
 }
 
-template <int D, bool FP16>
+// MASKED: some tile may hold keys that do not count (lengths, a mask, or Lk not a multiple of 128); without it nothing looks.
+template <int D, bool FP16, bool MASKED>
 __global__ void __launch_bounds__(THREADS, 1)
 cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                   const __grid_constant__ CUtensorMap tmap_v, const TileParams p) {
@@ -131,20 +160,23 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     const uint32_t q_smem = smem_base;
     const uint32_t kv_smem = q_smem + C::Q_BYTES;
     const uint32_t out_smem = kv_smem + C::KV_BYTES;
-    const uint32_t bar_base = out_smem + C::OUT_BYTES;
+    const uint32_t mask_smem = out_smem + C::OUT_BYTES, ones_smem = mask_smem + C::STAGES * C::COL_BYTES, zeros_smem = ones_smem + C::COL_BYTES;
+    const uint32_t ml_smem = mask_smem + C::MASK_BYTES;   // [query tile][row]: (m, l)
+    const uint32_t bar_base = ml_smem + C::ML_BYTES;
     Bars bars;
-    bars.q_full = bar_base;
-    bars.q_empty = bar_base + 8;
-    bars.kv_full = bar_base + 16;
+    bars.kv_full = bar_base;
     bars.kv_empty = bars.kv_full + 8 * C::STAGES;
     bars.kv_raw = bars.kv_empty + 8 * C::STAGES;
-    bars.s_full = bars.kv_raw + 8 * C::STAGES;
+    bars.q_full = bars.kv_raw + 8 * C::STAGES;
+    bars.q_empty = bars.q_full + 8 * NQ;
+    bars.s_full = bars.q_empty + 8 * NQ;
     bars.p_full = bars.s_full + 8 * NQ;
     bars.o_full = bars.p_full + 8 * NQ;
     bars.o_free = bars.o_full + 8 * NQ;
     bars.pv_done = bars.o_free + 8 * NQ;
-    bars.s_free = bars.pv_done + 8 * NQ;   // only [0] is used, by both tiles in turn
-    bars.s_req = bars.s_free + 8 * NQ;
+    bars.ml_full = bars.pv_done + 8 * NQ;
+    bars.s_req = bars.ml_full + 8 * NQ;
+    bars.s_free = bars.s_req + 8 * NQ;   // one place for S: one barrier, used by both tiles in turn
 
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     volatile int *abort_ptr = &abort_flag;
@@ -154,34 +186,116 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
 
     if (warp == TMA_WARP && lane == 0) {
         abort_flag = 0;
-        mbar_init(bars.q_full, 1);
-        mbar_init(bars.q_empty, 2);   // a commit of each MMA warp
         for (int s = 0; s < C::STAGES; ++s) {
             mbar_init(bars.kv_full + 8 * s, 1);
-            mbar_init(bars.kv_empty + 8 * s, 2);
+            mbar_init(bars.kv_empty + 8 * s, 2);   // a commit of each MMA warp
             mbar_init(bars.kv_raw + 8 * s, 1);
         }
         for (int q = 0; q < NQ; ++q) {
+            mbar_init(bars.q_full + 8 * q, 1);
+            mbar_init(bars.q_empty + 8 * q, 1);
             mbar_init(bars.s_full + 8 * q, 1);
             mbar_init(bars.p_full + 8 * q, 128);
-            mbar_init(bars.s_free + 8 * q, 128);
             mbar_init(bars.o_full + 8 * q, 1);
             mbar_init(bars.o_free + 8 * q, 128);
             mbar_init(bars.pv_done + 8 * q, 1);
+            mbar_init(bars.ml_full + 8 * q, 128);
             mbar_init(bars.s_req + 8 * q, 128);
         }
+        mbar_init(bars.s_free, 128);
         fence_mbar_init();
     }
     if (warp == 0) {
         tmem_alloc(smem_u32(&tmem_base_slot), 512);
         tmem_relinquish();
     }
+    if (MASKED && warp == ZERO_WARP) {   // the constant columns: 1, 0, 0, ... and zeros
+        for (int r = lane; r < TILE; r += 32) {
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %2, %2};" ::"r"(ones_smem + r * 16), "r"(FP16 ? 0x3C00u : 0x3F80u), "r"(0) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(zeros_smem + r * 16), "r"(0) : "memory");
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = tmem_base_slot;
 
-    if (warp >= TMA_WARP) {
+    if (warp >= OUT_WARP) {
+        reg_dealloc<REGS_OUT>();
+        // ------------------------------------------------------------ epilogue of both query tiles
+        const int row_in_tile = (warp % 4) * 32 + lane;
+        const uint32_t lane_addr = ((uint32_t)((warp % 4) * 32)) << 16;
+        const uint32_t stage = out_smem + (warp % 4) * 4096, my_row = stage + lane * 128;
+        const int piece = lane & 7;
+        uint32_t phase = 0;
+        bool ok = true;
+        Cursor it;
+        for (it.first_item(p); it.valid && ok; it.next_item(p)) {
+            for (int q = 0; q < NQ && ok; ++q) {
+                const int q_row = it.row0() + q * TILE + row_in_tile;
+                const bool row_valid = q_row < p.c.Lq;
+                const long long lse_at = ((long long)it.b * p.c.H + it.h) * p.c.Lq + q_row;
+                uint16_t *gbase = p.c.out + it.b * p.c.os[0] + (long long)(q_row - lane) * p.c.os[1] + it.h * p.c.os[2];   // row 0 of this warp
+                float m = -INFINITY, l = 0.f;
+                const bool keys = it.tiles > 0;   // (no tile of a request without keys ever ran: O is not read)
+                const uint32_t o_tmem = tmem_base + lane_addr + C::O_COL + q * D;
+                if (keys) {
+                    ok = wait_all(bars.ml_full + 8 * q, phase) && wait_all(bars.o_full + 8 * q, phase);
+                    if (!ok) break;
+                    tc_fence_after();
+                    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(m), "=f"(l) : "r"(ml_smem + (q * TILE + row_in_tile) * 8) : "memory");
+                }
+                const float inv_l = l == 0.f ? 0.f : 1.0f / l;   // a row without keys: OUT = 0, LSE = -inf
+                if (row_valid && p.c.lse != nullptr) p.c.lse[lse_at] = l == 0.f ? -INFINITY : LN2 * (m + log2f(l));
+                // Rows leave through warp-private shared memory: 128 bytes of every row at a time (swizzled), read back so
+                // that 8 lanes hold the 128 contiguous bytes of one row.
+                const int rows_left = p.c.Lq - (q_row - lane);   // valid rows of this warp's 32
+#pragma unroll
+                for (int c0 = 0; c0 < D; c0 += 64) {
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        uint32_t o[32];
+                        if (keys) {
+                            tmem_ld_x32(o_tmem + c0 + 32 * half, o);
+                            tmem_wait_ld();
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) o[c] = 0u;
+                        }
+                        if (keys && c0 + 64 >= D && half == 1) {   // O and (m, l) are read: the next item's first P V may overwrite O
+                            tc_fence_before();
+                            mbar_arrive(bars.o_free + 8 * q);
+                        }
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t v[4];
+#pragma unroll
+                            for (int u = 0; u < 4; ++u)
+                                v[u] = pack_half2<FP16>(__uint_as_float(o[8 * c + 2 * u]) * inv_l, __uint_as_float(o[8 * c + 2 * u + 1]) * inv_l);
+                            const uint32_t dst = my_row + (uint32_t)(((4 * half + c) ^ (lane & 7)) << 4);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+                        }
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int r = i * 4 + (lane >> 3);
+                        uint4 v;
+                        const uint32_t src = stage + r * 128 + (uint32_t)((piece ^ (r & 7)) << 4);
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(src) : "memory");
+                        if (r < rows_left) __stcs(reinterpret_cast<uint4 *>(gbase + r * p.c.os[1] + c0 + piece * 8), v);
+                    }
+                    __syncwarp();
+                }
+            }
+            if (it.tiles > 0) phase ^= 1u;
+        }
+        if (!ok && lane == 0) {
+            if (!*abort_ptr) atomicOr(p.c.status, STATUS_WAIT_TIMEOUT);
+            *abort_ptr = 1;
+        }
+    } else if (warp >= TMA_WARP) {
         reg_dealloc<REGS_OTHER>();
         if (warp == TMA_WARP) {
             // -------------------------------------------------------- TMA producer
@@ -191,34 +305,46 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 prefetch_tensormap(&tmap_v);
                 uint32_t q_phase = 0, st = 0, ph = 0;
                 bool ok = true;
-                for (long long w = blockIdx.x; w < p.items && ok; w += gridDim.x) {
-                    const Item it = decode(p, w);
-                    if (it.tiles == 0) continue;
-                    ok = wait(bars.q_empty, q_phase ^ 1u);
-                    if (!ok) break;
-                    mbar_arrive_expect_tx(bars.q_full, C::Q_BYTES);
+                auto load_q = [&](const Cursor &it) {
 #pragma unroll
-                    for (int q = 0; q < NQ; ++q)
-#pragma unroll
-                        for (int hf = 0; hf < C::NHALF; ++hf)
-                            tma_load_4d(q_smem + q * C::TILE_BYTES + hf * C::HALF_BYTES, &tmap_q, bars.q_full, hf * 64, it.h * p.mq.mul_h,
-                                        it.row0 + q * TILE, it.b * p.mq.mul_b);
-                    q_phase ^= 1u;
-                    for (int n = 0; n < 2 * it.tiles; ++n) {
-                        bool is_k;
-                        int t;
-                        place_of(n, it.tiles, is_k, t);
-                        ok = wait(bars.kv_empty + 8 * st, ph ^ 1u);
+                    for (int q = 0; q < NQ; ++q) {
+                        ok = ok && wait(bars.q_empty + 8 * q, q_phase ^ 1u);
                         if (!ok) break;
-                        // V tiles with rows to zero land on a barrier of their own; the zeroing warp passes them on
-                        const uint32_t bar = (!is_k && v_needs_zeroing(p.c, it, t) ? bars.kv_raw : bars.kv_full) + 8 * st;
-                        mbar_arrive_expect_tx(bar, C::TILE_BYTES);
-                        const int h = it.hk * (is_k ? p.mk.mul_h : p.mv.mul_h), b = it.b * (is_k ? p.mk.mul_b : p.mv.mul_b);
+                        mbar_arrive_expect_tx(bars.q_full + 8 * q, C::TILE_BYTES);
 #pragma unroll
                         for (int hf = 0; hf < C::NHALF; ++hf)
-                            tma_load_4d(kv_smem + st * C::TILE_BYTES + hf * C::HALF_BYTES, is_k ? &tmap_k : &tmap_v, bar, hf * 64, h, t * TILE, b);
-                        if (++st == C::STAGES) { st = 0; ph ^= 1u; }
+                            tma_load_4d(q_smem + q * C::TILE_BYTES + hf * C::HALF_BYTES, &tmap_q, bars.q_full + 8 * q, hf * 64,
+                                        it.h * p.mq.mul_h, it.row0() + q * TILE, it.b * p.mq.mul_b);
                     }
+                    q_phase ^= 1u;
+                };
+                auto load_kv = [&](const Cursor &it, bool is_k) {
+                    ok = ok && wait(bars.kv_empty + 8 * st, ph ^ 1u);
+                    if (!ok) return;
+                    // tiles with keys that do not count land on a barrier of their own; the masking warp passes them on
+                    const uint32_t bar = (MASKED && it.masked(p.c) ? bars.kv_raw : bars.kv_full) + 8 * st;
+                    mbar_arrive_expect_tx(bar, C::TILE_BYTES);
+                    const int hk = p.c.rep == 1 ? it.h : it.h / p.c.rep;
+                    const int h = hk * (is_k ? p.mk.mul_h : p.mv.mul_h), b = it.b * (is_k ? p.mk.mul_b : p.mv.mul_b);
+#pragma unroll
+                    for (int hf = 0; hf < C::NHALF; ++hf)
+                        tma_load_4d(kv_smem + st * C::TILE_BYTES + hf * C::HALF_BYTES, is_k ? &tmap_k : &tmap_v, bar, hf * 64, h, it.t * TILE, b);
+                    if (++st == C::STAGES) { st = 0; ph ^= 1u; }
+                };
+                Cursor cur;
+                cur.first(p);
+                if (cur.valid) {
+                    load_q(cur);
+                    load_kv(cur, true);
+                }
+                while (cur.valid && ok) {
+                    Cursor nxt = cur;
+                    nxt.advance(p);
+                    if (nxt.valid) load_kv(nxt, true);
+                    load_kv(cur, false);
+                    // (after this V: nothing that Q's place waits for is behind it)
+                    if (nxt.valid && nxt.t == 0) load_q(nxt);
+                    cur = nxt;
                 }
                 if (!ok) {
                     if (!*abort_ptr) atomicOr(p.c.status, STATUS_WAIT_TIMEOUT);
@@ -229,121 +355,156 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 }
             }
         } else if (warp == ZERO_WARP) {
-            // -------------------------------------------------------- V rows of keys that do not count
-            if (p.c.key_mask != nullptr || p.c.key_lens != nullptr) {
-                uint32_t st = 0, raw_ph = 0;   // ring stage; parity of every stage's kv_raw (one bit each)
-                bool ok = true;
-                for (long long w = blockIdx.x; w < p.items && ok; w += gridDim.x) {
-                    const Item it = decode(p, w);
-                    for (int n = 0; n < 2 * it.tiles; ++n) {
-                        bool is_k;
-                        int t;
-                        place_of(n, it.tiles, is_k, t);
-                        if (!is_k && v_needs_zeroing(p.c, it, t)) {
-                            uint32_t bits[4];
-                            tile_bits(p.c, it, t, lane, bits);
-                            ok = wait_all(bars.kv_raw + 8 * st, (raw_ph >> st) & 1u);
-                            if (!ok) break;
-                            raw_ph ^= 1u << st;
+          if constexpr (MASKED) {
+            // -------------------------------------------------------- tiles with keys that do not count
+            uint32_t st = 0, raw_ph = 0;   // ring stage; parity of every stage's kv_raw (one bit each)
+            bool ok = true;
+            auto mask_tile = [&](const Cursor &it, bool is_k) {
+                if (it.masked(p.c)) {
+                    const uint8_t *m = p.c.key_mask ? p.c.key_mask + it.b * p.c.mask_stride : nullptr;
+                    bool on[4];
 #pragma unroll
-                            for (int wd = 0; wd < 4; ++wd)
-                                if (!(bits[wd] >> lane & 1u)) {
-                                    const uint32_t row = kv_smem + st * C::TILE_BYTES + (32 * wd + lane) * 128;
-#pragma unroll
-                                    for (int c = 0; c < C::NHALF * 8; ++c)   // (pieces in a lane's own order: the rows' banks coincide)
-                                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(row + (c >> 3) * C::HALF_BYTES + (((c + lane) & 7) << 4)), "r"(0) : "memory");
-                                }
-                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(bars.kv_full + 8 * st);
-                        }
-                        if (++st == C::STAGES) st = 0;
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = it.t * TILE + 32 * i + lane;
+                        on[i] = key < it.len && (m == nullptr || __ldg(m + key) != 0);
                     }
+                    ok = wait_all(bars.kv_raw + 8 * st, (raw_ph >> st) & 1u);
+                    if (!ok) return;
+                    raw_ph ^= 1u << st;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = 32 * i + lane;
+                        if (!on[i] && it.t * TILE + r < p.c.Lk) {   // (rows behind Lk are zeros: the tensor map ends there)
+                            const uint32_t row = kv_smem + st * C::TILE_BYTES + r * 128;
+#pragma unroll
+                            for (int c = 0; c < C::NHALF * 8; ++c)   // (pieces in a lane's own order: the rows' banks coincide)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(row + (c >> 3) * C::HALF_BYTES + (((c + lane) & 7) << 4)), "r"(0) : "memory");
+                        }
+                        if (is_k)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %2, %2};" ::"r"(mask_smem + st * C::COL_BYTES + r * 16), "r"(on[i] ? 0u : FP16 ? 0xFC00u : 0xFF80u), "r"(0) : "memory");
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bars.kv_full + 8 * st);
                 }
-                if (!ok) {
-                    if (lane == 0 && !*abort_ptr) atomicOr(p.c.status, STATUS_WAIT_TIMEOUT);
-                    *abort_ptr = 1;
-                }
+                if (++st == C::STAGES) st = 0;
+            };
+            Cursor cur;
+            cur.first(p);
+            if (cur.valid) mask_tile(cur, true);
+            while (cur.valid && ok) {
+                Cursor nxt = cur;
+                nxt.advance(p);
+                if (nxt.valid) mask_tile(nxt, true);
+                if (ok) mask_tile(cur, false);
+                cur = nxt;
             }
+            if (!ok) {
+                if (lane == 0 && !*abort_ptr) atomicOr(p.c.status, STATUS_WAIT_TIMEOUT);
+                *abort_ptr = 1;
+            }
+          }
         } else {
             // -------------------------------------------------------- MMA issuer of query tile mq
             const bool leader = (lane == 0);
             const int mq = warp - MMA_WARP;
-            constexpr uint32_t IDESC_QK = make_idesc_bf16_f32(128, TILE, false, FP16);
-            constexpr uint32_t IDESC_PV = make_idesc_bf16_f32(128, D, true, FP16);
             const uint64_t qdesc = make_smem_desc_sw128(q_smem + mq * C::TILE_BYTES, 16, 1024);
             const uint64_t kdesc0 = make_smem_desc_sw128(kv_smem, 16, 1024);
             const uint64_t vdesc0 = make_smem_desc_sw128(kv_smem, C::HALF_BYTES, 1024);
-            auto issue_qk = [&](uint32_t st) {
+            const uint64_t ones_desc = make_smem_desc_plain(ones_smem, zeros_smem - ones_smem, 128);
+            // S = Q K^T for the K tile in ring stage `st`; -inf for keys that do not count
+            auto issue_qk = [&](uint32_t st, bool masked) {
+                constexpr uint32_t IDESC_QK = make_idesc_bf16_f32(128, TILE, false, FP16);
                 const uint64_t b0 = kdesc0 + (uint64_t)((st * C::TILE_BYTES) >> 4);
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) {
                     const uint32_t koff = ((kk / 4) * C::HALF_BYTES + (kk % 4) * 32) >> 4;
                     if (leader) mma_ss(tmem_base + C::S_COL, qdesc + koff, b0 + koff, IDESC_QK, kk > 0 ? 1u : 0u);
                 }
+                if (MASKED && masked) {
+                    const uint32_t col = mask_smem + st * C::COL_BYTES;
+                    if (leader) mma_ss(tmem_base + C::S_COL, ones_desc, make_smem_desc_plain(col, zeros_smem - col, 128), IDESC_QK, 1u);
+                }
             };
+            // O (+)= P V
             auto issue_pv = [&](uint32_t st, bool accumulate) {
+                constexpr uint32_t IDESC_PV = make_idesc_bf16_f32(128, D, true, FP16);
                 const uint64_t b0 = vdesc0 + (uint64_t)((st * C::TILE_BYTES) >> 4);
                 const uint32_t d = tmem_base + C::O_COL + mq * D, a = tmem_base + C::P_COL + mq * C::P_STRIDE;
 #pragma unroll
                 for (int kk = 0; kk < TILE / 16; ++kk)
                     if (leader) mma_ts(d, a + kk * 8, b0 + (uint64_t)((kk * 2048) >> 4), IDESC_PV, (accumulate || kk > 0) ? 1u : 0u);
             };
-            uint32_t abs0 = 0, q_phase = 0, of_phase = 0, t_phase = 0;   // abs0: K/V tiles before this item
             // The one place for S is used by the tiles in turn, tile 0 first: a phase of s_free is one read of S.
             const uint32_t s_turn = mq ? 0u : 1u;
+            uint32_t place = 0, q_phase = 0, of_phase = 0, t_phase = 0;   // place: K/V tiles of the stream so far
             bool ok = true;
-            for (long long w = blockIdx.x; w < p.items && ok; w += gridDim.x) {
-                const Item it = decode(p, w);
-                if (it.tiles == 0) continue;
-                uint32_t st = abs0 % C::STAGES;
-                ok = wait_all(bars.q_full, q_phase) && wait_all(bars.kv_full + 8 * st, (abs0 / C::STAGES) & 1u) && wait_all(bars.s_free, s_turn);
-                if (!ok) break;
-                q_phase ^= 1u;
-                tc_fence_after();
-                issue_qk(st);
-                if (leader) {
-                    tc_commit(bars.s_full + 8 * mq);
-                    tc_commit(bars.kv_empty + 8 * st);
-                    if (it.tiles == 1) tc_commit(bars.q_empty);
+            Cursor cur;
+            cur.first(p);
+            if (cur.valid) {   // the stream's first Q K^T
+                ok = wait_all(bars.q_full + 8 * mq, 0u) && wait_all(bars.kv_full, 0u) && wait_all(bars.s_free, s_turn);
+                if (ok) {
+                    q_phase = 1u;
+                    tc_fence_after();
+                    issue_qk(0, cur.masked(p.c));
+                    if (leader) {
+                        tc_commit(bars.s_full + 8 * mq);
+                        tc_commit(bars.kv_empty);
+                        if (cur.tiles == 1) tc_commit(bars.q_empty + 8 * mq);
+                    }
+                    place = 1;
                 }
-                for (int k = 0; k < it.tiles; ++k) {
-                    const bool more = (k + 1 < it.tiles);
-                    const uint32_t av = abs0 + v_place(k, it.tiles);
-                    const uint32_t stv = av % C::STAGES;
+            }
+            while (cur.valid && ok) {
+                // (the next item is looked up while this one's first tiles run)
+                Cursor nxt = cur;
+                nxt.t = nxt.tiles - 1;
+                nxt.advance(p);
+                const bool next_item = nxt.valid, next_single = nxt.tiles == 1;
+                const bool next_masked = MASKED && nxt.masked(p.c), any_mask = MASKED && p.c.key_mask != nullptr;
+                const bool ragged = MASKED && cur.len < cur.tiles * TILE;
+                const int tiles = cur.tiles;
+                for (int k = 0; k < tiles; ++k) {
+                    const bool within = k + 1 < tiles, more = within || next_item;
+                    const uint32_t av = place + (more ? 1u : 0u), stv = av % C::STAGES;   // V of this tile
                     ok = wait_all(bars.s_req + 8 * mq, t_phase);   // the softmax will be ready for its next S shortly
                     if (!ok) break;
-                    if (more) {   // Q K_{k+1}^T first: the softmax waits for it; K, V and the place for S behind one vote
-                        const uint32_t ak = abs0 + k_place(k + 1);
-                        st = ak % C::STAGES;
-                        const bool r = wait(bars.kv_full + 8 * st, (ak / C::STAGES) & 1u) && wait(bars.kv_full + 8 * stv, (av / C::STAGES) & 1u) &&
-                                       wait(bars.s_free, s_turn);
+                    if (more) {   // the next tile's Q K^T first: the softmax waits for it.  What it needs, and V, behind one vote
+                        const uint32_t st = place % C::STAGES;
+                        bool r = wait(bars.kv_full + 8 * st, (place / C::STAGES) & 1u) && wait(bars.kv_full + 8 * stv, (av / C::STAGES) & 1u) &&
+                                 wait(bars.s_free, s_turn);
+                        if (!within) {
+                            r = r && wait(bars.q_full + 8 * mq, q_phase);
+                            q_phase ^= 1u;
+                        }
                         ok = __all_sync(0xFFFFFFFFu, r) != 0;
                         if (!ok) break;
                         tc_fence_after();
-                        issue_qk(st);
+                        issue_qk(st, within ? any_mask || (ragged && k + 2 == tiles) : next_masked);
                         if (leader) {
                             tc_commit(bars.s_full + 8 * mq);
                             tc_commit(bars.kv_empty + 8 * st);
-                            if (k + 2 == it.tiles) tc_commit(bars.q_empty);   // that was the item's last Q K^T
+                            if (within ? k + 2 == tiles : next_single) tc_commit(bars.q_empty + 8 * mq);   // its item's last Q K^T
                         }
                     }
-                    ok = wait_all(bars.p_full + 8 * mq, t_phase);   // P_k is stored
-                    if (!ok) break;
-                    if (!more) ok = wait_all(bars.kv_full + 8 * stv, (av / C::STAGES) & 1u);
-                    if (!ok) break;
-                    if (k == 0) ok = wait_all(bars.o_free + 8 * mq, of_phase ^ 1u);   // the previous item's epilogue has drained O
+                    ok = wait_all(bars.p_full + 8 * mq, t_phase);   // P is stored
+                    if (ok && !more) ok = wait_all(bars.kv_full + 8 * stv, (av / C::STAGES) & 1u);
+                    if (ok && k == 0) {   // the epilogue of the item before has drained O
+                        ok = wait_all(bars.o_free + 8 * mq, of_phase ^ 1u);
+                        of_phase ^= 1u;
+                    }
                     if (!ok) break;
                     tc_fence_after();
                     issue_pv(stv, k > 0);
                     if (leader) {
-                        tc_commit(more ? bars.pv_done + 8 * mq : bars.o_full + 8 * mq);
+                        tc_commit(bars.pv_done + 8 * mq);
+                        if (!within) tc_commit(bars.o_full + 8 * mq);
                         tc_commit(bars.kv_empty + 8 * stv);
                     }
                     t_phase ^= 1u;
+                    place = av + 1;
                 }
-                of_phase ^= 1u;
-                abs0 += 2u * (uint32_t)it.tiles;
+                cur = nxt;
             }
             if (!ok) {
                 if (leader && !*abort_ptr) atomicOr(p.c.status, STATUS_WAIT_TIMEOUT);
@@ -352,40 +513,24 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         }
     } else {
         reg_alloc<REGS_SOFTMAX>();
-        // ------------------------------------------------------------ softmax and epilogue of query tile q
+        // ------------------------------------------------------------ softmax of query tile q
         const int q = warp / 4;
         const int row_in_tile = (warp % 4) * 32 + lane;
         const uint32_t lane_addr = ((uint32_t)((warp % 4) * 32)) << 16;
         const uint32_t s_tmem = tmem_base + lane_addr + C::S_COL;
         const uint32_t p_tmem = tmem_base + lane_addr + C::P_COL + q * C::P_STRIDE;
         const uint32_t o_tmem = tmem_base + lane_addr + C::O_COL + q * D;
-        uint32_t s_phase = 0, o_phase = 0, pv_phase = 0;
-        bool ok = true;
-        for (long long w = blockIdx.x; w < p.items && ok; w += gridDim.x) {
-            const Item it = decode(p, w);
-            const int q_row = it.row0 + q * TILE + row_in_tile;
-            const bool row_valid = q_row < p.c.Lq;
-            uint16_t *out_row = p.c.out + it.b * p.c.os[0] + (long long)q_row * p.c.os[1] + it.h * p.c.os[2];
-            const long long lse_at = ((long long)it.b * p.c.H + it.h) * p.c.Lq + q_row;
-            if (it.tiles == 0) {   // rows without keys
-                if (row_valid) {
-#pragma unroll
-                    for (int c = 0; c < D; c += 8) *reinterpret_cast<uint4 *>(out_row + c) = make_uint4(0, 0, 0, 0);
-                    if (p.c.lse != nullptr) p.c.lse[lse_at] = -INFINITY;
-                }
-                continue;
-            }
+        uint32_t s_phase = 0, pv_phase = 0, p_items = 0;   // p_items: items handed to the epilogue
+        bool ok = true, p_stored = false;   // p_stored: P's columns hold an earlier tile's P, which its P V may still read
+        Cursor it;
+        for (it.first(p); it.valid && ok; ) {
             float m_used = -INFINITY, l_sum = 0.f;
             for (int t = 0; t < it.tiles; ++t) {
-                // keys of this tile that count (looked up before the wait for S); all of them in most tiles
-                const bool partial = p.c.key_mask != nullptr || it.len < (t + 1) * TILE;
-                uint32_t bits[4] = {~0u, ~0u, ~0u, ~0u};
-                if (partial) tile_bits(p.c, it, t, lane, bits);
                 ok = wait_all(bars.s_full + 8 * q, s_phase);
                 if (!ok) break;
                 s_phase ^= 1u;
                 tc_fence_after();
-                uint32_t s[4][32];   // this thread's row of S: 128 fp32 logits (before scaling)
+                uint32_t s[4][32];   // this thread's row of S: fp32 logits (before scaling), -inf for keys that do not count
                 tmem_ld_x32(s_tmem + 0, s[0]);
                 tmem_ld_x32(s_tmem + 32, s[1]);
                 tmem_ld_x32(s_tmem + 64, s[2]);
@@ -393,11 +538,6 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 tmem_wait_ld();
                 tc_fence_before();
                 mbar_arrive(bars.s_free);   // S has been read: the next Q K^T may overwrite it
-                if (partial) {
-#pragma unroll
-                    for (int c = 0; c < 128; ++c)
-                        if (!(bits[c >> 5] >> (c & 31) & 1u)) s[c >> 5][c & 31] = 0xFF800000u;   // -inf
-                }
                 float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};   // four chains of three-input max
 #pragma unroll
                 for (int c = 0; c < 128; c += 8) {
@@ -406,11 +546,11 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                         mx4[u] = fmax3(mx4[u], __uint_as_float(s[(c + 2 * u) >> 5][(c + 2 * u) & 31]), __uint_as_float(s[(c + 2 * u + 1) >> 5][(c + 2 * u + 1) & 31]));
                 }
                 const float m_tile = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.c.scale_log2;
-                bool p_place_free = t == 0;   // P's columns may still be read by the previous tile's P V
+                bool p_place_free = !p_stored;
                 if (t == 0) {
                     m_used = m_tile;
                 } else if (__any_sync(0xFFFFFFFFu, m_tile > m_used + RESCALE_AT)) {
-                    // (O may only be touched once P_{t-1} V_{t-1} is complete)
+                    // (O may only be touched once the P V of the tile before is complete)
                     ok = wait_all(bars.pv_done + 8 * q, pv_phase);
                     if (!ok) break;
                     pv_phase ^= 1u;
@@ -426,24 +566,28 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 const float2 sc2 = make_float2(p.c.scale_log2, p.c.scale_log2), nm2 = make_float2(-m_ref, -m_ref);
                 float2 rs4[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                 uint32_t pk2[2][32];   // P as packed 16-bit pairs (even key in the low half)
+                auto exps = [&](int piece) {   // 32 keys
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-#pragma unroll
-                    for (int c = half * 64; c < half * 64 + 64; c += 2) {
+                    for (int c = piece * 32; c < piece * 32 + 32; c += 2) {
                         const float s0 = __uint_as_float(s[c >> 5][c & 31]), s1 = __uint_as_float(s[(c + 1) >> 5][(c + 1) & 31]);
                         const float2 x = __ffma2_rn(make_float2(s0, s1), sc2, nm2);
                         const float2 pp = make_float2(ex2_approx(x.x), ex2_approx(x.y));
                         rs4[(c >> 1) & 3] = __fadd2_rn(rs4[(c >> 1) & 3], pp);
-                        pk2[half][(c >> 1) & 31] = pack_half2<FP16>(pp.x, pp.y);
+                        pk2[c >> 6][(c >> 1) & 31] = pack_half2<FP16>(pp.x, pp.y);
                     }
-                    if (half == 0) mbar_arrive(bars.s_req + 8 * q);   // half of the exponentials are done: ask for the next S
-                }
-                if (!p_place_free) {   // P V of tile t-1 is done with P's columns
+                };
+                exps(0);
+                exps(1);
+                mbar_arrive(bars.s_req + 8 * q);   // half of the exponentials are done: ask for the next S
+                exps(2);
+                exps(3);
+                if (!p_place_free) {   // the P V of the tile before (of this item or the last) is done with P's columns
                     ok = wait_all(bars.pv_done + 8 * q, pv_phase);
                     if (!ok) break;
                     pv_phase ^= 1u;
                     tc_fence_after();
                 }
+                p_stored = true;
                 tmem_st_x32(p_tmem, pk2[0]);
                 tmem_st_x32(p_tmem + 32, pk2[1]);
                 const float2 r2 = __fadd2_rn(__fadd2_rn(rs4[0], rs4[1]), __fadd2_rn(rs4[2], rs4[3]));
@@ -453,49 +597,15 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 mbar_arrive(bars.p_full + 8 * q);
             }
             if (!ok) break;
-            ok = wait_all(bars.o_full + 8 * q, o_phase);
+            // (m, l) for the epilogue, once it has read the item before's: it hands O back behind that (with more than one tile it
+            // has long done so).  Without this wait ml_full could complete twice before the epilogue looks.
+            if (p_items > 0) ok = wait_all(bars.o_free + 8 * q, (p_items - 1) & 1u);
             if (!ok) break;
-            o_phase ^= 1u;
-            tc_fence_after();
-            const float inv_l = l_sum == 0.f ? 0.f : 1.0f / l_sum;   // a row without keys: OUT = 0, LSE = -inf
-            if (row_valid && p.c.lse != nullptr) p.c.lse[lse_at] = l_sum == 0.f ? -INFINITY : LN2 * (m_used + log2f(l_sum));
-            // Rows leave through warp-private shared memory: 128 bytes of every row at a time (swizzled), read back so
-            // that 8 lanes hold the 128 contiguous bytes of one row.
-            const uint32_t stage = out_smem + warp * 4096, my_row = stage + lane * 128;
-            const int rows_left = p.c.Lq - (q_row - lane);   // valid rows of this warp's 32
-            uint16_t *gbase = out_row - (long long)lane * p.c.os[1];
-            const int piece = lane & 7;
-#pragma unroll
-            for (int c0 = 0; c0 < D; c0 += 64) {
-                uint32_t o[2][32];
-                tmem_ld_x32(o_tmem + c0, o[0]);
-                tmem_ld_x32(o_tmem + c0 + 32, o[1]);
-                tmem_wait_ld();
-                if (c0 + 64 >= D) {   // O is read: the next item's first P V may overwrite it
-                    tc_fence_before();
-                    mbar_arrive(bars.o_free + 8 * q);
-                }
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    const uint32_t (&oo)[32] = o[(8 * c) / 32];
-                    const int b0 = (8 * c) % 32;
-                    uint32_t v[4];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) v[u] = pack_half2<FP16>(__uint_as_float(oo[b0 + 2 * u]) * inv_l, __uint_as_float(oo[b0 + 2 * u + 1]) * inv_l);
-                    const uint32_t dst = my_row + (uint32_t)((c ^ (lane & 7)) << 4);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
-                }
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int r = i * 4 + (lane >> 3);
-                    uint4 v;
-                    const uint32_t src = stage + r * 128 + (uint32_t)((piece ^ (r & 7)) << 4);
-                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(src) : "memory");
-                    if (r < rows_left) __stcs(reinterpret_cast<uint4 *>(gbase + r * p.c.os[1] + c0 + piece * 8), v);
-                }
-                __syncwarp();
-            }
+            ++p_items;
+            asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(ml_smem + (q * TILE + row_in_tile) * 8), "f"(m_used), "f"(l_sum) : "memory");
+            mbar_arrive(bars.ml_full + 8 * q);
+            it.t = it.tiles - 1;
+            it.advance(p);
         }
         if (!ok && lane == 0) {
             if (!*abort_ptr) atomicOr(p.c.status, STATUS_WAIT_TIMEOUT);
@@ -530,44 +640,57 @@ CUresult encode(void *fn, CUtensorMap *tm, MapCoord *mul, const void *base, cons
                                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
-template <int D, bool FP16>
+template <int D, bool FP16, bool MASKED>
 cudaError_t configure_one() {
     cudaFuncAttributes attr;
-    cudaError_t e = cudaFuncGetAttributes(&attr, cross_tile_kernel<D, FP16>);
+    cudaError_t e = cudaFuncGetAttributes(&attr, cross_tile_kernel<D, FP16, MASKED>);
     if (e != cudaSuccess) return e;
     if (attr.numRegs != LAUNCH_REGS) return cudaErrorInvalidConfiguration;   // the register hand-over would not balance
-    return cudaFuncSetAttribute(cross_tile_kernel<D, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::SMEM_BYTES);
+    return cudaFuncSetAttribute(cross_tile_kernel<D, FP16, MASKED>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::SMEM_BYTES);
+}
+template <int D, bool FP16>
+cudaError_t configure() {
+    cudaError_t e = configure_one<D, FP16, false>();
+    return e == cudaSuccess ? configure_one<D, FP16, true>() : e;
+}
+
+template <int D, bool FP16>
+cudaError_t launch(int grid, const CUtensorMap &tq, const CUtensorMap &tk, const CUtensorMap &tv, const TileParams &p, cudaStream_t st) {
+    if (p.c.key_lens != nullptr || p.c.key_mask != nullptr || p.c.Lk % TILE != 0)
+        cross_tile_kernel<D, FP16, true><<<grid, THREADS, Cfg<D>::SMEM_BYTES, st>>>(tq, tk, tv, p);
+    else
+        cross_tile_kernel<D, FP16, false><<<grid, THREADS, Cfg<D>::SMEM_BYTES, st>>>(tq, tk, tv, p);
+    return cudaGetLastError();
 }
 
 }  // namespace
 
 cudaError_t cross_tiles_configure() {
     cudaError_t e;
-    if ((e = configure_one<64, false>()) != cudaSuccess) return e;
-    if ((e = configure_one<64, true>()) != cudaSuccess) return e;
-    if ((e = configure_one<128, false>()) != cudaSuccess) return e;
-    return configure_one<128, true>();
+    if ((e = configure<64, false>()) != cudaSuccess) return e;
+    if ((e = configure<64, true>()) != cudaSuccess) return e;
+    if ((e = configure<128, false>()) != cudaSuccess) return e;
+    return configure<128, true>();
 }
 
 cudaError_t launch_cross_tiles(const CrossParams &c, int D, bool fp16, const OpsDevice &dev, cudaStream_t st) {
     TileParams p = {};
     p.c = c;
     p.qblocks = (c.Lq + NQ * TILE - 1) / (NQ * TILE);
-    p.items = (long long)c.B * c.H * p.qblocks;
+    const long long items = (long long)c.B * c.H * p.qblocks;
+    if (items > 0x3FFFFFFF) return cudaErrorInvalidValue;   // (2^38 query rows)
+    p.items = (int)items;
+    const int grid = p.items < dev.sms ? p.items : dev.sms;
+    p.dq = grid % p.qblocks;
+    p.dh = grid / p.qblocks % c.H;
+    p.db = grid / p.qblocks / c.H;
     CUtensorMap tq, tk, tv;
     if (encode(dev.encode_tiled, &tq, &p.mq, c.q, c.qs, c.B, c.Lq, c.H, D, fp16) != CUDA_SUCCESS ||
         encode(dev.encode_tiled, &tk, &p.mk, c.k, c.ks, c.B, c.Lk, c.Hkv, D, fp16) != CUDA_SUCCESS ||
         encode(dev.encode_tiled, &tv, &p.mv, c.v, c.vs, c.B, c.Lk, c.Hkv, D, fp16) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
-    const unsigned grid = (unsigned)(p.items < dev.sms ? p.items : dev.sms);
-    if (D == 64) {
-        if (fp16) cross_tile_kernel<64, true><<<grid, THREADS, Cfg<64>::SMEM_BYTES, st>>>(tq, tk, tv, p);
-        else cross_tile_kernel<64, false><<<grid, THREADS, Cfg<64>::SMEM_BYTES, st>>>(tq, tk, tv, p);
-    } else {
-        if (fp16) cross_tile_kernel<128, true><<<grid, THREADS, Cfg<128>::SMEM_BYTES, st>>>(tq, tk, tv, p);
-        else cross_tile_kernel<128, false><<<grid, THREADS, Cfg<128>::SMEM_BYTES, st>>>(tq, tk, tv, p);
-    }
-    return cudaGetLastError();
+    if (D == 64) return fp16 ? launch<64, true>(grid, tq, tk, tv, p, st) : launch<64, false>(grid, tq, tk, tv, p, st);
+    return fp16 ? launch<128, true>(grid, tq, tk, tv, p, st) : launch<128, false>(grid, tq, tk, tv, p, st);
 }
 
 }  // namespace dt

@@ -300,6 +300,25 @@ def test_cross_masks_with_nan_in_masked_places(Lk, Lq, D, dtype):
         assert (out[none] == 0).all() and torch.isinf(lse[none]).all() and none.any()
 
 
+@pytest.mark.parametrize("D,dtype", [(64, BF16), (128, FP16)])
+@pytest.mark.parametrize("Lk", [1, 77, 128, 129, 226, 300, 640])
+def test_cross_many_blocks_of_rows_per_sm(Lk, D, dtype):
+    """More blocks of 256 rows than the GPU has SMs, so that every SM takes several one after the other: one tile of keys each,
+    two, more, and (lengths) a mix with none.  A few (request, head) pairs are compared element by element."""
+    B, Lq, H = 3, 4000, 12
+    q, k, v = rnd((B, Lq, H, D), 1, dtype, 1.3), rnd((B, Lk, H, D), 2, dtype, 1.3), rnd((B, Lk, H, D), 3, dtype)
+    for lens in (None, torch.tensor([Lk, 0, (Lk + 1) // 2], dtype=torch.int32, device="cuda")):
+        out, lse = torch.full_like(q, 5.0), torch.full((B, H, Lq), 5.0, device="cuda")
+        dt.dt_cross_attn(q, k, v, out, D ** -0.5, key_lens=lens, lse_out=lse)
+        torch.cuda.synchronize()
+        dt.dt_poll_ops()
+        keep = keep_of(B, Lk, lens, None)
+        for h in (0, 5, 11):
+            wo, wl, to, tl = ref.cross(q[:, :, h:h + 1], k[:, :, h:h + 1], v[:, :, h:h + 1], D ** -0.5, keep)
+            check(lse[:, h:h + 1], wl, tl, (Lk, D, h, "lse"))
+            check(out[:, :, h:h + 1], wo, to, (Lk, D, h, "out"))
+
+
 @pytest.mark.parametrize("Lq,Lk", [(1, 0), (300, 0), (0, 5), (0, 0)])
 def test_cross_without_keys_or_queries(Lq, Lk):
     q, k = rnd((2, Lq, 4, 64), 1, BF16), rnd((2, Lk, 4, 64), 2, BF16)
