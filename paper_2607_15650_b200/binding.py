@@ -6,8 +6,8 @@ and streams.  If the shared library is missing this module raises: there is no f
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
-import struct
 
 import numpy as np
 import torch
@@ -201,56 +201,37 @@ def dt_plan_static(lse_state, offsets, B, H, L, mask_dev, eps=0.0, target_fracti
 
 
 # ---------------------------------------------------------------- operators around the self-attention (no context)
-# A call on small tensors takes as long as its marshalling: configs and strides are packed as the C structs' bytes in one
-# call each (struct.pack; the layouts are the structures' above) and a tensor's device is compared by its index.
-_VALUE = {torch.bfloat16: DT_VALUE_BF16, torch.float16: DT_VALUE_FP16, torch.float32: DT_VALUE_FP32}
-_S3, _S4 = struct.Struct("3q").pack, struct.Struct("4q").pack
-_ROPE_CFG, _NORM_CFG, _CROSS_CFG = struct.Struct("10if").pack, struct.Struct("4i2q2i8qf4x").pack, struct.Struct("7if").pack
+# dt_rope, dt_add_rmsnorm and dt_cross_attn are marshalled in C (csrc/ops_py.c); like the library they load on first use.
+OPS_PATH = os.path.join(_HERE, "_ditango_ops.so")
+_OPS = ("dt_rope", "dt_add_rmsnorm", "dt_cross_attn")
 
 
-def _on_device(index, fn, args, stream):
-    """One call with the tensors' device current: the stream's pointer goes last, a status other than DT_OK raises."""
-    if stream is None:
-        stream = torch._C._cuda_getCurrentRawStream(index)
-    else:
-        stream = stream.cuda_stream
-    if torch._C._cuda_getDevice() == index:
-        s = fn(*args, stream)
-    else:
+def _load_ops():
+    L = lib()
+    if not os.path.exists(OPS_PATH):
+        raise ImportError(f"{OPS_PATH} is missing: run `python -m paper_2607_15650_b200.build`")
+    spec = importlib.util.spec_from_file_location("_ditango_ops", OPS_PATH)
+    ops = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ops)
+
+    def on_device(index, name, args, kw):
         with torch.cuda.device(index):
-            s = fn(*args, stream)
-    if s != DT_OK:
-        raise DitangoError(s, status_str(s), lib().dt_last_error(None).decode())
+            return getattr(ops, name)(*args, **kw)
+
+    def raise_status(s):
+        raise DitangoError(s, status_str(s), L.dt_last_error(None).decode())
+
+    ops._bind(tuple(C.cast(getattr(L, n), C.c_void_p).value for n in _OPS),
+              (torch.bfloat16, torch.float16, torch.float32, torch.float64, torch.int32, torch.uint8, torch.bool, torch.float8_e4m3fn),
+              (torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, on_device, raise_status))
+    globals().update({n: getattr(ops, n) for n in _OPS}, _norm_rows=ops._norm_rows)
 
 
-def dt_rope(q, k, q_out, k_out, freqs, positions=None, layout=DT_ROPE_INTERLEAVED, attn_factor=1.0, transpose=False, stream=None):
-    """Rotary positions on q [B, L, H, D] and k [B, L, H_k, D] (k may be None) into q_out, k_out (which may be q, k).
-    `freqs` is float64 [axes, rotary_dim / 2] on the device, `positions` int32 [B, L, axes] ([B, L] for one axis; any
-    strides, expanded batches too) or None for the token's index."""
-    shape, dtype, dev = q.shape, q.dtype, q.get_device()
-    B, L, H, D = shape
-    axes, pairs = freqs.shape
-    assert dev >= 0 and q_out.shape == shape and q_out.dtype is dtype and q_out.get_device() == dev
-    assert freqs.dtype is torch.float64 and freqs.is_contiguous() and freqs.get_device() == dev
-    Hk, ks, kos, kp, kop = 0, None, None, None, None
-    if k is not None:
-        Hk = k.shape[2]
-        assert k.shape == (B, L, Hk, D) and k_out.shape == k.shape and k.dtype is dtype and k_out.dtype is dtype
-        assert k.get_device() == dev and k_out.get_device() == dev
-        ks, kos, kp, kop = _S4(*k.stride()), _S4(*k_out.stride()), k.data_ptr(), k_out.data_ptr()
-    pp = ps = None
-    if positions is not None:
-        assert positions.dtype is torch.int32 and positions.get_device() == dev
-        if positions.dim() == 3:
-            assert positions.shape == (B, L, axes)
-            ps = _S3(*positions.stride())
-        else:
-            assert axes == 1 and positions.shape == (B, L)
-            ps = _S3(*positions.stride(), 0)
-        pp = positions.data_ptr()
-    cfg = _ROPE_CFG(_VALUE[dtype], B, L, H, Hk, D, 2 * pairs, layout, axes, 1 if transpose else 0, attn_factor)
-    _on_device(dev, (_lib or lib()).dt_rope, (cfg, q.data_ptr(), _S4(*q.stride()), q_out.data_ptr(), _S4(*q_out.stride()), kp, ks, kop, kos,
-                                    freqs.data_ptr(), pp, ps), stream)
+def __getattr__(name):
+    if name in _OPS or name == "_norm_rows":
+        _load_ops()
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
 def dt_rope_freqs(rotary_dim, base=10000.0, kind=DT_ROPE_NONE, factor=1.0, trained_length=0, turns_fast=32.0, turns_slow=1.0):
@@ -273,100 +254,6 @@ def dt_rope_grid_freqs(dims, base=10000.0):
         table[a, at:at + d // 2] = dt_rope_freqs(d, base)[0]
         at += d // 2
     return table
-
-
-def _rows(t):
-    """(n0, n1, (stride0, stride1)) of the rows of t [..., width], whose leading dimensions have to collapse into two."""
-    dims = [(n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n != 1]
-    out = []
-    for n, s in dims:
-        if out and out[-1][1] == n * s:
-            out[-1] = (out[-1][0] * n, s)
-        else:
-            out.append((n, s))
-    assert len(out) <= 2 and (t.stride(-1) == 1 or t.shape[-1] == 1), "rows must have two strides at most, values stride 1"
-    out = [(1, 0)] * (2 - len(out)) + out
-    return out
-
-
-def _norm_rows(tensors):
-    """The rows of several tensors of one shape as one n0 x n1 and strides for each."""
-    if all(t.is_contiguous() for t in tensors):
-        w = tensors[0].shape[-1]
-        n = tensors[0].numel() // w if w else 0
-        return 1, n, [(0, w)] * len(tensors)
-    rows = [_rows(t) for t in tensors]
-    # a tensor whose rows collapse further than another's is split the same way
-    n0, n1 = next(((a[0], b[0]) for a, b in rows if a[0] != 1), (rows[0][0][0], rows[0][1][0]))
-    strides = []
-    for a, b in rows:
-        if (a[0], b[0]) == (n0, n1):
-            strides.append((a[1], b[1]))
-        else:
-            assert a[0] == 1 and b[0] == n0 * n1, "the tensors' rows do not have common strides"
-            strides.append((n1 * b[1], b[1]))
-    return n0, n1, strides
-
-
-def dt_add_rmsnorm(x, weight, y, eps, residual=None, residual_out=None, scales=None, stream=None):
-    """Norm of x (+ residual) over the last dimension into y: x's type, or float8_e4m3fn with `scales` fp32
-    [..., width / group] (group: 32, 64, 128 or the whole row).  residual_out takes the sum; it may be residual or x."""
-    shape, dtype, dev = x.shape, x.dtype, x.get_device()
-    w = shape[-1]
-    q8 = y.dtype is torch.float8_e4m3fn
-    assert dev >= 0 and y.shape == shape and (q8 or y.dtype is dtype) and y.get_device() == dev
-    rt, rp, rop = dtype, None, None
-    tensors = (x, y)
-    if residual is not None:
-        rt = residual.dtype
-        assert residual.shape == shape and residual_out.shape == shape and residual_out.dtype is rt
-        assert residual.get_device() == dev and residual_out.get_device() == dev
-        tensors = (x, y, residual, residual_out)
-        rp, rop = residual.data_ptr(), residual_out.data_ptr()
-    else:
-        assert residual_out is None
-    wt, wp = dtype, None
-    if weight is not None:
-        wt, wp = weight.dtype, weight.data_ptr()
-        assert weight.shape == (w,) and weight.get_device() == dev and weight.is_contiguous()
-    group, sp = 0, None
-    if q8:
-        per_row = scales.shape[-1]
-        assert scales.dtype is torch.float32 and scales.is_contiguous() and scales.get_device() == dev
-        assert scales.shape[:-1] == shape[:-1] and per_row > 0 and w % per_row == 0
-        group = 0 if per_row == 1 else w // per_row
-        sp = scales.data_ptr()
-    n0, n1, st = _norm_rows(tensors)
-    xs, ys, rs, ros = st if len(st) == 4 else (*st, (0, 0), (0, 0))
-    cfg = _NORM_CFG(_VALUE[dtype], _VALUE[wt], _VALUE[rt], DT_NORM_OUT_E4M3 if q8 else DT_NORM_OUT_SAME, n0, n1, w, group,
-                    *xs, *rs, *ros, *ys, eps)
-    _on_device(dev, (_lib or lib()).dt_add_rmsnorm, (cfg, x.data_ptr(), wp, rp, rop, y.data_ptr(), sp), stream)
-
-
-def dt_cross_attn(q, k, v, out, softmax_scale, key_lens=None, key_mask=None, lse_out=None, stream=None):
-    """Attention of q [B, Lq, H, D] to an encoder's k, v [B, Lk, H_kv, D]; key_lens int32 [B], key_mask uint8 or bool
-    [B, Lk] (expanded batches too), lse_out fp32 [B, H, Lq]."""
-    shape, kshape, dtype, dev = q.shape, k.shape, q.dtype, q.get_device()
-    B, Lq, H, D = shape
-    Bk, Lk, Hkv, Dk = kshape
-    assert dev >= 0 and Bk == B and Dk == D and v.shape == kshape and out.shape == shape
-    assert k.dtype is dtype and v.dtype is dtype and out.dtype is dtype
-    assert k.get_device() == dev and v.get_device() == dev and out.get_device() == dev
-    lp = mp = op = None
-    ms = 0
-    if key_lens is not None:
-        assert key_lens.dtype is torch.int32 and key_lens.shape == (B,) and key_lens.is_contiguous() and key_lens.get_device() == dev
-        lp = key_lens.data_ptr()
-    if key_mask is not None:
-        assert key_mask.dtype in (torch.uint8, torch.bool) and key_mask.shape == (B, Lk) and key_mask.get_device() == dev
-        assert Lk <= 1 or key_mask.stride(1) == 1
-        mp, ms = key_mask.data_ptr(), key_mask.stride(0)
-    if lse_out is not None:
-        assert lse_out.dtype is torch.float32 and lse_out.shape == (B, H, Lq) and lse_out.is_contiguous() and lse_out.get_device() == dev
-        op = lse_out.data_ptr()
-    _on_device(dev, (_lib or lib()).dt_cross_attn,
-               (_CROSS_CFG(_VALUE[dtype], B, Lq, Lk, H, Hkv, D, softmax_scale), q.data_ptr(), _S4(*q.stride()), k.data_ptr(), _S4(*k.stride()),
-                v.data_ptr(), _S4(*v.stride()), lp, mp, ms, out.data_ptr(), _S4(*out.stride()), op), stream)
 
 
 def dt_poll_ops(device=None):

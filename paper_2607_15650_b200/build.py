@@ -11,6 +11,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -18,17 +19,29 @@ LIB = os.path.join(HERE, "libditango.so")
 SOURCES = ["api.cu", "attn_states.cu", "state_merge.cu", "plan.cu", "planner.cu", "ops_api.cu", "rope.cu", "add_rmsnorm.cu",
            "cross_attn.cu", "cross_tiles.cu"]
 HEADERS = ["dt_internal.h", "ops.h", "cross_attn.h", "ptx_sm100.cuh", os.path.join("..", "..", "include", "ditango.h")]
+OPS_LIB = os.path.join(HERE, "_ditango_ops.so")   # Python entry points of the context-free operators
+OPS_SOURCE = "ops_py.c"
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 
-def _stale() -> bool:
-    if not os.path.exists(LIB):
+def _stale(lib=LIB, files=SOURCES + HEADERS) -> bool:
+    if not os.path.exists(lib):
         return True
-    t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in SOURCES + HEADERS)
+    t = os.path.getmtime(lib)
+    return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in files)
+
+
+def _build_ops(force: bool) -> None:
+    if not force and not _stale(OPS_LIB, [OPS_SOURCE, HEADERS[-1]]):
+        return
+    tmp = OPS_LIB + f".tmp{os.getpid()}"
+    subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-std=c11", "-shared", "-fPIC", "-Wall", "-I" + sysconfig.get_paths()["include"],
+                    "-o", tmp, os.path.join(CSRC, OPS_SOURCE)], check=True)
+    os.replace(tmp, OPS_LIB)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    _build_ops(force)
     if not force and not _stale():
         return LIB
     tmp = LIB + f".tmp{os.getpid()}"

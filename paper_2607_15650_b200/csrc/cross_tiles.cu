@@ -118,7 +118,6 @@ struct Cursor {
         do next_item(p);
         while (valid && tiles == 0);
     }
-    __device__ __forceinline__ bool last() const { return t + 1 == tiles; }
     __device__ __forceinline__ int row0() const { return qb * (NQ * TILE); }
     // keys in the tile that do not count: a mask may have holes anywhere, the last tile may be ragged
     __device__ __forceinline__ bool masked(const CrossParams &c) const { return c.key_mask != nullptr || len < (t + 1) * TILE; }
@@ -359,29 +358,34 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             // -------------------------------------------------------- tiles with keys that do not count
             uint32_t st = 0, raw_ph = 0;   // ring stage; parity of every stage's kv_raw (one bit each)
             bool ok = true;
-            auto mask_tile = [&](const Cursor &it, bool is_k) {
-                if (it.masked(p.c)) {
-                    const uint8_t *m = p.c.key_mask ? p.c.key_mask + it.b * p.c.mask_stride : nullptr;
-                    bool on[4];
+            // which of this lane's four keys of a tile count (looked up a tile ahead: the bytes' latency is not on the way)
+            auto keys_on = [&](const Cursor &it) {
+                const uint8_t *m = p.c.key_mask ? p.c.key_mask + it.b * p.c.mask_stride : nullptr;
+                uint32_t on = 0;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key = it.t * TILE + 32 * i + lane;
-                        on[i] = key < it.len && (m == nullptr || __ldg(m + key) != 0);
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    const int key = it.t * TILE + 32 * i + lane;
+                    if (it.valid && key < it.len && (m == nullptr || __ldg(m + key) != 0)) on |= 1u << i;
+                }
+                return on;
+            };
+            auto mask_tile = [&](const Cursor &it, uint32_t on, bool is_k) {
+                if (it.masked(p.c)) {
                     ok = wait_all(bars.kv_raw + 8 * st, (raw_ph >> st) & 1u);
                     if (!ok) return;
                     raw_ph ^= 1u << st;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int r = 32 * i + lane;
-                        if (!on[i] && it.t * TILE + r < p.c.Lk) {   // (rows behind Lk are zeros: the tensor map ends there)
+                        const bool here = on >> i & 1u;
+                        if (!here && it.t * TILE + r < p.c.Lk) {   // (rows behind Lk are zeros: the tensor map ends there)
                             const uint32_t row = kv_smem + st * C::TILE_BYTES + r * 128;
 #pragma unroll
                             for (int c = 0; c < C::NHALF * 8; ++c)   // (pieces in a lane's own order: the rows' banks coincide)
                                 asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(row + (c >> 3) * C::HALF_BYTES + (((c + lane) & 7) << 4)), "r"(0) : "memory");
                         }
                         if (is_k)
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %2, %2};" ::"r"(mask_smem + st * C::COL_BYTES + r * 16), "r"(on[i] ? 0u : FP16 ? 0xFC00u : 0xFF80u), "r"(0) : "memory");
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %2, %2};" ::"r"(mask_smem + st * C::COL_BYTES + r * 16), "r"(here ? 0u : FP16 ? 0xFC00u : 0xFF80u), "r"(0) : "memory");
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
@@ -389,15 +393,25 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 }
                 if (++st == C::STAGES) st = 0;
             };
-            Cursor cur;
+            Cursor cur, nxt;
             cur.first(p);
-            if (cur.valid) mask_tile(cur, true);
-            while (cur.valid && ok) {
-                Cursor nxt = cur;
+            uint32_t on_cur = keys_on(cur), on_nxt = 0;
+            if (cur.valid) {
+                nxt = cur;
                 nxt.advance(p);
-                if (nxt.valid) mask_tile(nxt, true);
-                if (ok) mask_tile(cur, false);
+                on_nxt = keys_on(nxt);
+                mask_tile(cur, on_cur, true);
+            }
+            while (cur.valid && ok) {
+                Cursor far = nxt;
+                if (nxt.valid) far.advance(p);
+                const uint32_t on_far = keys_on(far);
+                if (nxt.valid) mask_tile(nxt, on_nxt, true);
+                if (ok) mask_tile(cur, on_cur, false);
                 cur = nxt;
+                nxt = far;
+                on_cur = on_nxt;
+                on_nxt = on_far;
             }
             if (!ok) {
                 if (lane == 0 && !*abort_ptr) atomicOr(p.c.status, STATUS_WAIT_TIMEOUT);

@@ -136,16 +136,7 @@ def test_frequency_refusals(lib, kw):
         dt.dt_rope_freqs(**kw)
 
 
-def test_packed_configs_have_the_layout_of_the_structures(lib):
-    pair = C.c_int64 * 2
-    for packed, st in ((dt._ROPE_CFG(*range(10), 1.5), dt.dt_rope_config(*range(10), 1.5)),
-                       (dt._CROSS_CFG(*range(7), 0.5), dt.dt_cross_config(*range(7), 0.5)),
-                       (dt._NORM_CFG(*range(8), 10, 11, 12, 13, 14, 15, 16, 17, 2.5),
-                        dt.dt_norm_config(*range(8), pair(10, 11), pair(12, 13), pair(14, 15), pair(16, 17), 2.5))):
-        assert packed == bytes(st)
-
-
-def test_rows_of_views_collapse_to_two_strides():
+def test_rows_of_views_collapse_to_two_strides(lib):
     x = torch.empty(2, 5, 9, 64)
     assert dt._norm_rows([x])[:2] == (1, 90)
     assert dt._norm_rows([x[:, :, :3], torch.empty(2, 5, 3, 64)]) == (10, 3, [(9 * 64, 64), (3 * 64, 64)])
@@ -154,3 +145,21 @@ def test_rows_of_views_collapse_to_two_strides():
         dt._norm_rows([x[:, :4, :3]])          # three strides
     with pytest.raises(AssertionError):
         dt._norm_rows([x[..., ::2]])
+
+
+def test_the_binding_refuses_what_it_can_see_without_a_device(lib):
+    x = torch.zeros((2, 3, 4, 64), dtype=torch.bfloat16)
+    f = torch.ones((1, 32), dtype=torch.float64)
+    with pytest.raises(AssertionError):
+        dt.dt_rope(x, None, x, None, f)                       # not on a GPU
+    with pytest.raises(AssertionError):
+        dt.dt_add_rmsnorm(x, None, x, 1e-6)
+    with pytest.raises(AssertionError):
+        dt.dt_cross_attn(x, x, x, x, 0.1)
+    for call in (lambda: dt.dt_rope(x, None, x), lambda: dt.dt_rope(x, None, x, None, f, turn=1), lambda: dt.dt_rope(x, None, x, None, f, q=x),
+                 lambda: dt.dt_add_rmsnorm(*[x] * 9), lambda: dt.dt_cross_attn(x, x, x, out=x)):
+        with pytest.raises(TypeError):
+            call()
+    with pytest.raises(AttributeError):
+        dt.dt_cross_attn(1, 2, 3, 4, 0.1)
+    assert "key_mask" in dt.dt_cross_attn.__doc__ and "scales" in dt.dt_add_rmsnorm.__doc__ and "freqs" in dt.dt_rope.__doc__
