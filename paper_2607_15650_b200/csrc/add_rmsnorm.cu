@@ -3,15 +3,18 @@
 //
 // Mathematics: the sum h is formed, squared, summed and scaled in fp32 and never rounded on the way to y; residual_out is
 // that same h rounded once to the residual's type.  scale = max(amax |y|, 2^-100) / 448 (448 = largest e4m3 value; the
-// floor keeps a row of zeros from dividing by zero), value = e4m3(y * 448 / amax), rounded to nearest even.
+// floor keeps a row of zeros from dividing by zero), value = e4m3(y * 448 / amax), rounded to nearest even.  With r =
+// 1 / sqrt(mean + eps) > 0, amax |y| = r amax |h weight|: both of a row's reductions are made at once, before r is known.
 //
 // Bound: HBM.  Every row is read once and stays in registers through its reductions, so a pass moves x, the residual in
-// and out, y and the scales, and nothing else.
+// and out, y and the scales, and nothing else.  What holds the rate up is how many rows are on the way at a time, since a
+// row's reductions are a chain of latencies: 8 to 32 lanes a row up to a width of 256, a warp up to 1024, a block above.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include "dt_internal.h"
 #include "ops.h"
+#include "ptx_sm100.cuh"
 
 namespace dt {
 namespace {
@@ -31,46 +34,45 @@ struct NormParams {
     float eps, inv_width;
 };
 
-// 8 values <-> fp32
+// 8 values <-> fp32, as pairs (the packed fp32 instructions take two at a time: large inputs are bound by instructions
+// before they are by HBM, 263 a vector of 8 with scalar ones and per-row loops)
+struct F8 { float2 v[4]; };
+__device__ __forceinline__ float2 both(float f) { return make_float2(f, f); }
 template <bool FP16>
-__device__ __forceinline__ void unpack8(const uint4 &r, float (&v)[8]) {
+__device__ __forceinline__ F8 unpack8(const uint4 &r) {
     const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    F8 f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if constexpr (FP16) {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
-            v[2 * i] = f.x; v[2 * i + 1] = f.y;
-        } else {
-            v[2 * i] = __uint_as_float(w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        }
+        if constexpr (FP16) f.v[i] = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+        else f.v[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
     }
+    return f;
 }
 template <bool FP16>
-__device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
+__device__ __forceinline__ uint4 pack8(const F8 &f) {
     uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (FP16) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
-        else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
-    }
+    for (int i = 0; i < 4; ++i) w[i] = pack_half2<FP16>(f.v[i].x, f.v[i].y);
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 // 8 values to e4m3, rounded to nearest even, saturated at +-448
-__device__ __forceinline__ uint2 pack8_e4m3(const float (&v)[8], float mul) {
-    uint32_t w[2];
+__device__ __forceinline__ uint2 pack8_e4m3(const F8 &f) {
+    uint16_t h[4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        uint16_t lo, hi;
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(v[4 * i + 1] * mul), "f"(v[4 * i] * mul));
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(v[4 * i + 3] * mul), "f"(v[4 * i + 2] * mul));
-        w[i] = (uint32_t)lo | ((uint32_t)hi << 16);
-    }
-    return make_uint2(w[0], w[1]);
+    for (int i = 0; i < 4; ++i) asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h[i]) : "f"(f.v[i].y), "f"(f.v[i].x));
+    return make_uint2((uint32_t)h[0] | ((uint32_t)h[1] << 16), (uint32_t)h[2] | ((uint32_t)h[3] << 16));
 }
-__device__ __forceinline__ void load8_f32(const float *p, float (&v)[8]) {
-    const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+__device__ __forceinline__ F8 f8_of(const float4 &a, const float4 &b) {
+    return {{make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)}};
+}
+__device__ __forceinline__ void mul8(F8 &f, const F8 &g) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.v[i] = __fmul2_rn(f.v[i], g.v[i]);
+}
+__device__ __forceinline__ void mul8(F8 &f, float m) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.v[i] = __fmul2_rn(f.v[i], both(m));
 }
 
 enum : int { RES_NONE = 0, RES_SAME = 1, RES_FP32 = 2 };
@@ -91,155 +93,226 @@ __device__ __forceinline__ void load_raw(const NormParams &p, long long xo, long
     }
 }
 template <bool FP16, int RES>
-__device__ __forceinline__ void sum_raw(const Raw<RES> &v, float (&h)[8]) {
-    unpack8<FP16>(v.x, h);
-    if constexpr (RES == RES_FP32) {
-        const uint32_t w[8] = {v.r[0].x, v.r[0].y, v.r[0].z, v.r[0].w, v.r[1].x, v.r[1].y, v.r[1].z, v.r[1].w};
+__device__ __forceinline__ F8 sum_raw(const Raw<RES> &v) {
+    F8 h = unpack8<FP16>(v.x);
+    if constexpr (RES != RES_NONE) {
+        F8 r;
+        if constexpr (RES == RES_FP32) r = f8_of(*reinterpret_cast<const float4 *>(&v.r[0]), *reinterpret_cast<const float4 *>(&v.r[1]));
+        else r = unpack8<FP16>(v.r[0]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] += __uint_as_float(w[e]);
-    } else if constexpr (RES == RES_SAME) {
-        float r[8];
-        unpack8<FP16>(v.r[0], r);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] += r[e];
+        for (int i = 0; i < 4; ++i) h.v[i] = __fadd2_rn(h.v[i], r.v[i]);
     }
+    return h;
 }
 template <bool FP16, int RES>
-__device__ __forceinline__ void store_h(const NormParams &p, long long ro, int vec, const float (&h)[8]) {
+__device__ __forceinline__ void store_h(const NormParams &p, long long ro, int vec, const F8 &h) {
     if constexpr (RES == RES_FP32) {
         float4 *r = reinterpret_cast<float4 *>(static_cast<float *>(p.residual_out) + ro + vec * 8);
-        r[0] = make_float4(h[0], h[1], h[2], h[3]);
-        r[1] = make_float4(h[4], h[5], h[6], h[7]);
+        r[0] = make_float4(h.v[0].x, h.v[0].y, h.v[1].x, h.v[1].y);
+        r[1] = make_float4(h.v[2].x, h.v[2].y, h.v[3].x, h.v[3].y);
     } else if constexpr (RES == RES_SAME) {
         *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.residual_out) + ro + vec * 8) = pack8<FP16>(h);
     }
 }
 template <bool FP16>
-__device__ __forceinline__ void load_weight(const NormParams &p, int vec, float (&w)[8]) {
-    if (p.weight == nullptr) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = 1.0f;
-    } else if (p.w_fp32) {
-        load8_f32(static_cast<const float *>(p.weight) + vec * 8, w);
-    } else {
-        unpack8<FP16>(__ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.weight) + vec * 8)), w);
+__device__ __forceinline__ F8 load_weight(const NormParams &p, int vec) {
+    if (p.weight == nullptr) return {{both(1.f), both(1.f), both(1.f), both(1.f)}};
+    if (p.w_fp32) {
+        const float4 *w = reinterpret_cast<const float4 *>(static_cast<const float *>(p.weight) + vec * 8);
+        return f8_of(__ldg(w), __ldg(w + 1));
     }
+    return unpack8<FP16>(__ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.weight) + vec * 8)));
 }
 // this vector's share of mean(h^2): divided before it is summed, so that only a mean beyond fp32 overflows
-__device__ __forceinline__ float meansq8(const float (&h)[8], float inv_width) {
-    float s = 0.f;
+__device__ __forceinline__ float meansq8(const F8 &h, float inv_width) {
+    float2 s = both(0.f);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s = fmaf(h[e] * inv_width, h[e], s);
-    return s;
+    for (int i = 0; i < 4; ++i) s = __ffma2_rn(__fmul2_rn(h.v[i], both(inv_width)), h.v[i], s);
+    return s.x + s.y;
 }
-__device__ __forceinline__ float amax8(const float (&y)[8]) {
+__device__ __forceinline__ float amax8(const F8 &y) {
     float m = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(y[e]));
+    for (int i = 0; i < 4; ++i) m = fmax3(m, fabsf(y.v[i].x), fabsf(y.v[i].y));
     return m;
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float s) {
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    return s;
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_max(float m) {
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    return m;
+}
+// over 4, 8 or 16 neighbouring lanes
+__device__ __forceinline__ float group_max(float m, int group_vecs) {
+    m = lanes_max<4>(m);
+    if (group_vecs > 4) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 4));
+    if (group_vecs > 8) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
+    return m;
+}
+// One vector of y from g = h * weight and the row's r; amax: of |g| over what shares a scale; scale: where it goes, or null.
+template <bool FP16, bool Q8>
+__device__ __forceinline__ void store_y(const NormParams &p, long long yo, int vec, F8 &g, float r, float amax, float *scale) {
+    if constexpr (Q8) {
+        const float top = fmaxf(amax * r, AMAX_FLOOR);
+        if (scale != nullptr) *scale = top * (1.0f / E4M3_MAX);
+        mul8(g, r);
+        mul8(g, __fdividef(E4M3_MAX, top));   // (not r * 448 / top at once: that may overflow where neither product does)
+        *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.y) + yo + vec * 8) = pack8_e4m3(g);
+    } else {
+        mul8(g, r);
+        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.y) + yo + vec * 8) = pack8<FP16>(g);
+    }
 }
 
 // Offsets of a row's x, residual, residual_out and y.
 struct RowAt { long long x, r, ro, y; };
 __device__ __forceinline__ RowAt row_at(const NormParams &p, uint32_t row) {
-    const uint32_t i0 = p.n0 == 1 ? 0u : row / (uint32_t)p.n1, i1 = row - i0 * (uint32_t)p.n1;
+    if (p.n0 == 1) return {row * p.xs[1], row * p.rs[1], row * p.ros[1], row * p.ys[1]};
+    const uint32_t i0 = row / (uint32_t)p.n1, i1 = row - i0 * (uint32_t)p.n1;
     return {i0 * p.xs[0] + i1 * p.xs[1], i0 * p.rs[0] + i1 * p.rs[1], i0 * p.ros[0] + i1 * p.ros[1], i0 * p.ys[0] + i1 * p.ys[1]};
 }
 
-// One row at a time per block, NV vectors of 8 values per thread (vector i * blockDim + thread).  Blocks stay and walk the
-// rows; the next row's loads go out before this row's reductions, so that bytes are in flight throughout.
-template <int NV, bool FP16, int RES, bool Q8>
+// A row per block (width > 1024), NV vectors of 8 values per thread (vector i * blockDim + thread).  STAY: blocks stay and walk
+// the rows with the weight in shared memory, and the next row's loads go out before this row's reductions; else a block has
+// one row (few rows: latency).
+template <int NV, bool FP16, int RES, bool Q8, bool STAY>
 __global__ void __launch_bounds__(512) norm_row_kernel(const NormParams p, const uint32_t rows) {
-  __shared__ float red[2][2][16];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-  Raw<RES> raw[NV] = {};
-  RowAt at = row_at(p, blockIdx.x);
+    extern __shared__ __align__(16) float weights[];
+    __shared__ float2 red[2][16];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+    const int groups = p.group_vecs ? p.vecs / p.group_vecs : 1;
+    Raw<RES> raw[NV] = {};
+    RowAt at = row_at(p, blockIdx.x);
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
-      if (i * (int)blockDim.x + tid < p.vecs) load_raw<RES>(p, at.x, at.r, i * blockDim.x + tid, raw[i]);
-  int turn = 0;
-  for (uint32_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
-    const long long roo = at.ro, yo = at.y;
-    float h[NV][8];
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) sum_raw<FP16, RES>(raw[i], h[i]);   // (vectors behind the row's end are zeros)
-    if (row + gridDim.x < rows) {
-        at = row_at(p, row + gridDim.x);
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (i * (int)blockDim.x + tid < p.vecs) load_raw<RES>(p, at.x, at.r, i * blockDim.x + tid, raw[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int vec = i * blockDim.x + tid;
-        s += meansq8(h[i], p.inv_width);
-        if (RES != RES_NONE && vec < p.vecs) store_h<FP16, RES>(p, roo, vec, h[i]);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    if (lane == 0) red[turn][0][warp] = s;   // (two sets in turn: a warp may be a row ahead of another that still reads)
-    __syncthreads();
-    s = 0.f;
-    for (int w = 0; w < warps; ++w) s += red[turn][0][w];
-    const float r = rsqrtf(s + p.eps);
-    float row_amax = 0.f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int vec = i * blockDim.x + tid;
-        if (vec >= p.vecs) continue;
-        float w[8];
-        load_weight<FP16>(p, vec, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[i][e] = h[i][e] * r * w[e];
-        if constexpr (Q8) row_amax = fmaxf(row_amax, amax8(h[i]));
-    }
-    if constexpr (!Q8) {
+    for (int i = 0; i < NV; ++i)
+        if (i * (int)blockDim.x + tid < p.vecs) load_raw<RES>(p, at.x, at.r, i * blockDim.x + tid, raw[i]);
+    if constexpr (STAY) {   // (every thread reads back only what it wrote itself)
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int vec = i * blockDim.x + tid;
-            if (vec < p.vecs) *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.y) + yo + vec * 8) = pack8<FP16>(h[i]);
+            if (vec >= p.vecs) continue;
+            const F8 w = load_weight<FP16>(p, vec);
+            *reinterpret_cast<float4 *>(weights + vec * 8) = make_float4(w.v[0].x, w.v[0].y, w.v[1].x, w.v[1].y);
+            *reinterpret_cast<float4 *>(weights + vec * 8 + 4) = make_float4(w.v[2].x, w.v[2].y, w.v[3].x, w.v[3].y);
         }
-    } else if (p.group_vecs == 0) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) row_amax = fmaxf(row_amax, __shfl_xor_sync(0xFFFFFFFFu, row_amax, o));
-        if (lane == 0) red[turn][1][warp] = row_amax;
-        __syncthreads();
-        for (int w = 0; w < warps; ++w) row_amax = fmaxf(row_amax, red[turn][1][w]);
-        row_amax = fmaxf(row_amax, AMAX_FLOOR);
-        if (tid == 0) p.scales[row] = row_amax * (1.0f / E4M3_MAX);
-        const float mul = __fdividef(E4M3_MAX, row_amax);
+    }
+    int turn = 0;
+    for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
+        const RowAt now = at;
+        F8 g[NV];
+        float s = 0.f, top = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int vec = i * blockDim.x + tid;
-            if (vec < p.vecs) *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.y) + yo + vec * 8) = pack8_e4m3(h[i], mul);
+            g[i] = sum_raw<FP16, RES>(raw[i]);   // h (vectors behind the row's end are zeros)
+            if (RES != RES_NONE && vec < p.vecs) store_h<FP16, RES>(p, now.ro, vec, g[i]);
         }
-    } else {
-        // a group is 4, 8 or 16 neighbouring vectors: as many neighbouring lanes (a block is a multiple of 32 threads, the
-        // width a multiple of the group, so a group is either all there or not at all)
-        const int groups = p.vecs / p.group_vecs;
+        if (STAY && row + gridDim.x < rows) {
+            at = row_at(p, (uint32_t)(row + gridDim.x));
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (i * (int)blockDim.x + tid < p.vecs) load_raw<RES>(p, at.x, at.r, i * blockDim.x + tid, raw[i]);
+        }
+        float amax[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int vec = i * blockDim.x + tid;
-            float m = vec < p.vecs ? amax8(h[i]) : 0.f;
-            for (int o = p.group_vecs >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-            m = fmaxf(m, AMAX_FLOOR);
+            s += meansq8(g[i], p.inv_width);
             if (vec < p.vecs) {
-                if ((vec & (p.group_vecs - 1)) == 0) p.scales[(long long)row * groups + vec / p.group_vecs] = m * (1.0f / E4M3_MAX);
-                *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.y) + yo + vec * 8) = pack8_e4m3(h[i], __fdividef(E4M3_MAX, m));
+                if constexpr (STAY) mul8(g[i], f8_of(*reinterpret_cast<const float4 *>(weights + vec * 8), *reinterpret_cast<const float4 *>(weights + vec * 8 + 4)));
+                else mul8(g[i], load_weight<FP16>(p, vec));
+            }
+            if constexpr (Q8) {
+                amax[i] = amax8(g[i]);
+                // a group is 4, 8 or 16 neighbouring vectors: as many neighbouring lanes (a block is a multiple of 32 threads,
+                // the width a multiple of the group, so a group is either all there or not at all)
+                if (p.group_vecs) amax[i] = group_max(amax[i], p.group_vecs);
+                else top = fmaxf(top, amax[i]);
             }
         }
+        s = lanes_sum<32>(s);
+        if (Q8 && !p.group_vecs) top = lanes_max<32>(top);
+        if (lane == 0) red[turn][warp] = make_float2(s, top);   // (two sets in turn: a warp may be a row ahead of another that still reads)
+        __syncthreads();
+        const float2 other = lane < warps ? red[turn][lane] : make_float2(0.f, 0.f);   // at most 16 warps
+        s = lanes_sum<16>(other.x);
+        if (Q8 && !p.group_vecs) top = lanes_max<16>(other.y);
+        s = __shfl_sync(0xFFFFFFFFu, s, 0);     // (lanes 16 to 31 hold nothing of it)
+        top = __shfl_sync(0xFFFFFFFFu, top, 0);
+        const float r = rsqrtf(s + p.eps);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int vec = i * blockDim.x + tid;
+            if (vec >= p.vecs) continue;
+            float *scale = nullptr;
+            if (Q8 && p.group_vecs) {
+                if ((vec & (p.group_vecs - 1)) == 0) scale = p.scales + (long long)row * groups + vec / p.group_vecs;
+            } else if (Q8 && vec == 0) {
+                scale = p.scales + row;
+            }
+            store_y<FP16, Q8>(p, now.y, vec, g[i], r, Q8 && p.group_vecs ? amax[i] : top, scale);
+        }
+        if (!STAY) break;
     }
-  }
+}
+
+// A row per warp (256 < width <= 1024), NV vectors per lane (vector 32 i + lane).
+template <int NV, bool FP16, int RES, bool Q8>
+__global__ void __launch_bounds__(256) norm_warp_kernel(const NormParams p, const uint32_t rows) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t row = blockIdx.x * 8u + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    const RowAt at = row_at(p, row);
+    const int groups = p.group_vecs ? p.vecs / p.group_vecs : 1;
+    Raw<RES> raw[NV] = {};
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (32 * i + lane < p.vecs) load_raw<RES>(p, at.x, at.r, 32 * i + lane, raw[i]);
+    F8 g[NV];
+    float amax[NV], s = 0.f, top = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int vec = 32 * i + lane;
+        g[i] = sum_raw<FP16, RES>(raw[i]);
+        if (RES != RES_NONE && vec < p.vecs) store_h<FP16, RES>(p, at.ro, vec, g[i]);
+        s += meansq8(g[i], p.inv_width);
+        if (vec < p.vecs) mul8(g[i], load_weight<FP16>(p, vec));
+        if constexpr (Q8) {
+            amax[i] = amax8(g[i]);
+            if (p.group_vecs) amax[i] = group_max(amax[i], p.group_vecs);
+            else top = fmaxf(top, amax[i]);
+        }
+    }
+    const float r = rsqrtf(lanes_sum<32>(s) + p.eps);
+    if (Q8 && !p.group_vecs) top = lanes_max<32>(top);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int vec = 32 * i + lane;
+        if (vec >= p.vecs) continue;
+        float *scale = nullptr;
+        if (Q8 && p.group_vecs) {
+            if ((vec & (p.group_vecs - 1)) == 0) scale = p.scales + (long long)row * groups + vec / p.group_vecs;
+        } else if (Q8 && vec == 0) {
+            scale = p.scales + row;
+        }
+        store_y<FP16, Q8>(p, at.y, vec, g[i], r, Q8 && p.group_vecs ? amax[i] : top, scale);
+    }
 }
 
 // Short rows (width <= 256): 8, 16 or 32 lanes of a warp per row, one vector per lane, SHORT_ROWS rows one after the other of
 // which all loads go out first.
 constexpr int SHORT_ROWS = 4;
-template <bool FP16, int RES, bool Q8>
-__global__ void __launch_bounds__(256) norm_short_kernel(const NormParams p, const int lanes, const uint32_t rows) {
-    const int vec = threadIdx.x & (lanes - 1), per_pass = 256 / lanes;
-    const uint32_t row0 = blockIdx.x * (uint32_t)(per_pass * SHORT_ROWS) + threadIdx.x / lanes;
+template <int LANES, bool FP16, int RES, bool Q8>
+__global__ void __launch_bounds__(256) norm_short_kernel(const NormParams p, const uint32_t rows) {
+    constexpr int per_pass = 256 / LANES;
+    const int vec = threadIdx.x & (LANES - 1);
+    const uint32_t row0 = blockIdx.x * (uint32_t)(per_pass * SHORT_ROWS) + threadIdx.x / LANES;
     Raw<RES> raw[SHORT_ROWS] = {};
 #pragma unroll
     for (int i = 0; i < SHORT_ROWS; ++i) {
@@ -249,34 +322,48 @@ __global__ void __launch_bounds__(256) norm_short_kernel(const NormParams p, con
             load_raw<RES>(p, at.x, at.r, vec, raw[i]);
         }
     }
-    float w[8] = {};
-    if (vec < p.vecs) load_weight<FP16>(p, vec, w);
-    const int groups = p.group_vecs ? p.vecs / p.group_vecs : 1, g = p.group_vecs ? p.group_vecs : lanes;
+    F8 w = {};
+    if (vec < p.vecs) w = load_weight<FP16>(p, vec);
+    const int groups = p.group_vecs ? p.vecs / p.group_vecs : 1, share = p.group_vecs ? p.group_vecs : LANES;   // lanes that share a scale
 #pragma unroll
     for (int i = 0; i < SHORT_ROWS; ++i) {
         const uint32_t row = row0 + i * per_pass;
         const bool here = row < rows && vec < p.vecs;
         const RowAt at = row_at(p, here ? row : 0);
-        float h[8];
-        sum_raw<FP16, RES>(raw[i], h);
+        F8 h = sum_raw<FP16, RES>(raw[i]);
         if (RES != RES_NONE && here) store_h<FP16, RES>(p, at.ro, vec, h);
-        float s = meansq8(h, p.inv_width);
-        for (int o = lanes >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-        const float r = rsqrtf(s + p.eps);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = here ? h[e] * r * w[e] : 0.f;
-        if constexpr (!Q8) {
-            if (here) *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.y) + at.y + vec * 8) = pack8<FP16>(h);
-        } else {
-            float m = amax8(h);
-            for (int o = g >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-            m = fmaxf(m, AMAX_FLOOR);
-            if (here) {
-                if ((vec & (g - 1)) == 0) p.scales[(long long)row * groups + vec / g] = m * (1.0f / E4M3_MAX);
-                *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.y) + at.y + vec * 8) = pack8_e4m3(h, __fdividef(E4M3_MAX, m));
-            }
+        const float r = rsqrtf(lanes_sum<LANES>(meansq8(h, p.inv_width)) + p.eps);
+        mul8(h, w);
+        float amax = 0.f;
+        if constexpr (Q8) {
+            amax = here ? amax8(h) : 0.f;
+            amax = p.group_vecs ? group_max(amax, p.group_vecs) : lanes_max<LANES>(amax);
         }
+        if (here) store_y<FP16, Q8>(p, at.y, vec, h, r, amax, Q8 && (vec & (share - 1)) == 0 ? p.scales + (long long)row * groups + vec / share : nullptr);
     }
+}
+
+template <int NV, bool FP16, int RES, bool Q8>
+cudaError_t launch_rows(const NormParams &p, uint32_t rows, uint32_t sms, cudaStream_t st) {
+    const int threads = ((p.vecs + NV - 1) / NV + 31) / 32 * 32;
+    if (rows <= sms * 8u) {
+        norm_row_kernel<NV, FP16, RES, Q8, false><<<rows, threads, 0, st>>>(p, rows);
+    } else {
+        auto kernel = norm_row_kernel<NV, FP16, RES, Q8, true>;
+        const int smem = p.width * (int)sizeof(float);
+        cudaError_t e = cudaSuccess;
+        if (smem > 46 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        int per_sm = 1;
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem);
+        if (e != cudaSuccess) return e;
+        // Whole waves of blocks, about 16 rows each: fewer and longer-lived blocks save the weight's way into shared memory,
+        // more of them even out the memory's pace (75600 x 5120 with an fp32 residual: 754 us in one wave, 660 in eight; 20000 x
+        // 8192 without one, to e4m3: 115 and 148).
+        const uint32_t wave = sms * (uint32_t)(per_sm < 1 ? 1 : per_sm), waves = rows / 16 / wave;
+        const uint32_t grid = (waves < 1 ? 1 : waves) * wave;
+        kernel<<<rows < grid ? rows : grid, threads, smem, st>>>(p, rows);
+    }
+    return cudaGetLastError();
 }
 
 template <bool FP16, int RES, bool Q8>
@@ -284,15 +371,16 @@ cudaError_t launch_norm(const NormParams &p, uint32_t sms, cudaStream_t st) {
     const uint32_t rows = (uint32_t)(p.n0 * p.n1);
     if (p.vecs <= 32) {
         const int lanes = p.vecs <= 8 ? 8 : p.vecs <= 16 ? 16 : 32;
-        const uint32_t per_block = (256 / lanes) * SHORT_ROWS;
-        norm_short_kernel<FP16, RES, Q8><<<(rows - 1) / per_block + 1, 256, 0, st>>>(p, lanes, rows);
+        const uint32_t grid = (rows - 1) / ((256 / lanes) * SHORT_ROWS) + 1;
+        if (lanes == 8) norm_short_kernel<8, FP16, RES, Q8><<<grid, 256, 0, st>>>(p, rows);
+        else if (lanes == 16) norm_short_kernel<16, FP16, RES, Q8><<<grid, 256, 0, st>>>(p, rows);
+        else norm_short_kernel<32, FP16, RES, Q8><<<grid, 256, 0, st>>>(p, rows);
     } else {
-        const int nv = p.vecs <= 256 ? 1 : p.vecs <= 1024 ? 2 : 4;
-        const int threads = ((p.vecs + nv - 1) / nv + 31) / 32 * 32;
-        const uint32_t most = sms * 32u, grid = rows < most ? rows : most;
-        if (nv == 1) norm_row_kernel<1, FP16, RES, Q8><<<grid, threads, 0, st>>>(p, rows);
-        else if (nv == 2) norm_row_kernel<2, FP16, RES, Q8><<<grid, threads, 0, st>>>(p, rows);
-        else norm_row_kernel<4, FP16, RES, Q8><<<grid, threads, 0, st>>>(p, rows);
+        // more vectors per thread: fewer instructions per row that all threads repeat (2048 to e4m3: 141 us with one, 110 with two)
+        if (p.vecs <= 64) norm_warp_kernel<2, FP16, RES, Q8><<<(rows - 1) / 8 + 1, 256, 0, st>>>(p, rows);
+        else if (p.vecs <= 128) norm_warp_kernel<4, FP16, RES, Q8><<<(rows - 1) / 8 + 1, 256, 0, st>>>(p, rows);
+        // (few rows: more threads per row, which is latency: 3 x 5120 3.7 us with four vectors per thread, 3.1 with two)
+        else return p.vecs <= 256 || (p.vecs <= 1024 && rows <= sms * 8u) ? launch_rows<2, FP16, RES, Q8>(p, rows, sms, st) : launch_rows<4, FP16, RES, Q8>(p, rows, sms, st);
     }
     return cudaGetLastError();
 }

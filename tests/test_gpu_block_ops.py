@@ -195,6 +195,42 @@ def test_norm_odd_widths(width):
         norm_check(x, None, res, ro, got, sc, 1e-5, h, y, (width, out))
 
 
+@pytest.mark.parametrize("width", [264, 1536, 2176, 5120, 8200, 16384])
+@pytest.mark.parametrize("residual", ["none", "same", "fp32"])
+@pytest.mark.parametrize("out,group", [("same", 0), ("e4m3", 0), ("e4m3", 128)])
+def test_norm_of_many_rows(width, residual, out, group):
+    """More rows than the GPU has places for blocks (they stream through the blocks), some of them in place, of a strided
+    view, and rows behind the last that stay as they were."""
+    if group and width % group:
+        group = 8 * math.gcd(width // 8, 4)
+        group = group if group in (32, 64) else 0
+    rows = 2500 + 37
+    buf = rnd((rows + 2, width + 64), 1, BF16)
+    x = buf[:rows, :width]
+    res = None if residual == "none" else rnd((rows + 2, width), 3, FP32 if residual == "fp32" else BF16, 3.0)
+    behind = None if res is None else res[rows:].clone()
+    w = rnd((width,), 2, FP32, 0.3) + 1
+    h, y = ref.norm(x, w, 1e-6, None if res is None else res[:rows])
+    sc = None
+    if out == "e4m3":
+        got = torch.full((rows + 2, width), 9.0, device="cuda").to(E4M3)
+        sc = torch.full((rows + 2, width // group if group else 1), 9.0, device="cuda")
+    else:
+        got = buf[:, :width]            # y in x's place
+        last = got[rows:].clone()
+    ro = None if res is None else res[:rows]
+    dt.dt_add_rmsnorm(x, w, got[:rows], 1e-6, residual=ro, residual_out=ro, scales=None if sc is None else sc[:rows])
+    torch.cuda.synchronize()
+    dt.dt_poll_ops()
+    norm_check(x, w, ro, ro, got[:rows], None if sc is None else sc[:rows], 1e-6, h, y, (width, residual, out, group))
+    if res is not None:
+        assert torch.equal(res[rows:], behind)
+    if sc is not None:
+        assert (got[rows:].float() == 9).all() and (sc[rows:] == 9).all()
+    else:
+        assert torch.equal(got[rows:], last) and torch.equal(buf[:, width:], rnd((rows + 2, width + 64), 1, BF16)[:, width:])
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_norm_over_heads_of_a_packed_projection_in_place(D):
     qkv = rnd((2, 70, 9, D), 1, BF16)
