@@ -3,7 +3,7 @@
 //
 // One persistent CTA per SM, 16 warps --
 //   warps 0-3 / 4-7  softmax of query tile 0 / 1 (128 rows each, one row per thread)
-//   warp 8           TMA producer: Q of an item, K and V tiles through a ring in the order the MMAs consume them
+//   warp 8           TMA producer: Q of every item, K and V tiles through a ring in the order the MMAs consume them
 //   warps 9, 10      MMA issuers of query tile 0 / 1
 //   warp 11          masks: in tiles that hold keys that do not count, it zeroes their K and V rows in shared memory and
 //                    writes the tile's column of -inf / 0
@@ -48,7 +48,7 @@ struct Cfg {
     static constexpr int NHALF = D / 64;                      // 64-element (128-byte) swizzle atoms per row
     static constexpr int HALF_BYTES = TILE * 128;
     static constexpr int TILE_BYTES = NHALF * HALF_BYTES;
-    static constexpr int STAGES = (D == 128) ? 4 : 8;
+    static constexpr int STAGES = (D == 128) ? 4 : 6;         // K/V ring (D = 64: eight, or two places for Q, measured no better)
     static constexpr int Q_BYTES = NQ * TILE_BYTES;
     static constexpr int KV_BYTES = STAGES * TILE_BYTES;
     static constexpr int OUT_BYTES = TILE * 128;              // epilogue staging: 4 warps x [32 rows x 128 bytes]
@@ -74,6 +74,7 @@ struct MapCoord { int mul_l, mul_h, mul_b; };
 struct TileParams {
     CrossParams c;
     MapCoord mq, mk, mv;
+    bool same_tail;          // neither lengths nor a mask: only the end of Lk may be ragged, alike for every item
     int qblocks;             // ceil(Lq / 256)
     int items;               // B * H * qblocks
     int dq, dh, db;          // gridDim.x items on, in blocks, heads and requests
@@ -213,6 +214,9 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %2, %2};" ::"r"(ones_smem + r * 16), "r"(FP16 ? 0x3C00u : 0x3F80u), "r"(0) : "memory");
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(zeros_smem + r * 16), "r"(0) : "memory");
         }
+        if (p.same_tail)   // one column for every last tile (its rows behind Lk are zeros already: the tensor maps end there)
+            for (int r = lane; r < TILE; r += 32)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %2, %2};" ::"r"(mask_smem + r * 16), "r"(r < p.c.Lk % TILE ? 0u : FP16 ? 0xFC00u : 0xFF80u), "r"(0) : "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     tc_fence_before();
@@ -302,26 +306,26 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 prefetch_tensormap(&tmap_q);
                 prefetch_tensormap(&tmap_k);
                 prefetch_tensormap(&tmap_v);
-                uint32_t q_phase = 0, st = 0, ph = 0;
+                uint32_t st = 0, ph = 0, q_ph = 0;
                 bool ok = true;
                 auto load_q = [&](const Cursor &it) {
 #pragma unroll
                     for (int q = 0; q < NQ; ++q) {
-                        ok = ok && wait(bars.q_empty + 8 * q, q_phase ^ 1u);
-                        if (!ok) break;
+                        ok = ok && wait(bars.q_empty + 8 * q, q_ph ^ 1u);
+                        if (!ok) return;
                         mbar_arrive_expect_tx(bars.q_full + 8 * q, C::TILE_BYTES);
 #pragma unroll
                         for (int hf = 0; hf < C::NHALF; ++hf)
                             tma_load_4d(q_smem + q * C::TILE_BYTES + hf * C::HALF_BYTES, &tmap_q, bars.q_full + 8 * q, hf * 64,
                                         it.h * p.mq.mul_h, it.row0() + q * TILE, it.b * p.mq.mul_b);
                     }
-                    q_phase ^= 1u;
+                    q_ph ^= 1u;
                 };
                 auto load_kv = [&](const Cursor &it, bool is_k) {
                     ok = ok && wait(bars.kv_empty + 8 * st, ph ^ 1u);
                     if (!ok) return;
                     // tiles with keys that do not count land on a barrier of their own; the masking warp passes them on
-                    const uint32_t bar = (MASKED && it.masked(p.c) ? bars.kv_raw : bars.kv_full) + 8 * st;
+                    const uint32_t bar = (MASKED && !p.same_tail && it.masked(p.c) ? bars.kv_raw : bars.kv_full) + 8 * st;
                     mbar_arrive_expect_tx(bar, C::TILE_BYTES);
                     const int hk = p.c.rep == 1 ? it.h : it.h / p.c.rep;
                     const int h = hk * (is_k ? p.mk.mul_h : p.mv.mul_h), b = it.b * (is_k ? p.mk.mul_b : p.mv.mul_b);
@@ -354,9 +358,9 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 }
             }
         } else if (warp == ZERO_WARP) {
-          if constexpr (MASKED) {
+          if constexpr (MASKED) if (!p.same_tail) {
             // -------------------------------------------------------- tiles with keys that do not count
-            uint32_t st = 0, raw_ph = 0;   // ring stage; parity of every stage's kv_raw (one bit each)
+            uint32_t raw_ph = 0;   // parity of every stage's kv_raw (one bit each)
             bool ok = true;
             // which of this lane's four keys of a tile count (looked up a tile ahead: the bytes' latency is not on the way)
             auto keys_on = [&](const Cursor &it) {
@@ -369,45 +373,50 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 }
                 return on;
             };
-            auto mask_tile = [&](const Cursor &it, uint32_t on, bool is_k) {
-                if (it.masked(p.c)) {
-                    ok = wait_all(bars.kv_raw + 8 * st, (raw_ph >> st) & 1u);
-                    if (!ok) return;
-                    raw_ph ^= 1u << st;
+            // zeroes the rows of a landed tile (those behind Lk are zeros: the tensor map ends there)
+            auto zero_rows = [&](const Cursor &it, uint32_t on, uint32_t st) {
+                ok = ok && wait_all(bars.kv_raw + 8 * st, (raw_ph >> st) & 1u);
+                if (!ok) return;
+                raw_ph ^= 1u << st;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = 32 * i + lane;
-                        const bool here = on >> i & 1u;
-                        if (!here && it.t * TILE + r < p.c.Lk) {   // (rows behind Lk are zeros: the tensor map ends there)
-                            const uint32_t row = kv_smem + st * C::TILE_BYTES + r * 128;
+                for (int i = 0; i < 4; ++i) {
+                    const int r = 32 * i + lane;
+                    if ((on >> i & 1u) || it.t * TILE + r >= p.c.Lk) continue;
+                    const uint32_t row = kv_smem + st * C::TILE_BYTES + r * 128;
 #pragma unroll
-                            for (int c = 0; c < C::NHALF * 8; ++c)   // (pieces in a lane's own order: the rows' banks coincide)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(row + (c >> 3) * C::HALF_BYTES + (((c + lane) & 7) << 4)), "r"(0) : "memory");
-                        }
-                        if (is_k)
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %2, %2};" ::"r"(mask_smem + st * C::COL_BYTES + r * 16), "r"(here ? 0u : FP16 ? 0xFC00u : 0xFF80u), "r"(0) : "memory");
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bars.kv_full + 8 * st);
+                    for (int c = 0; c < C::NHALF * 8; ++c)   // (pieces in a lane's own order: the rows' banks coincide)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(row + (c >> 3) * C::HALF_BYTES + (((c + lane) & 7) << 4)), "r"(0) : "memory");
                 }
-                if (++st == C::STAGES) st = 0;
+            };
+            // V of a tile and K of the next land one behind the other: both are passed on at once, behind one fence
+            auto pass_on = [&](bool k, const Cursor &kt, uint32_t k_on, uint32_t k_st, bool v, const Cursor &vt, uint32_t v_on, uint32_t v_st) {
+                if (k) {
+                    zero_rows(kt, k_on, k_st);
+                    if (!ok) return;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %2, %2};" ::"r"(mask_smem + k_st * C::COL_BYTES + (32 * i + lane) * 16), "r"(k_on >> i & 1u ? 0u : FP16 ? 0xFC00u : 0xFF80u), "r"(0) : "memory");
+                }
+                if (v) zero_rows(vt, v_on, v_st);
+                if (!ok || !(k || v)) return;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0 && k) mbar_arrive(bars.kv_full + 8 * k_st);
+                if (lane == 0 && v) mbar_arrive(bars.kv_full + 8 * v_st);
             };
             Cursor cur, nxt;
             cur.first(p);
-            uint32_t on_cur = keys_on(cur), on_nxt = 0;
-            if (cur.valid) {
-                nxt = cur;
-                nxt.advance(p);
-                on_nxt = keys_on(nxt);
-                mask_tile(cur, on_cur, true);
-            }
+            nxt = cur;
+            if (cur.valid) nxt.advance(p);
+            uint32_t st = 1 % C::STAGES, on_cur = keys_on(cur), on_nxt = keys_on(nxt);
+            if (cur.valid) pass_on(cur.masked(p.c), cur, on_cur, 0, false, cur, 0, 0);   // K of the first tile
             while (cur.valid && ok) {
                 Cursor far = nxt;
                 if (nxt.valid) far.advance(p);
-                const uint32_t on_far = keys_on(far);
-                if (nxt.valid) mask_tile(nxt, on_nxt, true);
-                if (ok) mask_tile(cur, on_cur, false);
+                const uint32_t on_far = keys_on(far), k_st = st;
+                if (nxt.valid && ++st == C::STAGES) st = 0;
+                pass_on(nxt.valid && nxt.masked(p.c), nxt, on_nxt, k_st, cur.masked(p.c), cur, on_cur, st);
+                if (++st == C::STAGES) st = 0;
                 cur = nxt;
                 nxt = far;
                 on_cur = on_nxt;
@@ -436,7 +445,7 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     if (leader) mma_ss(tmem_base + C::S_COL, qdesc + koff, b0 + koff, IDESC_QK, kk > 0 ? 1u : 0u);
                 }
                 if (MASKED && masked) {
-                    const uint32_t col = mask_smem + st * C::COL_BYTES;
+                    const uint32_t col = mask_smem + (p.same_tail ? 0u : st * C::COL_BYTES);
                     if (leader) mma_ss(tmem_base + C::S_COL, ones_desc, make_smem_desc_plain(col, zeros_smem - col, 128), IDESC_QK, 1u);
                 }
             };
@@ -458,8 +467,8 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             if (cur.valid) {   // the stream's first Q K^T
                 ok = wait_all(bars.q_full + 8 * mq, 0u) && wait_all(bars.kv_full, 0u) && wait_all(bars.s_free, s_turn);
                 if (ok) {
-                    q_phase = 1u;
                     tc_fence_after();
+                    q_phase = 1u;
                     issue_qk(0, cur.masked(p.c));
                     if (leader) {
                         tc_commit(bars.s_full + 8 * mq);
@@ -611,9 +620,9 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 mbar_arrive(bars.p_full + 8 * q);
             }
             if (!ok) break;
-            // (m, l) for the epilogue, once it has read the item before's: it hands O back behind that (with more than one tile it
-            // has long done so).  Without this wait ml_full could complete twice before the epilogue looks.
-            if (p_items > 0) ok = wait_all(bars.o_free + 8 * q, (p_items - 1) & 1u);
+            // (m, l) for the epilogue, once it has read the item before's: it hands O back behind that, and with more than one tile
+            // P V of the second has waited for it.  Without this wait ml_full could complete twice before the epilogue looks.
+            if (p_items > 0 && it.tiles == 1) ok = wait_all(bars.o_free + 8 * q, (p_items - 1) & 1u);
             if (!ok) break;
             ++p_items;
             asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(ml_smem + (q * TILE + row_in_tile) * 8), "f"(m_used), "f"(l_sum) : "memory");
@@ -698,6 +707,7 @@ cudaError_t launch_cross_tiles(const CrossParams &c, int D, bool fp16, const Ops
     p.dq = grid % p.qblocks;
     p.dh = grid / p.qblocks % c.H;
     p.db = grid / p.qblocks / c.H;
+    p.same_tail = c.key_lens == nullptr && c.key_mask == nullptr;
     CUtensorMap tq, tk, tv;
     if (encode(dev.encode_tiled, &tq, &p.mq, c.q, c.qs, c.B, c.Lq, c.H, D, fp16) != CUDA_SUCCESS ||
         encode(dev.encode_tiled, &tk, &p.mk, c.k, c.ks, c.B, c.Lk, c.Hkv, D, fp16) != CUDA_SUCCESS ||

@@ -355,6 +355,33 @@ def test_cross_many_blocks_of_rows_per_sm(Lk, D, dtype):
             check(out[:, :, h:h + 1], wo, to, (Lk, D, h, "out"))
 
 
+@pytest.mark.parametrize("D,dtype", [(64, FP16), (128, BF16)])
+@pytest.mark.parametrize("Lk", [5, 128, 200, 226, 512, 700])
+def test_cross_masks_in_many_blocks_of_rows(Lk, D, dtype):
+    """Masks with holes, lengths, and both, with NaN in masked places, where every SM takes several blocks of rows; the groups of
+    heads share keys, and one request has no key."""
+    B, Lq, H, Hk = 3, 3000, 12, 4
+    q, k, v = rnd((B, Lq, H, D), 1, dtype, 1.3), rnd((B, Lk, Hk, D), 2, dtype, 1.3), rnd((B, Lk, Hk, D), 3, dtype)
+    g = torch.Generator(device="cuda"); g.manual_seed(Lk)
+    holes = (torch.rand((B, Lk), generator=g, device="cuda") < 0.7).to(torch.uint8)
+    holes[1] = 0
+    lens = torch.tensor([Lk, Lk, (Lk + 2) // 3], dtype=torch.int32, device="cuda")
+    for ln, mk in ((None, holes), (lens, None), (lens, holes)):
+        keep = keep_of(B, Lk, ln, mk)
+        kk, vv = k.clone(), v.clone()
+        kk[~keep] = float("nan")
+        vv[~keep] = float("inf")
+        out, lse = torch.full_like(q, 5.0), torch.full((B, H, Lq), 5.0, device="cuda")
+        dt.dt_cross_attn(q, kk, vv, out, D ** -0.5, key_lens=ln, key_mask=mk, lse_out=lse)
+        torch.cuda.synchronize()
+        dt.dt_poll_ops()
+        for h in (0, 5, 11):
+            ks = kk[:, :, h // 3:h // 3 + 1], vv[:, :, h // 3:h // 3 + 1]
+            wo, wl, to, tl = ref.cross(q[:, :, h:h + 1], *ks, D ** -0.5, keep)
+            check(lse[:, h:h + 1], wl, tl, (Lk, D, h, "lse"))
+            check(out[:, :, h:h + 1], wo, to, (Lk, D, h, "out"))
+
+
 @pytest.mark.parametrize("Lq,Lk", [(1, 0), (300, 0), (0, 5), (0, 0)])
 def test_cross_without_keys_or_queries(Lq, Lk):
     q, k = rnd((2, Lq, 4, 64), 1, BF16), rnd((2, Lk, 4, 64), 2, BF16)
