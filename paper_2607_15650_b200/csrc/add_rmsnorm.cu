@@ -356,10 +356,11 @@ cudaError_t launch_rows(const NormParams &p, uint32_t rows, uint32_t sms, cudaSt
         int per_sm = 1;
         if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem);
         if (e != cudaSuccess) return e;
-        // Whole waves of blocks, about 16 rows each: fewer and longer-lived blocks save the weight's way into shared memory,
-        // more of them even out the memory's pace (75600 x 5120 with an fp32 residual: 754 us in one wave, 660 in eight; 20000 x
-        // 8192 without one, to e4m3: 115 and 148).
-        const uint32_t wave = sms * (uint32_t)(per_sm < 1 ? 1 : per_sm), waves = rows / 16 / wave;
+        // One wave of blocks: the weight is brought into shared memory once per block, and in a long run of such calls every
+        // instruction counts (75600 x 5120 with an fp32 residual: 688 us in one wave, 702 in ten).  Narrow rows (NV = 2) take
+        // whole waves of about 16 rows per block, which evens out the memory's pace (80000 x 2048 with a residual: 212 us, 234 in
+        // one wave).
+        const uint32_t wave = sms * (uint32_t)(per_sm < 1 ? 1 : per_sm), waves = NV == 4 ? 1 : rows / 16 / wave;
         const uint32_t grid = (waves < 1 ? 1 : waves) * wave;
         kernel<<<rows < grid ? rows : grid, threads, smem, st>>>(p, rows);
     }
