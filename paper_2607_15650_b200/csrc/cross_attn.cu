@@ -35,29 +35,6 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_arrive_wait() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ float ld_cluster(uint32_t smem_addr, uint32_t rank) {
-    float v;
-    asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}"
-                 : "=f"(v) : "r"(smem_addr), "r"(rank) : "memory");
-    return v;
-}
-__device__ __forceinline__ float4 ld_cluster4(uint32_t smem_addr, uint32_t rank) {
-    float4 v;
-    asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [a];\n\t}"
-                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(smem_addr), "r"(rank) : "memory");
-    return v;
-}
-// weight of a partial state with maximum m in a state with maximum top (m = -inf: no keys)
-__device__ __forceinline__ float state_weight(float m, float top) { return m == -INFINITY ? 0.f : ex2_approx(m - top); }
-
 // Shared memory: the warps' rings, and after the last chunk, in the same place, the states to be joined.
 template <int D, int ROWS>
 struct FewCfg {
@@ -417,12 +394,15 @@ extern "C" dt_status dt_cross_attn(const dt_cross_config *cfg, const void *q_dev
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool fp16 = c.dtype == DT_VALUE_FP16;
     // Few rows or many?  The few-row kernel costs by blocks of 16 rows x keys (5.5e-5 us for D = 128, 3.8e-5 for 64, measured), the
-    // tiles by rounds of the GPU's SMs x 128 keys (1.5 and 1.4 us): the former as long as its blocks are at most 200 (290) per
-    // round.  H = 12, D = 128, 8192 keys: 256 rows 94 us against 101, 512 rows 184 against 101; 2 heads: 1024 rows 51 against 100.
-    const long long few_blocks = ((long long)c.Lq * p.rep + 15) / 16 * c.B * c.H_kv;
-    const long long rounds = ((long long)c.B * c.H * (((long long)c.Lq + 255) / 256) + dev->sms - 1) / dev->sms;
+    // tiles by rounds of the GPU's SMs x tiles of 128 keys (1.5 and 1.4 us; about three tiles' worth for joining splits): the
+    // former as long as its blocks are at most 200 (290) per round.  D = 128, 12 heads: 128 rows, 1024 keys 13 us against 13, 512
+    // rows 29 against 15; 8192 keys: 64 rows 29 against 28, 512 rows 184 against 37.
+    const long long few_blocks = ((long long)c.Lq * p.rep + 15) / 16 * c.B * c.H_kv, tiles = ((long long)c.Lk + 127) / 128;
+    const long long items = (long long)c.B * c.H * (((long long)c.Lq + 255) / 256);
+    const int splits = cross_tile_splits(items, tiles, dev->sms);
+    const long long steps = splits > 1 ? (tiles + splits - 1) / splits + 3 : (items + dev->sms - 1) / dev->sms * tiles;
     cudaError_t e;
-    if (c.Lk > 0 && few_blocks > rounds * (c.D == 64 ? 290 : 200)) e = launch_cross_tiles(p, c.D, fp16, *dev, st);
+    if (c.Lk > 0 && few_blocks * tiles > steps * (c.D == 64 ? 290 : 200)) e = launch_cross_tiles(p, c.D, fp16, splits, *dev, st);
     else e = c.D == 64 ? (fp16 ? launch_few<64, true>(p, dev->sms, st) : launch_few<64, false>(p, dev->sms, st))
                        : (fp16 ? launch_few<128, true>(p, dev->sms, st) : launch_few<128, false>(p, dev->sms, st));
     return e == cudaSuccess ? DT_OK : ops_fail_cuda(e, "cross-attention launch");

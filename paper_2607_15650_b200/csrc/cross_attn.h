@@ -25,8 +25,40 @@ __device__ __forceinline__ int keys_of(const CrossParams &p, int b) {
     return p.key_lens ? min(max(__ldg(p.key_lens + b), 0), p.Lk) : p.Lk;
 }
 
-// Many query rows (Lk > 0): tensor-memory tiles.
-cudaError_t launch_cross_tiles(const CrossParams &p, int D, bool fp16, const OpsDevice &dev, cudaStream_t st);
+// ---- clusters: states in the blocks' shared memory, joined across them
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_arrive_wait() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float ld_cluster(uint32_t smem_addr, uint32_t rank) {
+    float v;
+    asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}"
+                 : "=f"(v) : "r"(smem_addr), "r"(rank) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t smem_addr, uint32_t rank) {
+    float4 v;
+    asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [a];\n\t}"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(smem_addr), "r"(rank) : "memory");
+    return v;
+}
+// weight of a partial state with maximum m in a state with maximum top (m = -inf: no keys)
+__device__ __forceinline__ float state_weight(float m, float top) { return m == -INFINITY ? 0.f : ex2_approx(m - top); }
+
+// Many query rows (Lk > 0): tensor-memory tiles, the keys of a block of 256 rows split over `splits` CTAs.
+cudaError_t launch_cross_tiles(const CrossParams &p, int D, bool fp16, int splits, const OpsDevice &dev, cudaStream_t st);
+// Splits for so many blocks of 256 rows (of a head) and tiles of keys: as many as find a place at once (with one CTA per SM, 15
+// clusters of 8 do on 148 SMs), two tiles each at least; 1 where the blocks alone fill the GPU or there are few tiles (512 rows
+// x 12 heads: 8192 keys 101 us alone, 37 in four; 1024 keys 18 and 15; 512 keys 12 and 15).
+inline int cross_tile_splits(long long items, long long tiles, int sms) {
+    int s = 1;
+    while (tiles >= 8 && s < 8 && items * s * 2 <= (s == 1 ? sms : s == 2 ? sms * 15 / 16 : sms * 13 / 16) && tiles >= s * 4) s *= 2;
+    return s;
+}
 cudaError_t cross_tiles_configure();   // both per device, once
 cudaError_t cross_few_configure();
 

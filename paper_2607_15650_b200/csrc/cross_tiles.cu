@@ -22,6 +22,9 @@
 // (NaN, infinities) has no effect.  The softmax does nothing for a mask (selecting 128 logits by bits took 800 cycles a tile).
 // Tiles behind the last key that counts are never loaded, and the last tile's P V stops at its last 16 keys that may.
 //
+// Few items and many keys: the item's tiles are split over the CTAs of a cluster, which leave their states (O, m, l) in shared
+// memory, where K and V were, and join them across the cluster (as the few-row kernel does).
+//
 // Every wait on an mbarrier is bounded; on expiry the CTA records STATUS_WAIT_TIMEOUT, leaves its loops, frees TMEM and
 // returns.
 #include <cuda_bf16.h>
@@ -70,7 +73,7 @@ struct Bars {
 };
 
 // Tensor maps' coordinates: a dimension of one entry, or one that repeats (stride 0), has one entry in the map too.
-struct MapCoord { int mul_l, mul_h, mul_b; };
+struct MapCoord { int mul_h, mul_b; };
 struct TileParams {
     CrossParams c;
     MapCoord mq, mk, mv;
@@ -78,17 +81,21 @@ struct TileParams {
     int qblocks;             // ceil(Lq / 256)
     int items;               // B * H * qblocks
     int dq, dh, db;          // gridDim.x items on, in blocks, heads and requests
+    int splits;              // SPLIT: CTAs (a cluster) that share an item's keys
 };
 
 // The stream of a CTA's tiles: item after item, the items without keys left out.  K and V are loaded (and consumed) in the
 // order K_0, K_1, V_0, K_2, V_1, ..., K_n, V_{n-1}, ..., V_last, across items.  Stepping costs additions only: divisions here
 // were on the way to the next Q K^T (1400 cycles per item).
-struct Cursor {
+// SPLIT: few items and many keys; the CTAs of a cluster take a part of one item's tiles each.
+template <bool SPLIT>
+struct CursorOf {
     int w, qb, h, b;         // item: block of 256 rows, head, request
-    int len, tiles, t;       // its keys and tiles; the current tile
+    int len, tiles, t;       // its keys, and this CTA's tiles of them; the current tile
+    int t0;                  // SPLIT: the first of them
     bool valid;
     __device__ __forceinline__ void first_item(const TileParams &p) {
-        w = blockIdx.x;
+        w = SPLIT ? blockIdx.x / p.splits : blockIdx.x;
         const int bh = w / p.qblocks;
         qb = w - bh * p.qblocks;
         b = bh / p.c.H;
@@ -96,6 +103,11 @@ struct Cursor {
         look(p);
     }
     __device__ __forceinline__ void next_item(const TileParams &p) {
+        if constexpr (SPLIT) {
+            valid = false;
+            tiles = len = 0;
+            return;
+        }
         w += gridDim.x;
         qb += p.dq;
         h += p.dh;
@@ -109,7 +121,13 @@ struct Cursor {
         valid = w < p.items;
         len = valid ? keys_of(p.c, b) : 0;
         tiles = (len + TILE - 1) / TILE;
+        if constexpr (SPLIT) {
+            const int part = blockIdx.x - w * p.splits, all = tiles;
+            t0 = (int)((long long)all * part / p.splits);
+            tiles = (int)((long long)all * (part + 1) / p.splits) - t0;
+        }
     }
+    __device__ __forceinline__ int key0() const { return ((SPLIT ? t0 : 0) + t) * TILE; }   // of the current tile
     __device__ __forceinline__ void first(const TileParams &p) {
         first_item(p);
         while (valid && tiles == 0) next_item(p);
@@ -121,7 +139,7 @@ struct Cursor {
     }
     __device__ __forceinline__ int row0() const { return qb * (NQ * TILE); }
     // keys in the tile that do not count: a mask may have holes anywhere, the last tile may be ragged
-    __device__ __forceinline__ bool masked(const CrossParams &c) const { return c.key_mask != nullptr || len < (t + 1) * TILE; }
+    __device__ __forceinline__ bool masked(const CrossParams &c) const { return c.key_mask != nullptr || len < key0() + TILE; }
 };
 
 // Shared-memory matrix descriptor without swizzle: core matrices of 8 rows x 16 bytes; `lbo`: to the next 16 bytes of a row,
@@ -147,11 +165,12 @@ __device__ __noinline__ void scale_o(uint32_t o_tmem, float alpha) {
 }
 
 // MASKED: some tile may hold keys that do not count (lengths, a mask, or Lk not a multiple of 128); without it nothing looks.
-template <int D, bool FP16, bool MASKED>
+template <int D, bool FP16, bool MASKED, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1)
 cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                   const __grid_constant__ CUtensorMap tmap_v, const TileParams p) {
     using C = Cfg<D>;
+    using Cursor = CursorOf<SPLIT>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_flag;
@@ -234,7 +253,33 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         uint32_t phase = 0;
         bool ok = true;
         Cursor it;
-        for (it.first_item(p); it.valid && ok; it.next_item(p)) {
+        it.first_item(p);
+        if constexpr (SPLIT) {
+            // This CTA's state goes to where K and V were (every P V is complete): rows of fp32, 16-byte piece c of row r at
+            // c ^ (r & 15); it is joined with the cluster's others below.
+            if (it.tiles > 0)
+                ok = wait_all(bars.ml_full, 0u) && wait_all(bars.ml_full + 8, 0u) && wait_all(bars.o_full, 0u) && wait_all(bars.o_full + 8, 0u);
+            tc_fence_after();
+            for (int q = 0; q < NQ && ok; ++q) {
+                const int r = q * TILE + row_in_tile;
+                if (it.tiles == 0) {
+                    asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(ml_smem + r * 8), "f"(-INFINITY), "f"(0.f) : "memory");
+                    continue;
+                }
+#pragma unroll 1
+                for (int c0 = 0; c0 < D; c0 += 32) {
+                    uint32_t o[32];
+                    tmem_ld_x32(tmem_base + lane_addr + C::O_COL + q * D + c0, o);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(kv_smem + r * (D * 4) + (((c0 / 4 + c) ^ (r & 15)) << 4)), "r"(o[4 * c]),
+                                     "r"(o[4 * c + 1]), "r"(o[4 * c + 2]), "r"(o[4 * c + 3]) : "memory");
+                }
+            }
+            it.valid = false;
+        }
+        for (; it.valid && ok; it.next_item(p)) {
             for (int q = 0; q < NQ && ok; ++q) {
                 const int q_row = it.row0() + q * TILE + row_in_tile;
                 const bool row_valid = q_row < p.c.Lq;
@@ -331,7 +376,7 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     const int h = hk * (is_k ? p.mk.mul_h : p.mv.mul_h), b = it.b * (is_k ? p.mk.mul_b : p.mv.mul_b);
 #pragma unroll
                     for (int hf = 0; hf < C::NHALF; ++hf)
-                        tma_load_4d(kv_smem + st * C::TILE_BYTES + hf * C::HALF_BYTES, is_k ? &tmap_k : &tmap_v, bar, hf * 64, h, it.t * TILE, b);
+                        tma_load_4d(kv_smem + st * C::TILE_BYTES + hf * C::HALF_BYTES, is_k ? &tmap_k : &tmap_v, bar, hf * 64, h, it.key0(), b);
                     if (++st == C::STAGES) { st = 0; ph ^= 1u; }
                 };
                 Cursor cur;
@@ -368,7 +413,7 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 uint32_t on = 0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int key = it.t * TILE + 32 * i + lane;
+                    const int key = it.key0() + 32 * i + lane;
                     if (it.valid && key < it.len && (m == nullptr || __ldg(m + key) != 0)) on |= 1u << i;
                 }
                 return on;
@@ -381,7 +426,7 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int r = 32 * i + lane;
-                    if ((on >> i & 1u) || it.t * TILE + r >= p.c.Lk) continue;
+                    if ((on >> i & 1u) || it.key0() + r >= p.c.Lk) continue;
                     const uint32_t row = kv_smem + st * C::TILE_BYTES + r * 128;
 #pragma unroll
                     for (int c = 0; c < C::NHALF * 8; ++c)   // (pieces in a lane's own order: the rows' banks coincide)
@@ -485,7 +530,7 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 nxt.advance(p);
                 const bool next_item = nxt.valid, next_single = nxt.tiles == 1;
                 const bool next_masked = MASKED && nxt.masked(p.c), any_mask = MASKED && p.c.key_mask != nullptr;
-                const bool ragged = MASKED && cur.len < cur.tiles * TILE;
+                const bool ragged = MASKED && cur.len < cur.key0() + cur.tiles * TILE;   // (cur.t is 0)
                 const int tiles = cur.tiles;
                 for (int k = 0; k < tiles; ++k) {
                     const bool within = k + 1 < tiles, more = within || next_item;
@@ -639,6 +684,61 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    if constexpr (SPLIT) {
+        cluster_arrive_wait();   // every CTA of the cluster has written its state (or given up: then the results do not count)
+        if (warp < TMA_WARP) {   // (the softmax warps: they have the registers)
+            Cursor it;
+            it.first_item(p);
+            const int part = blockIdx.x - it.w * p.splits, per = NQ * TILE / p.splits;   // rows this CTA joins
+            // a row's weights first, one thread each: the states' shares of OUT, and LSE
+            if (threadIdx.x < per) {
+                const int r = part * per + threadIdx.x, q_row = it.row0() + r;
+                float ms[8], ls[8], top = -INFINITY, sum = 0.f;
+#pragma unroll
+                for (int s = 0; s < 8; ++s) {
+                    ms[s] = s < p.splits ? ld_cluster(ml_smem + r * 8, s) : -INFINITY;
+                    ls[s] = s < p.splits ? ld_cluster(ml_smem + r * 8 + 4, s) : 0.f;
+                }
+#pragma unroll
+                for (int s = 0; s < 8; ++s) top = fmaxf(top, ms[s]);
+#pragma unroll
+                for (int s = 0; s < 8; ++s) {
+                    ms[s] = ls[s] == 0.f ? 0.f : state_weight(ms[s], top);   // (l = 0: no keys there, and of a CTA without tiles no O)
+                    sum = fmaf(ms[s], ls[s], sum);
+                }
+                const float inv = sum == 0.f ? 0.f : 1.0f / sum;   // a row without keys: OUT = 0, LSE = -inf
+#pragma unroll
+                for (int s = 0; s < 8; ++s)
+                    asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(out_smem + (threadIdx.x * 8 + s) * 8), "f"(ms[s] * inv), "f"(ls[s]) : "memory");
+                if (q_row < p.c.Lq && p.c.lse != nullptr)
+                    p.c.lse[((long long)it.b * p.c.H + it.h) * p.c.Lq + q_row] = sum == 0.f ? -INFINITY : LN2 * (top + log2f(sum));
+            }
+            asm volatile("bar.sync 1, %0;" ::"n"(SOFTMAX_THREADS) : "memory");
+            // then OUT, 4 values at a time; every state's piece is on its way before the first is used
+            const int pieces = min(per, p.c.Lq - it.row0() - part * per) * (D / 4);
+#pragma unroll 2
+            for (int i = threadIdx.x; i < pieces; i += SOFTMAX_THREADS) {
+                const int rr = i / (D / 4), r = part * per + rr, c = i % (D / 4);
+                float4 x[8];
+                float2 w[8];
+#pragma unroll
+                for (int s = 0; s < 8; ++s) {
+                    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(w[s].x), "=f"(w[s].y) : "r"(out_smem + (rr * 8 + s) * 8) : "memory");
+                    x[s] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (w[s].y != 0.f) x[s] = ld_cluster4(kv_smem + r * (D * 4) + ((c ^ (r & 15)) << 4), s);
+                }
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int s = 0; s < 8; ++s) {
+                    acc.x = fmaf(w[s].x, x[s].x, acc.x); acc.y = fmaf(w[s].x, x[s].y, acc.y);
+                    acc.z = fmaf(w[s].x, x[s].z, acc.z); acc.w = fmaf(w[s].x, x[s].w, acc.w);
+                }
+                uint16_t *dst = p.c.out + it.b * p.c.os[0] + (long long)(it.row0() + r) * p.c.os[1] + it.h * p.c.os[2] + 4 * c;
+                *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_half2<FP16>(acc.x, acc.y), pack_half2<FP16>(acc.z, acc.w));
+            }
+        }
+        cluster_arrive_wait();   // no CTA leaves while another still reads its shared memory
+    }
     if (warp == 0) tmem_dealloc(tmem_base, 512);
 }
 
@@ -651,7 +751,6 @@ CUresult encode(void *fn, CUtensorMap *tm, MapCoord *mul, const void *base, cons
     const bool one_b = B <= 1 || s[0] == 0, one_h = H <= 1;
     mul->mul_b = one_b ? 0 : 1;
     mul->mul_h = one_h ? 0 : 1;
-    mul->mul_l = 1;
     cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)(one_h ? 1 : H), (cuuint64_t)L, (cuuint64_t)(one_b ? 1 : B)};
     // (the stride of a dimension of one entry is never used, but has to be a valid one)
     cuuint64_t strides[3] = {one_h ? (cuuint64_t)D * 2 : (cuuint64_t)s[2] * 2, L <= 1 ? (cuuint64_t)D * 2 : (cuuint64_t)s[1] * 2,
@@ -663,27 +762,45 @@ CUresult encode(void *fn, CUtensorMap *tm, MapCoord *mul, const void *base, cons
                                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
-template <int D, bool FP16, bool MASKED>
+template <int D, bool FP16, bool MASKED, bool SPLIT>
 cudaError_t configure_one() {
     cudaFuncAttributes attr;
-    cudaError_t e = cudaFuncGetAttributes(&attr, cross_tile_kernel<D, FP16, MASKED>);
+    cudaError_t e = cudaFuncGetAttributes(&attr, cross_tile_kernel<D, FP16, MASKED, SPLIT>);
     if (e != cudaSuccess) return e;
     if (attr.numRegs != LAUNCH_REGS) return cudaErrorInvalidConfiguration;   // the register hand-over would not balance
-    return cudaFuncSetAttribute(cross_tile_kernel<D, FP16, MASKED>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::SMEM_BYTES);
+    return cudaFuncSetAttribute(cross_tile_kernel<D, FP16, MASKED, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::SMEM_BYTES);
 }
 template <int D, bool FP16>
 cudaError_t configure() {
-    cudaError_t e = configure_one<D, FP16, false>();
-    return e == cudaSuccess ? configure_one<D, FP16, true>() : e;
+    cudaError_t e;
+    if ((e = configure_one<D, FP16, false, false>()) != cudaSuccess) return e;
+    if ((e = configure_one<D, FP16, true, false>()) != cudaSuccess) return e;
+    if ((e = configure_one<D, FP16, false, true>()) != cudaSuccess) return e;
+    return configure_one<D, FP16, true, true>();
 }
 
+template <int D, bool FP16, bool MASKED>
+cudaError_t launch(int grid, const CUtensorMap &tq, const CUtensorMap &tk, const CUtensorMap &tv, const TileParams &p, cudaStream_t st) {
+    if (p.splits == 1) {
+        cross_tile_kernel<D, FP16, MASKED, false><<<grid, THREADS, Cfg<D>::SMEM_BYTES, st>>>(tq, tk, tv, p);
+        return cudaGetLastError();
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(p.items * p.splits));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = Cfg<D>::SMEM_BYTES;
+    cfg.stream = st;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)p.splits; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, cross_tile_kernel<D, FP16, MASKED, true>, tq, tk, tv, p);
+}
 template <int D, bool FP16>
 cudaError_t launch(int grid, const CUtensorMap &tq, const CUtensorMap &tk, const CUtensorMap &tv, const TileParams &p, cudaStream_t st) {
-    if (p.c.key_lens != nullptr || p.c.key_mask != nullptr || p.c.Lk % TILE != 0)
-        cross_tile_kernel<D, FP16, true><<<grid, THREADS, Cfg<D>::SMEM_BYTES, st>>>(tq, tk, tv, p);
-    else
-        cross_tile_kernel<D, FP16, false><<<grid, THREADS, Cfg<D>::SMEM_BYTES, st>>>(tq, tk, tv, p);
-    return cudaGetLastError();
+    const bool masked = p.c.key_lens != nullptr || p.c.key_mask != nullptr || p.c.Lk % TILE != 0;
+    return masked ? launch<D, FP16, true>(grid, tq, tk, tv, p, st) : launch<D, FP16, false>(grid, tq, tk, tv, p, st);
 }
 
 }  // namespace
@@ -696,7 +813,7 @@ cudaError_t cross_tiles_configure() {
     return configure<128, true>();
 }
 
-cudaError_t launch_cross_tiles(const CrossParams &c, int D, bool fp16, const OpsDevice &dev, cudaStream_t st) {
+cudaError_t launch_cross_tiles(const CrossParams &c, int D, bool fp16, int splits, const OpsDevice &dev, cudaStream_t st) {
     TileParams p = {};
     p.c = c;
     p.qblocks = (c.Lq + NQ * TILE - 1) / (NQ * TILE);
@@ -707,6 +824,7 @@ cudaError_t launch_cross_tiles(const CrossParams &c, int D, bool fp16, const Ops
     p.dq = grid % p.qblocks;
     p.dh = grid / p.qblocks % c.H;
     p.db = grid / p.qblocks / c.H;
+    p.splits = splits;
     p.same_tail = c.key_lens == nullptr && c.key_mask == nullptr;
     CUtensorMap tq, tk, tv;
     if (encode(dev.encode_tiled, &tq, &p.mq, c.q, c.qs, c.B, c.Lq, c.H, D, fp16) != CUDA_SUCCESS ||

@@ -382,6 +382,25 @@ def test_cross_masks_in_many_blocks_of_rows(Lk, D, dtype):
             check(out[:, :, h:h + 1], wo, to, (Lk, D, h, "out"))
 
 
+@pytest.mark.parametrize("D,dtype", [(64, FP16), (128, BF16), (128, FP16)])
+@pytest.mark.parametrize("B,Lq,H,Hk,Lk", [(1, 700, 8, 8, 2500), (2, 1000, 4, 4, 3001), (1, 2000, 2, 1, 1152), (1, 3000, 1, 1, 5000), (3, 513, 12, 4, 1024),
+                                          (1, 2049, 8, 8, 520)])
+def test_cross_long_states_of_many_tokens(B, Lq, H, Hk, Lk, D, dtype):
+    """Too few blocks of rows to fill the GPU: the keys are split as well.  All keys, lengths that leave some of the splits
+    nothing (or a request nothing), and a mask with NaN in masked places."""
+    q, k, v = rnd((B, Lq, H, D), 1, dtype, 1.3), rnd((B, Lk, Hk, D), 2, dtype, 1.3), rnd((B, Lk, Hk, D), 3, dtype)
+    g = torch.Generator(device="cuda"); g.manual_seed(Lk)
+    holes = (torch.rand((B, Lk), generator=g, device="cuda") < 0.5).to(torch.uint8)
+    holes[0, Lk // 4:Lk // 2 + 300] = 0
+    for lens, mask in ((None, None), (torch.tensor([100, 0, Lk][:B], dtype=torch.int32, device="cuda"), None), (None, holes),
+                       (torch.tensor([Lk - 7, Lk // 2, 1][:B], dtype=torch.int32, device="cuda"), holes)):
+        keep = keep_of(B, Lk, lens, mask)
+        kk, vv = k.clone(), v.clone()
+        kk[~keep] = float("nan")
+        vv[~keep] = float("nan")
+        cross_run(q, kk, vv, D ** -0.5, lens, mask, what=(Lq, Lk, H))
+
+
 @pytest.mark.parametrize("Lq,Lk", [(1, 0), (300, 0), (0, 5), (0, 0)])
 def test_cross_without_keys_or_queries(Lq, Lk):
     q, k = rnd((2, Lq, 4, 64), 1, BF16), rnd((2, Lk, 4, 64), 2, BF16)
@@ -446,7 +465,7 @@ def test_cross_offsets_beyond_32_bits():
 
 def test_cross_repeats_bit_for_bit_on_other_streams_and_in_graphs():
     """Calls on two streams at once, and two captured graphs replayed in turn, give the bits of plain calls."""
-    cases = [(2, 1, 300, 8, 2, 128), (1, 300, 512, 4, 4, 64), (1, 40, 226, 2, 2, 128)]
+    cases = [(2, 1, 300, 8, 2, 128), (1, 3000, 512, 16, 16, 64), (1, 40, 226, 2, 2, 128), (1, 1000, 2000, 4, 4, 128), (2, 9000, 300, 12, 12, 128)]
     ins = [(rnd((B, Lq, H, D), i, BF16), rnd((B, Lk, Hk, D), i + 10, BF16), rnd((B, Lk, Hk, D), i + 20, BF16)) for i, (B, Lq, Lk, H, Hk, D) in enumerate(cases)]
     plain = []
     for q, k, v in ins:
