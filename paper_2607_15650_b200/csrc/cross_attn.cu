@@ -11,7 +11,10 @@
 // 8 or 16 rows that share a key head (query heads of the group x tokens) per block.  The keys are split over the warps of a
 // block and over the blocks of a cluster, whose states are joined in shared memory and then across the cluster (no
 // workspace, no atomics, one launch).  Every warp streams chunks of 16 keys through a ring of its own in shared memory
-// (cp.async, no barrier between warps), so that two thirds of the ring are in flight while it computes.
+// (cp.async, no barrier between warps), so that two thirds of the ring are in flight while it computes.  Measured: 2 requests x 40
+// heads on 8 key heads x 128, 32760 keys: 42 us, 5.3 TB/s; 40 heads, 32760 keys 103 us, 6.5 TB/s; 40 heads, 512 keys 5.4 us.  With
+// rows of Q as the 16 rows of mma.sync and fragments loaded straight from global memory the first took 92 us: one warp per
+// scheduler, bound by the chain of its instructions.
 #include <cuda_bf16.h>
 
 #include <cmath>

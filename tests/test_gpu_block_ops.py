@@ -257,6 +257,63 @@ def test_norm_residual_in_place_and_rows_behind_the_last_stay():
     assert (buf[9:] == 9).all() and (ybuf[9:].float() == 9).all() and (sc[9:] == 9).all()
 
 
+@pytest.mark.parametrize("rows,width", [(5, 64), (3000, 384), (9, 5120), (2000, 2560)])
+def test_norm_sum_in_the_place_of_x_and_one_row_for_all(rows, width):
+    x, res = rnd((rows, width), 1, BF16), rnd((1, width), 2, BF16, 2.0).expand(rows, width)
+    h, want = ref.norm(x, None, 1e-6, res)
+    y = torch.empty_like(x)
+    dt.dt_add_rmsnorm(x, None, y, 1e-6, residual=res, residual_out=x)
+    torch.cuda.synchronize()
+    norm_check(None, None, res, x, y, None, 1e-6, h, want, (rows, width))
+
+
+def test_norm_and_rope_offsets_beyond_32_bits():
+    far = 2 ** 31 // 40 // 8 * 8 + 8
+    room = torch.empty(far * 50 + 4096, device="cuda", dtype=BF16)
+    for width, n in ((128, 51), (1024, 51), (2560, 51)):
+        x = room.as_strided((n, width), (far, 1))
+        x.copy_(rnd((n, width), 1, BF16))
+        _, want = ref.norm(x, None, 1e-6, None)
+        dt.dt_add_rmsnorm(x, None, x, 1e-6)
+        torch.cuda.synchronize()
+        norm_check(None, None, None, None, x, None, 1e-6, None, want, width)
+    q = room.as_strided((1, 51, 2, 64), (0, far, 64, 1))
+    q.copy_(rnd((1, 51, 2, 64), 2, BF16))
+    angle = (torch.arange(51, device="cuda").double()[None, :, None] * dt.dt_rope_freqs(64)[0].cuda()).expand(1, 51, 32)
+    want, tol = ref.rope(q, angle, False, 64)
+    dt.dt_rope(q, None, q, None, dt.dt_rope_freqs(64)[0][None].cuda())
+    torch.cuda.synchronize()
+    check(q, want, tol, "far")
+
+
+def test_rope_and_norm_repeat_bit_for_bit_on_other_streams_and_in_graphs():
+    q, k = rnd((2, 700, 6, 128), 1, FP16), rnd((2, 700, 2, 128), 2, FP16)
+    f = dt.dt_rope_freqs(128)[0][None].cuda()
+    x, res = rnd((3000, 1536), 3, BF16), rnd((3000, 1536), 4, FP32)
+
+    def passes(stream=None):
+        qo, ko = torch.empty_like(q), torch.empty_like(k)
+        y, sc, ro = torch.empty((3000, 1536), device="cuda", dtype=E4M3), torch.empty((3000, 12), device="cuda"), torch.empty_like(res)
+        dt.dt_rope(q, k, qo, ko, f, layout=dt.DT_ROPE_HALF, stream=stream)
+        dt.dt_add_rmsnorm(x, None, y, 1e-6, residual=res, residual_out=ro, scales=sc, stream=stream)
+        return qo, ko, y.view(torch.uint8), sc, ro
+    plain = passes()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [passes(s) for s in streams for _ in range(3)]
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        held = passes()
+    for t in held:
+        t.zero_()
+    g.replay()
+    g.replay()
+    torch.cuda.synchronize()
+    for other in got + [held]:
+        assert all(torch.equal(a, b) for a, b in zip(plain, other))
+
+
 def test_norm_of_zero_rows_large_values_and_no_rows():
     x = torch.zeros((3, 512), device="cuda", dtype=BF16)
     x[1] = rnd((512,), 1, BF16) * 1e18        # squares stay inside fp32
@@ -450,6 +507,29 @@ def test_cross_long_states_of_single_tokens():
         q, k, v = rnd((B, 1, H, D), 1, FP16), rnd((B, Lk, Hk, D), 2, FP16), rnd((B, Lk, Hk, D), 3, FP16)
         lens = torch.tensor([Lk - 11 * b for b in range(B)], dtype=torch.int32, device="cuda")
         cross_run(q, k, v, D ** -0.5, lens, what=("long", Lk))
+
+
+@pytest.mark.parametrize("B,Lq,H,Hk,Lk", [(2, 3, 8, 2, 300), (2, 5000, 12, 12, 200), (1, 600, 4, 4, 2000)])
+def test_cross_output_in_the_place_of_q(B, Lq, H, Hk, Lk):
+    """Few rows, many blocks of rows, keys split over a cluster."""
+    q, k, v = rnd((B, Lq, H, 128), 1, BF16), rnd((B, Lk, Hk, 128), 2, BF16), rnd((B, Lk, Hk, 128), 3, BF16)
+    out = torch.empty_like(q)
+    dt.dt_cross_attn(q, k, v, out, 0.1)
+    dt.dt_cross_attn(q, k, v, q, 0.1)
+    torch.cuda.synchronize()
+    dt.dt_poll_ops()
+    assert torch.equal(q, out)
+
+
+@pytest.mark.parametrize("Lq,Lk", [(1, 300), (4000, 300), (600, 2000)])
+def test_cross_where_no_request_has_a_key(Lq, Lk):
+    q, k = rnd((2, Lq, 4, 64), 1, FP16), torch.full((2, Lk, 4, 64), float("nan"), device="cuda", dtype=FP16)
+    for kw in (dict(key_lens=torch.tensor([0, -3], dtype=torch.int32, device="cuda")), dict(key_mask=torch.zeros((2, Lk), dtype=torch.uint8, device="cuda"))):
+        out, lse = torch.full_like(q, 3), torch.full((2, 4, Lq), 3.0, device="cuda")
+        dt.dt_cross_attn(q, k, k, out, 0.125, lse_out=lse, **kw)
+        torch.cuda.synchronize()
+        dt.dt_poll_ops()
+        assert (out == 0).all() and (lse == -math.inf).all()
 
 
 def test_cross_offsets_beyond_32_bits():
