@@ -398,7 +398,8 @@ dt_status dt_rope_freqs(const dt_rope_scaling *scaling, int32_t rotary_dim, doub
  * in fp32; y is made from the unrounded h.  DT_NORM_OUT_E4M3: per row, or per scale_group neighbouring values of it,
  *     scale = max(max |y|, 2^-100) / 448,  value = e4m3(y / scale) (to nearest even, saturated)
  * so that value * scale stands for y.
- *   x, y            device, n0 x n1 rows, row (i, j) at i * strides[0] + j * strides[1] (multiples of 8 elements)
+ *   x, y            device, n0 x n1 rows, row (i, j) at i * strides[0] + j * strides[1] (multiples of 8 elements; an input's
+ *                   may be 0, an output's rows may not overlap)
  *   weight_dev      device [width], x's type or fp32; NULL: 1
  *   residual_dev, residual_out_dev   device, as x, of x's type or fp32; both NULL: no residual.  residual_out may be
  *                   residual or (in x's type) x, y may be x: same base and strides
@@ -420,12 +421,12 @@ dt_status dt_add_rmsnorm(const dt_norm_config *cfg, const void *x_dev, const voi
  *     LSE = log sum_j exp(softmax_scale * q.k_j),  OUT = sum_j exp(softmax_scale * q.k_j - LSE) v_j
  * -- a state (Eq. 1), so it composes with others by Eq. 2.  A row without keys has OUT = 0 and LSE = -inf.  What stands in
  * K and V at keys that do not count (NaN and infinities too) has no effect.
- *   q, out          device [B, Lq, H, D]; out may be q (same strides)
+ *   q, out          device [B, Lq, H, D]; out may be q (same strides), out's rows may not overlap
  *   k, v            device [B, Lk, H_kv, D], strides of their own; query head h reads key head h / (H / H_kv)
  *   key_lens_dev    device, int32 [B] (values outside [0, Lk] are clamped), or NULL: Lk
  *   key_mask_dev    device, uint8 rows of Lk, key_mask_stride bytes apart (0: one row for all), or NULL
  *   lse_out_dev     device, fp32 [B, H, Lq], or NULL
- * Limits: D in {64, 128}; B * H <= 65535; Lq, Lk from 0 (Lq = 0: nothing to do; Lk = 0: rows without keys). */
+ * Limits: D in {64, 128}; B * H <= 65535; Lq * H <= 2^30; Lk <= 2^26; Lq, Lk from 0 (Lq = 0: nothing to do; Lk = 0: rows without keys). */
 typedef struct {
     int32_t dtype;                    /* DT_VALUE_BF16 or DT_VALUE_FP16 */
     int32_t B, Lq, Lk, H, H_kv, D;

@@ -23,6 +23,7 @@
 namespace dt {
 namespace {
 
+constexpr int MAX_WIDTH = 16384;
 constexpr float E4M3_MAX = 448.0f;
 constexpr float AMAX_FLOOR = 7.888609052210118e-31f;   // 2^-100
 
@@ -166,7 +167,9 @@ __device__ __forceinline__ void store_y(const NormParams &p, long long yo, int v
         const float top = fmaxf(amax * r, AMAX_FLOOR);
         if (scale != nullptr) *scale = top * (1.0f / E4M3_MAX);
         mul8(g, r);
-        mul8(g, __fdividef(E4M3_MAX, top));   // (not r * 448 / top at once: that may overflow where neither product does)
+        // (not r * 448 / top at once: that may overflow where neither product does; both sides quartered: the fast division
+        // gives 0 for a divisor above 2^126)
+        mul8(g, __fdividef(0.25f * E4M3_MAX, 0.25f * top));
         *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.y) + yo + vec * 8) = pack8_e4m3(g);
     } else {
         mul8(g, r);
@@ -356,7 +359,8 @@ cudaError_t launch_rows(const NormParams &p, uint32_t rows, uint32_t sms, cudaSt
         auto kernel = norm_row_kernel<NV, FP16, RES, Q8, true>;
         const int smem = p.width * (int)sizeof(float);
         cudaError_t e = cudaSuccess;
-        if (smem > 46 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        // (always the same value: another thread may be about to launch the kernel with a width of its own)
+        if (smem > 46 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_WIDTH * (int)sizeof(float));
         int per_sm = 1;
         if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem);
         if (e != cudaSuccess) return e;
@@ -400,6 +404,11 @@ cudaError_t launch_res(const NormParams &p, int res, bool q8, uint32_t sms, cuda
     return res == RES_SAME ? launch_out<FP16, RES_SAME>(p, q8, sms, st) : launch_out<FP16, RES_FP32>(p, q8, sms, st);
 }
 
+// An output and an input with one base: in place, which needs values of one size and the same strides.
+bool bad_place(const void *out, const int64_t so[2], const void *in, const int64_t si[2], bool same_size, int64_t n0, int64_t n1) {
+    return out && out == in && !(same_size && (n0 <= 1 || so[0] == si[0]) && (n1 <= 1 || so[1] == si[1]));
+}
+
 // Row strides: multiples of 8 values, no negative ones; a stride of a dimension of one entry is not looked at.
 bool bad_strides(const int64_t s[2], int64_t n0, int64_t n1, int width, bool output) {
     const int64_t n[2] = {n0, n1};
@@ -420,7 +429,7 @@ extern "C" dt_status dt_add_rmsnorm(const dt_norm_config *cfg, const void *x_dev
     if (c.dtype != DT_VALUE_BF16 && c.dtype != DT_VALUE_FP16) return ops_fail(DT_ERR_UNSUPPORTED, "x must be bf16 or fp16");
     if (c.weight_dtype != c.dtype && c.weight_dtype != DT_VALUE_FP32) return ops_fail(DT_ERR_UNSUPPORTED, "weight must be of x's type or fp32");
     if (c.out_kind != DT_NORM_OUT_SAME && c.out_kind != DT_NORM_OUT_E4M3) return ops_fail(DT_ERR_UNSUPPORTED, "unknown output kind");
-    if (c.width % 8 != 0 || c.width > 16384) return ops_fail(DT_ERR_UNSUPPORTED, "width must be a multiple of 8, at most 16384");
+    if (c.width % 8 != 0 || c.width > MAX_WIDTH) return ops_fail(DT_ERR_UNSUPPORTED, "width must be a multiple of 8, at most 16384");
     if (!(c.eps >= 0.f) || c.eps > 3.0e38f) return ops_fail(DT_ERR_INVALID_ARG, "eps must be finite and not negative");
     const bool q8 = c.out_kind == DT_NORM_OUT_E4M3;
     if (q8 && c.scale_group != 0 && c.scale_group != 32 && c.scale_group != 64 && c.scale_group != 128)
@@ -436,6 +445,12 @@ extern "C" dt_status dt_add_rmsnorm(const dt_norm_config *cfg, const void *x_dev
         (residual_dev && (bad_strides(c.residual_strides, c.n0, c.n1, c.width, false) ||
                           bad_strides(c.residual_out_strides, c.n0, c.n1, c.width, true))))
         return ops_fail(DT_ERR_INVALID_ARG, "row strides must be multiples of 8, and an output's rows must not overlap");
+    const bool res_same = c.residual_dtype == c.dtype;
+    if (y_dev == residual_out_dev || bad_place(y_dev, c.y_strides, x_dev, c.x_strides, !q8, c.n0, c.n1) ||
+        bad_place(y_dev, c.y_strides, residual_dev, c.residual_strides, !q8 && res_same, c.n0, c.n1) ||
+        bad_place(residual_out_dev, c.residual_out_strides, residual_dev, c.residual_strides, true, c.n0, c.n1) ||
+        bad_place(residual_out_dev, c.residual_out_strides, x_dev, c.x_strides, res_same, c.n0, c.n1))
+        return ops_fail(DT_ERR_INVALID_ARG, "in place needs the same type and strides, and y and residual_out differ");
     const uintptr_t y_align = q8 ? 7u : 15u;
     if ((reinterpret_cast<uintptr_t>(x_dev) | reinterpret_cast<uintptr_t>(weight_dev) | reinterpret_cast<uintptr_t>(residual_dev) |
          reinterpret_cast<uintptr_t>(residual_out_dev)) & 15u || reinterpret_cast<uintptr_t>(y_dev) & y_align ||

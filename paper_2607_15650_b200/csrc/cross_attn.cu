@@ -121,8 +121,9 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) cross_few_kernel(const CrossPa
         const uint16_t *src = p.q + b * p.qs[0] + l * p.qs[1] + h * p.qs[2] + 2 * t;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
-            qf[n][i][0] = row < rows ? __ldg(reinterpret_cast<const uint32_t *>(src + 16 * i)) : 0u;
-            qf[n][i][1] = row < rows ? __ldg(reinterpret_cast<const uint32_t *>(src + 16 * i + 8)) : 0u;
+            // (plain loads: OUT may take Q's place)
+            qf[n][i][0] = row < rows ? *reinterpret_cast<const uint32_t *>(src + 16 * i) : 0u;
+            qf[n][i][1] = row < rows ? *reinterpret_cast<const uint32_t *>(src + 16 * i + 8) : 0u;
         }
     }
     // O^T: rows g, g + 8 of every 16 values, columns (query rows) 2 t, 2 t + 1; maximum and sum of those columns
@@ -366,16 +367,20 @@ extern "C" dt_status dt_cross_attn(const dt_cross_config *cfg, const void *q_dev
     if (c.B < 0 || c.Lq < 0 || c.Lk < 0 || c.H < 1 || c.H_kv < 1) return ops_fail(DT_ERR_INVALID_ARG, "bad shape");
     if (c.H % c.H_kv != 0) return ops_fail(DT_ERR_INVALID_ARG, "H must be a multiple of H_kv");
     if ((long long)c.B * c.H > 65535) return ops_fail(DT_ERR_UNSUPPORTED, "B*H exceeds 65535");
-    if ((long long)c.Lq * c.H > 0x3FFFFFFFLL || c.Lk > 0x3FFFFFFF) return ops_fail(DT_ERR_UNSUPPORTED, "Lq*H or Lk exceeds 2^30");
+    if ((long long)c.Lq * c.H > 0x3FFFFFFFLL || c.Lk > (1 << 26))   // (2^26 keys: 0.8 s of tiles, within what the kernel's bounded waits allow)
+        return ops_fail(DT_ERR_UNSUPPORTED, "Lq*H exceeds 2^30 or Lk 2^26");
     if (!(c.softmax_scale > 0.f) || !std::isfinite(c.softmax_scale)) return ops_fail(DT_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
     if (c.B == 0 || c.Lq == 0) return DT_OK;
     dt_status s;
-    if ((s = check_blhd("q", q_dev, q_strides_blhd, c.B, c.Lq, c.H, false)) != DT_OK) return s;
-    if ((s = check_blhd("out", out_dev, out_strides_blhd, c.B, c.Lq, c.H, true)) != DT_OK) return s;
+    if ((s = check_blhd("q", q_dev, q_strides_blhd, c.B, c.Lq, c.H, c.D, false)) != DT_OK) return s;
+    if ((s = check_blhd("out", out_dev, out_strides_blhd, c.B, c.Lq, c.H, c.D, true)) != DT_OK) return s;
     if (c.Lk > 0) {
-        if ((s = check_blhd("k", k_dev, k_strides_blhd, c.B, c.Lk, c.H_kv, false)) != DT_OK) return s;
-        if ((s = check_blhd("v", v_dev, v_strides_blhd, c.B, c.Lk, c.H_kv, false)) != DT_OK) return s;
+        if ((s = check_blhd("k", k_dev, k_strides_blhd, c.B, c.Lk, c.H_kv, c.D, false)) != DT_OK) return s;
+        if ((s = check_blhd("v", v_dev, v_strides_blhd, c.B, c.Lk, c.H_kv, c.D, false)) != DT_OK) return s;
+        if (out_dev == k_dev || out_dev == v_dev) return ops_fail(DT_ERR_INVALID_ARG, "out is k or v");
     }
+    if (out_dev == q_dev && !same_strides(q_strides_blhd, out_strides_blhd, c.B, c.Lq, c.H))
+        return ops_fail(DT_ERR_INVALID_ARG, "out in the place of q needs the same strides");
     if (key_mask_dev && c.B > 1 && (key_mask_stride < 0 || (key_mask_stride != 0 && key_mask_stride < c.Lk)))
         return ops_fail(DT_ERR_INVALID_ARG, "key_mask_stride must be 0 (one mask for all) or at least Lk");
     if ((reinterpret_cast<uintptr_t>(key_lens_dev) | reinterpret_cast<uintptr_t>(lse_out_dev)) & 3u)

@@ -20,7 +20,7 @@
 // Keys that do not count are masked by the MMA itself: Q K^T of such a tile gets one more k-step, a column of ones times a
 // column of -inf / 0, which leaves -inf in S for every one of them; their K and V rows are zeroed, so that what stands there
 // (NaN, infinities) has no effect.  The softmax does nothing for a mask (selecting 128 logits by bits took 800 cycles a tile).
-// Tiles behind the last key that counts are never loaded, and the last tile's P V stops at its last 16 keys that may.
+// Tiles behind a request's length are never loaded.
 //
 // Few items and many keys: the item's tiles are split over the CTAs of a cluster, which leave their states (O, m, l) in shared
 // memory, where K and V were, and join them across the cluster (as the few-row kernel does).
@@ -29,7 +29,7 @@
 // tokens x 40 heads against 512 keys run in 662 us alone (1197 TFLOP/s, tensor pipe 66 % busy), 680 in short runs and 790 to
 // 820 at the power cap, where Q and OUT cost 1.9 TB/s of HBM besides; 2048 keys 604 us for as much work, 1312 TFLOP/s.  D = 64: the
 // exponentials, if the two tiles' fall beside each other (32760 x 40 x 512 keys: 207 us, 828 TFLOP/s; in step 285), and the
-// latency of a tile's chain where an item has two tiles (2 x 17550 x 32 heads, 226 keys 110 us, with masks or lengths 150).
+// latency of a tile's chain where an item has two tiles (2 x 17550 x 32 heads, 226 keys 110 us, with masks or lengths 140 to 160).
 //
 // Every wait on an mbarrier is bounded; on expiry the CTA records STATUS_WAIT_TIMEOUT, leaves its loops, frees TMEM and
 // returns.
@@ -143,6 +143,14 @@ struct CursorOf {
         do next_item(p);
         while (valid && tiles == 0);
     }
+    // whether any key of this CTA's tiles counts (a whole warp asks)
+    __device__ __forceinline__ bool any_key(const CrossParams &c) const {
+        const int from = (SPLIT ? t0 : 0) * TILE, to = min(len, from + tiles * TILE);
+        bool any = false;
+#pragma unroll 1
+        for (int key = from + (int)(threadIdx.x & 31); key < to; key += 32) any |= __ldg(c.key_mask + b * c.mask_stride + key) != 0;
+        return __any_sync(0xFFFFFFFFu, any) != 0;
+    }
     __device__ __forceinline__ int row0() const { return qb * (NQ * TILE); }
     // keys in the tile that do not count: a mask may have holes anywhere, the last tile may be ragged
     __device__ __forceinline__ bool masked(const CrossParams &c) const { return c.key_mask != nullptr || len < key0() + TILE; }
@@ -167,6 +175,16 @@ __device__ __noinline__ void scale_o(uint32_t o_tmem, float alpha) {
         for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * alpha);
         tmem_st_x32(o_tmem + c0, o);
     }
+    tmem_wait_st();
+}
+
+template <int D>
+__device__ __noinline__ void zero_o(uint32_t o_tmem) {
+    uint32_t o[32];
+#pragma unroll
+    for (int c = 0; c < 32; ++c) o[c] = 0u;
+#pragma unroll 1
+    for (int c0 = 0; c0 < D; c0 += 32) tmem_st_x32(o_tmem + c0, o);
     tmem_wait_st();
 }
 
@@ -671,6 +689,19 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 mbar_arrive(bars.p_full + 8 * q);
             }
             if (!ok) break;
+            // A request's mask may leave no key at all.  Its tiles run all the same, and give zeros and m = -inf -- but for rows
+            // of Q with a NaN or an infinity, which times a key's zeros is NaN: then O is zeroed here, before the epilogue reads it.
+            if (MASKED && p.c.key_mask != nullptr && __any_sync(0xFFFFFFFFu, l_sum != l_sum) && !it.any_key(p.c)) {
+                ok = wait_all(bars.pv_done + 8 * q, pv_phase);
+                if (!ok) break;
+                pv_phase ^= 1u;
+                p_stored = false;
+                tc_fence_after();
+                zero_o<D>(o_tmem);
+                tc_fence_before();
+                m_used = -INFINITY;
+                l_sum = 0.f;
+            }
             // (m, l) for the epilogue, once it has read the item before's: it hands O back behind that, and with more than one tile
             // P V of the second has waited for it.  Without this wait ml_full could complete twice before the epilogue looks.
             if (p_items > 0 && it.tiles == 1) ok = wait_all(bars.o_free + 8 * q, (p_items - 1) & 1u);

@@ -22,7 +22,9 @@ dt_status ops_device(const OpsDevice **out);
 const char *ops_last_error();
 
 // B, L, H, D strides in elements: D's is 1, the others are multiples of 8 (a stride of a dimension of one entry is not
-// looked at), the base is 16-byte aligned.  Inputs may repeat (stride 0) along the batch; outputs may not.
-dt_status check_blhd(const char *name, const void *base, const int64_t *s, int B, int L, int H, bool output);
+// looked at), the base is 16-byte aligned.  Inputs may repeat (stride 0) along the batch; an output's rows may not overlap.
+dt_status check_blhd(const char *name, const void *base, const int64_t *s, int B, int L, int H, int D, bool output);
+// An output and an input with one base: in place, which needs the same strides.
+bool same_strides(const int64_t *a, const int64_t *b, int B, int L, int H);
 
 }  // namespace dt

@@ -1,4 +1,5 @@
 // What the context-free operators share: error text, facts about the current device, argument checks.
+#include <algorithm>
 #include <atomic>
 #include <cstdio>
 #include <cstring>
@@ -57,7 +58,7 @@ dt_status ops_device(const OpsDevice **out) {
     return DT_OK;
 }
 
-dt_status check_blhd(const char *name, const void *base, const int64_t *s, int B, int L, int H, bool output) {
+dt_status check_blhd(const char *name, const void *base, const int64_t *s, int B, int L, int H, int D, bool output) {
     char text[128];
     const char *why = nullptr;
     const int n[3] = {B, L, H};
@@ -70,9 +71,23 @@ dt_status check_blhd(const char *name, const void *base, const int64_t *s, int B
             const bool repeats = d == 0 && s[d] == 0 && !output;
             if (!repeats && (s[d] <= 0 || s[d] % 8 != 0)) why = "strides of B, L, H must be positive multiples of 8 elements";
         }
+    if (!why && output) {   // from the innermost dimension outwards, each step beyond what lies within
+        int at[3] = {0, 1, 2};
+        std::sort(at, at + 3, [&](int i, int j) { return s[i] < s[j]; });
+        int64_t extent = D;
+        for (int d : at) {
+            if (n[d] <= 1) continue;
+            if (s[d] < extent) why = "an output's rows must not overlap";
+            extent += s[d] * (n[d] - 1);
+        }
+    }
     if (!why) return DT_OK;
     snprintf(text, sizeof text, "%s: %s", name, why);
     return ops_fail(DT_ERR_INVALID_ARG, text);
+}
+
+bool same_strides(const int64_t *a, const int64_t *b, int B, int L, int H) {
+    return (B <= 1 || a[0] == b[0]) && (L <= 1 || a[1] == b[1]) && (H <= 1 || a[2] == b[2]);
 }
 
 }  // namespace dt

@@ -255,10 +255,6 @@ cudaError_t launch_rope(const RopeParams &p, int unit, cudaStream_t st) {
     return cudaGetLastError();
 }
 
-bool same_strides(const int64_t a[4], const int64_t b[4], int B, int L, int H) {
-    return (B <= 1 || a[0] == b[0]) && (L <= 1 || a[1] == b[1]) && (H <= 1 || a[2] == b[2]);
-}
-
 }  // namespace
 }  // namespace dt
 
@@ -280,15 +276,17 @@ extern "C" dt_status dt_rope(const dt_rope_config *cfg, const void *q_dev, const
     if ((long long)c.B * c.L > 0x7FFFFFFFLL) return ops_fail(DT_ERR_UNSUPPORTED, "more than 2^31 - 1 tokens");
     if ((long long)c.B * c.L == 0) return DT_OK;
     dt_status s;
-    if ((s = check_blhd("q", q_dev, q_strides_blhd, c.B, c.L, c.H, false)) != DT_OK) return s;
-    if ((s = check_blhd("q_out", q_out_dev, q_out_strides_blhd, c.B, c.L, c.H, true)) != DT_OK) return s;
+    if ((s = check_blhd("q", q_dev, q_strides_blhd, c.B, c.L, c.H, c.D, false)) != DT_OK) return s;
+    if ((s = check_blhd("q_out", q_out_dev, q_out_strides_blhd, c.B, c.L, c.H, c.D, true)) != DT_OK) return s;
     if (q_dev == q_out_dev && !same_strides(q_strides_blhd, q_out_strides_blhd, c.B, c.L, c.H))
         return ops_fail(DT_ERR_INVALID_ARG, "q in place needs the same strides");
     if (c.H_k > 0) {
-        if ((s = check_blhd("k", k_dev, k_strides_blhd, c.B, c.L, c.H_k, false)) != DT_OK) return s;
-        if ((s = check_blhd("k_out", k_out_dev, k_out_strides_blhd, c.B, c.L, c.H_k, true)) != DT_OK) return s;
+        if ((s = check_blhd("k", k_dev, k_strides_blhd, c.B, c.L, c.H_k, c.D, false)) != DT_OK) return s;
+        if ((s = check_blhd("k_out", k_out_dev, k_out_strides_blhd, c.B, c.L, c.H_k, c.D, true)) != DT_OK) return s;
         if (k_dev == k_out_dev && !same_strides(k_strides_blhd, k_out_strides_blhd, c.B, c.L, c.H_k))
             return ops_fail(DT_ERR_INVALID_ARG, "k in place needs the same strides");
+        if (q_out_dev == k_out_dev || q_out_dev == k_dev || k_out_dev == q_dev)
+            return ops_fail(DT_ERR_INVALID_ARG, "an output of one of q and k is the other's tensor");
     }
     if (!freqs_dev || (reinterpret_cast<uintptr_t>(freqs_dev) & 7u)) return ops_fail(DT_ERR_INVALID_ARG, "freqs must be an 8-byte aligned device pointer");
     if (!positions_dev && c.axes != 1) return ops_fail(DT_ERR_INVALID_ARG, "more than one axis needs positions");

@@ -24,7 +24,7 @@ def s4(b=4096, l=128, h=64, d=1):
     return (C.c_int64 * 4)(b, l, h, d)
 
 
-def rope_call(lib, q=P, qs=None, qo=P, qos=None, k=P, ks=None, ko=P, kos=None, f=P, pos=P, ps=(0, 1, 0), **kw):
+def rope_call(lib, q=P, qs=None, qo=P, qos=None, k=P + 2 ** 20, ks=None, ko=P + 2 ** 20, kos=None, f=P, pos=P, ps=(0, 1, 0), **kw):
     c = dict(dtype=0, B=2, L=3, H=2, H_k=2, D=64, rotary_dim=64, layout=0, axes=1, transpose=0, attn_factor=1.0)
     c.update(kw)
     cfg = dt.dt_rope_config(*[c[n] for n, _ in dt.dt_rope_config._fields_])
@@ -41,6 +41,8 @@ def rope_call(lib, q=P, qs=None, qo=P, qos=None, k=P, ks=None, ko=P, kos=None, f
     (dict(q=P + 8), INV), (dict(ko=P + 2), INV), (dict(qs=s4(d=2)), INV), (dict(qs=s4(l=-128)), INV), (dict(qs=s4(h=60)), INV),
     (dict(qos=s4(b=0)), INV), (dict(kos=s4(l=0)), INV), (dict(ks=s4(l=0)), INV), (dict(qos=s4(l=256)), INV), (dict(kos=s4(b=8192)), INV),
     (dict(pos=None, axes=2), INV), (dict(ps=None), INV), (dict(pos=P + 2), INV),
+    (dict(qo=P + 2 ** 20, q=P + 2 ** 21), INV), (dict(ko=P, q=P + 2 ** 21), INV), (dict(ko=P), INV),
+    (dict(qo=P + 64, qos=s4(h=32)), INV), (dict(qo=P + 64, qos=s4(l=64)), INV), (dict(qo=P + 64, qos=s4(b=320)), INV),
 ])
 def test_rope_refusals(lib, kw, status):
     assert rope_call(lib, **kw) == status
@@ -56,7 +58,7 @@ def test_empty_calls_are_fine_without_a_device(lib):
     assert lib.dt_cross_attn(None, None, None, None, None, None, None, None, None, 0, None, None, None, None) == INV
 
 
-def norm_call(lib, x=P, w=P, r=P, ro=P, y=P, sc=P, **kw):
+def norm_call(lib, x=P, w=P, r=P + 2 ** 20, ro=P + 2 ** 20, y=P + 2 ** 21, sc=P, **kw):
     c = dict(dtype=0, weight_dtype=2, residual_dtype=2, out_kind=1, n0=2, n1=3, width=512, scale_group=0, x_strides=(1536, 512),
              residual_strides=(1536, 512), residual_out_strides=(1536, 512), y_strides=(1536, 512), eps=1e-6)
     c.update(kw)
@@ -74,13 +76,15 @@ def norm_call(lib, x=P, w=P, r=P, ro=P, y=P, sc=P, **kw):
     (dict(x_strides=(1536, 516)), INV), (dict(x_strides=(-1536, 512)), INV), (dict(y_strides=(1536, 0)), INV), (dict(y_strides=(1536, 504)), INV),
     (dict(residual_out_strides=(0, 512)), INV), (dict(residual_strides=(1, 512)), INV),
     (dict(x=P + 8), INV), (dict(w=P + 4), INV), (dict(y=P + 4), INV), (dict(y=P + 8, out_kind=0), INV), (dict(sc=P + 2), INV), (dict(ro=P + 8), INV),
+    (dict(y=P), INV), (dict(y=P, out_kind=0, y_strides=(1536, 520)), INV), (dict(y=P + 2 ** 20), INV), (dict(ro=P), INV),
+    (dict(residual_out_strides=(4096, 512)), INV), (dict(ro=P, residual_dtype=0, residual_out_strides=(1600, 512)), INV),
 ])
 def test_norm_refusals(lib, kw, status):
     assert norm_call(lib, **kw) == status
     assert lib.dt_last_error(None)
 
 
-def cross_call(lib, q=P, qs=None, k=P, ks=None, v=P, vs=None, lens=None, mask=None, ms=0, o=P, os=None, lse=None, **kw):
+def cross_call(lib, q=P, qs=None, k=P + 2 ** 20, ks=None, v=P + 2 ** 20, vs=None, lens=None, mask=None, ms=0, o=P, os=None, lse=None, **kw):
     c = dict(dtype=0, B=2, Lq=3, Lk=5, H=4, H_kv=2, D=64, softmax_scale=0.125)
     c.update(kw)
     cfg = dt.dt_cross_config(*[c[n] for n, _ in dt.dt_cross_config._fields_])
@@ -95,6 +99,7 @@ def cross_call(lib, q=P, qs=None, k=P, ks=None, v=P, vs=None, lens=None, mask=No
     (dict(q=None), INV), (dict(k=None), INV), (dict(v=None), INV), (dict(o=None), INV), (dict(q=P + 8), INV), (dict(o=P + 2), INV),
     (dict(ks=s4(l=0)), INV), (dict(ks=s4(h=0)), INV), (dict(vs=s4(d=2)), INV), (dict(vs=s4(l=260)), INV), (dict(os=s4(b=0)), INV), (dict(qs=s4(l=-256)), INV),
     (dict(mask=P, ms=4), INV), (dict(mask=P, ms=-5), INV), (dict(lens=P + 2), INV), (dict(lse=P + 1), INV),
+    (dict(Lk=2 ** 26 + 1), UNS), (dict(o=P + 2 ** 20), INV), (dict(os=s4(l=512)), INV), (dict(o=P + 64, os=s4(l=128)), INV),
 ])
 def test_cross_refusals(lib, kw, status):
     assert cross_call(lib, **kw) == status

@@ -1,9 +1,11 @@
 """Operators around the self-attention (rotary positions, norm with the residual, cross attention) on the GPU against plain
 64-bit forms, at the sizes, strides and masks where they can go wrong.  Tolerances: tests/block_ops_reference.py."""
+import ctypes
 import math
 import os
 import subprocess
 import sys
+import threading
 
 import pytest
 import torch
@@ -530,6 +532,103 @@ def test_cross_where_no_request_has_a_key(Lq, Lk):
         torch.cuda.synchronize()
         dt.dt_poll_ops()
         assert (out == 0).all() and (lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Lq,Lk", [(2, 300), (4000, 300), (600, 2000)])
+def test_cross_rows_of_q_without_a_number_and_without_keys(Lq, Lk, D, dtype):
+    """A request whose mask leaves no key gives OUT = 0, LSE = -inf for every q; the other request is as it was."""
+    q, k, v = (rnd((2, n, 4, D), i, dtype) for i, n in enumerate((Lq, Lk, Lk)))
+    mask = torch.ones((2, Lk), dtype=torch.bool, device="cuda")
+    mask[1] = False
+    want = torch.empty_like(q)
+    dt.dt_cross_attn(q, k, v, want, 0.1, key_mask=mask)
+    q[1, ::3] = float("nan")
+    q[1, 1::3] = float("inf")
+    out, lse = torch.empty_like(q), torch.empty((2, 4, Lq), device="cuda")
+    dt.dt_cross_attn(q, k, v, out, 0.1, key_mask=mask, lse_out=lse)
+    torch.cuda.synchronize()
+    dt.dt_poll_ops()
+    assert torch.equal(out[0], want[0]) and torch.isfinite(lse[0]).all()
+    assert (out[1] == 0).all() and (lse[1] == -math.inf).all()
+
+
+@pytest.mark.parametrize("Lq,Lk", [(2, 300), (4000, 300), (600, 2000)])
+def test_cross_a_row_of_q_without_a_number_stays_alone(Lq, Lk):
+    """A NaN in a row of q with keys gives NaN there, and changes no other row."""
+    q, k, v = (rnd((1, n, 4, 128), i, BF16) for i, n in enumerate((Lq, Lk, Lk)))
+    wo, wl, to, tl = ref.cross(q, k, v, 0.1)
+    q[0, Lq // 2, 1, 5] = float("nan")
+    out, lse = torch.empty_like(q), torch.empty((1, 4, Lq), device="cuda")
+    dt.dt_cross_attn(q, k, v, out, 0.1, lse_out=lse)
+    torch.cuda.synchronize()
+    dt.dt_poll_ops()
+    assert out[0, Lq // 2, 1].isnan().all() and lse[0, 1, Lq // 2].isnan()
+    out[0, Lq // 2, 1], lse[0, 1, Lq // 2] = wo[0, Lq // 2, 1].to(BF16), wl[0, 1, Lq // 2].float()
+    check(out, wo, to, "out")
+    check(lse, wl, tl, "lse")
+
+
+@pytest.mark.parametrize("width", [64, 512, 2048, 5120])
+def test_norm_scales_near_the_end_of_fp32(width):
+    """y of 10^38: the scale is 10^38 / 448 and the largest values are 448."""
+    x = rnd((7, width), 1, BF16).sign()
+    x[x == 0] = 1
+    y, sc = torch.empty((7, width), device="cuda", dtype=E4M3), torch.empty((7, 1), device="cuda")
+    dt.dt_add_rmsnorm(x, torch.full((width,), 1e38, device="cuda"), y, 0.0, scales=sc)
+    torch.cuda.synchronize()
+    assert torch.equal(y.float(), 448 * x.float())
+    # r, r * w, and the quotient by 448, of a few roundings each
+    assert ((sc.double() * 448 / 1e38 - 1).abs() <= 2 ** -20).all()
+
+
+def test_norm_called_from_two_threads():
+    """Rows of two widths, both beyond the shared memory that a launch has without asking, from two threads at once (through
+    ctypes, which lets go of the interpreter)."""
+    lib = dt.lib()
+    n = 3000
+    work, status = [], []
+    for i, width in enumerate((12800, 16384)):
+        x = rnd((n, width), i, BF16)
+        y = torch.empty_like(x)
+        pair = ctypes.c_int64 * 2
+        cfg = dt.dt_norm_config(0, 0, 0, 0, 1, n, width, 0, pair(0, width), pair(0, width), pair(0, width), pair(0, width), 1e-6)
+        work.append((x, y, cfg, torch.cuda.Stream()))
+
+    def run(x, y, cfg, stream):
+        status.extend(lib.dt_add_rmsnorm(ctypes.byref(cfg), x.data_ptr(), None, None, None, y.data_ptr(), None, stream.cuda_stream) for _ in range(300))
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=run, args=w) for w in work]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert status == [dt.DT_OK] * 600
+    for x, y, _, _ in work:
+        h, want = ref.norm(x, None, 1e-6, None)
+        norm_check(None, None, None, None, y, None, 1e-6, h, want, x.shape)
+
+
+@pytest.mark.parametrize("call", ["dt.dt_rope(q, None, q, None, f)", "dt.dt_add_rmsnorm(q, None, q, 1e-6)",
+                                  "dt.dt_cross_attn(q[:, :1], q, q, o[:, :1], 0.1)", "dt.dt_cross_attn(q, q, q, o, 0.1)"])
+def test_first_call_of_a_process_inside_a_capture(call):
+    text = f"""
+import torch
+from paper_2607_15650_b200 import binding as dt
+q, o = torch.ones((1, 3000, 16, 64), device="cuda", dtype=torch.bfloat16), torch.zeros((1, 3000, 16, 64), device="cuda", dtype=torch.bfloat16)
+f = dt.dt_rope_freqs(64)[0][None].cuda()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    {call}
+g.replay()
+torch.cuda.synchronize()
+dt.dt_poll_ops()
+print(q.isfinite().all().item() and o.isfinite().all().item())
+"""
+    r = subprocess.run([sys.executable, "-c", text], cwd=ROOT, capture_output=True, text=True, timeout=240)
+    assert r.returncode == 0 and r.stdout.split()[-1] == "True", r.stdout + r.stderr
 
 
 def test_cross_offsets_beyond_32_bits():
