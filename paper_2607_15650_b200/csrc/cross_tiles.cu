@@ -28,8 +28,14 @@
 // Bound, D = 128: MMA and exponentials alike (2048 cycles each per pair of 128 x 128 tiles; the loop takes 2850), then power: 75600
 // tokens x 40 heads against 512 keys run in 662 us alone (1197 TFLOP/s, tensor pipe 66 % busy), 680 in short runs and 790 to
 // 820 at the power cap, where Q and OUT cost 1.9 TB/s of HBM besides; 2048 keys 604 us for as much work, 1312 TFLOP/s.  D = 64: the
-// exponentials, if the two tiles' fall beside each other (32760 x 40 x 512 keys: 207 us, 828 TFLOP/s; in step 285), and the
-// latency of a tile's chain where an item has two tiles (2 x 17550 x 32 heads, 226 keys 110 us, with masks or lengths 140 to 160).
+// exponentials, if the two tiles' fall beside each other (32760 x 40 x 512 keys: 212 us, 810 TFLOP/s; in step 285), and the
+// latency of a tile's chain where an item has two tiles (2 x 17550 x 32 heads, 226 keys 125 us, with a mask 118, lengths 131).
+//
+// Size: warps of six roles share each scheduler's instruction cache, and straight-line code waits for its own instructions
+// (traced: 1000 cycles for issuing a P V of 8 MMAs).  So every role has one loop with one place for each step, its prologue
+// included, and in the masked kernels the MMAs' and the epilogue's loops stay rolled: 57 KB for 84, and 157 -> 142 us
+// (226 keys with a mask, as above) and 154 -> 138 (lengths); with the masking warp's bytes asked for a tile ahead, 118 and 131.  Without
+// masks there is room: rolled MMAs cost there (D = 128, 512 keys: 680 -> 740 us).
 //
 // Every wait on an mbarrier is bounded; on expiry the CTA records STATUS_WAIT_TIMEOUT, leaves its loops, frees TMEM and
 // returns.
@@ -49,7 +55,7 @@ constexpr int THREADS = SOFTMAX_THREADS + 256;
 constexpr int LAUNCH_REGS = 128, REGS_SOFTMAX = 184, REGS_OTHER = 64, REGS_OUT = 80;
 static_assert((REGS_SOFTMAX - LAUNCH_REGS) * SOFTMAX_THREADS <= (LAUNCH_REGS - REGS_OTHER) * 128 + (LAUNCH_REGS - REGS_OUT) * 128,
               "softmax warps would wait forever for registers nobody releases");
-constexpr long long WAIT_LIMIT_CYCLES = 4000000000ll;   // SM clock cycles: about 2 s
+constexpr uint32_t WAIT_LIMIT_NS = 2000000000u;
 constexpr float RESCALE_AT = 8.0f;
 
 template <int D>
@@ -134,14 +140,14 @@ struct CursorOf {
         }
     }
     __device__ __forceinline__ int key0() const { return ((SPLIT ? t0 : 0) + t) * TILE; }   // of the current tile
-    __device__ __forceinline__ void first(const TileParams &p) {
-        first_item(p);
+    __device__ __forceinline__ void skip_empty(const TileParams &p) {
+#pragma unroll 1
         while (valid && tiles == 0) next_item(p);
     }
     __device__ __forceinline__ void advance(const TileParams &p) {
         if (++t < tiles) return;
-        do next_item(p);
-        while (valid && tiles == 0);
+        next_item(p);
+        skip_empty(p);
     }
     // whether any key of this CTA's tiles counts (a whole warp asks)
     __device__ __forceinline__ bool any_key(const CrossParams &c) const {
@@ -188,6 +194,22 @@ __device__ __noinline__ void zero_o(uint32_t o_tmem) {
     tmem_wait_st();
 }
 
+// mbar_wait_bounded in fewer instructions: the kernel has thirty of them, and loses by its size.
+__device__ __forceinline__ uint32_t timer_ns_lo() {   // wraps after 4.3 s
+    uint32_t t;
+    asm volatile("mov.u32 %0, %%globaltimer_lo;" : "=r"(t));
+    return t;
+}
+__device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity, const volatile int *abort_flag) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const uint32_t since = timer_ns_lo();
+    uint32_t n = 0;
+#pragma unroll 1
+    while (!mbar_try_wait(bar, parity))
+        if ((++n & 0x3Fu) == 0u && (*abort_flag || timer_ns_lo() - since > WAIT_LIMIT_NS)) return false;
+    return true;
+}
+
 // MASKED: some tile may hold keys that do not count (lengths, a mask, or Lk not a multiple of 128); without it nothing looks.
 template <int D, bool FP16, bool MASKED, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1)
@@ -195,6 +217,7 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                   const __grid_constant__ CUtensorMap tmap_v, const TileParams p) {
     using C = Cfg<D>;
     using Cursor = CursorOf<SPLIT>;
+    constexpr int MMA_UNROLL = MASKED ? 2 : 8, OUT_UNROLL = MASKED ? 1 : 2;   // (see "Size" above)
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_flag;
@@ -223,7 +246,7 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
 
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     volatile int *abort_ptr = &abort_flag;
-    auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_bounded(bar, parity, abort_ptr, WAIT_LIMIT_CYCLES); };
+    auto wait = [&](uint32_t bar, uint32_t parity) { return wait_bounded(bar, parity, abort_ptr); };
     // Every wait of a whole warp ends in a vote, so that no lane runs two phases ahead of another.
     auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, wait(bar, parity)) != 0; };
 
@@ -276,8 +299,7 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         const int piece = lane & 7;
         uint32_t phase = 0;
         bool ok = true;
-        Cursor it;
-        it.first_item(p);
+        Cursor it; it.first_item(p);
         if constexpr (SPLIT) {
             // This CTA's state goes to where K and V were (every P V is complete): rows of fp32, 16-byte piece c of row r at
             // c ^ (r & 15); it is joined with the cluster's others below.
@@ -303,7 +325,9 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             }
             it.valid = false;
         }
+#pragma unroll 1
         for (; it.valid && ok; it.next_item(p)) {
+#pragma unroll 1
             for (int q = 0; q < NQ && ok; ++q) {
                 const int q_row = it.row0() + q * TILE + row_in_tile;
                 const bool row_valid = q_row < p.c.Lq;
@@ -323,9 +347,9 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 // Rows leave through warp-private shared memory: 128 bytes of every row at a time (swizzled), read back so
                 // that 8 lanes hold the 128 contiguous bytes of one row.
                 const int rows_left = p.c.Lq - (q_row - lane);   // valid rows of this warp's 32
-#pragma unroll
+#pragma unroll OUT_UNROLL
                 for (int c0 = 0; c0 < D; c0 += 64) {
-#pragma unroll
+#pragma unroll OUT_UNROLL
                     for (int half = 0; half < 2; ++half) {
                         uint32_t o[32];
                         if (keys) {
@@ -378,7 +402,7 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 uint32_t st = 0, ph = 0, q_ph = 0;
                 bool ok = true;
                 auto load_q = [&](const Cursor &it) {
-#pragma unroll
+#pragma unroll 1
                     for (int q = 0; q < NQ; ++q) {
                         ok = ok && wait(bars.q_empty + 8 * q, q_ph ^ 1u);
                         if (!ok) return;
@@ -403,20 +427,19 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                         tma_load_4d(kv_smem + st * C::TILE_BYTES + hf * C::HALF_BYTES, is_k ? &tmap_k : &tmap_v, bar, hf * 64, h, it.key0(), b);
                     if (++st == C::STAGES) { st = 0; ph ^= 1u; }
                 };
-                Cursor cur;
-                cur.first(p);
-                if (cur.valid) {
-                    load_q(cur);
-                    load_kv(cur, true);
-                }
-                while (cur.valid && ok) {
-                    Cursor nxt = cur;
-                    nxt.advance(p);
-                    if (nxt.valid) load_kv(nxt, true);
-                    load_kv(cur, false);
+                Cursor nxt; nxt.first_item(p); Cursor cur = nxt;
+                nxt.skip_empty(p);
+                bool have = false;   // a tile whose V is still to be loaded
+#pragma unroll 1
+                while (ok && (have || nxt.valid)) {
+#pragma unroll 1
+                    for (int v = 0; v < 2; ++v)   // K of the next tile, V of this one
+                        if (v ? have : nxt.valid) load_kv(v ? cur : nxt, v == 0);
                     // (after this V: nothing that Q's place waits for is behind it)
                     if (nxt.valid && nxt.t == 0) load_q(nxt);
                     cur = nxt;
+                    have = nxt.valid;
+                    if (have) nxt.advance(p);
                 }
                 if (!ok) {
                     if (!*abort_ptr) atomicOr(p.c.status, STATUS_WAIT_TIMEOUT);
@@ -431,15 +454,23 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             // -------------------------------------------------------- tiles with keys that do not count
             uint32_t raw_ph = 0;   // parity of every stage's kv_raw (one bit each)
             bool ok = true;
-            // which of this lane's four keys of a tile count (looked up a tile ahead: the bytes' latency is not on the way)
-            auto keys_on = [&](const Cursor &it) {
+            // which of this lane's four keys of a tile count: the bytes are asked for a tile ahead and looked at a tile later
+            struct Four { uint32_t v[4]; };
+            auto load_bytes = [&](const Cursor &it) {
                 const uint8_t *m = p.c.key_mask ? p.c.key_mask + it.b * p.c.mask_stride : nullptr;
-                uint32_t on = 0;
+                Four x;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int key = it.key0() + 32 * i + lane;
-                    if (it.valid && key < it.len && (m == nullptr || __ldg(m + key) != 0)) on |= 1u << i;
+                    x.v[i] = it.valid && key < it.len;
+                    if (x.v[i] != 0u && m != nullptr) x.v[i] = __ldg(m + key);
                 }
+                return x;
+            };
+            auto bits_of = [&](const Four &x) {
+                uint32_t on = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) on |= (uint32_t)(x.v[i] != 0u) << i;
                 return on;
             };
             // zeroes the rows of a landed tile (those behind Lk are zeros: the tensor map ends there)
@@ -447,7 +478,7 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 ok = ok && wait_all(bars.kv_raw + 8 * st, (raw_ph >> st) & 1u);
                 if (!ok) return;
                 raw_ph ^= 1u << st;
-#pragma unroll
+#pragma unroll 1
                 for (int i = 0; i < 4; ++i) {
                     const int r = 32 * i + lane;
                     if ((on >> i & 1u) || it.key0() + r >= p.c.Lk) continue;
@@ -458,38 +489,37 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 }
             };
             // V of a tile and K of the next land one behind the other: both are passed on at once, behind one fence
-            auto pass_on = [&](bool k, const Cursor &kt, uint32_t k_on, uint32_t k_st, bool v, const Cursor &vt, uint32_t v_on, uint32_t v_st) {
-                if (k) {
-                    zero_rows(kt, k_on, k_st);
-                    if (!ok) return;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %2, %2};" ::"r"(mask_smem + k_st * C::COL_BYTES + (32 * i + lane) * 16), "r"(k_on >> i & 1u ? 0u : FP16 ? 0xFC00u : 0xFF80u), "r"(0) : "memory");
-                }
-                if (v) zero_rows(vt, v_on, v_st);
-                if (!ok || !(k || v)) return;
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0 && k) mbar_arrive(bars.kv_full + 8 * k_st);
-                if (lane == 0 && v) mbar_arrive(bars.kv_full + 8 * v_st);
-            };
-            Cursor cur, nxt;
-            cur.first(p);
-            nxt = cur;
-            if (cur.valid) nxt.advance(p);
-            uint32_t st = 1 % C::STAGES, on_cur = keys_on(cur), on_nxt = keys_on(nxt);
-            if (cur.valid) pass_on(cur.masked(p.c), cur, on_cur, 0, false, cur, 0, 0);   // K of the first tile
-            while (cur.valid && ok) {
+            Cursor nxt; nxt.first_item(p); Cursor cur = nxt;
+            nxt.skip_empty(p);
+            bool have = false;   // a tile whose V is still to be passed on
+            uint32_t st = 0, on_cur = 0, on_nxt = bits_of(load_bytes(nxt));
+#pragma unroll 1
+            while (ok && (have || nxt.valid)) {
                 Cursor far = nxt;
                 if (nxt.valid) far.advance(p);
-                const uint32_t on_far = keys_on(far), k_st = st;
+                const Four far_bytes = load_bytes(far);
+                const uint32_t k_st = st;
+                const bool k = nxt.valid && nxt.masked(p.c), v = have && cur.masked(p.c);
                 if (nxt.valid && ++st == C::STAGES) st = 0;
-                pass_on(nxt.valid && nxt.masked(p.c), nxt, on_nxt, k_st, cur.masked(p.c), cur, on_cur, st);
-                if (++st == C::STAGES) st = 0;
+#pragma unroll 1
+                for (int i = 0; i < 2 && ok; ++i)
+                    if (i ? v : k) zero_rows(i ? cur : nxt, i ? on_cur : on_nxt, i ? st : k_st);
+                if (k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %2, %2};" ::"r"(mask_smem + k_st * C::COL_BYTES + (32 * i + lane) * 16), "r"(on_nxt >> i & 1u ? 0u : FP16 ? 0xFC00u : 0xFF80u), "r"(0) : "memory");
+                if (ok && (k || v)) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0 && k) mbar_arrive(bars.kv_full + 8 * k_st);
+                    if (lane == 0 && v) mbar_arrive(bars.kv_full + 8 * st);
+                }
+                if (have && ++st == C::STAGES) st = 0;
+                have = nxt.valid;
                 cur = nxt;
                 nxt = far;
                 on_cur = on_nxt;
-                on_nxt = on_far;
+                on_nxt = bits_of(far_bytes);
             }
             if (!ok) {
                 if (lane == 0 && !*abort_ptr) atomicOr(p.c.status, STATUS_WAIT_TIMEOUT);
@@ -508,7 +538,7 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             auto issue_qk = [&](uint32_t st, bool masked) {
                 constexpr uint32_t IDESC_QK = make_idesc_bf16_f32(128, TILE, false, FP16);
                 const uint64_t b0 = kdesc0 + (uint64_t)((st * C::TILE_BYTES) >> 4);
-#pragma unroll
+#pragma unroll MMA_UNROLL
                 for (int kk = 0; kk < D / 16; ++kk) {
                     const uint32_t koff = ((kk / 4) * C::HALF_BYTES + (kk % 4) * 32) >> 4;
                     if (leader) mma_ss(tmem_base + C::S_COL, qdesc + koff, b0 + koff, IDESC_QK, kk > 0 ? 1u : 0u);
@@ -523,47 +553,30 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 constexpr uint32_t IDESC_PV = make_idesc_bf16_f32(128, D, true, FP16);
                 const uint64_t b0 = vdesc0 + (uint64_t)((st * C::TILE_BYTES) >> 4);
                 const uint32_t d = tmem_base + C::O_COL + mq * D, a = tmem_base + C::P_COL + mq * C::P_STRIDE;
-#pragma unroll
+#pragma unroll MMA_UNROLL
                 for (int kk = 0; kk < TILE / 16; ++kk)
                     if (leader) mma_ts(d, a + kk * 8, b0 + (uint64_t)((kk * 2048) >> 4), IDESC_PV, (accumulate || kk > 0) ? 1u : 0u);
             };
             // The one place for S is used by the tiles in turn, tile 0 first: a phase of s_free is one read of S.
             const uint32_t s_turn = mq ? 0u : 1u;
-            uint32_t place = 0, q_phase = 0, of_phase = 0, t_phase = 0;   // place: K/V tiles of the stream so far
+            uint32_t st = 0, ph = 0, q_phase = 0, of_phase = 0, t_phase = 0;   // place: K/V tiles of the stream so far
             bool ok = true;
-            Cursor cur;
-            cur.first(p);
-            if (cur.valid) {   // the stream's first Q K^T
-                ok = wait_all(bars.q_full + 8 * mq, 0u) && wait_all(bars.kv_full, 0u) && wait_all(bars.s_free, s_turn);
-                if (ok) {
-                    tc_fence_after();
-                    q_phase = 1u;
-                    issue_qk(0, cur.masked(p.c));
-                    if (leader) {
-                        tc_commit(bars.s_full + 8 * mq);
-                        tc_commit(bars.kv_empty);
-                        if (cur.tiles == 1) tc_commit(bars.q_empty + 8 * mq);
-                    }
-                    place = 1;
-                }
-            }
-            while (cur.valid && ok) {
-                // (the next item is looked up while this one's first tiles run)
-                Cursor nxt = cur;
-                nxt.t = nxt.tiles - 1;
-                nxt.advance(p);
-                const bool next_item = nxt.valid, next_single = nxt.tiles == 1;
-                const bool next_masked = MASKED && nxt.masked(p.c), any_mask = MASKED && p.c.key_mask != nullptr;
-                const bool ragged = MASKED && cur.len < cur.key0() + cur.tiles * TILE;   // (cur.t is 0)
-                const int tiles = cur.tiles;
+            Cursor nxt; nxt.first_item(p);
+            nxt.skip_empty(p);
+            int tiles = 1;                                // of the current item; before the first: a step without a P V
+            bool have = false, any_mask = false, ragged = false;
+#pragma unroll 1
+            while (ok && (have || nxt.valid)) {
+                const bool next_item = nxt.valid, next_single = nxt.tiles == 1, next_masked = MASKED && nxt.masked(p.c);
+#pragma unroll 1
                 for (int k = 0; k < tiles; ++k) {
                     const bool within = k + 1 < tiles, more = within || next_item;
-                    const uint32_t av = place + (more ? 1u : 0u), stv = av % C::STAGES;   // V of this tile
-                    ok = wait_all(bars.s_req + 8 * mq, t_phase);   // the softmax will be ready for its next S shortly
+                    uint32_t stv = st, phv = ph;   // V of this tile
+                    if (more && ++stv == C::STAGES) { stv = 0; phv ^= 1u; }
+                    if (have) ok = wait_all(bars.s_req + 8 * mq, t_phase);   // the softmax will be ready for its next S shortly
                     if (!ok) break;
                     if (more) {   // the next tile's Q K^T first: the softmax waits for it.  What it needs, and V, behind one vote
-                        const uint32_t st = place % C::STAGES;
-                        bool r = wait(bars.kv_full + 8 * st, (place / C::STAGES) & 1u) && wait(bars.kv_full + 8 * stv, (av / C::STAGES) & 1u) &&
+                        bool r = wait(bars.kv_full + 8 * st, ph) && (!have || wait(bars.kv_full + 8 * stv, phv)) &&
                                  wait(bars.s_free, s_turn);
                         if (!within) {
                             r = r && wait(bars.q_full + 8 * mq, q_phase);
@@ -579,8 +592,11 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                             if (within ? k + 2 == tiles : next_single) tc_commit(bars.q_empty + 8 * mq);   // its item's last Q K^T
                         }
                     }
+                    st = stv;
+                    ph = phv;
+                    if (!have) break;
                     ok = wait_all(bars.p_full + 8 * mq, t_phase);   // P is stored
-                    if (ok && !more) ok = wait_all(bars.kv_full + 8 * stv, (av / C::STAGES) & 1u);
+                    if (ok && !more) ok = wait_all(bars.kv_full + 8 * stv, phv);
                     if (ok && k == 0) {   // the epilogue of the item before has drained O
                         ok = wait_all(bars.o_free + 8 * mq, of_phase ^ 1u);
                         of_phase ^= 1u;
@@ -594,9 +610,16 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                         tc_commit(bars.kv_empty + 8 * stv);
                     }
                     t_phase ^= 1u;
-                    place = av + 1;
+                    if (++st == C::STAGES) { st = 0; ph ^= 1u; }
                 }
-                cur = nxt;
+                have = next_item;
+                if (have) {   // (the item after is looked up while this one's first tiles run)
+                    tiles = nxt.tiles;
+                    any_mask = MASKED && p.c.key_mask != nullptr;
+                    ragged = MASKED && nxt.len < nxt.key0() + tiles * TILE;   // (nxt.t is 0)
+                    nxt.t = tiles - 1;
+                    nxt.advance(p);
+                }
             }
             if (!ok) {
                 if (leader && !*abort_ptr) atomicOr(p.c.status, STATUS_WAIT_TIMEOUT);
@@ -614,9 +637,12 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         const uint32_t o_tmem = tmem_base + lane_addr + C::O_COL + q * D;
         uint32_t s_phase = 0, pv_phase = 0, p_items = 0;   // p_items: items handed to the epilogue
         bool ok = true, p_stored = false;   // p_stored: P's columns hold an earlier tile's P, which its P V may still read
-        Cursor it;
-        for (it.first(p); it.valid && ok; ) {
+        Cursor it; it.first_item(p);
+        it.skip_empty(p);
+#pragma unroll 1
+        while (it.valid && ok) {
             float m_used = -INFINITY, l_sum = 0.f;
+#pragma unroll 1
             for (int t = 0; t < it.tiles; ++t) {
                 ok = wait_all(bars.s_full + 8 * q, s_phase);
                 if (!ok) break;
@@ -724,8 +750,7 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     if constexpr (SPLIT) {
         cluster_arrive_wait();   // every CTA of the cluster has written its state (or given up: then the results do not count)
         if (warp < TMA_WARP) {   // (the softmax warps: they have the registers)
-            Cursor it;
-            it.first_item(p);
+            Cursor it; it.first_item(p);
             const int part = blockIdx.x - it.w * p.splits, per = NQ * TILE / p.splits;   // rows this CTA joins
             // a row's weights first, one thread each: the states' shares of OUT, and LSE
             if (threadIdx.x < per) {
