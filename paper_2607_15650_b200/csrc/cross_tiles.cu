@@ -33,7 +33,7 @@
 //
 // Size: warps of six roles share each scheduler's instruction cache, and straight-line code waits for its own instructions
 // (traced: 1000 cycles for issuing a P V of 8 MMAs).  So every role has one loop with one place for each step, its prologue
-// included, and in the masked kernels the MMAs' and the epilogue's loops stay rolled: 57 KB for 84, and 157 -> 142 us
+// included, and in the masked kernels the MMAs' and the epilogue's loops stay rolled: 59 KB for 84, and 157 -> 142 us
 // (226 keys with a mask, as above) and 154 -> 138 (lengths); with the masking warp's bytes asked for a tile ahead, 118 and 131.  Without
 // masks there is room: rolled MMAs cost there (D = 128, 512 keys: 680 -> 740 us).
 //
