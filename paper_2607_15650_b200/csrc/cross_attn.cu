@@ -26,7 +26,6 @@ namespace {
 
 // ------------------------------------------------------------------------------------------------ few rows
 constexpr int FEW_KEYS = 16, FEW_WARPS = 4, FEW_THREADS = FEW_WARPS * 32;
-constexpr float RESCALE_AT = 8.0f;   // binades that a logit may exceed the running reference by (P <= 2^8, exact in both types)
 
 template <bool FP16>
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -179,7 +178,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) cross_few_kernel(const CrossPa
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 x[e] = (now >> (e >> 1) & 1u) ? (s[n][0][e] + s[n][1][e]) * p.scale_log2 : -INFINITY;
-                over |= x[e] > m[n][e & 1] + RESCALE_AT;
+                over |= x[e] > m[n][e & 1] + P_TOP<FP16>;
             }
             if (__any_sync(0xFFFFFFFFu, over)) {
 #pragma unroll
@@ -188,7 +187,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) cross_few_kernel(const CrossPa
                     top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
                     top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
                     top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
-                    const float mn = fmaxf(m[n][c], top);
+                    const float mn = fmaxf(m[n][c], reference_of<FP16>(p, top));
                     const float alpha = mn == -INFINITY ? 1.f : ex2_approx(m[n][c] - mn);   // m = -inf: 0
                     m[n][c] = mn;
                     l[n][c] *= alpha;
@@ -205,8 +204,8 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) cross_few_kernel(const CrossPa
                 pr[e] = ex2_approx(x[e] - (m[n][e & 1] == -INFINITY ? 0.f : m[n][e & 1]));
                 l[n][e & 1] += pr[e];
             }
-            pf[n][0] = transpose8x8(pack_half2<FP16>(pr[0], pr[1]));
-            pf[n][1] = transpose8x8(pack_half2<FP16>(pr[2], pr[3]));
+            pf[n][0] = transpose8x8(pack_p<FP16>(pr[0], pr[1]));
+            pf[n][1] = transpose8x8(pack_p<FP16>(pr[2], pr[3]));
         }
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) {
@@ -399,6 +398,7 @@ extern "C" dt_status dt_cross_attn(const dt_cross_config *cfg, const void *q_dev
     p.B = c.B; p.Lq = c.Lq; p.Lk = c.Lk; p.H = c.H; p.Hkv = c.H_kv; p.rep = c.H / c.H_kv;
     p.scale_log2 = c.softmax_scale * LOG2E;
     p.status = dev->status;
+    p.ref_below = reference_below(c.Lk);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool fp16 = c.dtype == DT_VALUE_FP16;
     // Few rows or many?  The few-row kernel costs by blocks of 16 rows x keys (5.5e-5 us for D = 128, 3.8e-5 for 64, measured), the

@@ -18,8 +18,38 @@ struct CrossParams {
     long long qs[3], ks[3], vs[3], os[3];   // B, L, H strides in elements
     int B, Lq, Lk, H, Hkv, rep;
     float scale_log2;
+    float ref_below;                 // fp16: see reference_below
     int32_t *status;
 };
+
+// P = 2^(x - reference) is rounded to the inputs' type ahead of P V.  The reference is taken ref_below binades under the row's
+// maximum, and anew when a logit exceeds it by more than P_TOP: P <= 2^P_TOP, finite in both types.
+template <bool FP16>
+constexpr float P_TOP = FP16 ? 15.0f : 8.0f;
+// bf16 has fp32's range: every P is rounded by half a step (2^-9), and the reference stands at the maximum.  fp16's normal range
+// ends at 2^-14, and a P under 2^-25 is zero though the sum counts it: with the reference at the maximum, 2^20 keys of
+// 2^-25.4 of the largest weight each lost their 2 % of OUT altogether.  So fp16's reference stands lower: keys down to
+// 2^-(14 + ref_below) of the largest weight are rounded by half a step (2^-11), and smaller ones are off by 2^-(25 + ref_below) of
+// it each at most, which for all keys together is 2^-21 of the largest value of V up to 2^17 keys, and 2^-12 for 2^26.  What is left
+// up to P_TOP is how far a later tile's maximum may climb before O is rescaled: 8 binades for a prompt, where a rescaled tile is
+// one of a few (2048 keys x 32760 rows x 12 heads: 314 us with 8 binades, 322 with 6, 356 with 4, 390 with 2), down to 2 for very
+// many keys, whose maximum settles in the first of them (32760 keys x 8192 rows x 8 heads: 1140 us, 1040 with the reference at the
+// maximum and its small P zero).
+inline float reference_below(int Lk) {   // fp16's
+    int b = 7;
+    while (b < 13 && Lk > (2048 << (b - 7))) ++b;
+    return (float)b;
+}
+template <bool FP16>
+__device__ __forceinline__ float reference_of(const CrossParams &p, float top) { return FP16 ? top - p.ref_below : top; }
+// P as 16-bit pairs.  Logits beyond 2^24 are themselves off by binades in fp32 and may pass P_TOP by them: P stays finite.
+template <bool FP16>
+__device__ __forceinline__ uint32_t pack_p(float lo, float hi) {
+    if constexpr (!FP16) return pack_bf16x2(lo, hi);
+    uint32_t r;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
 
 __device__ __forceinline__ int keys_of(const CrossParams &p, int b) {
     return p.key_lens ? min(max(__ldg(p.key_lens + b), 0), p.Lk) : p.Lk;

@@ -13,9 +13,8 @@
 // all items of a CTA are one stream (the next item's first Q K^T is issued like any other, ahead of this item's last P V), and
 // the epilogue has warps of its own: with the softmax warps doing it, their turn at S held up the other tile for the whole of
 // it, 14100 cycles per item of 256 rows x 512 keys against 8192 of exponentials and as many of MMA.
-// The running maximum is exact: every tile's row maximum is taken, and when it exceeds the reference by more than RESCALE_AT
-// binades, O and l are rescaled (P <= 2^RESCALE_AT in between, which bf16 and fp16 hold at full precision), so no logit is out
-// of range.
+// Every tile's row maximum is taken, and when it exceeds the reference by more than P_TOP binades, O and l are rescaled, so no
+// logit is out of range (cross_attn.h says where the reference stands and what that costs small weights).
 //
 // Keys that do not count are masked by the MMA itself: Q K^T of such a tile gets one more k-step, a column of ones times a
 // column of -inf / 0, which leaves -inf in S for every one of them; their K and V rows are zeroed, so that what stands there
@@ -56,7 +55,6 @@ constexpr int LAUNCH_REGS = 128, REGS_SOFTMAX = 184, REGS_OTHER = 64, REGS_OUT =
 static_assert((REGS_SOFTMAX - LAUNCH_REGS) * SOFTMAX_THREADS <= (LAUNCH_REGS - REGS_OTHER) * 128 + (LAUNCH_REGS - REGS_OUT) * 128,
               "softmax warps would wait forever for registers nobody releases");
 constexpr uint32_t WAIT_LIMIT_NS = 2000000000u;
-constexpr float RESCALE_AT = 8.0f;
 
 template <int D>
 struct Cfg {
@@ -666,17 +664,18 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 const float m_tile = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.c.scale_log2;
                 bool p_place_free = !p_stored;
                 if (t == 0) {
-                    m_used = m_tile;
-                } else if (__any_sync(0xFFFFFFFFu, m_tile > m_used + RESCALE_AT)) {
+                    m_used = reference_of<FP16>(p.c, m_tile);
+                } else if (__any_sync(0xFFFFFFFFu, m_tile > m_used + P_TOP<FP16>)) {
                     // (O may only be touched once the P V of the tile before is complete)
                     ok = wait_all(bars.pv_done + 8 * q, pv_phase);
                     if (!ok) break;
                     pv_phase ^= 1u;
                     p_place_free = true;
                     tc_fence_after();
-                    const bool need = m_tile > m_used + RESCALE_AT;
-                    const float alpha = need ? ex2_approx(m_used - m_tile) : 1.0f;   // m_used = -inf: 0
-                    if (need) m_used = m_tile;
+                    const bool need = m_tile > m_used + P_TOP<FP16>;
+                    const float m_new = need ? reference_of<FP16>(p.c, m_tile) : m_used;
+                    const float alpha = need ? ex2_approx(m_used - m_new) : 1.0f;   // m_used = -inf: 0
+                    m_used = m_new;
                     l_sum *= alpha;
                     scale_o<D>(o_tmem, alpha);
                 }
@@ -691,7 +690,7 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                         const float2 x = __ffma2_rn(make_float2(s0, s1), sc2, nm2);
                         const float2 pp = make_float2(ex2_approx(x.x), ex2_approx(x.y));
                         rs4[(c >> 1) & 3] = __fadd2_rn(rs4[(c >> 1) & 3], pp);
-                        pk2[c >> 6][(c >> 1) & 31] = pack_half2<FP16>(pp.x, pp.y);
+                        pk2[c >> 6][(c >> 1) & 31] = pack_p<FP16>(pp.x, pp.y);
                     }
                 };
                 exps(0);

@@ -1,0 +1,92 @@
+"""Operators around the self-attention at the ends of their types' ranges, on the GPU against plain 64-bit forms."""
+import math
+
+import pytest
+import torch
+
+from paper_2607_15650_b200 import binding as dt
+from paper_2607_15650_b200 import build
+
+pytestmark = pytest.mark.gpu
+BF16, FP16 = torch.bfloat16, torch.float16
+U32 = 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    build.build()
+    dt.lib()
+
+
+# ---------------------------------------------------------------------------------------------- cross attention
+def falling(Lq, H, Lk, D, dtype, below, v):
+    """One key in every 16 of the first 512 has logit 0 and V = 0, all others stand `below` (binades, a tensor [Lk]) under it;
+    every query row is the same.  Returns the tensors and, for one row in 64 bits, LSE, OUT and what OUT may be off by."""
+    j = torch.arange(Lk, device="cuda")
+    first = (j < 512) & (j % 16 == 0)
+    x = torch.where(first, torch.zeros_like(below), -below)
+    q = torch.zeros((1, Lq, H, D), device="cuda", dtype=dtype)
+    q[..., 0], q[..., 1] = 1.0, 2.0 ** -6
+    k = torch.zeros((1, Lk, 1, D), device="cuda", dtype=dtype)
+    k[0, :, 0, 0] = x.to(dtype)
+    k[0, :, 0, 1] = ((x - k[0, :, 0, 0].float()) * 64).to(dtype)     # (what the type's step leaves of x)
+    vv = torch.where(first[:, None], torch.zeros_like(v), v).to(dtype)[None, :, None]
+    scale = math.log(2.0)
+    logit = (k[0, :, 0, 0].double() + k[0, :, 0, 1].double() / 64) * scale
+    lse = torch.logsumexp(logit, 0)
+    p = (logit - lse).exp()
+    vd = vv[0, :, 0].double()
+    u = torch.finfo(dtype).eps / 2
+    # a P of the type's normal range is off by u of itself; under it by half of fp16's fixed step, 2^-25, where the largest P is
+    # 2^top or more (bf16's range is fp32's).  The logit: two products and the scale in fp32.  The sums over the keys: in the tiles a
+    # thread adds 16 pairs four ways and then tile by tile, in the few-row kernel a lane one key in 8 of every 64th; O likewise, with
+    # a step of the running sum per addition of 16.
+    rel = u + 2 * (8 * U32 * logit.abs().max()) + 2 * (32 + Lk / 8) * U32
+    tol = (p @ vd.abs()) * rel + (p @ vd).abs() * u
+    if dtype == FP16:
+        top = min(13, max(7, math.ceil(math.log2(Lk)) - 4))
+        tol = tol + vd.abs().sum(0) * 2.0 ** -(25 + top) * p.max() + 2.0 ** -25
+    return q, k, vv, scale, lse, p @ vd, tol
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("Lq,H,Lk", [(1, 2, 32760), (1, 8, 2 ** 20), (1, 2, 1000), (256, 76, 1000), (256, 76, 6000), (256, 76, 32760), (256, 76, 2 ** 18), (512, 4, 32760)])
+@pytest.mark.parametrize("kind", ["equal", "spread", "deep"])
+def test_cross_many_small_weights_behind_a_large_one(kind, Lq, H, Lk, dtype):
+    """Few rows, tiles, and tiles split over a cluster.  The keys behind the large ones have 2^-25.4 of their weight each, or 2^-10 to
+    2^-25, or 2^-20 to 2^-34, and together they are all that OUT has."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(Lk)
+    r = torch.rand((Lk,), generator=g, device="cuda")
+    below = {"equal": torch.full_like(r, 25.4), "spread": 10 + 15 * r, "deep": 20 + 14 * r}[kind]
+    v = torch.randn((Lk, 64), generator=g, device="cuda") * 0.3 + 1
+    q, k, v, scale, wl, wo, tol = falling(Lq, H, Lk, 64, dtype, below, v)
+    out, lse = torch.full_like(q, 5.0), torch.full((1, H, Lq), 5.0, device="cuda")
+    dt.dt_cross_attn(q, k, v, out, scale, lse_out=lse)
+    torch.cuda.synchronize()
+    dt.dt_poll_ops()
+    assert ((lse.double() - wl).abs() <= 8 * U32 * 34 + (32 + Lk / 8) * U32 + 4 * U32 * (1 + abs(wl))).all()
+    over = (out.double() - wo).abs() - tol
+    assert over.max() <= 0, (over.max().item(), (out.double() - wo).abs().max().item(), wo.abs().max().item())
+
+
+@pytest.mark.parametrize("Lq,H", [(1, 2), (256, 76), (512, 4)])
+def test_cross_logits_just_within_reach_of_the_reference(Lq, H):
+    """Later keys that exceed the first ones by up to fp16's headroom, a binade at a time: P stays finite, and exact powers of two
+    come out exactly where all V are one."""
+    Lk, D = 4096, 64
+    for step in (1, 3, 4, 5, 15, 16):
+        j = torch.arange(Lk, device="cuda")
+        x = (j // 512).float() * step
+        q = torch.zeros((1, Lq, H, D), device="cuda", dtype=FP16)
+        q[..., 0] = 1.0
+        k = torch.zeros((1, Lk, 1, D), device="cuda", dtype=FP16)
+        k[0, :, 0, 0] = x.to(FP16)
+        v = torch.ones_like(k)
+        out, lse = torch.zeros_like(q), torch.zeros((1, H, Lq), device="cuda")
+        dt.dt_cross_attn(q, k, v, out, math.log(2.0), lse_out=lse)
+        torch.cuda.synchronize()
+        dt.dt_poll_ops()
+        want = torch.logsumexp(x.double() * math.log(2.0), 0)
+        assert (out == 1).all(), (step, out.min().item(), out.max().item())
+        assert ((lse.double() - want).abs() <= 8 * U32 * (x.max().item() + 1) + (32 + Lk / 8) * U32 + 4 * U32 * (1 + abs(want))).all()
