@@ -3,15 +3,17 @@
 //
 // Mathematics: the sum h is formed, squared, summed and scaled in fp32 and never rounded on the way to y; residual_out is
 // that same h rounded once to the residual's type.  scale = max(amax |y|, 2^-100) / 448 (448 = largest e4m3 value; the
-// floor keeps a row of zeros from dividing by zero), value = e4m3(y * 448 / amax), rounded to nearest even.  With r =
-// 1 / sqrt(mean + eps) > 0, amax |y| = r amax |h weight|: both of a row's reductions are made at once, before r is known.
+// floor keeps a row of zeros from dividing by zero), value = e4m3(y * 448 / amax), rounded to nearest even.  y is (h r) weight
+// with r = 1 / sqrt(mean + eps), in this order: h r is of the order of one, whereas h * weight may leave fp32 where y does not.  So
+// amax is taken once r is known, behind the first of a row's two reductions (amax |y| = r amax |h weight| would make both at
+// once: 20000 x 8192 to e4m3 without a residual 117 us for 132, 75600 x 5120 with one 750 for 680).
 //
 // Bound: HBM.  Every row is read once and stays in registers through its reductions, so a pass moves x, the residual in
 // and out, y and the scales, and nothing else.  What holds the rate up is how many rows are on the way at a time, since a
 // row's reductions are a chain of latencies: 8 to 32 lanes a row up to a width of 256, a warp up to 1024, a block above.
 // Measured in long runs: 75600 x 5120 bf16 with an fp32 residual, to e4m3, 692 us, 6.15 TB/s; 32760 x 5120 with a bf16 residual, by
 // groups of 128, 218 us, 5.4 TB/s; 561600 x 64 to fp16 25 us, 5.8 TB/s; without a residual and to 8 bits the instructions bind
-// first (20000 x 8192: 117 us, 4.2 TB/s); 3 rows of 5120 3.1 us.  Rows streamed through a ring in shared memory by bulk copies
+// first (20000 x 8192: 132 us, 3.7 TB/s); 3 rows of 5120 2.8 us.  Rows streamed through a ring in shared memory by bulk copies
 // instead of the next row in registers: slower throughout (246 us for the second).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -160,20 +162,17 @@ __device__ __forceinline__ float group_max(float m, int group_vecs) {
     if (group_vecs > 8) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
     return m;
 }
-// One vector of y from g = h * weight and the row's r; amax: of |g| over what shares a scale; scale: where it goes, or null.
+// One vector of y to memory; amax: of |y| over what shares a scale; scale: where it goes, or null.
 template <bool FP16, bool Q8>
-__device__ __forceinline__ void store_y(const NormParams &p, long long yo, int vec, F8 &g, float r, float amax, float *scale) {
+__device__ __forceinline__ void store_y(const NormParams &p, long long yo, int vec, F8 &y, float amax, float *scale) {
     if constexpr (Q8) {
-        const float top = fmaxf(amax * r, AMAX_FLOOR);
+        const float top = fmaxf(amax, AMAX_FLOOR);
         if (scale != nullptr) *scale = top * (1.0f / E4M3_MAX);
-        mul8(g, r);
-        // (not r * 448 / top at once: that may overflow where neither product does; both sides quartered: the fast division
-        // gives 0 for a divisor above 2^126)
-        mul8(g, __fdividef(0.25f * E4M3_MAX, 0.25f * top));
-        *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.y) + yo + vec * 8) = pack8_e4m3(g);
+        // (both sides quartered: the fast division gives 0 for a divisor above 2^126)
+        mul8(y, __fdividef(0.25f * E4M3_MAX, 0.25f * top));
+        *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.y) + yo + vec * 8) = pack8_e4m3(y);
     } else {
-        mul8(g, r);
-        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.y) + yo + vec * 8) = pack8<FP16>(g);
+        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.y) + yo + vec * 8) = pack8<FP16>(y);
     }
 }
 
@@ -191,7 +190,7 @@ __device__ __forceinline__ RowAt row_at(const NormParams &p, uint32_t row) {
 template <int NV, bool FP16, int RES, bool Q8, bool STAY>
 __global__ void __launch_bounds__(512) norm_row_kernel(const NormParams p, const uint32_t rows) {
     extern __shared__ __align__(16) float weights[];
-    __shared__ float2 red[2][16];
+    __shared__ float red[2][16], red_top[16];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
     const int groups = p.group_vecs ? p.vecs / p.group_vecs : 1;
     Raw<RES> raw[NV] = {};
@@ -209,16 +208,22 @@ __global__ void __launch_bounds__(512) norm_row_kernel(const NormParams p, const
             *reinterpret_cast<float4 *>(weights + vec * 8 + 4) = make_float4(w.v[2].x, w.v[2].y, w.v[3].x, w.v[3].y);
         }
     }
+    F8 w[STAY ? 1 : NV];   // one row: the weight comes to registers ahead of the reductions
+    if constexpr (!STAY) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i * (int)blockDim.x + tid < p.vecs) w[i] = load_weight<FP16>(p, i * blockDim.x + tid);
+    }
     int turn = 0;
     for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
         const RowAt now = at;
-        F8 g[NV];
+        F8 y[NV];
         float s = 0.f, top = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int vec = i * blockDim.x + tid;
-            g[i] = sum_raw<FP16, RES>(raw[i]);   // h (vectors behind the row's end are zeros)
-            if (RES != RES_NONE && vec < p.vecs) store_h<FP16, RES>(p, now.ro, vec, g[i]);
+            y[i] = sum_raw<FP16, RES>(raw[i]);   // h (vectors behind the row's end are zeros)
+            if (RES != RES_NONE && vec < p.vecs) store_h<FP16, RES>(p, now.ro, vec, y[i]);
         }
         if (STAY && row + gridDim.x < rows) {
             at = row_at(p, (uint32_t)(row + gridDim.x));
@@ -226,33 +231,38 @@ __global__ void __launch_bounds__(512) norm_row_kernel(const NormParams p, const
             for (int i = 0; i < NV; ++i)
                 if (i * (int)blockDim.x + tid < p.vecs) load_raw<RES>(p, at.x, at.r, i * blockDim.x + tid, raw[i]);
         }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) s += meansq8(y[i], p.inv_width);
+        s = lanes_sum<32>(s);
+        if (lane == 0) red[turn][warp] = s;   // (two sets in turn: a warp may be a row ahead of another that still reads)
+        __syncthreads();
+        s = lanes_sum<16>(lane < warps ? red[turn][lane] : 0.f);   // at most 16 warps
+        s = __shfl_sync(0xFFFFFFFFu, s, 0);     // (lanes 16 to 31 hold nothing of it)
+        const float r = rsqrtf(s + p.eps);
         float amax[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int vec = i * blockDim.x + tid;
-            s += meansq8(g[i], p.inv_width);
             if (vec < p.vecs) {
-                if constexpr (STAY) mul8(g[i], f8_of(*reinterpret_cast<const float4 *>(weights + vec * 8), *reinterpret_cast<const float4 *>(weights + vec * 8 + 4)));
-                else mul8(g[i], load_weight<FP16>(p, vec));
+                mul8(y[i], r);
+                if constexpr (STAY) mul8(y[i], f8_of(*reinterpret_cast<const float4 *>(weights + vec * 8), *reinterpret_cast<const float4 *>(weights + vec * 8 + 4)));
+                else mul8(y[i], w[i]);
             }
             if constexpr (Q8) {
-                amax[i] = amax8(g[i]);
+                amax[i] = vec < p.vecs ? amax8(y[i]) : 0.f;
                 // a group is 4, 8 or 16 neighbouring vectors: as many neighbouring lanes (a block is a multiple of 32 threads,
                 // the width a multiple of the group, so a group is either all there or not at all)
                 if (p.group_vecs) amax[i] = group_max(amax[i], p.group_vecs);
                 else top = fmaxf(top, amax[i]);
             }
         }
-        s = lanes_sum<32>(s);
-        if (Q8 && !p.group_vecs) top = lanes_max<32>(top);
-        if (lane == 0) red[turn][warp] = make_float2(s, top);   // (two sets in turn: a warp may be a row ahead of another that still reads)
-        __syncthreads();
-        const float2 other = lane < warps ? red[turn][lane] : make_float2(0.f, 0.f);   // at most 16 warps
-        s = lanes_sum<16>(other.x);
-        if (Q8 && !p.group_vecs) top = lanes_max<16>(other.y);
-        s = __shfl_sync(0xFFFFFFFFu, s, 0);     // (lanes 16 to 31 hold nothing of it)
-        top = __shfl_sync(0xFFFFFFFFu, top, 0);
-        const float r = rsqrtf(s + p.eps);
+        if (Q8 && !p.group_vecs) {
+            top = lanes_max<32>(top);
+            if (lane == 0) red_top[warp] = top;   // (read behind this barrier and ahead of the next row's first)
+            __syncthreads();
+            top = lanes_max<16>(lane < warps ? red_top[lane] : 0.f);
+            top = __shfl_sync(0xFFFFFFFFu, top, 0);
+        }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int vec = i * blockDim.x + tid;
@@ -263,7 +273,7 @@ __global__ void __launch_bounds__(512) norm_row_kernel(const NormParams p, const
             } else if (Q8 && vec == 0) {
                 scale = p.scales + row;
             }
-            store_y<FP16, Q8>(p, now.y, vec, g[i], r, Q8 && p.group_vecs ? amax[i] : top, scale);
+            store_y<FP16, Q8>(p, now.y, vec, y[i], Q8 && p.group_vecs ? amax[i] : top, scale);
         }
         if (!STAY) break;
     }
@@ -281,22 +291,29 @@ __global__ void __launch_bounds__(256) norm_warp_kernel(const NormParams p, cons
 #pragma unroll
     for (int i = 0; i < NV; ++i)
         if (32 * i + lane < p.vecs) load_raw<RES>(p, at.x, at.r, 32 * i + lane, raw[i]);
-    F8 g[NV];
+    F8 y[NV];
     float amax[NV], s = 0.f, top = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int vec = 32 * i + lane;
-        g[i] = sum_raw<FP16, RES>(raw[i]);
-        if (RES != RES_NONE && vec < p.vecs) store_h<FP16, RES>(p, at.ro, vec, g[i]);
-        s += meansq8(g[i], p.inv_width);
-        if (vec < p.vecs) mul8(g[i], load_weight<FP16>(p, vec));
+        y[i] = sum_raw<FP16, RES>(raw[i]);   // h
+        if (RES != RES_NONE && vec < p.vecs) store_h<FP16, RES>(p, at.ro, vec, y[i]);
+        s += meansq8(y[i], p.inv_width);
+    }
+    const float r = rsqrtf(lanes_sum<32>(s) + p.eps);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int vec = 32 * i + lane;
+        if (vec < p.vecs) {
+            mul8(y[i], r);
+            mul8(y[i], load_weight<FP16>(p, vec));
+        }
         if constexpr (Q8) {
-            amax[i] = amax8(g[i]);
+            amax[i] = vec < p.vecs ? amax8(y[i]) : 0.f;
             if (p.group_vecs) amax[i] = group_max(amax[i], p.group_vecs);
             else top = fmaxf(top, amax[i]);
         }
     }
-    const float r = rsqrtf(lanes_sum<32>(s) + p.eps);
     if (Q8 && !p.group_vecs) top = lanes_max<32>(top);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -308,7 +325,7 @@ __global__ void __launch_bounds__(256) norm_warp_kernel(const NormParams p, cons
         } else if (Q8 && vec == 0) {
             scale = p.scales + row;
         }
-        store_y<FP16, Q8>(p, at.y, vec, g[i], r, Q8 && p.group_vecs ? amax[i] : top, scale);
+        store_y<FP16, Q8>(p, at.y, vec, y[i], Q8 && p.group_vecs ? amax[i] : top, scale);
     }
 }
 
@@ -340,13 +357,14 @@ __global__ void __launch_bounds__(256) norm_short_kernel(const NormParams p, con
         F8 h = sum_raw<FP16, RES>(raw[i]);
         if (RES != RES_NONE && here) store_h<FP16, RES>(p, at.ro, vec, h);
         const float r = rsqrtf(lanes_sum<LANES>(meansq8(h, p.inv_width)) + p.eps);
+        mul8(h, r);
         mul8(h, w);
         float amax = 0.f;
         if constexpr (Q8) {
             amax = here ? amax8(h) : 0.f;
             amax = p.group_vecs ? group_max(amax, p.group_vecs) : lanes_max<LANES>(amax);
         }
-        if (here) store_y<FP16, Q8>(p, at.y, vec, h, r, amax, Q8 && (vec & (share - 1)) == 0 ? p.scales + (long long)row * groups + vec / share : nullptr);
+        if (here) store_y<FP16, Q8>(p, at.y, vec, h, amax, Q8 && (vec & (share - 1)) == 0 ? p.scales + (long long)row * groups + vec / share : nullptr);
     }
 }
 

@@ -6,6 +6,8 @@ import torch
 
 from paper_2607_15650_b200 import binding as dt
 from paper_2607_15650_b200 import build
+from tests import block_ops_reference as ref
+from tests.test_gpu_block_ops import norm_check
 
 pytestmark = pytest.mark.gpu
 BF16, FP16 = torch.bfloat16, torch.float16
@@ -90,3 +92,30 @@ def test_cross_logits_just_within_reach_of_the_reference(Lq, H):
         want = torch.logsumexp(x.double() * math.log(2.0), 0)
         assert (out == 1).all(), (step, out.min().item(), out.max().item())
         assert ((lse.double() - want).abs() <= 8 * U32 * (x.max().item() + 1) + (32 + Lk / 8) * U32 + 4 * U32 * (1 + abs(want))).all()
+
+
+# ---------------------------------------------------------------------------------------------- norm
+E4M3 = torch.float8_e4m3fn
+
+
+@pytest.mark.parametrize("rows,width", [(5, 64), (1000, 128), (7, 264), (5, 1024), (7, 2048), (2500, 2048), (9, 5120), (2500, 5120), (3, 16384), (1300, 16384)])
+@pytest.mark.parametrize("out,group", [("same", 0), ("e4m3", 0), ("e4m3", 128), ("e4m3", 32)])
+@pytest.mark.parametrize("residual", ["none", "same", "fp32"])
+@pytest.mark.parametrize("size,weight", [(100.0, 1e37), (1e6, 1e36), (1e-16, 1e-29)])
+def test_norm_of_rows_and_weights_whose_product_leaves_fp32(size, weight, residual, out, group, rows, width):
+    """Rows of hundreds or millions with weights near fp32's end, and tiny rows with tiny weights (eps 0): y is well inside
+    fp32, h * weight is not."""
+    if group and width % group:
+        group = 0
+    g = torch.Generator(device="cuda")
+    g.manual_seed(width + rows)
+    x = (torch.randn((rows, width), generator=g, device="cuda") * size).to(BF16)
+    w = (torch.rand((width,), generator=g, device="cuda") + 0.5) * weight
+    res = None if residual == "none" else (torch.randn((rows, width), generator=g, device="cuda") * size).to(torch.float32 if residual == "fp32" else BF16)
+    h, y = ref.norm(x, w, 0.0, res)
+    got = torch.full((rows, width), 3.0, device="cuda").to(BF16 if out == "same" else E4M3)
+    sc = torch.full((rows, width // group if group else 1), -1.0, device="cuda") if out == "e4m3" else None
+    ro = torch.empty_like(res) if res is not None else None
+    dt.dt_add_rmsnorm(x, w, got, 0.0, residual=res, residual_out=ro, scales=sc)
+    torch.cuda.synchronize()
+    norm_check(x, w, res, ro, got, sc, 0.0, h, y, (rows, width, out, group, residual))
