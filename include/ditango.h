@@ -399,7 +399,7 @@ dt_status dt_rope_freqs(const dt_rope_scaling *scaling, int32_t rotary_dim, doub
  *     scale = max(max |y|, 2^-100) / 448,  value = e4m3(y / scale) (to nearest even, saturated)
  * so that value * scale stands for y.
  *   x, y            device, n0 x n1 rows, row (i, j) at i * strides[0] + j * strides[1] (multiples of 8 elements; an input's
- *                   may be 0, an output's rows may not overlap)
+ *                   may be 0; of an output's two, the larger lies beyond all rows that the smaller one reaches)
  *   weight_dev      device [width], x's type or fp32; NULL: 1
  *   residual_dev, residual_out_dev   device, as x, of x's type or fp32; both NULL: no residual.  residual_out may be
  *                   residual or (in x's type) x, y may be x: same base and strides

@@ -427,12 +427,15 @@ bool bad_place(const void *out, const int64_t so[2], const void *in, const int64
     return out && out == in && !(same_size && (n0 <= 1 || so[0] == si[0]) && (n1 <= 1 || so[1] == si[1]));
 }
 
-// Row strides: multiples of 8 values, no negative ones; a stride of a dimension of one entry is not looked at.
+// Row strides: multiples of 8 values, no negative ones; a stride of a dimension of one entry is not looked at.  An output's outer
+// stride (either may be the outer) lies beyond what the inner dimension covers.
 bool bad_strides(const int64_t s[2], int64_t n0, int64_t n1, int width, bool output) {
     const int64_t n[2] = {n0, n1};
     for (int d = 0; d < 2; ++d)
         if (n[d] > 1 && (s[d] % 8 != 0 || s[d] < (output ? width : 0))) return true;
-    return false;
+    if (!output || n0 <= 1 || n1 <= 1) return false;
+    const int in = s[0] < s[1] ? 0 : 1;
+    return (s[1 - in] - width) / s[in] < n[in] - 1;   // s_outer < s_inner (n_inner - 1) + width, without overflowing
 }
 
 }  // namespace

@@ -1,0 +1,25 @@
+"""Host side of the operators around the self-attention: calls that the documentation rules out, and what the library and its
+Python entry points need to be built and loaded.  No GPU needed."""
+import pytest
+
+from paper_2607_15650_b200 import binding as dt
+from paper_2607_15650_b200 import build
+from tests.test_block_ops_cpu import norm_call
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return dt.lib()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(y_strides=(512, 512)), dict(y_strides=(1024, 512)), dict(y_strides=(512, 520)), dict(y_strides=(1528, 512)),
+    dict(residual_out_strides=(512, 512)), dict(residual_out_strides=(1024, 512)), dict(residual_out_strides=(512, 1016)),
+    dict(n0=3, n1=2, y_strides=(512, 1024)), dict(n0=2 ** 15, n1=2 ** 15, y_strides=(2 ** 24 - 8, 512)),
+    # in the residual's place, with the residual's own (overlapping) strides
+    dict(ro=2 ** 24, r=2 ** 24, residual_strides=(1024, 512), residual_out_strides=(1024, 512)),
+])
+def test_norm_refuses_outputs_whose_rows_meet_across_the_two_strides(lib, kw):
+    assert norm_call(lib, **kw) == dt.DT_ERR_INVALID_ARG
+    assert b"overlap" in lib.dt_last_error(None)

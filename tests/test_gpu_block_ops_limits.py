@@ -98,6 +98,19 @@ def test_cross_logits_just_within_reach_of_the_reference(Lq, H):
 E4M3 = torch.float8_e4m3fn
 
 
+def test_norm_rows_of_two_strides_either_way_round_and_packed():
+    """Rows (i, j) with the larger stride on i or on j, as tight as they go."""
+    for n0, n1, s0, s1 in ((2, 3, 1536, 512), (2, 3, 512, 1024), (3, 2, 1032, 512), (4, 5, 520, 2080)):
+        room = torch.full((8192 * 2,), 9.0, device="cuda", dtype=BF16)
+        x = torch.randn((n0, n1, 512), device="cuda").to(BF16)
+        y = room.as_strided((n0, n1, 512), (s0, s1, 1))
+        dt.dt_add_rmsnorm(x, None, y, 1e-6)
+        torch.cuda.synchronize()
+        norm_check(x, None, None, None, y, None, 1e-6, None, ref.norm(x, None, 1e-6, None)[1], (s0, s1))
+        y.fill_(9.0)
+        assert (room == 9).all()
+
+
 @pytest.mark.parametrize("rows,width", [(5, 64), (1000, 128), (7, 264), (5, 1024), (7, 2048), (2500, 2048), (9, 5120), (2500, 5120), (3, 16384), (1300, 16384)])
 @pytest.mark.parametrize("out,group", [("same", 0), ("e4m3", 0), ("e4m3", 128), ("e4m3", 32)])
 @pytest.mark.parametrize("residual", ["none", "same", "fp32"])
