@@ -36,8 +36,8 @@
 // (226 keys with a mask, as above) and 154 -> 138 (lengths); with the masking warp's bytes asked for a tile ahead, 118 and 131.  Without
 // masks there is room: rolled MMAs cost there (D = 128, 512 keys: 680 -> 740 us).
 //
-// Every wait on an mbarrier is bounded; on expiry the CTA records STATUS_WAIT_TIMEOUT, leaves its loops, frees TMEM and
-// returns.
+// Every wait on an mbarrier is bounded; on expiry the CTA records STATUS_WAIT_TIMEOUT, leaves its loops, lets what is under way
+// end, frees TMEM and returns.
 #include <cuda_bf16.h>
 
 #include "cross_attn.h"
@@ -442,9 +442,6 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 if (!ok) {
                     if (!*abort_ptr) atomicOr(p.c.status, STATUS_WAIT_TIMEOUT);
                     *abort_ptr = 1;
-                    // let loads that are still in flight land before the CTA's shared memory goes away
-                    const uint64_t t0 = global_timer_ns();
-                    while (global_timer_ns() - t0 < 200000ull) __nanosleep(1000);
                 }
             }
         } else if (warp == ZERO_WARP) {
@@ -746,6 +743,12 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    // Whoever's wait it was that ran out: loads, MMAs and commits of any role may still be under way.  They end by themselves within
+    // microseconds, and are given 200 of those before shared memory and TMEM go to another.
+    if (*abort_ptr) {
+        const uint32_t since = timer_ns_lo();
+        while (timer_ns_lo() - since < 200000u) __nanosleep(1000);
+    }
     if constexpr (SPLIT) {
         cluster_arrive_wait();   // every CTA of the cluster has written its state (or given up: then the results do not count)
         if (warp < TMA_WARP) {   // (the softmax warps: they have the registers)
