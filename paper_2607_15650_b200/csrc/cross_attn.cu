@@ -366,7 +366,7 @@ extern "C" dt_status dt_cross_attn(const dt_cross_config *cfg, const void *q_dev
     if (c.B < 0 || c.Lq < 0 || c.Lk < 0 || c.H < 1 || c.H_kv < 1) return ops_fail(DT_ERR_INVALID_ARG, "bad shape");
     if (c.H % c.H_kv != 0) return ops_fail(DT_ERR_INVALID_ARG, "H must be a multiple of H_kv");
     if ((long long)c.B * c.H > 65535) return ops_fail(DT_ERR_UNSUPPORTED, "B*H exceeds 65535");
-    if ((long long)c.Lq * c.H > 0x3FFFFFFFLL || c.Lk > (1 << 26))   // (2^26 keys: 0.8 s of tiles, within what the kernel's bounded waits allow)
+    if ((long long)c.Lq * c.H > 0x3FFFFFFFLL || c.Lk > (1 << 26))   // (2^26 keys: 0.7 to 1.1 s of tiles, within what the kernel's bounded waits allow)
         return ops_fail(DT_ERR_UNSUPPORTED, "Lq*H exceeds 2^30 or Lk 2^26");
     if (!(c.softmax_scale > 0.f) || !std::isfinite(c.softmax_scale)) return ops_fail(DT_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
     if (c.B == 0 || c.Lq == 0) return DT_OK;

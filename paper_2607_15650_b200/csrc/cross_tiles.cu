@@ -54,7 +54,6 @@ constexpr int THREADS = SOFTMAX_THREADS + 256;
 constexpr int LAUNCH_REGS = 128, REGS_SOFTMAX = 184, REGS_OTHER = 64, REGS_OUT = 80;
 static_assert((REGS_SOFTMAX - LAUNCH_REGS) * SOFTMAX_THREADS <= (LAUNCH_REGS - REGS_OTHER) * 128 + (LAUNCH_REGS - REGS_OUT) * 128,
               "softmax warps would wait forever for registers nobody releases");
-constexpr uint32_t WAIT_LIMIT_NS = 2000000000u;
 
 template <int D>
 struct Cfg {
@@ -93,6 +92,26 @@ struct TileParams {
     int dq, dh, db;          // gridDim.x items on, in blocks, heads and requests
     int splits;              // SPLIT: CTAs (a cluster) that share an item's keys
 };
+// The epilogue waits for a whole item: 1.1 s for 2^26 keys at 1.9 GHz (2.1 us a tile: D = 128, a mask, NaN in Q; 1.4 without), more at
+// lower clocks.  Well within the 4.3 s after which the timer's low word wraps.  (A limit by the number of keys, a parameter, cost
+// 2 % of a masked prompt.)
+constexpr uint32_t WAIT_LIMIT_NS = 3500000000u;
+
+// Whether any of mask bytes [from, to) is not zero; a whole warp asks, 256 bytes at a time, as far as the first.  Out of line: only
+// rows of Q without a number get here.
+__device__ __noinline__ bool any_key_of(const uint8_t *mask, int from, int to) {
+#pragma unroll 1
+    for (int at = from; at < to; at += 256) {
+        uint32_t v = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int key = at + 32 * i + (int)(threadIdx.x & 31);
+            if (key < to) v |= __ldg(mask + key);
+        }
+        if (__any_sync(0xFFFFFFFFu, v != 0u)) return true;
+    }
+    return false;
+}
 
 // The stream of a CTA's tiles: item after item, the items without keys left out.  K and V are loaded (and consumed) in the
 // order K_0, K_1, V_0, K_2, V_1, ..., K_n, V_{n-1}, ..., V_last, across items.  Stepping costs additions only: divisions here
@@ -149,11 +168,8 @@ struct CursorOf {
     }
     // whether any key of this CTA's tiles counts (a whole warp asks)
     __device__ __forceinline__ bool any_key(const CrossParams &c) const {
-        const int from = (SPLIT ? t0 : 0) * TILE, to = min(len, from + tiles * TILE);
-        bool any = false;
-#pragma unroll 1
-        for (int key = from + (int)(threadIdx.x & 31); key < to; key += 32) any |= __ldg(c.key_mask + b * c.mask_stride + key) != 0;
-        return __any_sync(0xFFFFFFFFu, any) != 0;
+        const int from = (SPLIT ? t0 : 0) * TILE;
+        return any_key_of(c.key_mask + b * c.mask_stride, from, min(len, from + tiles * TILE));
     }
     __device__ __forceinline__ int row0() const { return qb * (NQ * TILE); }
     // keys in the tile that do not count: a mask may have holes anywhere, the last tile may be ragged

@@ -94,6 +94,47 @@ def test_cross_logits_just_within_reach_of_the_reference(Lq, H):
         assert ((lse.double() - want).abs() <= 8 * U32 * (x.max().item() + 1) + (32 + Lk / 8) * U32 + 4 * U32 * (1 + abs(want))).all()
 
 
+@pytest.mark.parametrize("Lq,B,H", [(256, 75, 1), (512, 2, 8)])
+@pytest.mark.parametrize("D,dtype", [(64, FP16), (128, BF16)])
+def test_cross_rows_without_a_number_under_masks_of_many_keys(D, dtype, Lq, B, H):
+    """A request whose mask has one key, far behind the others, one without any, and one with all: whole items of tiles, and split ones.
+    The rows of Q without a number look through the mask."""
+    Lk = 2 ** 20 + 77
+    q = torch.zeros((B, Lq, H, D), device="cuda", dtype=dtype)
+    q[:, 3::7] = float("nan")
+    kv = torch.ones((1, Lk, 1, D), device="cuda", dtype=dtype).expand(B, Lk, 1, D)
+    mask = torch.ones((B, Lk), device="cuda", dtype=torch.uint8)
+    mask[0] = 0
+    mask[1] = 0
+    mask[1, Lk - 1] = 1
+    out, lse = torch.full_like(q, 5.0), torch.full((B, H, Lq), 5.0, device="cuda")
+    dt.dt_cross_attn(q, kv, kv, out, 0.1, key_mask=mask, lse_out=lse)
+    torch.cuda.synchronize()
+    dt.dt_poll_ops()
+    nan = torch.zeros(Lq, dtype=torch.bool, device="cuda")
+    nan[3::7] = True
+    assert (out[0] == 0).all() and (lse[0] == -math.inf).all()
+    assert out[1:, nan].isnan().all() and lse[1:, :, nan].isnan().all()
+    assert (out[1:, ~nan] == 1).all()
+    # equal logits of zero: LSE is the logarithm of the number of keys, whose sum is exact up to 2^24
+    assert (lse[1, :, ~nan].abs() <= 2 * U32).all()
+    assert ((lse[2:, :, ~nan].double() - math.log(Lk)).abs() <= 16 * U32 * math.log(Lk)).all()
+
+
+def test_cross_of_as_many_keys_as_there_may_be():
+    """2^26 keys in one item, masked altogether, with rows of Q without a number: the longest that a part of the kernel waits for another."""
+    B, Lk, D = 75, 2 ** 26, 64
+    q = torch.zeros((B, 256, 1, D), device="cuda", dtype=FP16)
+    q[:, ::2] = float("nan")
+    kv = torch.zeros((1, Lk, 1, D), device="cuda", dtype=FP16).expand(B, Lk, 1, D)
+    mask = torch.zeros((B, Lk), device="cuda", dtype=torch.uint8)
+    out, lse = torch.full_like(q, 5.0), torch.full((B, 1, 256), 5.0, device="cuda")
+    dt.dt_cross_attn(q, kv, kv, out, 0.1, key_mask=mask, lse_out=lse)
+    torch.cuda.synchronize()
+    dt.dt_poll_ops()
+    assert (out == 0).all() and (lse == -math.inf).all()
+
+
 # ---------------------------------------------------------------------------------------------- norm
 E4M3 = torch.float8_e4m3fn
 
