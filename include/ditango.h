@@ -441,6 +441,10 @@ dt_status dt_cross_attn(const dt_cross_config *cfg, const void *q_dev, const int
  * DT_ERR_TIMEOUT. */
 dt_status dt_poll_ops(void);
 
+/* Self-test of the operators' bounded waits: one warp waits for at most `limit_us` (up to 1000000) on a barrier that is never
+ * completed; the next dt_poll_ops on the device reports DT_ERR_TIMEOUT. */
+dt_status dt_selftest_ops_timeout(uint32_t limit_us, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

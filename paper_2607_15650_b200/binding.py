@@ -31,7 +31,7 @@ EXPORTS = [
     "dt_launch_count", "dt_selftest_wait_timeout", "dt_poll", "dt_status_str", "dt_last_error",
     "dt_attn_fused", "dt_num_slots", "dt_slot_ranges", "dt_group_compose", "dt_group_fit", "dt_group_reset",
     "dt_plan_sums", "dt_plan_from_sums",
-    "dt_rope", "dt_rope_freqs", "dt_add_rmsnorm", "dt_cross_attn", "dt_poll_ops",
+    "dt_rope", "dt_rope_freqs", "dt_add_rmsnorm", "dt_cross_attn", "dt_poll_ops", "dt_selftest_ops_timeout",
 ]
 
 
@@ -127,6 +127,7 @@ def lib():
         "dt_add_rmsnorm": (C.c_int, [vp] * 8),
         "dt_cross_attn": (C.c_int, [vp] * 9 + [C.c_int64] + [vp] * 4),
         "dt_poll_ops": (C.c_int, []),
+        "dt_selftest_ops_timeout": (C.c_int, [C.c_uint32, vp]),
         "dt_status_str": (C.c_char_p, [C.c_int]),
         "dt_last_error": (C.c_char_p, [vp]),
     }
@@ -260,6 +261,14 @@ def dt_poll_ops(device=None):
     """Raises DitangoError if an operator recorded a condition on the (current) device; synchronises it."""
     with torch.cuda.device(device):
         s = lib().dt_poll_ops()
+    if s != DT_OK:
+        raise DitangoError(s, status_str(s), lib().dt_last_error(None).decode())
+
+
+def dt_selftest_ops_timeout(limit_us=1000, device=None, stream=None):
+    """Makes a bounded wait of the operators run out on the (current) device; the next dt_poll_ops there raises."""
+    with torch.cuda.device(device):
+        s = lib().dt_selftest_ops_timeout(int(limit_us), _stream_ptr(stream))
     if s != DT_OK:
         raise DitangoError(s, status_str(s), lib().dt_last_error(None).decode())
 

@@ -214,13 +214,13 @@ __device__ __forceinline__ uint32_t timer_ns_lo() {   // wraps after 4.3 s
     asm volatile("mov.u32 %0, %%globaltimer_lo;" : "=r"(t));
     return t;
 }
-__device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity, const volatile int *abort_flag) {
+__device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity, const volatile int *abort_flag, uint32_t limit_ns = WAIT_LIMIT_NS) {
     if (mbar_try_wait(bar, parity)) return true;
     const uint32_t since = timer_ns_lo();
     uint32_t n = 0;
 #pragma unroll 1
     while (!mbar_try_wait(bar, parity))
-        if ((++n & 0x3Fu) == 0u && (*abort_flag || timer_ns_lo() - since > WAIT_LIMIT_NS)) return false;
+        if ((++n & 0x3Fu) == 0u && (*abort_flag || timer_ns_lo() - since > limit_ns)) return false;
     return true;
 }
 
@@ -822,6 +822,20 @@ cross_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     if (warp == 0) tmem_dealloc(tmem_base, 512);
 }
 
+// One warp waits, as the tile kernel does, on a barrier that nothing completes.
+__global__ void wait_selftest_kernel(int32_t *status, uint32_t limit_ns) {
+    __shared__ uint64_t bar;
+    __shared__ int abort_flag;
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        mbar_init(smem_u32(&bar), 1);
+        fence_mbar_init();
+    }
+    __syncwarp();
+    const bool ok = __all_sync(0xFFFFFFFFu, wait_bounded(smem_u32(&bar), 0, &abort_flag, limit_ns)) != 0;
+    if (!ok && threadIdx.x == 0) atomicOr(status, STATUS_WAIT_TIMEOUT);
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                   const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -891,6 +905,11 @@ cudaError_t cross_tiles_configure() {
     if ((e = configure<64, true>()) != cudaSuccess) return e;
     if ((e = configure<128, false>()) != cudaSuccess) return e;
     return configure<128, true>();
+}
+
+cudaError_t launch_wait_selftest(int32_t *status, uint32_t limit_ns, cudaStream_t st) {
+    wait_selftest_kernel<<<1, 32, 0, st>>>(status, limit_ns);
+    return cudaGetLastError();
 }
 
 cudaError_t launch_cross_tiles(const CrossParams &c, int D, bool fp16, int splits, const OpsDevice &dev, cudaStream_t st) {

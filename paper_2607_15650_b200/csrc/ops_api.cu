@@ -104,3 +104,12 @@ extern "C" dt_status dt_poll_ops(void) {
     if (word & dt::STATUS_WAIT_TIMEOUT) return dt::ops_fail(DT_ERR_TIMEOUT, "a bounded device-side wait expired");
     return DT_OK;
 }
+
+extern "C" dt_status dt_selftest_ops_timeout(uint32_t limit_us, void *stream) {
+    if (limit_us > 1000000u) return dt::ops_fail(DT_ERR_INVALID_ARG, "limit_us must be at most 1000000");
+    const dt::OpsDevice *dev;
+    dt_status s = dt::ops_device(&dev);
+    if (s != DT_OK) return s;
+    const cudaError_t e = dt::launch_wait_selftest(dev->status, limit_us * 1000u, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? DT_OK : dt::ops_fail_cuda(e, "self-test launch");
+}

@@ -13,6 +13,10 @@ def lib():
     return dt.lib()
 
 
+def test_selftest_refuses_long_limits(lib):
+    assert lib.dt_selftest_ops_timeout(1000001, None) == dt.DT_ERR_INVALID_ARG and lib.dt_last_error(None)
+
+
 @pytest.mark.parametrize("kw", [
     dict(y_strides=(512, 512)), dict(y_strides=(1024, 512)), dict(y_strides=(512, 520)), dict(y_strides=(1528, 512)),
     dict(residual_out_strides=(512, 512)), dict(residual_out_strides=(1024, 512)), dict(residual_out_strides=(512, 1016)),

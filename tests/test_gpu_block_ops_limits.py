@@ -135,6 +135,25 @@ def test_cross_of_as_many_keys_as_there_may_be():
     assert (out == 0).all() and (lse == -math.inf).all()
 
 
+def test_a_wait_that_runs_out_is_reported_once_and_the_next_call_is_right():
+    q, k = (torch.randn((1, n, 4, 64), device="cuda").to(BF16) for n in (700, 500))
+    out, again = torch.empty_like(q), torch.empty_like(q)
+    dt.dt_cross_attn(q, k, k, out, 0.125)
+    dt.dt_poll_ops()
+    dt.dt_selftest_ops_timeout(limit_us=500)
+    dt.dt_cross_attn(q, k, k, again, 0.125)
+    with pytest.raises(dt.DitangoError) as e:
+        dt.dt_poll_ops()
+    assert e.value.status == dt.DT_ERR_TIMEOUT
+    dt.dt_poll_ops()
+    assert torch.equal(out, again) and out.isfinite().all()
+    s = torch.cuda.Stream()
+    dt.dt_selftest_ops_timeout(limit_us=0, stream=s)
+    with pytest.raises(dt.DitangoError):
+        dt.dt_poll_ops()
+    dt.dt_poll_ops()
+
+
 # ---------------------------------------------------------------------------------------------- norm
 E4M3 = torch.float8_e4m3fn
 
