@@ -303,15 +303,20 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) cross_few_kernel(const CrossPa
 }
 
 template <int D, bool FP16, int NT>
-cudaError_t launch_few(const CrossParams &p, int sms, cudaStream_t st) {
+cudaError_t launch_few(const CrossParams &p, const OpsDevice &dev, cudaStream_t st) {
     using C = FewCfg<D, 8 * NT>;
+    static OncePerDevice once;
+    const cudaError_t e = once(dev, [] {
+        return cudaFuncSetAttribute(cross_few_kernel<D, FP16, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem(C::MAX_STAGES));
+    });
+    if (e != cudaSuccess) return e;
     const long long rows = (long long)p.Lq * p.rep, row_blocks = (rows + 8 * NT - 1) / (8 * NT);
     const long long groups = row_blocks * p.B * p.Hkv;
     // Split the keys while that still gives every warp a chunk of its own and the blocks fit the GPU at once (2 per SM).
     // Clusters of 8 at most: with 16 blocks they do not all find a place at once (2 x 8 key heads, 32760 keys: 57 us with 16,
     // 45 with 8, 63 with 4).
     int splits = 1;
-    while (splits < 8 && groups * splits * 2 <= 2LL * sms && splits * FEW_WARPS * FEW_KEYS < p.Lk) splits *= 2;
+    while (splits < 8 && groups * splits * 2 <= 2LL * dev.sms && splits * FEW_WARPS * FEW_KEYS < p.Lk) splits *= 2;
     const int chunks = (p.Lk + splits * FEW_WARPS * FEW_KEYS - 1) / (splits * FEW_WARPS * FEW_KEYS);   // of a warp
     const int stages = chunks >= C::MAX_STAGES ? C::MAX_STAGES : chunks >= 3 ? 3 : 2;
     cudaLaunchConfig_t cfg = {};
@@ -327,31 +332,11 @@ cudaError_t launch_few(const CrossParams &p, int sms, cudaStream_t st) {
     return cudaLaunchKernelEx(&cfg, cross_few_kernel<D, FP16, NT>, p, splits, stages);
 }
 template <int D, bool FP16>
-cudaError_t launch_few(const CrossParams &p, int sms, cudaStream_t st) {
-    return (long long)p.Lq * p.rep <= 8 ? launch_few<D, FP16, 1>(p, sms, st) : launch_few<D, FP16, 2>(p, sms, st);
-}
-
-template <int D, bool FP16, int NT>
-cudaError_t configure_few() {
-    return cudaFuncSetAttribute(cross_few_kernel<D, FP16, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                FewCfg<D, 8 * NT>::smem(FewCfg<D, 8 * NT>::MAX_STAGES));
-}
-template <int D, bool FP16>
-cudaError_t configure_few() {
-    cudaError_t e = configure_few<D, FP16, 1>();
-    return e == cudaSuccess ? configure_few<D, FP16, 2>() : e;
+cudaError_t launch_few(const CrossParams &p, const OpsDevice &dev, cudaStream_t st) {
+    return (long long)p.Lq * p.rep <= 8 ? launch_few<D, FP16, 1>(p, dev, st) : launch_few<D, FP16, 2>(p, dev, st);
 }
 
 }  // namespace
-
-cudaError_t cross_few_configure() {
-    cudaError_t e;
-    if ((e = configure_few<64, false>()) != cudaSuccess) return e;
-    if ((e = configure_few<64, true>()) != cudaSuccess) return e;
-    if ((e = configure_few<128, false>()) != cudaSuccess) return e;
-    return configure_few<128, true>();
-}
-
 }  // namespace dt
 
 extern "C" dt_status dt_cross_attn(const dt_cross_config *cfg, const void *q_dev, const int64_t q_strides_blhd[4], const void *k_dev,
@@ -411,7 +396,7 @@ extern "C" dt_status dt_cross_attn(const dt_cross_config *cfg, const void *q_dev
     const long long steps = splits > 1 ? (tiles + splits - 1) / splits + 3 : (items + dev->sms - 1) / dev->sms * tiles;
     cudaError_t e;
     if (c.Lk > 0 && few_blocks * tiles > steps * (c.D == 64 ? 290 : 200)) e = launch_cross_tiles(p, c.D, fp16, splits, *dev, st);
-    else e = c.D == 64 ? (fp16 ? launch_few<64, true>(p, dev->sms, st) : launch_few<64, false>(p, dev->sms, st))
-                       : (fp16 ? launch_few<128, true>(p, dev->sms, st) : launch_few<128, false>(p, dev->sms, st));
+    else e = c.D == 64 ? (fp16 ? launch_few<64, true>(p, *dev, st) : launch_few<64, false>(p, *dev, st))
+                       : (fp16 ? launch_few<128, true>(p, *dev, st) : launch_few<128, false>(p, *dev, st));
     return e == cudaSuccess ? DT_OK : ops_fail_cuda(e, "cross-attention launch");
 }

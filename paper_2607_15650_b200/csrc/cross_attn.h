@@ -89,8 +89,5 @@ inline int cross_tile_splits(long long items, long long tiles, int sms) {
     while (tiles >= 8 && s < 8 && items * s * 2 <= (s == 1 ? sms : s == 2 ? sms * 15 / 16 : sms * 13 / 16) && tiles >= s * 4) s *= 2;
     return s;
 }
-cudaError_t launch_wait_selftest(int32_t *status, uint32_t limit_ns, cudaStream_t st);
-cudaError_t cross_tiles_configure();   // both per device, once
-cudaError_t cross_few_configure();
 
 }  // namespace dt

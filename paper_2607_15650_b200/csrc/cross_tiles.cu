@@ -50,7 +50,7 @@ constexpr int SOFTMAX_THREADS = NQ * 128;
 constexpr int TMA_WARP = SOFTMAX_THREADS / 32, MMA_WARP = TMA_WARP + 1, ZERO_WARP = TMA_WARP + 3, OUT_WARP = TMA_WARP + 4;
 constexpr int THREADS = SOFTMAX_THREADS + 256;
 // setmaxnreg.inc only takes registers that a setmaxnreg.dec of the same CTA has released; LAUNCH_REGS is what ptxas
-// assigns under __launch_bounds__(512, 1), checked by cross_tiles_configure().
+// assigns under __launch_bounds__(512, 1), checked before a variant's first launch.
 constexpr int LAUNCH_REGS = 128, REGS_SOFTMAX = 184, REGS_OTHER = 64, REGS_OUT = 80;
 static_assert((REGS_SOFTMAX - LAUNCH_REGS) * SOFTMAX_THREADS <= (LAUNCH_REGS - REGS_OTHER) * 128 + (LAUNCH_REGS - REGS_OUT) * 128,
               "softmax warps would wait forever for registers nobody releases");
@@ -857,25 +857,19 @@ CUresult encode(void *fn, CUtensorMap *tm, MapCoord *mul, const void *base, cons
 }
 
 template <int D, bool FP16, bool MASKED, bool SPLIT>
-cudaError_t configure_one() {
+cudaError_t configure() {
     cudaFuncAttributes attr;
     cudaError_t e = cudaFuncGetAttributes(&attr, cross_tile_kernel<D, FP16, MASKED, SPLIT>);
     if (e != cudaSuccess) return e;
     if (attr.numRegs != LAUNCH_REGS) return cudaErrorInvalidConfiguration;   // the register hand-over would not balance
     return cudaFuncSetAttribute(cross_tile_kernel<D, FP16, MASKED, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::SMEM_BYTES);
 }
-template <int D, bool FP16>
-cudaError_t configure() {
-    cudaError_t e;
-    if ((e = configure_one<D, FP16, false, false>()) != cudaSuccess) return e;
-    if ((e = configure_one<D, FP16, true, false>()) != cudaSuccess) return e;
-    if ((e = configure_one<D, FP16, false, true>()) != cudaSuccess) return e;
-    return configure_one<D, FP16, true, true>();
-}
-
-template <int D, bool FP16, bool MASKED>
-cudaError_t launch(int grid, const CUtensorMap &tq, const CUtensorMap &tk, const CUtensorMap &tv, const TileParams &p, cudaStream_t st) {
-    if (p.splits == 1) {
+template <int D, bool FP16, bool MASKED, bool SPLIT>
+cudaError_t launch(int grid, const CUtensorMap &tq, const CUtensorMap &tk, const CUtensorMap &tv, const TileParams &p, const OpsDevice &dev, cudaStream_t st) {
+    static OncePerDevice once;
+    const cudaError_t e = once(dev, configure<D, FP16, MASKED, SPLIT>);
+    if (e != cudaSuccess) return e;
+    if constexpr (!SPLIT) {
         cross_tile_kernel<D, FP16, MASKED, false><<<grid, THREADS, Cfg<D>::SMEM_BYTES, st>>>(tq, tk, tv, p);
         return cudaGetLastError();
     }
@@ -892,25 +886,13 @@ cudaError_t launch(int grid, const CUtensorMap &tq, const CUtensorMap &tk, const
     return cudaLaunchKernelEx(&cfg, cross_tile_kernel<D, FP16, MASKED, true>, tq, tk, tv, p);
 }
 template <int D, bool FP16>
-cudaError_t launch(int grid, const CUtensorMap &tq, const CUtensorMap &tk, const CUtensorMap &tv, const TileParams &p, cudaStream_t st) {
+cudaError_t launch(int grid, const CUtensorMap &tq, const CUtensorMap &tk, const CUtensorMap &tv, const TileParams &p, const OpsDevice &dev, cudaStream_t st) {
     const bool masked = p.c.key_lens != nullptr || p.c.key_mask != nullptr || p.c.Lk % TILE != 0;
-    return masked ? launch<D, FP16, true>(grid, tq, tk, tv, p, st) : launch<D, FP16, false>(grid, tq, tk, tv, p, st);
+    if (p.splits > 1) return masked ? launch<D, FP16, true, true>(grid, tq, tk, tv, p, dev, st) : launch<D, FP16, false, true>(grid, tq, tk, tv, p, dev, st);
+    return masked ? launch<D, FP16, true, false>(grid, tq, tk, tv, p, dev, st) : launch<D, FP16, false, false>(grid, tq, tk, tv, p, dev, st);
 }
 
 }  // namespace
-
-cudaError_t cross_tiles_configure() {
-    cudaError_t e;
-    if ((e = configure<64, false>()) != cudaSuccess) return e;
-    if ((e = configure<64, true>()) != cudaSuccess) return e;
-    if ((e = configure<128, false>()) != cudaSuccess) return e;
-    return configure<128, true>();
-}
-
-cudaError_t launch_wait_selftest(int32_t *status, uint32_t limit_ns, cudaStream_t st) {
-    wait_selftest_kernel<<<1, 32, 0, st>>>(status, limit_ns);
-    return cudaGetLastError();
-}
 
 cudaError_t launch_cross_tiles(const CrossParams &c, int D, bool fp16, int splits, const OpsDevice &dev, cudaStream_t st) {
     TileParams p = {};
@@ -930,8 +912,18 @@ cudaError_t launch_cross_tiles(const CrossParams &c, int D, bool fp16, int split
         encode(dev.encode_tiled, &tk, &p.mk, c.k, c.ks, c.B, c.Lk, c.Hkv, D, fp16) != CUDA_SUCCESS ||
         encode(dev.encode_tiled, &tv, &p.mv, c.v, c.vs, c.B, c.Lk, c.Hkv, D, fp16) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
-    if (D == 64) return fp16 ? launch<64, true>(grid, tq, tk, tv, p, st) : launch<64, false>(grid, tq, tk, tv, p, st);
-    return fp16 ? launch<128, true>(grid, tq, tk, tv, p, st) : launch<128, false>(grid, tq, tk, tv, p, st);
+    if (D == 64) return fp16 ? launch<64, true>(grid, tq, tk, tv, p, dev, st) : launch<64, false>(grid, tq, tk, tv, p, dev, st);
+    return fp16 ? launch<128, true>(grid, tq, tk, tv, p, dev, st) : launch<128, false>(grid, tq, tk, tv, p, dev, st);
 }
 
 }  // namespace dt
+
+extern "C" dt_status dt_selftest_ops_timeout(uint32_t limit_us, void *stream) {
+    if (limit_us > 1000000u) return dt::ops_fail(DT_ERR_INVALID_ARG, "limit_us must be at most 1000000");
+    const dt::OpsDevice *dev;
+    dt_status s = dt::ops_device(&dev);
+    if (s != DT_OK) return s;
+    dt::wait_selftest_kernel<<<1, 32, 0, static_cast<cudaStream_t>(stream)>>>(dev->status, limit_us * 1000u);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? DT_OK : dt::ops_fail_cuda(e, "self-test launch");
+}

@@ -5,15 +5,31 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/ditango.h"
 
 namespace dt {
 
 // What the operators need to know of the current device, looked up on the first call on it.
 struct OpsDevice {
-    int sms;
+    int ordinal, sms;
     int32_t *status;      // device status word of the operators (dt_poll_ops)
     void *encode_tiled;   // cuTensorMapEncodeTiled
+};
+
+// What a kernel needs before its first launch on a device (a shared-memory limit): done by the first call that launches it, so that
+// no operator loads another's kernels.  Threads that get here at once do the same.
+struct OncePerDevice {
+    std::atomic<uint64_t> done{0};
+    template <typename F>
+    cudaError_t operator()(const OpsDevice &dev, F &&configure) {
+        const uint64_t bit = 1ull << dev.ordinal;
+        if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+        const cudaError_t e = configure();
+        if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+        return e;
+    }
 };
 
 dt_status ops_fail(dt_status s, const char *what);                 // keeps the text for dt_last_error(NULL)

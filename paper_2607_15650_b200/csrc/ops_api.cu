@@ -1,10 +1,10 @@
 // What the context-free operators share: error text, facts about the current device, argument checks.
 #include <algorithm>
-#include <atomic>
 #include <cstdio>
 #include <cstring>
 
-#include "cross_attn.h"
+#include "dt_internal.h"
+#include "ops.h"
 
 namespace dt {
 namespace {
@@ -12,9 +12,32 @@ namespace {
 thread_local char g_error[192] = "";
 __device__ int32_t g_status;   // conditions only the device can see; zero at load time, cleared by dt_poll_ops
 
-constexpr int MAX_DEVICES = 64;
+constexpr int MAX_DEVICES = 64;   // bits of OncePerDevice::done
 OpsDevice g_devices[MAX_DEVICES];
 std::atomic<int> g_ready[MAX_DEVICES];
+std::atomic_flag g_looking_up = ATOMIC_FLAG_INIT;
+
+// Fills g_devices[dev] with g_looking_up held.
+dt_status look_up(int dev) {
+    OpsDevice d = {};
+    d.ordinal = dev;
+    cudaError_t e;
+    int major = 0;
+    if ((e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev)) != cudaSuccess ||
+        (e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess)
+        return ops_fail_cuda(e, "device attributes");
+    if (major != 10) return ops_fail(DT_ERR_UNSUPPORTED, "the kernels are built for sm_100 only");
+    void *word = nullptr;
+    if ((e = cudaGetSymbolAddress(&word, g_status)) != cudaSuccess) return ops_fail_cuda(e, "status word");
+    d.status = static_cast<int32_t *>(word);
+    cudaDriverEntryPointQueryResult qres;
+    e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &d.encode_tiled, cudaEnableDefault, &qres);
+    if (e != cudaSuccess) return ops_fail_cuda(e, "cuTensorMapEncodeTiled");
+    if (qres != cudaDriverEntryPointSuccess || !d.encode_tiled) return ops_fail(DT_ERR_CUDA, "cuTensorMapEncodeTiled not found");
+    g_devices[dev] = d;
+    g_ready[dev].store(1, std::memory_order_release);
+    return DT_OK;
+}
 
 }  // namespace
 
@@ -36,23 +59,10 @@ dt_status ops_device(const OpsDevice **out) {
     if (e != cudaSuccess) return ops_fail_cuda(e, "cudaGetDevice");
     if (dev < 0 || dev >= MAX_DEVICES) return ops_fail(DT_ERR_UNSUPPORTED, "device ordinal beyond 63");
     if (!g_ready[dev].load(std::memory_order_acquire)) {
-        OpsDevice d = {};
-        int major = 0;
-        if ((e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev)) != cudaSuccess ||
-            (e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess)
-            return ops_fail_cuda(e, "device attributes");
-        if (major != 10) return ops_fail(DT_ERR_UNSUPPORTED, "the kernels are built for sm_100 only");
-        void *word = nullptr;
-        if ((e = cudaGetSymbolAddress(&word, g_status)) != cudaSuccess) return ops_fail_cuda(e, "status word");
-        d.status = static_cast<int32_t *>(word);
-        cudaDriverEntryPointQueryResult qres;
-        e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &d.encode_tiled, cudaEnableDefault, &qres);
-        if (e != cudaSuccess) return ops_fail_cuda(e, "cuTensorMapEncodeTiled");
-        if (qres != cudaDriverEntryPointSuccess || !d.encode_tiled) return ops_fail(DT_ERR_CUDA, "cuTensorMapEncodeTiled not found");
-        if ((e = cross_tiles_configure()) != cudaSuccess || (e = cross_few_configure()) != cudaSuccess) return ops_fail_cuda(e, "cross-attention kernels");
-        // two threads may get here at once: both write the same facts
-        g_devices[dev] = d;
-        g_ready[dev].store(1, std::memory_order_release);
+        while (g_looking_up.test_and_set(std::memory_order_acquire)) {}   // (no call in there waits for another thread)
+        const dt_status s = g_ready[dev].load(std::memory_order_acquire) ? DT_OK : look_up(dev);
+        g_looking_up.clear(std::memory_order_release);
+        if (s != DT_OK) return s;
     }
     *out = &g_devices[dev];
     return DT_OK;
@@ -103,13 +113,4 @@ extern "C" dt_status dt_poll_ops(void) {
     if (e != cudaSuccess) return dt::ops_fail_cuda(e, "dt_poll_ops");
     if (word & dt::STATUS_WAIT_TIMEOUT) return dt::ops_fail(DT_ERR_TIMEOUT, "a bounded device-side wait expired");
     return DT_OK;
-}
-
-extern "C" dt_status dt_selftest_ops_timeout(uint32_t limit_us, void *stream) {
-    if (limit_us > 1000000u) return dt::ops_fail(DT_ERR_INVALID_ARG, "limit_us must be at most 1000000");
-    const dt::OpsDevice *dev;
-    dt_status s = dt::ops_device(&dev);
-    if (s != DT_OK) return s;
-    const cudaError_t e = dt::launch_wait_selftest(dev->status, limit_us * 1000u, static_cast<cudaStream_t>(stream));
-    return e == cudaSuccess ? DT_OK : dt::ops_fail_cuda(e, "self-test launch");
 }
