@@ -1,5 +1,8 @@
 """Operators around the self-attention at the ends of their types' ranges, on the GPU against plain 64-bit forms."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -12,6 +15,7 @@ from tests.test_gpu_block_ops import norm_check
 pytestmark = pytest.mark.gpu
 BF16, FP16 = torch.bfloat16, torch.float16
 U32 = 2.0 ** -24
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -192,3 +196,48 @@ def test_norm_of_rows_and_weights_whose_product_leaves_fp32(size, weight, residu
     dt.dt_add_rmsnorm(x, w, got, 0.0, residual=res, residual_out=ro, scales=sc)
     torch.cuda.synchronize()
     norm_check(x, w, res, ro, got, sc, 0.0, h, y, (rows, width, out, group, residual))
+
+
+# ---------------------------------------------------------------------------------------------- first calls
+@pytest.mark.parametrize("call", [
+    "dt.dt_rope(q, None, o, None, f)", "dt.dt_rope(q, None, o, None, f, layout=dt.DT_ROPE_HALF)", "dt.dt_add_rmsnorm(q, w, o, 1e-6)",
+    "dt.dt_add_rmsnorm(q.view(100, 30720 // 2), None, o.view(100, 30720 // 2), 1e-6)",
+    "dt.dt_cross_attn(q[:, :1], q, q, o[:, :1], 0.1)", "dt.dt_cross_attn(q, q[:, :300], q[:, :300], o, 0.1)",
+    "dt.dt_cross_attn(q[:, :600], q, q, o[:, :600], 0.1)", "dt.dt_cross_attn(q, q, q, o, 0.1, key_mask=m)"])
+def test_the_first_call_of_a_process_captured_gives_what_a_plain_call_gives(call):
+    """The capture runs nothing; every replay writes the whole output, over what stood there, bit for bit as a call does."""
+    text = f"""
+import torch
+from paper_2607_15650_b200 import binding as dt
+g = torch.Generator(device="cuda"); g.manual_seed(1)
+q = torch.randn((1, 1500, 16, 64), generator=g, device="cuda").to(torch.bfloat16)
+w = torch.rand((64,), generator=g, device="cuda") + 0.5
+m = torch.rand((1, 1500), generator=g, device="cuda") < 0.7
+f = dt.dt_rope_freqs(64)[0][None].cuda()
+o = torch.full_like(q, float("nan"))
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    {call}
+torch.cuda.synchronize()
+assert o.isnan().all()
+got = []
+for _ in range(2):
+    o.fill_(float("nan"))
+    graph.replay()
+    torch.cuda.synchronize()
+    got.append(o.clone())
+o.fill_(float("nan"))
+{call}
+torch.cuda.synchronize()
+dt.dt_poll_ops()
+written = ~o.isnan()
+assert written.any() and (o[written] != q[written]).any()
+rows = written.all(-1).all(-1)[0]
+n = int(rows.sum())
+assert n in (1, 600, 1500) and rows[:n].all() and not written[0, n:].any(), n
+for x in got:
+    assert torch.equal(x.view(torch.int16), o.view(torch.int16))
+print("same")
+"""
+    r = subprocess.run([sys.executable, "-c", text], cwd=ROOT, capture_output=True, text=True, timeout=240)
+    assert r.returncode == 0 and r.stdout.split()[-1] == "same", r.stdout + r.stderr
