@@ -210,7 +210,7 @@ _OPS = ("dt_rope", "dt_add_rmsnorm", "dt_cross_attn")
 def _load_ops():
     L = lib()
     if not os.path.exists(OPS_PATH):
-        raise ImportError(f"{OPS_PATH} is missing: run `python -m paper_2607_15650_b200.build`")
+        raise ImportError(f"{OPS_PATH} is missing: run `python -m paper_2607_15650_b200.build` (a C compiler and Python's headers)")
     spec = importlib.util.spec_from_file_location("_ditango_ops", OPS_PATH)
     ops = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(ops)

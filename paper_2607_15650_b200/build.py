@@ -4,14 +4,18 @@
 
 nvcc cross-compiles without a GPU.  The library links the static CUDA runtime and resolves the
 one driver entry point it needs (tensor-map encoding) at run time, so it has no link-time
-dependency on libcuda.
+dependency on libcuda.  The Python entry points of the context-free operators are a module of
+their own, which needs a C compiler and Python's headers; without those the library is built alone.
 """
 from __future__ import annotations
 
 import os
+import shlex
+import shutil
 import subprocess
 import sys
 import sysconfig
+import warnings
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -34,16 +38,18 @@ def _stale(lib=LIB, files=SOURCES + HEADERS) -> bool:
 def _build_ops(force: bool) -> None:
     if not force and not _stale(OPS_LIB, [OPS_SOURCE, HEADERS[-1]]):
         return
+    cc, include = shlex.split(os.environ.get("CC") or "gcc"), sysconfig.get_paths()["include"]
+    if shutil.which(cc[0]) is None or not os.path.exists(os.path.join(include, "Python.h")):
+        warnings.warn(f"no Python entry points of the context-free operators: {cc[0]} or {include}/Python.h is missing")
+        return
     tmp = OPS_LIB + f".tmp{os.getpid()}"
-    subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-std=c11", "-shared", "-fPIC", "-Wall", "-I" + sysconfig.get_paths()["include"],
-                    "-o", tmp, os.path.join(CSRC, OPS_SOURCE)], check=True)
+    subprocess.run([*cc, "-O2", "-std=c11", "-shared", "-fPIC", "-Wall", "-I" + include, "-o", tmp, os.path.join(CSRC, OPS_SOURCE)], check=True)
     os.replace(tmp, OPS_LIB)
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    _build_ops(force)
-    if not force and not _stale():
-        return LIB
+def _build_lib(force: bool, verbose: bool) -> None:
+    if not force and not _stale(LIB):
+        return
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [NVCC, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
            "-shared", "-Xcompiler", "-fPIC", 
@@ -53,6 +59,11 @@ def build(force: bool = False, verbose: bool = False) -> str:
     cmd += [os.path.join(CSRC, f) for f in SOURCES]
     subprocess.run(cmd, check=True)
     os.replace(tmp, LIB)
+
+
+def build(force: bool = False, verbose: bool = False) -> str:
+    _build_lib(force, verbose)
+    _build_ops(force)
     return LIB
 
 

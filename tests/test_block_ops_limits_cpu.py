@@ -41,3 +41,46 @@ def test_rotation_and_norm_stand_without_the_attention_kernels(lib, tmp_path):
                    check=True)
     part = ctypes.CDLL(out)
     assert part.dt_rope(None, *[None] * 12) == dt.DT_ERR_INVALID_ARG and part.dt_add_rmsnorm(None, *[None] * 7) == dt.DT_ERR_INVALID_ARG
+
+
+@pytest.fixture()
+def elsewhere(monkeypatch, tmp_path):
+    """build() into a folder of its own, with nvcc replaced by something that leaves a file, and the commands as they run."""
+    ran, real = [], subprocess.run
+
+    def run(cmd, **kw):
+        ran.append(cmd[0])
+        if cmd[0] == build.NVCC:
+            open(cmd[cmd.index("-o") + 1], "w").close()
+            return None
+        return real(cmd, stderr=subprocess.DEVNULL, **kw)
+    monkeypatch.setattr(build.subprocess, "run", run)
+    monkeypatch.setattr(build, "LIB", str(tmp_path / "libditango.so"))
+    monkeypatch.setattr(build, "OPS_LIB", str(tmp_path / "ops.so"))
+    return ran
+
+
+@pytest.mark.parametrize("without", ["headers", "compiler"])
+def test_the_library_is_built_without_what_the_python_entry_points_need(elsewhere, monkeypatch, tmp_path, without):
+    if without == "headers":
+        monkeypatch.setattr(build.sysconfig, "get_paths", lambda *a, **k: {"include": str(tmp_path)})
+    else:
+        monkeypatch.setenv("CC", "no-such-compiler")
+    with pytest.warns(UserWarning, match="entry points"):
+        assert build.build(force=True) == build.LIB
+    assert os.path.exists(build.LIB) and not os.path.exists(build.OPS_LIB) and elsewhere == [build.NVCC]
+
+
+def test_entry_points_that_do_not_compile_are_an_error_behind_the_library(elsewhere, monkeypatch, tmp_path):
+    (tmp_path / "broken.c").write_text("#error\n")
+    monkeypatch.setattr(build, "OPS_SOURCE", str(tmp_path / "broken.c"))
+    with pytest.raises(subprocess.CalledProcessError):
+        build.build(force=True)
+    assert os.path.exists(build.LIB) and not os.path.exists(build.OPS_LIB)
+
+
+def test_the_whole_build_and_nothing_twice(elsewhere):
+    build.build()
+    assert os.path.exists(build.LIB) and os.path.exists(build.OPS_LIB) and len(elsewhere) == 2
+    build.build()
+    assert len(elsewhere) == 2
