@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import importlib.util
 import os
+import sysconfig
 
 import numpy as np
 import torch
@@ -203,7 +204,7 @@ def dt_plan_static(lse_state, offsets, B, H, L, mask_dev, eps=0.0, target_fracti
 
 # ---------------------------------------------------------------- operators around the self-attention (no context)
 # dt_rope, dt_add_rmsnorm and dt_cross_attn are marshalled in C (csrc/ops_py.c); like the library they load on first use.
-OPS_PATH = os.path.join(_HERE, "_ditango_ops.so")
+OPS_PATH = os.path.join(_HERE, "_ditango_ops" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))   # as build.py names it
 _OPS = ("dt_rope", "dt_add_rmsnorm", "dt_cross_attn")
 
 

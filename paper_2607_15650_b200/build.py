@@ -23,7 +23,8 @@ LIB = os.path.join(HERE, "libditango.so")
 SOURCES = ["api.cu", "attn_states.cu", "state_merge.cu", "plan.cu", "planner.cu", "ops_api.cu", "rope.cu", "add_rmsnorm.cu",
            "cross_attn.cu", "cross_tiles.cu"]
 HEADERS = ["dt_internal.h", "ops.h", "cross_attn.h", "ptx_sm100.cuh", os.path.join("..", "..", "include", "ditango.h")]
-OPS_LIB = os.path.join(HERE, "_ditango_ops.so")   # Python entry points of the context-free operators
+# Python entry points of the context-free operators, for this interpreter
+OPS_LIB = os.path.join(HERE, "_ditango_ops" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 OPS_SOURCE = "ops_py.c"
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 

@@ -3,6 +3,7 @@ Python entry points need to be built and loaded.  No GPU needed."""
 import ctypes
 import os
 import subprocess
+import sysconfig
 
 import pytest
 
@@ -84,3 +85,10 @@ def test_the_whole_build_and_nothing_twice(elsewhere):
     assert os.path.exists(build.LIB) and os.path.exists(build.OPS_LIB) and len(elsewhere) == 2
     build.build()
     assert len(elsewhere) == 2
+
+
+def test_the_module_of_entry_points_is_named_for_its_interpreter(lib):
+    """Two Python versions on one tree build and load a module each."""
+    suffix = sysconfig.get_config_var("EXT_SUFFIX")
+    assert suffix and build.OPS_LIB.endswith("_ditango_ops" + suffix) and dt.OPS_PATH == build.OPS_LIB and os.path.exists(build.OPS_LIB)
+    assert dt.dt_rope.__module__ == "_ditango_ops"
