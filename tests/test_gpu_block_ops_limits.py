@@ -10,7 +10,7 @@ import torch
 from paper_2607_15650_b200 import binding as dt
 from paper_2607_15650_b200 import build
 from tests import block_ops_reference as ref
-from tests.test_gpu_block_ops import norm_check
+from tests.test_gpu_block_ops import norm_check, rope_case
 
 pytestmark = pytest.mark.gpu
 BF16, FP16 = torch.bfloat16, torch.float16
@@ -241,3 +241,33 @@ print("same")
 """
     r = subprocess.run([sys.executable, "-c", text], cwd=ROOT, capture_output=True, text=True, timeout=240)
     assert r.returncode == 0 and r.stdout.split()[-1] == "same", r.stdout + r.stderr
+
+
+# ---------------------------------------------------------------------------------------------- rotary positions, rows of the norm
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("B,L,H,Hk,D,r,axes", [(1, 6007, 32, 8, 128, 38, 3), (2, 3001, 5, 3, 64, 18, 1), (1, 9001, 40, 40, 128, 100, 3), (1, 20011, 1, 1, 256, 250, 1),
+                                               (3, 4001, 7, 2, 72, 70, 1), (1, 30011, 3, 0, 8, 6, 1)])
+def test_rope_halves_off_16_byte_borders_in_several_waves(B, L, H, Hk, D, r, axes, dtype):
+    rope_case(B, L, H, Hk, D, r, True, axes, dtype, seed=9)
+    rope_case(B, L, H, Hk, D, r, True, axes, dtype, in_place=True, packed=True, transpose=True, factor=1.25, seed=9)
+
+
+def test_norm_of_tensors_whose_rows_collapse_differently():
+    """x of two strides, the residual of one, the output of two others: the same rows in each."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    n = lambda *s: torch.randn(s, generator=g, device="cuda").to(BF16)  # noqa: E731
+    x, res = n(3, 7, 9, 64)[:, :, 2:7], n(3, 7, 5, 64)
+    ybuf = torch.full((3, 7, 6, 64), 9.0, device="cuda", dtype=BF16)
+    h, want = ref.norm(x, None, 1e-6, res)
+    ro = torch.empty_like(res)
+    dt.dt_add_rmsnorm(x, None, ybuf[:, :, :5], 1e-6, residual=res, residual_out=ro)
+    torch.cuda.synchronize()
+    norm_check(x, None, res, ro, ybuf[:, :, :5], None, 1e-6, h, want, "collapse")
+    assert (ybuf[:, :, 5] == 9).all()
+    one = n(1, 1, 1, 64).expand(3, 7, 5, 64)           # one row for all
+    h, want = ref.norm(x, None, 1e-6, one)
+    y8, sc = torch.empty((3, 7, 5, 64), device="cuda", dtype=E4M3), torch.empty((3, 7, 5, 2), device="cuda")
+    dt.dt_add_rmsnorm(x, None, y8, 1e-6, residual=one, residual_out=ro, scales=sc)
+    torch.cuda.synchronize()
+    norm_check(x, None, one, ro, y8, sc, 1e-6, h, want, "one row")
