@@ -339,9 +339,11 @@ const char *dt_last_error(dt_ctx *ctx); /* text of the last error on this contex
                                            thread's last call of an operator below that failed */
 
 /* ------------------------------------------------------------------------------------------------------------------
- * Operators around the self-attention of a transformer block: rotary positions on Q and K before it, the norm with the
- * residual's addition that follows it and feeds the next projection in 8 bits, and the cross attention to an encoder's
- * states (the prompt).  The paper has no counterpart; its models' blocks (Table 1) are made of them.
+ * Operators around the self-attention of a transformer block: rotary positions on Q and K before it, the cross attention to
+ * an encoder's states (the prompt), and RMS norm.  The paper has no counterpart.  Of its models (Table 1), Wan's block calls the
+ * rotation, the cross attention, and the norm on Q and K (over the whole width, 16 bits, no residual), HunyuanVideo's the norm over
+ * a head.  The norm with the residual's addition and an 8-bit output is for blocks of the language-model kind (residual, RMS norm,
+ * 8-bit projection); the models of Table 1 add through a gate and norm with a shift instead.
  *   - No context: shapes come with the call.  The current device must be the one that owns `stream` and the buffers, and
  *     an sm_100.  The first call on a device looks up a few facts about it; every call is ONE kernel launch, stream-ordered,
  *     and may be captured into a graph.  Nothing is allocated, there is no workspace, and calls on different streams or

@@ -6,14 +6,15 @@
 // floor keeps a row of zeros from dividing by zero), value = e4m3(y * 448 / amax), rounded to nearest even.  y is (h r) weight
 // with r = 1 / sqrt(mean + eps), in this order: h r is of the order of one, whereas h * weight may leave fp32 where y does not.  So
 // amax is taken once r is known, behind the first of a row's two reductions (amax |y| = r amax |h weight| would make both at
-// once: 20000 x 8192 to e4m3 without a residual 117 us for 132, 75600 x 5120 with one 750 for 680).
+// once: 20000 x 8192 to e4m3 without a residual 117 us for 128; with a residual neither is faster on every GPU).
 //
 // Bound: HBM.  Every row is read once and stays in registers through its reductions, so a pass moves x, the residual in
 // and out, y and the scales, and nothing else.  What holds the rate up is how many rows are on the way at a time, since a
 // row's reductions are a chain of latencies: 8 to 32 lanes a row up to a width of 256, a warp up to 1024, a block above.
-// Measured in long runs: 75600 x 5120 bf16 with an fp32 residual, to e4m3, 692 us, 6.15 TB/s; 32760 x 5120 with a bf16 residual, by
-// groups of 128, 218 us, 5.4 TB/s; 561600 x 64 to fp16 25 us, 5.8 TB/s; without a residual and to 8 bits the instructions bind
-// first (20000 x 8192: 132 us, 3.7 TB/s); 3 rows of 5120 2.8 us.  Rows streamed through a ring in shared memory by bulk copies
+// Measured in long runs: 75600 x 5120 bf16 with an fp32 residual, to e4m3, 709 to 763 us by the GPU, 5.6 to 6.0 TB/s; 32760 x 5120 with a
+// bf16 residual, by groups of 128, 207 to 221 us, 5.3 to 5.7 TB/s; Wan's norm of Q and K, 75600 x 5120 to bf16 without a residual, 244 us,
+// 6.3 TB/s; 561600 x 64 to fp16 25 us, 5.8 TB/s; without a residual and to 8 bits the instructions bind
+// first (20000 x 8192: 128 us, 3.8 TB/s); 3 rows of 5120 2.8 us.  Rows streamed through a ring in shared memory by bulk copies
 // instead of the next row in registers: slower throughout (246 us for the second).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

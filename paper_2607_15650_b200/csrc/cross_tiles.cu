@@ -28,12 +28,14 @@
 // tokens x 40 heads against 512 keys run in 662 us alone (1197 TFLOP/s, tensor pipe 66 % busy), 680 in short runs and 790 to
 // 820 at the power cap, where Q and OUT cost 1.9 TB/s of HBM besides; 2048 keys 604 us for as much work, 1312 TFLOP/s.  D = 64: the
 // exponentials, if the two tiles' fall beside each other (32760 x 40 x 512 keys: 212 us, 810 TFLOP/s; in step 285), and the
-// latency of a tile's chain where an item has two tiles (2 x 17550 x 32 heads, 226 keys 125 us, with a mask 118, lengths 131).
+// latency of a tile's chain where an item has two tiles (2 x 17550 x 32 heads, 226 keys: 117 us, with a mask 118, lengths 124 on the
+// GPU alone, captured; called from Python 132 with a mask).
 //
 // Size: warps of six roles share each scheduler's instruction cache, and straight-line code waits for its own instructions
 // (traced: 1000 cycles for issuing a P V of 8 MMAs).  So every role has one loop with one place for each step, its prologue
 // included, and in the masked kernels the MMAs' and the epilogue's loops stay rolled: 59 KB for 84, and 157 -> 142 us
-// (226 keys with a mask, as above) and 154 -> 138 (lengths); with the masking warp's bytes asked for a tile ahead, 118 and 131.  Without
+// (226 keys with a mask, as above) and 154 -> 138 (lengths); with the masking warp's bytes asked for a tile ahead, 118 and 124
+// (all captured).  Without
 // masks there is room: rolled MMAs cost there (D = 128, 512 keys: 680 -> 740 us).
 //
 // Every wait on an mbarrier is bounded; on expiry the CTA records STATUS_WAIT_TIMEOUT, leaves its loops, lets what is under way

@@ -1,5 +1,5 @@
 /* Python entry points of the context-free operators (dt_rope, dt_add_rmsnorm, dt_cross_attn): argument marshalling only, in C
- * because on small tensors the marshalling is the call (through ctypes 8 to 11 us of host time against 3 to 6 us on the GPU).
+ * because on small tensors the marshalling is the call (through ctypes 8 to 11 us of host time a call, this way 5.7 to 6.1, against 3 to 5 us on the GPU).
  * Tensors are looked at through their Python attributes, so nothing here depends on torch's headers; the library's functions
  * are called through the addresses that binding.py hands to _bind. */
 #define PY_SSIZE_T_CLEAN

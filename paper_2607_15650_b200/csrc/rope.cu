@@ -8,8 +8,8 @@
 // registers and walk the heads.
 //
 // Bound: HBM (each value read and written once; the angles are D/2 per token against D * heads values).  Measured: 75600 tokens x
-// 80 heads x 128, three axes, 464 us, 6.68 TB/s (a plain copy runs at 6.57); 2 x 4441 x 64 heads x 64, a quarter turned, 30 us,
-// 4.8 TB/s (not two full waves of warps); few heads are bound by their angles (75600 x 3 heads x 64: 57 us, 1.0 TB/s); one
+// 80 heads x 128, three axes, 464 us, 6.68 TB/s (a plain copy runs at 6.57); 2 x 4441 x 64 heads x 64, half of each head turned, 30 us,
+// 4.8 TB/s (2.5 waves of warps: the half layout has three blocks per SM, 24 warps, and the third wave is half empty); few heads are bound by their angles (75600 x 3 heads x 64: 57 us, 1.0 TB/s); one
 // token 3.4 us.  Splitting a token's heads over more warps than fill the GPU costs more in angles than it gives (512 x 80
 // heads: 12 us, 19 with half as many heads per warp).
 #include <cuda_bf16.h>
