@@ -201,7 +201,7 @@ def test_norm_of_rows_and_weights_whose_product_leaves_fp32(size, weight, residu
 # ---------------------------------------------------------------------------------------------- first calls
 @pytest.mark.parametrize("call", [
     "dt.dt_rope(q, None, o, None, f)", "dt.dt_rope(q, None, o, None, f, layout=dt.DT_ROPE_HALF)", "dt.dt_add_rmsnorm(q, w, o, 1e-6)",
-    "dt.dt_add_rmsnorm(q.view(100, 30720 // 2), None, o.view(100, 30720 // 2), 1e-6)",
+    "dt.dt_add_rmsnorm(q.view(100, 15360), None, o.view(100, 15360), 1e-6)",
     "dt.dt_cross_attn(q[:, :1], q, q, o[:, :1], 0.1)", "dt.dt_cross_attn(q, q[:, :300], q[:, :300], o, 0.1)",
     "dt.dt_cross_attn(q[:, :600], q, q, o[:, :600], 0.1)", "dt.dt_cross_attn(q, q, q, o, 0.1, key_mask=m)"])
 def test_the_first_call_of_a_process_captured_gives_what_a_plain_call_gives(call):
