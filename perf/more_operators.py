@@ -37,27 +37,27 @@ def attn_case(name, shape, B, docs, Lq, Lk, H, Hk, D, dtype, causal, prefix, cap
 def listed():
     return [
         # one token of one request through a narrow projection: latency only
-        linear_case("linear, one token", 1, 1536, 1536, 8, 2, 1, "bf16", False),
+        linear_case("linear one token", 1, 1536, 1536, 8, 2, 1, "bf16", False),
         # the next token of each of seven requests, five adapters: the weights are read once
-        linear_case("linear, a token each", 7, 5120, 5120, 16, 5, 7, "fp16", False),
+        linear_case("linear a token each", 7, 5120, 5120, 16, 5, 7, "fp16", False),
         # the prompts of six requests on their way to keys, ragged lengths
-        linear_case("linear, prompts", 1807, 4096, 5120, 32, 4, 6, "bf16", True),
+        linear_case("linear prompts", 1807, 4096, 5120, 32, 4, 6, "bf16", True),
         # Wan's 1.3B width at 480p, three requests' latents
-        linear_case("linear, 480p", 32760, 1536, 1536, 24, 3, 3, "fp16", True),
+        linear_case("linear 480p", 32760, 1536, 1536, 24, 3, 3, "fp16", True),
         # Wan's 14B width at 720p, two requests' latents and a third without an adapter
-        linear_case("linear, 720p", 75600, 5120, 5120, 64, 2, 3, "bf16", True),
+        linear_case("linear 720p", 75600, 5120, 5120, 64, 2, 3, "bf16", True),
         # one new token of each of five prompts that are being written, heads in groups, capped logits: latency only
-        attn_case("attn, one token", "cache", 5, 1, 1, 512, 32, 8, 128, "bf16", True, False, True, "none"),
+        attn_case("attn one token", "cache", 5, 1, 1, 512, 32, 8, 128, "bf16", True, False, True, "none"),
         # one new token of each of two requests with long histories, a slope per head
-        attn_case("attn, one token, long", "cache", 2, 1, 1, 32760, 40, 8, 128, "fp16", True, False, False, "slopes"),
+        attn_case("attn one token far", "cache", 2, 1, 1, 32760, 40, 8, 128, "fp16", True, False, False, "slopes"),
         # a text encoder over packed prompts: D = 64, a bias for each distance, both directions
-        attn_case("attn, packed prompts", "packed", 1, 9, 2011, 2011, 64, 64, 64, "bf16", False, False, False, "table"),
+        attn_case("attn packed prompts", "packed", 1, 9, 2011, 2011, 64, 64, 64, "bf16", False, False, False, "table"),
         # two padded sequences whose first third is seen by all their tokens, heads in groups, capped logits
-        attn_case("attn, prefix", "padded", 2, 1, 4441, 4441, 32, 8, 128, "bf16", True, True, True, "none"),
+        attn_case("attn prefix", "padded", 2, 1, 4441, 4441, 32, 8, 128, "bf16", True, True, True, "none"),
         # latents of three requests in one row (Wan's 1.3B at 480p in all)
-        attn_case("attn, packed 480p", "packed", 1, 3, 32760, 32760, 12, 12, 128, "bf16", False, False, False, "none"),
+        attn_case("attn packed 480p", "packed", 1, 3, 32760, 32760, 12, 12, 128, "bf16", False, False, False, "none"),
         # a long sequence, causal, a slope per head
-        attn_case("attn, long causal", "padded", 1, 1, 17550, 17550, 40, 40, 128, "fp16", True, False, False, "slopes"),
+        attn_case("attn long causal", "padded", 1, 1, 17550, 17550, 40, 40, 128, "fp16", True, False, False, "slopes"),
     ]
 
 
