@@ -439,6 +439,66 @@ dt_status dt_cross_attn(const dt_cross_config *cfg, const void *q_dev, const int
                         const int32_t *key_lens_dev, const uint8_t *key_mask_dev, int64_t key_mask_stride, void *out_dev,
                         const int64_t out_strides_blhd[4], float *lse_out_dev, void *stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Operators for several requests packed into one batch: their rows stand behind one another, and int32 borders on the device say
+ * where each begins.  As above: no context, nothing is allocated, stream-ordered, capturable, no atomics.  Borders do not decrease
+ * (those outside the rows are clamped). */
+
+/* A projection that all rows share, with a low-rank adapter per segment of rows:
+ *     y[m] = W x[m] + bias + scales[a] B_a (A_a x[m]),   a = adapters_of[s] for starts[s] <= m < starts[s + 1].
+ * Rows in no segment, and those whose adapters_of is not in [0, adapters), have the projection alone; no row sees another's
+ * adapter, whatever it holds.  Sums are fp32 and y is rounded once; A_a x, scaled, is kept in x's type for more than 16 rows (fp16:
+ * beyond 65504 it is an infinity).
+ *   x, y            device, [rows][K] and [rows][N], row strides multiples of 8 elements; y overlaps no input
+ *   w_dev           device, [N][K], row stride a multiple of 8 elements
+ *   bias_dev        device [N], x's type or fp32, or NULL
+ *   a_dev, b_dev    device, contiguous, [adapters][rank][K] and [adapters][N][rank] (smaller ranks padded with zeros)
+ *   scales_dev      device, fp32 [adapters], or NULL: 1
+ *   starts_dev, adapters_of_dev   device, int32 [segments + 1] and [segments]
+ *   workspace_dev   device, dt_adapter_workspace_bytes(rows, rank) bytes of any content; calls that share one are ordered, and so are
+ *                   replays of graphs that do
+ * Without segments or adapters the last six are not looked at.  One launch for the projection and one, beside it, for the adapters.
+ * Limits: K, N multiples of 8, at most 2^20; rank a multiple of 8, 8 to 128; rows up to 2^30, adapters 65535, segments 2^20. */
+typedef struct {
+    int32_t dtype, bias_dtype;        /* DT_VALUE_*: bf16 or fp16; that or fp32 */
+    int64_t rows;
+    int32_t K, N, rank, adapters, segments;
+    int64_t x_stride, w_stride, y_stride;
+} dt_adapter_config;
+dt_status dt_adapter_workspace_bytes(int64_t rows, int32_t rank, size_t *bytes);
+dt_status dt_adapter_linear(const dt_adapter_config *cfg, const void *x_dev, const void *w_dev, const void *bias_dev, const void *a_dev,
+                            const void *b_dev, const float *scales_dev, const int32_t *starts_dev, const int32_t *adapters_of_dev,
+                            void *y_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* Attention within documents.  Document d of row b of the batch: queries q_starts[b][d] <= i < q_starts[b][d + 1] and keys
+ * k_starts[b][d] <= j < k_starts[b][d + 1]; without borders (docs = 0) one document per row, queries below q_lens[b] and keys
+ * below key_lens[b].  Its last query stands at its last key: a query's place among the keys is p_i = i - q_end + k_end, and
+ *     s_ij = softmax_scale q_i.k_j,   capped (softcap > 0): softcap tanh(s_ij / softcap),
+ *     x_ij = s_ij + bias_table[h][clamp(j - p_i, -bias_far, bias_far) + bias_far]   or   s_ij - bias_slopes[h] |j - p_i|,
+ *     LSE_i = log sum_j exp(x_ij),   OUT_i = sum_j exp(x_ij - LSE_i) v_j
+ * over the document's keys j; causal: those with j <= p_i, and the document's first prefix_lens[b][d] keys.  A row without keys has
+ * OUT = 0 and LSE = -inf; rows of q in no document are left as they were.  What stands in K and V at keys that do not count for a
+ * row (other documents', later ones, padding; NaN and infinities too) has no effect on it.
+ *   q, out          device [B, Lq, H, D]; out may be q (same strides), out's rows may not overlap
+ *   k, v            device [B, Lk, H_kv, D], strides of their own; query head h reads key head h / (H / H_kv)
+ *   q_starts, k_starts        device, int32 [B][docs + 1], or both NULL with docs = 0
+ *   q_lens, key_lens          device, int32 [B] (clamped to [0, Lq] and [0, Lk]), or NULL: all; only without borders
+ *   prefix_lens               device, int32 [B][docs or 1], or NULL: none; looked at only if causal
+ *   bias_table_dev            device, fp32 [H][2 bias_far + 1], or NULL;  bias_slopes_dev  device, fp32 [H], or NULL; not both
+ *   lse_out_dev               device, fp32 [B, H, Lq], or NULL
+ * Limits: D in {64, 128}; B * H <= 65535; Lq * H <= 2^30; Lk <= 2^24; docs <= 65536; bias_far <= 512. */
+typedef struct {
+    int32_t dtype;                    /* DT_VALUE_BF16 or DT_VALUE_FP16 */
+    int32_t B, Lq, Lk, H, H_kv, D;
+    int32_t docs, causal, bias_far;
+    float softmax_scale, softcap;     /* softcap 0: none */
+} dt_packed_config;
+dt_status dt_packed_attn(const dt_packed_config *cfg, const void *q_dev, const int64_t q_strides_blhd[4], const void *k_dev,
+                         const int64_t k_strides_blhd[4], const void *v_dev, const int64_t v_strides_blhd[4], const int32_t *q_starts_dev,
+                         const int32_t *k_starts_dev, const int32_t *q_lens_dev, const int32_t *key_lens_dev, const int32_t *prefix_lens_dev,
+                         const float *bias_table_dev, const float *bias_slopes_dev, void *out_dev, const int64_t out_strides_blhd[4],
+                         float *lse_out_dev, void *stream);
+
 /* Read (and clear) the current device's status word of the operators above; synchronises the device.  DT_OK or
  * DT_ERR_TIMEOUT. */
 dt_status dt_poll_ops(void);

@@ -33,6 +33,7 @@ EXPORTS = [
     "dt_attn_fused", "dt_num_slots", "dt_slot_ranges", "dt_group_compose", "dt_group_fit", "dt_group_reset",
     "dt_plan_sums", "dt_plan_from_sums",
     "dt_rope", "dt_rope_freqs", "dt_add_rmsnorm", "dt_cross_attn", "dt_poll_ops", "dt_selftest_ops_timeout",
+    "dt_adapter_workspace_bytes", "dt_adapter_linear", "dt_packed_attn",
 ]
 
 
@@ -67,6 +68,17 @@ class dt_norm_config(C.Structure):
 
 class dt_cross_config(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("dtype", "B", "Lq", "Lk", "H", "H_kv", "D")] + [("softmax_scale", C.c_float)]
+
+
+class dt_adapter_config(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("bias_dtype", C.c_int32), ("rows", C.c_int64)] + [
+        (n, C.c_int32) for n in ("K", "N", "rank", "adapters", "segments")] + [
+        (n, C.c_int64) for n in ("x_stride", "w_stride", "y_stride")]
+
+
+class dt_packed_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "B", "Lq", "Lk", "H", "H_kv", "D", "docs", "causal", "bias_far")] + [
+        ("softmax_scale", C.c_float), ("softcap", C.c_float)]
 
 
 class DitangoError(RuntimeError):
@@ -127,6 +139,9 @@ def lib():
         "dt_rope_freqs": (C.c_int, [C.POINTER(dt_rope_scaling), C.c_int32, vp, C.POINTER(C.c_float)]),
         "dt_add_rmsnorm": (C.c_int, [vp] * 8),
         "dt_cross_attn": (C.c_int, [vp] * 9 + [C.c_int64] + [vp] * 4),
+        "dt_adapter_workspace_bytes": (C.c_int, [C.c_int64, C.c_int32, szp]),
+        "dt_adapter_linear": (C.c_int, [vp] * 11 + [C.c_size_t, vp]),
+        "dt_packed_attn": (C.c_int, [vp] * 18),
         "dt_poll_ops": (C.c_int, []),
         "dt_selftest_ops_timeout": (C.c_int, [C.c_uint32, vp]),
         "dt_status_str": (C.c_char_p, [C.c_int]),
@@ -203,9 +218,9 @@ def dt_plan_static(lse_state, offsets, B, H, L, mask_dev, eps=0.0, target_fracti
 
 
 # ---------------------------------------------------------------- operators around the self-attention (no context)
-# dt_rope, dt_add_rmsnorm and dt_cross_attn are marshalled in C (csrc/ops_py.c); like the library they load on first use.
+# dt_rope, dt_add_rmsnorm, dt_cross_attn and the operators for packed requests are marshalled in C (csrc/ops_py.c); like the library they load on first use.
 OPS_PATH = os.path.join(_HERE, "_ditango_ops" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))   # as build.py names it
-_OPS = ("dt_rope", "dt_add_rmsnorm", "dt_cross_attn")
+_OPS = ("dt_rope", "dt_add_rmsnorm", "dt_cross_attn", "dt_adapter_linear", "dt_packed_attn")
 
 
 def _load_ops():
@@ -256,6 +271,15 @@ def dt_rope_grid_freqs(dims, base=10000.0):
         table[a, at:at + d // 2] = dt_rope_freqs(d, base)[0]
         at += d // 2
     return table
+
+
+def dt_adapter_workspace_bytes(rows, rank):
+    """Bytes of the workspace that dt_adapter_linear wants for so many rows and adapters of that rank."""
+    n = C.c_size_t()
+    s = lib().dt_adapter_workspace_bytes(int(rows), int(rank), C.byref(n))
+    if s != DT_OK:
+        raise DitangoError(s, status_str(s), lib().dt_last_error(None).decode())
+    return n.value
 
 
 def dt_poll_ops(device=None):

@@ -1,0 +1,257 @@
+// dt_adapter_linear: a projection that several requests share, with each request's own low-rank adapter.
+//
+// Mathematics: y[m] = W x[m] + bias + s_a B_a (A_a x[m]), a the adapter of the segment that row m lies in.  Both products of a row
+// are summed in fp32 in one accumulator and rounded once.  The adapters' inner products t = s_a A_a x (rank values a row) are made
+// by a kernel of their own, since every column of y wants them; the projection's kernel starts beside it (a programmatic launch)
+// and waits for t only where it adds B t.
+//
+// Few rows (here): bound by reading W once.  W's rows are the 16 rows of mma.sync and the tokens its 8 columns.  A lane loads 16
+// contiguous bytes of a row of W and of x and takes them as its fragments, so that the k-order is permuted alike on both sides and
+// nothing passes through shared memory; the 8 warps of a block split K and join in shared memory in a fixed order.  t stays in
+// fp32.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <cmath>
+
+#include "adapter_linear.h"
+#include "tile_wait.cuh"
+
+namespace dt {
+namespace {
+
+constexpr int ROWS_WARPS = 8, ROWS_THREADS = ROWS_WARPS * 32;
+constexpr int CHUNK = 32, BATCH = 4;          // k values that four lanes' pieces cover; chunks in flight per warp
+
+template <bool FP16>
+__device__ __forceinline__ float2 widen(uint32_t v) {
+    if constexpr (FP16) return __half22float2(*reinterpret_cast<const __half2 *>(&v));
+    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
+}
+template <bool FP16>
+__device__ __forceinline__ float dot8(uint4 a, uint4 b, float acc) {
+    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 u = widen<FP16>(x[i]), v = widen<FP16>(y[i]);
+        acc = fmaf(u.x, v.x, acc);
+        acc = fmaf(u.y, v.y, acc);
+    }
+    return acc;
+}
+
+// t[m][j] = s_a A_a[j] . x[m]: a warp per (m, j).
+template <bool FP16>
+__global__ void __launch_bounds__(ROWS_THREADS) shrink_rows_kernel(const AdapterParams p) {
+    let_next_start();
+    const int m = blockIdx.y, j = blockIdx.x * ROWS_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (j >= p.rank) return;
+    const int a = adapter_of_row(p, m);
+    if (a < 0) return;
+    const uint16_t *x = p.x + m * p.xs, *row = p.a + ((long long)a * p.rank + j) * p.K;
+    float acc[4] = {};
+    int k = lane * 8;
+    for (; k + 3 * 256 < p.K; k += 4 * 256) {
+        uint4 u[4], v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u[i] = __ldg(reinterpret_cast<const uint4 *>(row + k + i * 256));
+            v[i] = __ldg(reinterpret_cast<const uint4 *>(x + k + i * 256));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = dot8<FP16>(u[i], v[i], acc[i]);
+    }
+    for (; k < p.K; k += 256)
+        acc[0] = dot8<FP16>(__ldg(reinterpret_cast<const uint4 *>(row + k)), __ldg(reinterpret_cast<const uint4 *>(x + k)), acc[0]);
+    float sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+#pragma unroll
+    for (int i = 16; i > 0; i >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, i);
+    if (lane == 0) static_cast<float *>(p.t)[(long long)m * p.rank16 + j] = sum * (p.scales ? __ldg(p.scales + a) : 1.0f);
+}
+
+template <bool FP16>
+__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if constexpr (FP16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// NT: columns of 8 rows of x; blockIdx.y takes 8 NT rows each.
+template <bool FP16, int NT>
+__global__ void __launch_bounds__(ROWS_THREADS) adapter_rows_kernel(const AdapterParams p) {
+    __shared__ float part[ROWS_WARPS][8 * NT][17];   // (a column of padding: the lanes' rows fall on different banks)
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 8 * NT;
+    const int steps = (p.K + CHUNK - 1) / CHUNK;
+    const int from = steps * warp / ROWS_WARPS * CHUNK + 8 * t, to = min(steps * (warp + 1) / ROWS_WARPS * CHUNK, p.K);
+    const bool low = n0 + g < p.N, high = n0 + g + 8 < p.N;
+    const uint16_t *w0 = p.w + (low ? (n0 + g) * p.ws : 0), *w1 = p.w + (high ? (n0 + g + 8) * p.ws : 0);
+    const uint16_t *xr[NT];
+    bool live[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        live[n] = m0 + 8 * n + g < p.M;
+        xr[n] = p.x + (live[n] ? (m0 + 8 * n + g) * p.xs : 0);
+    }
+    float acc[NT][4] = {};
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    for (int k = from; k - 8 * t < to; k += BATCH * CHUNK) {
+        uint4 u[BATCH], v[BATCH], x[BATCH][NT];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int at = k + i * CHUNK;
+            const bool in = at < to;
+            u[i] = in && low ? __ldcs(reinterpret_cast<const uint4 *>(w0 + at)) : none;
+            v[i] = in && high ? __ldcs(reinterpret_cast<const uint4 *>(w1 + at)) : none;
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) x[i][n] = k + i * CHUNK < to && live[n] ? __ldg(reinterpret_cast<const uint4 *>(xr[n] + k + i * CHUNK)) : none;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                mma_16816<FP16>(acc[n], u[i].x, v[i].x, u[i].y, v[i].y, x[i][n].x, x[i][n].y);
+                mma_16816<FP16>(acc[n], u[i].z, v[i].z, u[i].w, v[i].w, x[i][n].z, x[i][n].w);
+            }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[warp][8 * n + 2 * t + (e & 1)][g + 8 * (e >> 1)] = acc[n][e];
+    __syncthreads();
+    // two threads a value of y: half of the warps' sums and half of the rank's pieces each
+    const int half = threadIdx.x & 1;
+    bool waited = false;
+#pragma unroll 1
+    for (int o = threadIdx.x >> 1; o < 128 * NT; o += ROWS_THREADS / 2) {
+        const int n = n0 + (o & 15), c = o >> 4, m = m0 + c;
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < ROWS_WARPS / 2; ++w) sum += part[half * (ROWS_WARPS / 2) + w][c][o & 15];
+        const bool valid = m < p.M && n < p.N;
+        const int a = valid && p.segments > 0 ? adapter_of_row(p, m) : -1;
+        if (p.segments > 0 && !waited) {
+            wait_for_previous();
+            waited = true;
+        }
+        if (a >= 0) {
+            const uint16_t *b = p.b + ((long long)a * p.N + n) * p.rank;
+            const float *tr = static_cast<const float *>(p.t) + (long long)m * p.rank16;
+#pragma unroll 2
+            for (int j = 8 * half; j < p.rank; j += 16) {
+                const uint4 v = __ldg(reinterpret_cast<const uint4 *>(b + j));
+                // (t was written beside this kernel: from L2)
+                const float4 t0 = __ldcg(reinterpret_cast<const float4 *>(tr + j)), t1 = __ldcg(reinterpret_cast<const float4 *>(tr + j + 4));
+                float2 q = widen<FP16>(v.x);
+                sum = fmaf(q.x, t0.x, sum); sum = fmaf(q.y, t0.y, sum);
+                q = widen<FP16>(v.y);
+                sum = fmaf(q.x, t0.z, sum); sum = fmaf(q.y, t0.w, sum);
+                q = widen<FP16>(v.z);
+                sum = fmaf(q.x, t1.x, sum); sum = fmaf(q.y, t1.y, sum);
+                q = widen<FP16>(v.w);
+                sum = fmaf(q.x, t1.z, sum); sum = fmaf(q.y, t1.w, sum);
+            }
+        }
+        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+        if (!valid || half) continue;
+        if (p.bias) sum += p.bias_fp32 ? __ldg(static_cast<const float *>(p.bias) + n)
+                                       : widen<FP16>(__ldg(static_cast<const uint16_t *>(p.bias) + n)).x;
+        p.y[m * p.ys + n] = (uint16_t)pack_half2<FP16>(sum, 0.f);
+    }
+}
+
+template <bool FP16, int NT>
+cudaError_t launch_rows(const AdapterParams &p, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((p.N + 15) / 16), (unsigned)((p.M + 8 * NT - 1) / (8 * NT)));
+    cfg.blockDim = dim3(ROWS_THREADS);
+    cfg.stream = st;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = p.segments > 0 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, adapter_rows_kernel<FP16, NT>, p);
+}
+template <bool FP16>
+cudaError_t launch_rows(const AdapterParams &p, cudaStream_t st) {
+    if (p.segments > 0) {
+        shrink_rows_kernel<FP16><<<dim3((unsigned)((p.rank + ROWS_WARPS - 1) / ROWS_WARPS), (unsigned)p.M), ROWS_THREADS, 0, st>>>(p);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+    }
+    return p.M <= 8 ? launch_rows<FP16, 1>(p, st) : launch_rows<FP16, 2>(p, st);
+}
+
+constexpr int FEW_ROWS = 16;
+
+size_t workspace_of(int64_t rows, int rank) { return (size_t)rows * (size_t)((rank + 15) / 16 * 16) * (rows <= FEW_ROWS ? 4 : 2); }
+
+}  // namespace
+
+cudaError_t launch_adapter_rows(const AdapterParams &p, bool fp16, cudaStream_t st) {
+    return fp16 ? launch_rows<true>(p, st) : launch_rows<false>(p, st);
+}
+
+}  // namespace dt
+
+extern "C" dt_status dt_adapter_workspace_bytes(int64_t rows, int32_t rank, size_t *bytes) {
+    using namespace dt;
+    if (!bytes || rows < 0 || rank < 0 || rows > (1 << 30) || rank > 128) return ops_fail(DT_ERR_INVALID_ARG, "bad shape");
+    *bytes = workspace_of(rows, rank);
+    return DT_OK;
+}
+
+extern "C" dt_status dt_adapter_linear(const dt_adapter_config *cfg, const void *x_dev, const void *w_dev, const void *bias_dev, const void *a_dev,
+                                       const void *b_dev, const float *scales_dev, const int32_t *starts_dev, const int32_t *adapters_of_dev,
+                                       void *y_dev, void *workspace_dev, size_t workspace_bytes, void *stream) {
+    using namespace dt;
+    if (!cfg) return ops_fail(DT_ERR_INVALID_ARG, "null config");
+    const dt_adapter_config &c = *cfg;
+    if (c.dtype != DT_VALUE_BF16 && c.dtype != DT_VALUE_FP16) return ops_fail(DT_ERR_UNSUPPORTED, "x, w, a, b and y must be bf16 or fp16");
+    if (c.bias_dtype != c.dtype && c.bias_dtype != DT_VALUE_FP32) return ops_fail(DT_ERR_UNSUPPORTED, "bias must be of x's type or fp32");
+    if (c.rows < 0 || c.K < 1 || c.N < 1 || c.segments < 0 || c.adapters < 0 || c.rank < 0) return ops_fail(DT_ERR_INVALID_ARG, "bad shape");
+    if (c.rows > (1 << 30) || c.K > (1 << 20) || c.N > (1 << 20) || c.adapters > 65535 || c.segments > (1 << 20))
+        return ops_fail(DT_ERR_UNSUPPORTED, "rows exceed 2^30, K, N or segments 2^20, or adapters 65535");
+    if (c.K % 8 != 0 || c.N % 8 != 0) return ops_fail(DT_ERR_UNSUPPORTED, "K and N must be multiples of 8");
+    const bool adapted = c.segments > 0 && c.adapters > 0;
+    if (adapted && (c.rank < 8 || c.rank > 128 || c.rank % 8 != 0)) return ops_fail(DT_ERR_UNSUPPORTED, "rank must be a multiple of 8, 8 to 128");
+    if (c.rows == 0) return DT_OK;
+    auto bad = [](const void *q, unsigned mask) { return !q || (reinterpret_cast<uintptr_t>(q) & mask) != 0; };
+    if (bad(x_dev, 15) || bad(w_dev, 15) || bad(y_dev, 15)) return ops_fail(DT_ERR_INVALID_ARG, "x, w and y must be 16-byte aligned and not null");
+    if ((c.rows > 1 && (c.x_stride < c.K || c.x_stride % 8 != 0)) || c.w_stride < c.K || c.w_stride % 8 != 0)
+        return ops_fail(DT_ERR_INVALID_ARG, "row strides of x and w must be multiples of 8 elements, at least K");
+    if (c.rows > 1 && (c.y_stride < c.N || c.y_stride % 8 != 0)) return ops_fail(DT_ERR_INVALID_ARG, "row stride of y must be a multiple of 8 elements, at least N");
+    if (y_dev == x_dev || y_dev == w_dev) return ops_fail(DT_ERR_INVALID_ARG, "y is x or w");
+    if (bias_dev && bad(bias_dev, c.bias_dtype == DT_VALUE_FP32 ? 3 : 1)) return ops_fail(DT_ERR_INVALID_ARG, "bias is not aligned");
+    if (adapted) {
+        if (bad(a_dev, 15) || bad(b_dev, 15)) return ops_fail(DT_ERR_INVALID_ARG, "a and b must be 16-byte aligned and not null");
+        if (bad(starts_dev, 3) || bad(adapters_of_dev, 3)) return ops_fail(DT_ERR_INVALID_ARG, "starts and adapters_of must be 4-byte aligned and not null");
+        if (scales_dev && bad(scales_dev, 3)) return ops_fail(DT_ERR_INVALID_ARG, "scales must be 4-byte aligned");
+        if (bad(workspace_dev, 15) || workspace_bytes < workspace_of(c.rows, c.rank))
+            return ops_fail(DT_ERR_INVALID_ARG, "workspace is null, not 16-byte aligned or smaller than dt_adapter_workspace_bytes()");
+    }
+    const OpsDevice *dev;
+    const dt_status s = ops_device(&dev);
+    if (s != DT_OK) return s;
+    AdapterParams p = {};
+    p.x = static_cast<const uint16_t *>(x_dev); p.w = static_cast<const uint16_t *>(w_dev); p.y = static_cast<uint16_t *>(y_dev);
+    p.bias = bias_dev; p.bias_fp32 = c.bias_dtype == DT_VALUE_FP32;
+    p.xs = c.x_stride; p.ws = c.w_stride; p.ys = c.y_stride;
+    p.M = (int)c.rows; p.K = c.K; p.N = c.N;
+    if (adapted) {
+        p.a = static_cast<const uint16_t *>(a_dev); p.b = static_cast<const uint16_t *>(b_dev);
+        p.scales = scales_dev; p.starts = starts_dev; p.which = adapters_of_dev; p.t = workspace_dev;
+        p.rank = c.rank; p.rank16 = (c.rank + 15) / 16 * 16; p.adapters = c.adapters; p.segments = c.segments;
+    }
+    p.status = dev->status;
+    const bool fp16 = c.dtype == DT_VALUE_FP16;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = p.M <= FEW_ROWS ? launch_adapter_rows(p, fp16, st) : launch_adapter_tiles(p, fp16, *dev, st);
+    return e == cudaSuccess ? DT_OK : ops_fail_cuda(e, "adapter launch");
+}

@@ -64,6 +64,13 @@ dt_status ops_device(const OpsDevice **out) {
         g_looking_up.clear(std::memory_order_release);
         if (s != DT_OK) return s;
     }
+    // The tensor maps' encoder is of the driver: it wants the device's context current in the calling thread, which the runtime only
+    // sees to in calls that need one itself.  A thread whose first CUDA call is an operator has had none.
+    thread_local uint64_t bound = 0;
+    if (!(bound >> dev & 1)) {
+        if ((e = cudaSetDevice(dev)) != cudaSuccess) return ops_fail_cuda(e, "cudaSetDevice");
+        bound |= 1ull << dev;
+    }
     *out = &g_devices[dev];
     return DT_OK;
 }

@@ -1,4 +1,4 @@
-/* Python entry points of the context-free operators (dt_rope, dt_add_rmsnorm, dt_cross_attn): argument marshalling only, in C
+/* Python entry points of the context-free operators (dt_rope, dt_add_rmsnorm, dt_cross_attn, dt_adapter_linear, dt_packed_attn): argument marshalling only, in C
  * because on small tensors the marshalling is the call (through ctypes 8 to 11 us of host time a call, this way 5.7 to 6.1, against 3 to 5 us on the GPU).
  * Tensors are looked at through their Python attributes, so nothing here depends on torch's headers; the library's functions
  * are called through the addresses that binding.py hands to _bind. */
@@ -25,6 +25,12 @@ static dt_status (*f_rope)(const dt_rope_config *, const void *, const int64_t *
 static dt_status (*f_norm)(const dt_norm_config *, const void *, const void *, const void *, void *, void *, float *, void *);
 static dt_status (*f_cross)(const dt_cross_config *, const void *, const int64_t *, const void *, const int64_t *, const void *,
                             const int64_t *, const int32_t *, const uint8_t *, int64_t, void *, const int64_t *, float *, void *);
+
+static dt_status (*f_adapter)(const dt_adapter_config *, const void *, const void *, const void *, const void *, const void *, const float *,
+                              const int32_t *, const int32_t *, void *, void *, size_t, void *);
+static dt_status (*f_packed)(const dt_packed_config *, const void *, const int64_t *, const void *, const int64_t *, const void *, const int64_t *,
+                             const int32_t *, const int32_t *, const int32_t *, const int32_t *, const int32_t *, const float *, const float *,
+                             void *, const int64_t *, float *, void *);
 
 static int ints_of(PyObject *seq, int64_t *out) {   /* a tuple's integers; steals the reference; -1 with an error set */
     if (!seq) return -1;
@@ -368,6 +374,129 @@ static PyObject *py_cross(PyObject *self, PyObject *const *args, Py_ssize_t narg
                         a[6] ? mask.stride[0] : 0, o.ptr, o.stride, a[7] ? lse.ptr : NULL, st));
 }
 
+/* A matrix's rows: its leading dimensions collapsed into one, with one stride; 0 if they do not. */
+static int one_stride(const Tensor *t, int64_t *n, int64_t *s) {
+    int64_t nn[2], ss[2];
+    *n = 0;
+    *s = t->shape[t->nd - 1];
+    for (int i = 0; i + 1 < t->nd; ++i)
+        if (t->shape[i] == 0) return 1;   /* no rows */
+    if (!rows_of(t, nn, ss) || (nn[0] != 1 && nn[1] != 1)) return 0;
+    const int at = nn[0] != 1 ? 0 : 1;
+    *n = nn[0] * nn[1];
+    if (*n > 1) *s = ss[at];
+    return 1;
+}
+
+static PyObject *py_adapter(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
+    static const char *const names[] = {"x", "weight", "y", "a", "b", "starts", "adapters_of", "workspace", "scales", "bias", "stream"};
+    PyObject *o[11];
+    if (take("dt_adapter_linear", names, 11, 8, args, nargs, kwnames, o) < 0) return NULL;
+    Tensor x, w, y, a, b, st, of, ws, sc, bias;
+    if (look(o[0], &x) < 0 || look(o[1], &w) < 0 || look(o[2], &y) < 0) return NULL;
+    NEED(x.nd >= 1 && x.device >= 0 && (x.dtype == T_BF16 || x.dtype == T_FP16));
+    NEED(w.nd == 2 && y.nd == x.nd && w.shape[1] == x.shape[x.nd - 1] && y.shape[y.nd - 1] == w.shape[0]);
+    for (int i = 0; i + 1 < x.nd; ++i) NEED(x.shape[i] == y.shape[i]);
+    NEED(w.dtype == x.dtype && y.dtype == x.dtype && w.device == x.device && y.device == x.device);
+    dt_adapter_config c = {0};
+    c.dtype = c.bias_dtype = x.dtype;
+    int64_t rows, y_rows, w_rows;
+    NEED(one_stride(&x, &rows, &c.x_stride) && one_stride(&y, &y_rows, &c.y_stride) && one_stride(&w, &w_rows, &c.w_stride) && "rows of one stride, values of stride 1");
+    NEED(w.shape[0] <= INT32_MAX && w.shape[1] <= INT32_MAX);
+    c.rows = rows;
+    c.N = (int32_t)w.shape[0]; c.K = (int32_t)w.shape[1];
+    const int adapted = o[3] != Py_None;
+    if (adapted) {
+        if (look(o[3], &a) < 0 || look(o[4], &b) < 0 || look(o[5], &st) < 0 || look(o[6], &of) < 0 || look(o[7], &ws) < 0) return NULL;
+        NEED(a.nd == 3 && b.nd == 3 && a.shape[0] == b.shape[0] && a.shape[1] == b.shape[2] && a.shape[2] == c.K && b.shape[1] == c.N);
+        NEED(a.dtype == x.dtype && b.dtype == x.dtype && contiguous(&a) && contiguous(&b) && a.device == x.device && b.device == x.device);
+        NEED(st.dtype == T_I32 && of.dtype == T_I32 && of.nd == 1 && st.nd == 1 && st.shape[0] == of.shape[0] + 1);
+        NEED(contiguous(&st) && contiguous(&of) && st.device == x.device && of.device == x.device);
+        NEED(ws.dtype == T_U8 && ws.nd == 1 && contiguous(&ws) && ws.device == x.device);
+        NEED(a.shape[0] <= INT32_MAX && a.shape[1] <= INT32_MAX && of.shape[0] <= INT32_MAX);
+        c.adapters = (int32_t)a.shape[0]; c.rank = (int32_t)a.shape[1]; c.segments = (int32_t)of.shape[0];
+        if (o[8]) {
+            if (look(o[8], &sc) < 0) return NULL;
+            NEED(sc.dtype == T_FP32 && is_shape(&sc, 1, c.adapters, 0, 0, 0) && contiguous(&sc) && sc.device == x.device);
+        }
+    }
+    if (o[9]) {
+        if (look(o[9], &bias) < 0) return NULL;
+        NEED(is_shape(&bias, 1, c.N, 0, 0, 0) && contiguous(&bias) && bias.device == x.device && (bias.dtype == x.dtype || bias.dtype == T_FP32));
+        c.bias_dtype = bias.dtype;
+    }
+    ON_DEVICE("dt_adapter_linear", x.device);
+    void *stream;
+    if (stream_of(o[10], x.device, &stream) < 0) return NULL;
+    return done(f_adapter(&c, x.ptr, w.ptr, o[9] ? bias.ptr : NULL, adapted ? a.ptr : NULL, adapted ? b.ptr : NULL, adapted && o[8] ? sc.ptr : NULL,
+                          adapted ? st.ptr : NULL, adapted ? of.ptr : NULL, y.ptr, adapted ? ws.ptr : NULL, adapted ? (size_t)ws.shape[0] : 0, stream));
+}
+
+static PyObject *py_packed(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
+    static const char *const names[] = {"q", "k", "v", "out", "softmax_scale", "causal", "softcap", "q_starts", "k_starts", "q_lens", "key_lens",
+                                        "prefix_lens", "bias_table", "bias_slopes", "lse_out", "stream"};
+    PyObject *a[16];
+    if (take("dt_packed_attn", names, 16, 5, args, nargs, kwnames, a) < 0) return NULL;
+    Tensor q, k, v, o, qst, kst, ql, kl, pre, tab, slo, lse;
+    if (look(a[0], &q) < 0 || look(a[1], &k) < 0 || look(a[2], &v) < 0 || look(a[3], &o) < 0) return NULL;
+    NEED(q.nd == 4 && q.device >= 0 && k.nd == 4);
+    NEED(q.dtype == T_BF16 || q.dtype == T_FP16);
+    NEED(k.shape[0] == q.shape[0] && k.shape[3] == q.shape[3] && same_shape(&k, &v) && same_shape(&q, &o));
+    NEED(k.dtype == q.dtype && v.dtype == q.dtype && o.dtype == q.dtype);
+    NEED(k.device == q.device && v.device == q.device && o.device == q.device);
+    const int64_t B = q.shape[0], Lq = q.shape[1], H = q.shape[2], Lk = k.shape[1];
+    NEED(B <= INT32_MAX && Lq <= INT32_MAX && H <= INT32_MAX && Lk <= INT32_MAX && k.shape[2] <= INT32_MAX && q.shape[3] <= INT32_MAX);
+    dt_packed_config c = {0};
+    c.dtype = q.dtype;
+    c.B = (int32_t)B; c.Lq = (int32_t)Lq; c.Lk = (int32_t)Lk; c.H = (int32_t)H; c.H_kv = (int32_t)k.shape[2]; c.D = (int32_t)q.shape[3];
+    NEED((a[7] == NULL) == (a[8] == NULL));
+    if (a[7]) {
+        if (look(a[7], &qst) < 0 || look(a[8], &kst) < 0) return NULL;
+        const int64_t n = qst.nd > 0 ? qst.shape[qst.nd - 1] : 0;
+        NEED(n >= 1 && n <= INT32_MAX && (is_shape(&qst, 2, B, n, 0, 0) || (B == 1 && is_shape(&qst, 1, n, 0, 0, 0))) && same_shape(&qst, &kst));
+        NEED(qst.dtype == T_I32 && kst.dtype == T_I32 && contiguous(&qst) && contiguous(&kst) && qst.device == q.device && kst.device == q.device);
+        c.docs = (int32_t)(n - 1);
+        NEED(c.docs > 0 && a[9] == NULL && a[10] == NULL);   /* documents have their lengths from the borders */
+    }
+    if (a[9]) {
+        if (look(a[9], &ql) < 0) return NULL;
+        NEED(ql.dtype == T_I32 && is_shape(&ql, 1, B, 0, 0, 0) && contiguous(&ql) && ql.device == q.device);
+    }
+    if (a[10]) {
+        if (look(a[10], &kl) < 0) return NULL;
+        NEED(kl.dtype == T_I32 && is_shape(&kl, 1, B, 0, 0, 0) && contiguous(&kl) && kl.device == q.device);
+    }
+    if (a[11]) {
+        if (look(a[11], &pre) < 0) return NULL;
+        const int64_t n = c.docs > 0 ? c.docs : 1;
+        NEED(is_shape(&pre, 2, B, n, 0, 0) || (n == 1 && is_shape(&pre, 1, B, 0, 0, 0)) || (B == 1 && is_shape(&pre, 1, n, 0, 0, 0)));
+        NEED(pre.dtype == T_I32 && contiguous(&pre) && pre.device == q.device);
+    }
+    if (a[12]) {
+        if (look(a[12], &tab) < 0) return NULL;
+        NEED(tab.dtype == T_FP32 && tab.nd == 2 && tab.shape[0] == H && tab.shape[1] % 2 == 1 && tab.shape[1] <= INT32_MAX && contiguous(&tab) && tab.device == q.device);
+        c.bias_far = (int32_t)(tab.shape[1] / 2);
+    }
+    if (a[13]) {
+        if (look(a[13], &slo) < 0) return NULL;
+        NEED(slo.dtype == T_FP32 && is_shape(&slo, 1, H, 0, 0, 0) && contiguous(&slo) && slo.device == q.device);
+    }
+    if (a[14]) {
+        if (look(a[14], &lse) < 0) return NULL;
+        NEED(lse.dtype == T_FP32 && is_shape(&lse, 3, B, H, Lq, 0) && contiguous(&lse) && lse.device == q.device);
+    }
+    c.softmax_scale = (float)PyFloat_AsDouble(a[4]);
+    c.causal = a[5] ? PyObject_IsTrue(a[5]) : 0;
+    c.softcap = a[6] ? (float)PyFloat_AsDouble(a[6]) : 0.0f;
+    if (PyErr_Occurred()) return NULL;
+    ON_DEVICE("dt_packed_attn", q.device);
+    void *st;
+    if (stream_of(a[15], q.device, &st) < 0) return NULL;
+    return done(f_packed(&c, q.ptr, q.stride, k.ptr, k.stride, v.ptr, v.stride, a[7] ? qst.ptr : NULL, a[8] ? kst.ptr : NULL, a[9] ? ql.ptr : NULL,
+                         a[10] ? kl.ptr : NULL, a[11] ? pre.ptr : NULL, a[12] ? tab.ptr : NULL, a[13] ? slo.ptr : NULL, o.ptr, o.stride,
+                         a[14] ? lse.ptr : NULL, st));
+}
+
 /* _norm_rows(tensors): (n0, n1, [(stride0, stride1), ...]) as dt_add_rmsnorm sees them (for tests) */
 static PyObject *py_rows(PyObject *self, PyObject *list) {
     Tensor t[4];
@@ -388,13 +517,15 @@ static PyObject *py_rows(PyObject *self, PyObject *list) {
 }
 
 static PyObject *py_bind(PyObject *self, PyObject *args) {
-    unsigned long long rope, norm, cross;
+    unsigned long long rope, norm, cross, adapter, packed;
     PyObject *types, *calls[4];
-    if (!PyArg_ParseTuple(args, "(KKK)O!(OOOO)", &rope, &norm, &cross, &PyTuple_Type, &types, &calls[0], &calls[1], &calls[2], &calls[3])) return NULL;
+    if (!PyArg_ParseTuple(args, "(KKKKK)O!(OOOO)", &rope, &norm, &cross, &adapter, &packed, &PyTuple_Type, &types, &calls[0], &calls[1], &calls[2], &calls[3])) return NULL;
     NEED(PyTuple_GET_SIZE(types) == T_COUNT);
     f_rope = (void *)(uintptr_t)rope;
     f_norm = (void *)(uintptr_t)norm;
     f_cross = (void *)(uintptr_t)cross;
+    f_adapter = (void *)(uintptr_t)adapter;
+    f_packed = (void *)(uintptr_t)packed;
     for (int i = 0; i < T_COUNT; ++i) Py_XSETREF(dtypes[i], Py_NewRef(PyTuple_GET_ITEM(types, i)));
     Py_XSETREF(raw_stream, Py_NewRef(calls[0]));
     Py_XSETREF(get_device, Py_NewRef(calls[1]));
@@ -418,6 +549,18 @@ static PyMethodDef methods[] = {
      "dt_cross_attn(q, k, v, out, softmax_scale, key_lens=None, key_mask=None, lse_out=None, stream=None)\n\n"
      "Attention of q [B, Lq, H, D] to an encoder's k, v [B, Lk, H_kv, D]; key_lens int32 [B], key_mask uint8 or bool [B, Lk]\n"
      "(expanded batches too), lse_out fp32 [B, H, Lq].  See ditango.h."},
+    {"dt_adapter_linear", (PyCFunction)(void (*)(void))py_adapter, METH_FASTCALL | METH_KEYWORDS,
+     "dt_adapter_linear(x, weight, y, a, b, starts, adapters_of, workspace, scales=None, bias=None, stream=None)\n\n"
+     "y [..., N] = x [..., K] weight [N, K]^T + bias, and for rows starts[s] <= m < starts[s + 1] scales[i] (x a[i]^T) b[i]^T besides,\n"
+     "i = adapters_of[s] (-1: none).  a is [adapters, rank, K], b [adapters, N, rank], starts int32 [segments + 1], adapters_of int32\n"
+     "[segments], workspace uint8 of dt_adapter_workspace_bytes(rows, rank), scales fp32 [adapters].  With a = None the projection\n"
+     "alone (b, starts, adapters_of and workspace None too).  See ditango.h."},
+    {"dt_packed_attn", (PyCFunction)(void (*)(void))py_packed, METH_FASTCALL | METH_KEYWORDS,
+     "dt_packed_attn(q, k, v, out, softmax_scale, causal=False, softcap=0.0, q_starts=None, k_starts=None, q_lens=None, key_lens=None,\n"
+     "               prefix_lens=None, bias_table=None, bias_slopes=None, lse_out=None, stream=None)\n\n"
+     "Attention of q [B, Lq, H, D] to k, v [B, Lk, H_kv, D] within documents: q_starts and k_starts int32 [B, docs + 1] ([docs + 1] for\n"
+     "one row), or one document per row of the batch with q_lens and key_lens int32 [B].  prefix_lens int32 [B, docs] ([B]),\n"
+     "bias_table fp32 [H, 2 far + 1], bias_slopes fp32 [H], lse_out fp32 [B, H, Lq].  See ditango.h."},
     {"_norm_rows", py_rows, METH_O, "rows of tensors as dt_add_rmsnorm sees them"},
     {"_bind", py_bind, METH_VARARGS, "addresses of the library's functions, torch's dtypes, callables"},
     {NULL, NULL, 0, NULL}};
