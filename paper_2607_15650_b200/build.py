@@ -21,8 +21,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libditango.so")
 SOURCES = ["api.cu", "attn_states.cu", "state_merge.cu", "plan.cu", "planner.cu", "ops_api.cu", "rope.cu", "add_rmsnorm.cu",
-           "cross_attn.cu", "cross_tiles.cu", "adapter_linear.cu", "adapter_tiles.cu", "packed_attn.cu"]
-HEADERS = ["dt_internal.h", "ops.h", "cross_attn.h", "adapter_linear.h", "tile_wait.cuh", "ptx_sm100.cuh", os.path.join("..", "..", "include", "ditango.h")]
+           "cross_attn.cu", "cross_tiles.cu", "adapter_linear.cu", "adapter_tiles.cu", "packed_attn.cu",
+           "packed_tiles.cu"]
+HEADERS = ["dt_internal.h", "ops.h", "cross_attn.h", "adapter_linear.h", "packed_attn.h", "tile_wait.cuh", "ptx_sm100.cuh", os.path.join("..", "..", "include", "ditango.h")]
 # Python entry points of the context-free operators, for this interpreter
 OPS_LIB = os.path.join(HERE, "_ditango_ops" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 OPS_SOURCE = "ops_py.c"

@@ -1,0 +1,83 @@
+// What the two kernels of dt_packed_attn share.
+#pragma once
+#include "cross_attn.h"
+
+namespace dt {
+
+enum : int { BIAS_NONE = 0, BIAS_TABLE = 1, BIAS_SLOPES = 2 };
+
+struct PackedParams {
+    const uint16_t *q, *k, *v;
+    uint16_t *out;
+    float *lse;                                       // [B][H][Lq] or null
+    const int32_t *q_starts, *k_starts;               // [B][docs + 1] or null: one document per row of the batch
+    const int32_t *q_lens, *key_lens, *prefix;        // [B], [B], [B][docs], or null
+    const float *table, *slopes;                      // [H][2 far + 1], [H]
+    long long qs[3], ks[3], vs[3], os[3];             // B, L, H strides in elements
+    int B, Lq, Lk, H, Hkv, rep, docs, causal, far;
+    float scale_log2;                                 // softmax scale x log2(e)
+    float cap_in, cap_log2;                           // scale / softcap, softcap x log2(e)
+    float ref_below;                                  // fp16: see reference_below
+    int32_t *status;
+};
+
+// A document: its queries and keys, the key at which query i stands (i + shift), the end of its prefix.
+struct Doc { int q0, q1, k0, k1, shift, prefix_end; };
+__device__ __forceinline__ int clamped(const int32_t *at, int most) { return min(max(__ldg(at), 0), most); }
+__device__ __forceinline__ Doc doc_of(const PackedParams &p, int b, int d) {
+    Doc r;
+    if (p.q_starts != nullptr) {
+        const long long at = (long long)b * (p.docs + 1) + d;
+        r.q0 = clamped(p.q_starts + at, p.Lq);
+        r.q1 = max(clamped(p.q_starts + at + 1, p.Lq), r.q0);
+        r.k0 = clamped(p.k_starts + at, p.Lk);
+        r.k1 = max(clamped(p.k_starts + at + 1, p.Lk), r.k0);
+    } else {
+        r.q0 = r.k0 = 0;
+        r.q1 = p.q_lens ? clamped(p.q_lens + b, p.Lq) : p.Lq;
+        r.k1 = p.key_lens ? clamped(p.key_lens + b, p.Lk) : p.Lk;
+    }
+    r.shift = r.k1 - r.q1;
+    r.prefix_end = r.k0;
+    if (p.causal && p.prefix != nullptr) r.prefix_end += clamped(p.prefix + (long long)b * p.docs + d, r.k1 - r.k0);
+    return r;
+}
+// The end of the keys of query i (its keys are the document's below it).
+__device__ __forceinline__ int keys_end(const PackedParams &p, const Doc &d, int i) {
+    return p.causal ? max(min(max(i + d.shift + 1, d.prefix_end), d.k1), d.k0) : d.k1;
+}
+
+// Blocks of `size` query rows, each of one document and counted from its first row.  Block j of document d is number
+// q0_d / size + d + j of its row of the batch: ceil(n / size) <= (q0 + n) / size - q0 / size + 1, so no two have the same number, and
+// Lq / size + docs numbers are enough.  No list is made; some numbers have no rows.
+__host__ __device__ inline int blocks_of(int Lq, int docs, int size, bool borders) { return borders ? Lq / size + docs : (Lq + size - 1) / size; }
+// The document and first row of block `u` of row b of the batch; false: no rows.
+__device__ __forceinline__ bool block_at(const PackedParams &p, int b, int u, int size, Doc &doc, int &row0) {
+    int d = 0;
+    if (p.q_starts != nullptr) {   // the last document whose number is not beyond u
+        const int32_t *at = p.q_starts + (long long)b * (p.docs + 1);
+        int hi = p.docs;
+        while (hi - d > 1) {
+            const int mid = (d + hi) >> 1;
+            if (clamped(at + mid, p.Lq) / size + mid <= u) d = mid;
+            else hi = mid;
+        }
+        u -= clamped(at + d, p.Lq) / size + d;
+    }
+    doc = doc_of(p, b, d);
+    if (u < 0 || u > (doc.q1 - doc.q0) / size) return false;
+    row0 = doc.q0 + u * size;
+    return row0 < doc.q1;
+}
+
+// softcap tanh(s / softcap) log2(e), given s / softcap: within 2^-22 of the cap.
+__device__ __forceinline__ float capped(float y, float cap_log2) {
+    return cap_log2 - cap_log2 * __fdividef(2.0f, 1.0f + ex2_approx(y * (2.0f * LOG2E)));
+}
+template <bool FP16>
+__device__ __forceinline__ float packed_reference(const PackedParams &p, float top) { return FP16 ? top - p.ref_below : top; }
+
+// Many query rows (Lk > 0): tensor-memory tiles.
+cudaError_t launch_packed_tiles(const PackedParams &p, int D, bool fp16, const OpsDevice &dev, cudaStream_t st);
+
+}  // namespace dt
