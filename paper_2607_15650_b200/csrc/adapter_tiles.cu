@@ -20,15 +20,16 @@ constexpr int TM = 128, BK = 64;              // rows of a tile; k values of a s
 constexpr int A_BYTES = TM * 128;
 
 // ------------------------------------------------------------------------------------------------ t = s A x
-constexpr int SHRINK_STAGES = 6, SHRINK_THREADS = 192;
-struct ShrinkShape {     // of one launch: A's rows, padded to 16, as the MMA's N
+// Bound by reading x: two CTAs fit an SM, so that one loads while the other begins or ends.
+constexpr int SHRINK_THREADS = 192, SHRINK_MOST = 112 * 1024, SHRINK_SLACK = 1024 + 256;
+struct ShrinkShape {
     int steps;           // k stages in all
     int splits;
+    int stages, smem;    // of the ring
 };
-constexpr int SHRINK_SMEM = 1024 + SHRINK_STAGES * (A_BYTES + 128 * 128) + 2 * SHRINK_STAGES * 8 + 16;
 
 template <bool FP16>
-__global__ void __launch_bounds__(SHRINK_THREADS, 1)
+__global__ void __launch_bounds__(SHRINK_THREADS, 2)
 shrink_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_a, const AdapterParams p, const ShrinkShape sh) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint32_t tmem_slot;
@@ -49,13 +50,13 @@ shrink_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     if (piece.adapter < 0) return;
 
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t b_smem = base + SHRINK_STAGES * A_BYTES, bars = b_smem + SHRINK_STAGES * 128 * 128;
-    const uint32_t full = bars, empty = bars + 8 * SHRINK_STAGES, done = empty + 8 * SHRINK_STAGES;
+    const uint32_t b_bytes = p.rank16 * 128, b_smem = base + sh.stages * A_BYTES, bars = b_smem + sh.stages * b_bytes;
+    const uint32_t full = bars, empty = bars + 8 * sh.stages, done = empty + 8 * sh.stages;
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     volatile int *abort_ptr = &abort_flag;
     if (threadIdx.x == 0) {
         abort_flag = 0;
-        for (int i = 0; i < SHRINK_STAGES; ++i) {
+        for (int i = 0; i < sh.stages; ++i) {
             mbar_init(full + 8 * i, 1);
             mbar_init(empty + 8 * i, 1);
         }
@@ -72,35 +73,36 @@ shrink_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     const uint32_t tmem = tmem_slot;
     const int k0 = sh.steps * part / sh.splits, k1 = sh.steps * (part + 1) / sh.splits;
     if (warp == 0) {
-        if (lane == 0) {
-            uint32_t st = 0, ph = 0;
-            const uint32_t bytes = A_BYTES + p.rank16 * 128;
-            for (int k = k0; k < k1; ++k) {
-                if (!wait_or_abort(empty + 8 * st, ph ^ 1u, abort_ptr)) { give_up(abort_ptr, p.status); break; }
-                mbar_arrive_expect_tx(full + 8 * st, bytes);
+        uint32_t st = 0, ph = 0;
+        for (int k = k0; k < k1; ++k) {
+            if (!wait_all_lanes(empty + 8 * st, ph ^ 1u, abort_ptr)) { give_up(abort_ptr, p.status); break; }
+            if (elect_lane()) {
+                mbar_arrive_expect_tx(full + 8 * st, A_BYTES + b_bytes);
                 tma_load_2d(base + st * A_BYTES, &map_x, full + 8 * st, k * BK, row0);
-                tma_load_3d(b_smem + st * 128 * 128, &map_a, full + 8 * st, k * BK, 0, piece.adapter);
-                if (++st == SHRINK_STAGES) { st = 0; ph ^= 1u; }
+                tma_load_3d(b_smem + st * b_bytes, &map_a, full + 8 * st, k * BK, 0, piece.adapter);
             }
+            __syncwarp();
+            if (++st == sh.stages) { st = 0; ph ^= 1u; }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t idesc = make_idesc_bf16_f32(TM, p.rank16, false, FP16);
-            uint32_t st = 0, ph = 0;
-            bool ok = true;
-            for (int k = k0; k < k1 && ok; ++k) {
-                ok = wait_or_abort(full + 8 * st, ph, abort_ptr);
-                if (!ok) break;
-                tc_fence_after();
-                const uint64_t ad = make_smem_desc_sw128(base + st * A_BYTES, 16, 1024), bd = make_smem_desc_sw128(b_smem + st * 128 * 128, 16, 1024);
+        const uint32_t idesc = make_idesc_bf16_f32(TM, p.rank16, false, FP16);
+        uint32_t st = 0, ph = 0;
+        bool ok = true;
+        for (int k = k0; k < k1 && ok; ++k) {
+            ok = wait_all_lanes(full + 8 * st, ph, abort_ptr);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t ad = make_smem_desc_sw128(base + st * A_BYTES, 16, 1024), bd = make_smem_desc_sw128(b_smem + st * b_bytes, 16, 1024);
+            if (elect_lane()) {
 #pragma unroll
                 for (int kk = 0; kk < BK / 16; ++kk) mma_ss(tmem, ad + 2 * kk, bd + 2 * kk, idesc, k > k0 || kk > 0 ? 1u : 0u);
                 tc_commit(empty + 8 * st);
-                if (++st == SHRINK_STAGES) { st = 0; ph ^= 1u; }
+                if (k + 1 == k1) tc_commit(done);
             }
-            if (ok) tc_commit(done);
-            else give_up(abort_ptr, p.status);
+            __syncwarp();
+            if (++st == sh.stages) { st = 0; ph ^= 1u; }
         }
+        if (!ok) give_up(abort_ptr, p.status);
     }
     __syncwarp();
     const float scale = p.scales ? __ldg(p.scales + piece.adapter) : 1.0f;
@@ -110,7 +112,7 @@ shrink_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     if (warp >= 2) {
         const int r = (warp % 4) * 32 + lane, row = row0 + r;
         const uint32_t at = tmem + (((uint32_t)((warp % 4) * 32)) << 16);
-        const bool ok = __all_sync(0xFFFFFFFFu, wait_or_abort(done, 0, abort_ptr)) != 0;
+        const bool ok = wait_or_abort_warp(done, 0, abort_ptr);
         if (!ok) give_up(abort_ptr, p.status);
         tc_fence_after();
         if (ok) {
@@ -172,20 +174,25 @@ shrink_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
 }
 
 // ------------------------------------------------------------------------------------------------ y = W x + bias + B t
-constexpr int LINEAR_THREADS = 192;
+constexpr int LINEAR_THREADS = 192, PM = 2 * TM;              // rows of a pair's tile
+constexpr int ATOMS = 2;                                      // of 64 k values in a stage
 
 template <int BN>
 struct LinearCfg {
-    static constexpr int STAGE = A_BYTES + BN * 128;
-    static constexpr int STAGES = BN == 256 ? 4 : BN == 128 ? 6 : 8;
+    static constexpr int B_BYTES = BN / 2 * 128;              // each CTA of the pair loads half of the columns
+    static constexpr int ATOM = A_BYTES + B_BYTES, STAGE = ATOMS * ATOM;
+    static constexpr int STAGES = 196608 / STAGE;
     static constexpr int OUT_BYTES = 4 * 32 * 128;            // a warp's staging: 32 rows x 128 bytes
     static constexpr int SMEM = 1024 + STAGES * STAGE + OUT_BYTES + (2 * STAGES + 4) * 8;
-    static_assert(SMEM + 64 <= 227 * 1024, "beyond the shared memory of a CTA");
+    static constexpr int PITCH = BN + 4;                      // SPLIT: floats of a row of partial sums, where the stages were
+    static_assert(SMEM + 64 <= 227 * 1024 && TM * PITCH * 4 <= STAGES * STAGE, "beyond the shared memory of a CTA");
+    static constexpr int COLS = 256;                          // TMEM columns from one accumulator to the next
 };
 
 struct LinearShape {
-    int mt, nt, tiles;        // tiles of 128 rows, of BN columns, in all
+    int mt, nt, tiles;        // tiles of 256 rows, of BN columns, in all
     int group;                // tiles of rows that are walked together, column by column of tiles: their x and W stay in L2
+    int splits;               // SPLIT: pairs of a cluster that share a tile's K
 };
 __device__ __forceinline__ void tile_at(const LinearShape &sh, int w, int &mi, int &ni) {
     const int per = sh.group * sh.nt, g = w / per, first = g * sh.group, high = min(sh.group, sh.mt - first), i = w - g * per;
@@ -193,7 +200,26 @@ __device__ __forceinline__ void tile_at(const LinearShape &sh, int w, int &mi, i
     mi = first + (i - ni * high);
 }
 
-template <int BN, bool FP16>
+// f[0..COUNT) += bias[col..col + COUNT)
+template <bool FP16, int COUNT>
+__device__ __forceinline__ void add_bias(const AdapterParams &p, int col, float (&f)[COUNT]) {
+    if (p.bias_fp32) {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) f[i] += __ldg(static_cast<const float *>(p.bias) + col + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            const uint32_t h = __ldg(static_cast<const uint16_t *>(p.bias) + col + i);
+            float b;
+            if constexpr (FP16) asm("{\n\t.reg .b16 h;\n\tcvt.u16.u32 h, %1;\n\tcvt.f32.f16 %0, h;\n\t}" : "=f"(b) : "r"(h));
+            else b = __uint_as_float(h << 16);
+            f[i] += b;
+        }
+    }
+}
+
+// SPLIT: a cluster of 2 to 4 pairs for one tile, each pair with a part of K; else pairs walk the tiles.
+template <int BN, bool FP16, bool SPLIT>
 __global__ void __launch_bounds__(LINEAR_THREADS, 1)
 linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_t,
               const __grid_constant__ CUtensorMap map_b, const AdapterParams p, const LinearShape sh) {
@@ -205,6 +231,9 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     const uint32_t out_smem = base + C::STAGES * C::STAGE, bars = out_smem + C::OUT_BYTES;
     const uint32_t full = bars, empty = full + 8 * C::STAGES, acc_full = empty + 8 * C::STAGES, acc_empty = acc_full + 16;
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const uint32_t rank = rank_in_cluster(), half = rank & 1u, leader = rank & ~1u;      // of the pair: this CTA's rows
+    const int part = SPLIT ? (int)(rank >> 1) : 0;
+    const int pair = SPLIT ? (int)blockIdx.x / (2 * sh.splits) : (int)blockIdx.x / 2, pairs = SPLIT ? sh.tiles : (int)gridDim.x / 2;
     volatile int *abort_ptr = &abort_flag;
     if (threadIdx.x == 0) {
         abort_flag = 0;
@@ -214,106 +243,129 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(acc_full + 8 * i, 1);
-            mbar_init(acc_empty + 8 * i, 128);
+            mbar_init(acc_empty + 8 * i, 8);   // a lane of each warp of both epilogues
         }
         fence_mbar_init();
     }
-    if (warp == 1) {
-        tmem_alloc(smem_u32(&tmem_slot), 2 * BN);
-        tmem_relinquish();
-    }
+    __syncwarp();
+    sync_cluster();
+    if (warp == 1) tmem_alloc_pair(smem_u32(&tmem_slot), 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
-    const int steps = (p.K + BK - 1) / BK;
+    const int all = (p.K + BK - 1) / BK, k_from = SPLIT ? all * part / sh.splits * BK : 0, k_to = SPLIT ? min(all * (part + 1) / sh.splits * BK, p.K) : p.K;
 
+    // (The loading and the issuing warp run their loops as whole warps and one elected lane issues: what the instructions take, descriptors
+    // and addresses, then stays in uniform registers.  With the loops inside `if (lane == 0)` an MMA took 62 cycles to issue.)
     if (warp == 0) {
-        if (lane == 0) {
-            prefetch_tensormap(&map_x);
-            prefetch_tensormap(&map_w);
-            uint32_t st = 0, ph = 0;
-            bool ok = true, t_ready = false;
-            auto stage = [&](const CUtensorMap *ma, const CUtensorMap *mb, int k, int row, int col, int adapter) {
-                ok = ok && wait_or_abort(empty + 8 * st, ph ^ 1u, abort_ptr);
-                if (!ok) return;
-                const uint32_t at = base + st * C::STAGE, bar = full + 8 * st;
-                mbar_arrive_expect_tx(bar, C::STAGE);
-                tma_load_2d(at, ma, bar, k, row);
-                if (adapter < 0) tma_load_2d(at + A_BYTES, mb, bar, k, col);
-                else tma_load_3d(at + A_BYTES, mb, bar, k, col, adapter);
-                if (++st == C::STAGES) { st = 0; ph ^= 1u; }
-            };
-#pragma unroll 1
-            for (int w = blockIdx.x; w < sh.tiles && ok; w += gridDim.x) {
-                int mi, ni;
-                tile_at(sh, w, mi, ni);
-                const int row0 = mi * TM, row1 = min(row0 + TM, p.M);
-#pragma unroll 1
-                for (int k = 0; k < steps && ok; ++k) stage(&map_x, &map_w, k * BK, row0, ni * BN, -1);
-#pragma unroll 1
-                for (int s = p.segments ? first_segment(p, row0) : 0; s < p.segments && border_of(p, s) < row1 && ok; ++s) {
-                    const Piece piece = piece_of(p, s, row0, row1);
-                    if (piece.adapter < 0) continue;
-                    if (!t_ready) {
-                        wait_for_previous();
-                        asm volatile("fence.proxy.async.global;" ::: "memory");
-                        t_ready = true;
-                    }
-#pragma unroll 1
-                    for (int k = 0; k < p.rank16 && ok; k += BK) stage(&map_t, &map_b, k, row0, ni * BN, piece.adapter);
+        uint32_t st = 0, ph = 0;
+        bool ok = true, t_ready = false;
+        const uint32_t full_at = at_rank(full, leader);
+        auto stage = [&](const CUtensorMap *ma, const CUtensorMap *mb, int k, int end, int row, int col, int adapter) {   // k values [k, end) of at most ATOMS atoms
+            ok = ok && wait_all_lanes(empty + 8 * st, ph ^ 1u, abort_ptr);
+            if (!ok) return;
+            const uint32_t bar = full_at + 8 * st, at = base + st * C::STAGE;
+            if (elect_lane()) {
+                if (half == 0) mbar_arrive_expect_tx(full + 8 * st, 2 * C::ATOM * ((end - k + BK - 1) / BK));   // both CTAs' bytes
+#pragma unroll
+                for (int i = 0; i < ATOMS; ++i) {
+                    if (k + i * BK >= end) break;
+                    tma_pair_2d(at + i * C::ATOM, ma, bar, k + i * BK, row);
+                    if (adapter < 0) tma_pair_2d(at + i * C::ATOM + A_BYTES, mb, bar, k + i * BK, col);
+                    else tma_pair_3d(at + i * C::ATOM + A_BYTES, mb, bar, k + i * BK, col, adapter);
                 }
             }
-            if (!ok) give_up(abort_ptr, p.status);
-            if (p.segments && !t_ready) wait_for_previous();   // (no launch behind this one starts before the shrink kernel's end)
+            __syncwarp();
+            if (++st == C::STAGES) { st = 0; ph ^= 1u; }
+        };
+#pragma unroll 1
+        for (int w = pair; w < sh.tiles && ok; w += pairs) {
+            int mi, ni;
+            tile_at(sh, w, mi, ni);
+            const int row0 = mi * PM, row1 = min(row0 + PM, p.M), row = row0 + (int)half * TM, col = ni * BN + (int)half * (BN / 2);
+#pragma unroll 1
+            for (int k = k_from; k < k_to && ok; k += ATOMS * BK) stage(&map_x, &map_w, k, min(k + ATOMS * BK, k_to), row, col, -1);
+            if (part != 0) continue;
+#pragma unroll 1
+            for (int s = p.segments ? first_segment(p, row0) : 0; s < p.segments && border_of(p, s) < row1 && ok; ++s) {
+                const Piece piece = piece_of(p, s, row0, row1);
+                if (piece.adapter < 0) continue;
+                if (!t_ready) {
+                    wait_for_previous();
+                    asm volatile("fence.proxy.async.global;" ::: "memory");
+                    t_ready = true;
+                }
+#pragma unroll 1
+                for (int k = 0; k < p.rank16 && ok; k += ATOMS * BK) stage(&map_t, &map_b, k, min(k + ATOMS * BK, p.rank16), row, col, piece.adapter);
+            }
         }
+        if (!ok) give_up(abort_ptr, p.status);
+        if (p.segments && !t_ready) wait_for_previous();   // (no launch behind this one starts before the shrink kernel's end)
     } else if (warp == 1) {
-        if (lane == 0) {
-            constexpr uint32_t IDESC = make_idesc_bf16_f32(TM, BN, false, FP16);
+        if (half == 0) {
+            constexpr uint32_t IDESC = make_idesc_bf16_f32(PM, BN, false, FP16);
+            const uint16_t both = (uint16_t)(3u << leader);
             uint32_t st = 0, ph = 0, n = 0;
             bool ok = true;
 #pragma unroll 1
-            for (int w = blockIdx.x; w < sh.tiles && ok; w += gridDim.x, ++n) {
+            for (int w = pair; w < sh.tiles && ok; w += pairs, ++n) {
                 int mi, ni;
                 tile_at(sh, w, mi, ni);
-                const uint32_t half = n & 1u, d = tmem + half * BN;
-                ok = wait_or_abort(acc_empty + 8 * half, ((n >> 1) & 1u) ^ 1u, abort_ptr);
+                const uint32_t acc = n & 1u, d = tmem + acc * C::COLS;
+                ok = wait_all_lanes(acc_empty + 8 * acc, ((n >> 1) & 1u) ^ 1u, abort_ptr);
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll 1
-                for (int k = 0; k < steps; ++k) {
-                    ok = wait_or_abort(full + 8 * st, ph, abort_ptr);
+                for (int k = k_from; k < k_to; k += ATOMS * BK) {
+                    ok = wait_all_lanes(full + 8 * st, ph, abort_ptr);
                     if (!ok) break;
                     tc_fence_after();
                     const uint64_t ad = make_smem_desc_sw128(base + st * C::STAGE, 16, 1024), bd = make_smem_desc_sw128(base + st * C::STAGE + A_BYTES, 16, 1024);
+                    if (elect_lane()) {
 #pragma unroll
-                    for (int kk = 0; kk < BK / 16; ++kk) mma_ss(d, ad + 2 * kk, bd + 2 * kk, IDESC, k > 0 || kk > 0 ? 1u : 0u);
-                    tc_commit(empty + 8 * st);
+                        for (int i = 0; i < ATOMS; ++i) {
+                            if (k + i * BK >= k_to) break;
+#pragma unroll
+                            for (int kk = 0; kk < BK / 16; ++kk)
+                                mma_pair(d, ad + i * (C::ATOM >> 4) + 2 * kk, bd + i * (C::ATOM >> 4) + 2 * kk, IDESC, k > k_from || i > 0 || kk > 0 ? 1u : 0u);
+                        }
+                        commit_pair(empty + 8 * st, both);
+                    }
+                    __syncwarp();
                     if (++st == C::STAGES) { st = 0; ph ^= 1u; }
                 }
-                const int row0 = mi * TM, row1 = min(row0 + TM, p.M);
+                const int row0 = mi * PM, row1 = min(row0 + PM, p.M);
 #pragma unroll 1
-                for (int s = p.segments ? first_segment(p, row0) : 0; s < p.segments && border_of(p, s) < row1 && ok; ++s) {
+                for (int s = p.segments && part == 0 ? first_segment(p, row0) : p.segments; s < p.segments && border_of(p, s) < row1 && ok; ++s) {
                     const Piece piece = piece_of(p, s, row0, row1);
                     if (piece.adapter < 0) continue;
-                    uint32_t off[4];
+                    uint32_t off[8];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < 8; ++i) {
                         const int from = min(max(piece.from - row0 - 32 * i, 0), 32), to = min(max(piece.to - row0 - 32 * i, 0), 32);
                         off[i] = ~((to == 32 ? 0xFFFFFFFFu : (1u << to) - 1u) & (from == 32 ? 0u : 0xFFFFFFFFu << from));
                     }
 #pragma unroll 1
-                    for (int k = 0; k < p.rank16; k += BK) {
-                        ok = wait_or_abort(full + 8 * st, ph, abort_ptr);
+                    for (int k = 0; k < p.rank16; k += ATOMS * BK) {
+                        ok = wait_all_lanes(full + 8 * st, ph, abort_ptr);
                         if (!ok) break;
                         tc_fence_after();
                         const uint64_t ad = make_smem_desc_sw128(base + st * C::STAGE, 16, 1024), bd = make_smem_desc_sw128(base + st * C::STAGE + A_BYTES, 16, 1024);
-                        for (int kk = 0; kk < min(BK, p.rank16 - k) / 16; ++kk) mma_ss_rows(d, ad + 2 * kk, bd + 2 * kk, IDESC, off);
-                        tc_commit(empty + 8 * st);
+                        if (elect_lane()) {
+#pragma unroll 1
+                            for (int kk = 0; kk < min(ATOMS * BK, p.rank16 - k) / 16; ++kk) {
+                                const uint32_t at = (kk >> 2) * (C::ATOM >> 4) + (kk & 3) * 2;
+                                mma_pair_rows(d, ad + at, bd + at, IDESC, off);
+                            }
+                            commit_pair(empty + 8 * st, both);
+                        }
+                        __syncwarp();
                         if (++st == C::STAGES) { st = 0; ph ^= 1u; }
                     }
                 }
-                if (ok) tc_commit(acc_full + 8 * half);
+                if (ok && elect_lane()) commit_pair(acc_full + 8 * acc, both);
+                __syncwarp();
             }
             if (!ok) give_up(abort_ptr, p.status);
         }
@@ -325,53 +377,54 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         uint32_t n = 0;
         bool ok = true;
 #pragma unroll 1
-        for (int w = blockIdx.x; w < sh.tiles; w += gridDim.x, ++n) {
+        for (int w = pair; w < sh.tiles; w += pairs, ++n) {
             int mi, ni;
             tile_at(sh, w, mi, ni);
-            const uint32_t half = n & 1u, acc = tmem + lane_addr + half * BN;
-            ok = __all_sync(0xFFFFFFFFu, wait_or_abort(acc_full + 8 * half, (n >> 1) & 1u, abort_ptr)) != 0;
+            const uint32_t which = n & 1u, acc = tmem + lane_addr + which * C::COLS;
+            ok = wait_or_abort_warp(acc_full + 8 * which, (n >> 1) & 1u, abort_ptr);
             if (!ok) break;
             tc_fence_after();
-            const int warp_row = mi * TM + quarter * 32, rows_left = p.M - warp_row;
+            if constexpr (SPLIT) {   // partial sums to where the stages were (every MMA is done), joined across the cluster below
+#pragma unroll 1
+                for (int c0 = 0; c0 < BN; c0 += 32) {
+                    uint32_t v[32];
+                    tmem_ld_x32(acc + c0, v);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (uint32_t)((quarter * 32 + lane) * C::PITCH + c0 + 4 * c) * 4u), "r"(v[4 * c]),
+                                     "r"(v[4 * c + 1]), "r"(v[4 * c + 2]), "r"(v[4 * c + 3]) : "memory");
+                }
+                break;
+            }
+            const int warp_row = mi * PM + (int)half * TM + quarter * 32, rows_left = p.M - warp_row;
             uint16_t *out = p.y + (long long)warp_row * p.ys;
 #pragma unroll 1
             for (int c0 = 0; c0 < BN; c0 += 64) {
+                constexpr bool WHOLE = BN % 64 == 0;
                 const int col = ni * BN + c0;
                 uint32_t v[2][32];
                 tmem_ld_x32(acc + c0, v[0]);
-                tmem_ld_x32(acc + c0 + 32, v[1]);
+                if (WHOLE || c0 + 64 <= BN) tmem_ld_x32(acc + c0 + 32, v[1]);
                 tmem_wait_ld();
                 if (c0 + 64 >= BN) {   // read: the tile after next may overwrite it
                     tc_fence_before();
-                    mbar_arrive(acc_empty + 8 * half);
+                    __syncwarp();
+                    if (lane == 0) arrive_at(at_rank(acc_empty + 8 * which, leader));
                 }
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
                     float f[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[c >> 2][(c & 3) * 8 + i]);
-                    if (p.bias != nullptr && col + 8 * c < p.N) {
-                        if (p.bias_fp32) {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) f[i] += __ldg(static_cast<const float *>(p.bias) + col + 8 * c + i);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const uint32_t h = __ldg(static_cast<const uint16_t *>(p.bias) + col + 8 * c + i);
-                                float b;
-                                if constexpr (FP16) asm("{\n\t.reg .b16 h;\n\tcvt.u16.u32 h, %1;\n\tcvt.f32.f16 %0, h;\n\t}" : "=f"(b) : "r"(h));
-                                else b = __uint_as_float(h << 16);
-                                f[i] += b;
-                            }
-                        }
-                    }
+                    if (p.bias != nullptr && col + 8 * c < p.N) add_bias<FP16, 8>(p, col + 8 * c, f);
                     uint32_t o[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[i] = pack_half2<FP16>(f[2 * i], f[2 * i + 1]);
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(my_row + (uint32_t)((c ^ (lane & 7)) << 4)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
                 }
                 __syncwarp();
-                const bool in = col + piece * 8 < p.N;
+                const bool in = col + piece * 8 < p.N && (WHOLE || c0 + piece * 8 < BN);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int r = i * 4 + (lane >> 3);
@@ -389,7 +442,33 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     __syncthreads();
     tc_fence_after();
     settle_if(*abort_ptr != 0);
-    if (warp == 1) tmem_dealloc(tmem, 2 * BN);
+    sync_cluster();   // no CTA leaves, or reuses its stages, while another's MMAs, commits or arrivals reach it
+    if constexpr (SPLIT) {
+        int mi, ni;
+        tile_at(sh, pair, mi, ni);
+        // rows part, part + splits, ... of this CTA's half: 4 columns at a time, the parts in order
+        constexpr int PIECES = BN / 4;
+        const int row0 = mi * PM + (int)half * TM, rows = min(TM, p.M - row0), count = (rows - part + sh.splits - 1) / sh.splits * PIECES;
+#pragma unroll 4
+        for (int i = threadIdx.x; i < count; i += LINEAR_THREADS) {
+            const int r = i / PIECES * sh.splits + part, c = i % PIECES * 4, col = ni * BN + c;
+            const uint32_t at = base + (uint32_t)(r * C::PITCH + c) * 4u;
+            float4 x[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                x[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (q < sh.splits)
+                    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x[q].x), "=f"(x[q].y), "=f"(x[q].z), "=f"(x[q].w) : "r"(at_rank(at, 2 * q + half)));
+            }
+            float f[4] = {((x[0].x + x[1].x) + x[2].x) + x[3].x, ((x[0].y + x[1].y) + x[2].y) + x[3].y,
+                          ((x[0].z + x[1].z) + x[2].z) + x[3].z, ((x[0].w + x[1].w) + x[2].w) + x[3].w};
+            if (col >= p.N) continue;
+            if (p.bias != nullptr) add_bias<FP16, 4>(p, col, f);
+            *reinterpret_cast<uint2 *>(p.y + (row0 + r) * p.ys + col) = make_uint2(pack_half2<FP16>(f[0], f[1]), pack_half2<FP16>(f[2], f[3]));
+        }
+        sync_cluster();
+    }
+    if (warp == 1) tmem_dealloc_pair(tmem, 512);
 }
 
 bool map_rows(void *fn, CUtensorMap *tm, const void *base, bool fp16, long long rows, int width, long long stride, int box_rows) {
@@ -407,17 +486,20 @@ bool map_adapters(void *fn, CUtensorMap *tm, const void *base, bool fp16, int ad
 template <bool FP16>
 cudaError_t launch_shrink(const CUtensorMap &mx, const CUtensorMap &ma, const AdapterParams &p, const OpsDevice &dev, cudaStream_t st) {
     static OncePerDevice once;
-    const cudaError_t e = once(dev, [] { return cudaFuncSetAttribute(shrink_kernel<FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SHRINK_SMEM); });
+    const cudaError_t e = once(dev, [] { return cudaFuncSetAttribute(shrink_kernel<FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SHRINK_MOST); });
     if (e != cudaSuccess) return e;
     const int pairs = (p.M + TM - 1) / TM + p.segments;
     ShrinkShape sh;
     sh.steps = (p.K + BK - 1) / BK;
     sh.splits = 1;
-    while (sh.splits < 8 && (long long)pairs * sh.splits * 2 <= dev.sms && sh.steps >= sh.splits * 4) sh.splits *= 2;
+    while (sh.splits < 8 && (long long)pairs * sh.splits * 2 <= 2 * dev.sms && sh.steps >= sh.splits * 4) sh.splits *= 2;
+    sh.stages = (SHRINK_MOST - SHRINK_SLACK) / (A_BYTES + p.rank16 * 128);
+    const int sums = sh.splits > 1 ? TM * (p.rank16 + 4) * 4 : 0;   // where the stages were
+    sh.smem = SHRINK_SLACK + (sh.stages * (A_BYTES + p.rank16 * 128) > sums ? sh.stages * (A_BYTES + p.rank16 * 128) : sums);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(pairs * sh.splits));
     cfg.blockDim = dim3(SHRINK_THREADS);
-    cfg.dynamicSmemBytes = SHRINK_SMEM;
+    cfg.dynamicSmemBytes = sh.smem;
     cfg.stream = st;
     cudaLaunchAttribute attr = {};
     attr.id = cudaLaunchAttributeClusterDimension;
@@ -427,35 +509,63 @@ cudaError_t launch_shrink(const CUtensorMap &mx, const CUtensorMap &ma, const Ad
     return cudaLaunchKernelEx(&cfg, shrink_kernel<FP16>, mx, ma, p, sh);
 }
 
-template <int BN, bool FP16>
-cudaError_t launch_linear(const CUtensorMap &mx, const AdapterParams &p, const OpsDevice &dev, cudaStream_t st) {
+template <int BN, bool FP16, bool SPLIT>
+cudaError_t launch_linear(const CUtensorMap &mx, const AdapterParams &p, LinearShape sh, const OpsDevice &dev, cudaStream_t st) {
     using C = LinearCfg<BN>;
     static OncePerDevice once;
-    const cudaError_t e = once(dev, [] { return cudaFuncSetAttribute(linear_kernel<BN, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); });
+    const cudaError_t e = once(dev, [] { return cudaFuncSetAttribute(linear_kernel<BN, FP16, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); });
     if (e != cudaSuccess) return e;
     CUtensorMap mw, mt, mb;
-    if (!map_rows(dev.encode_tiled, &mw, p.w, FP16, p.N, p.K, p.ws, BN)) return cudaErrorInvalidValue;
+    if (!map_rows(dev.encode_tiled, &mw, p.w, FP16, p.N, p.K, p.ws, BN / 2)) return cudaErrorInvalidValue;
     mt = mb = mw;
     if (p.segments && (!map_rows(dev.encode_tiled, &mt, p.t, FP16, p.M, p.rank16, p.rank16, TM) ||
-                       !map_adapters(dev.encode_tiled, &mb, p.b, FP16, p.adapters, p.N, p.rank, BN)))
+                       !map_adapters(dev.encode_tiled, &mb, p.b, FP16, p.adapters, p.N, p.rank, BN / 2)))
         return cudaErrorInvalidValue;
-    LinearShape sh;
-    sh.mt = (p.M + TM - 1) / TM;
-    sh.nt = (p.N + BN - 1) / BN;
-    if ((long long)sh.mt * sh.nt > 0x3FFFFFFF) return cudaErrorInvalidValue;
-    sh.tiles = sh.mt * sh.nt;
-    sh.group = 16;
+    const int pairs = dev.sms / 2;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(sh.tiles < dev.sms ? sh.tiles : dev.sms));
+    cfg.gridDim = dim3((unsigned)(SPLIT ? 2 * sh.splits * sh.tiles : 2 * (sh.tiles < pairs ? sh.tiles : pairs)));
     cfg.blockDim = dim3(LINEAR_THREADS);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = st;
-    cudaLaunchAttribute attr = {};
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = p.segments ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, linear_kernel<BN, FP16>, mx, mw, mt, mb, p, sh);
+    cudaLaunchAttribute attr[2] = {};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)(SPLIT ? 2 * sh.splits : 2); attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.segments ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, linear_kernel<BN, FP16, SPLIT>, mx, mw, mt, mb, p, sh);
+}
+template <int BN, bool FP16>
+cudaError_t launch_linear(const CUtensorMap &mx, const AdapterParams &p, const LinearShape &sh, const OpsDevice &dev, cudaStream_t st) {
+    return sh.splits > 1 ? launch_linear<BN, FP16, true>(mx, p, sh, dev, st) : launch_linear<BN, FP16, false>(mx, p, sh, dev, st);
+}
+
+// The tile's width and the parts of K: pairs of SMs walk the tiles in rounds, so the time goes by rounds x (columns of a tile + what a
+// tile costs besides); with few tiles K is split while the clusters still find a place at once.
+inline LinearShape shape_of(const AdapterParams &p, int sms, int &bn) {
+    LinearShape best = {};
+    double least = 0;
+    for (int w : {256, 224, 192, 160, 128}) {
+        LinearShape sh = {};
+        sh.mt = (p.M + PM - 1) / PM;
+        sh.nt = (p.N + w - 1) / w;
+        const long long tiles = (long long)sh.mt * sh.nt, pairs = sms / 2;
+        if (tiles > 0x3FFFFFFF) continue;
+        sh.tiles = (int)tiles;
+        sh.group = 8;
+        sh.splits = 1;
+        // clusters of 2, 4, 6 and 8 CTAs that find a place at once with one CTA per SM
+        const long long places[5] = {0, pairs, sms * 15 / 64, sms / 7, sms / 10 + 1};
+        while (sh.splits < 4 && tiles <= places[sh.splits + 1] && p.K >= (sh.splits + 1) * 4 * BK) ++sh.splits;
+        const double rounds = sh.splits > 1 ? 1.0 / sh.splits : (double)((tiles + pairs - 1) / pairs), cost = rounds * (w + 96) + (sh.splits > 1 ? w / 4 : 0);
+        if (best.tiles == 0 || cost < least) {
+            best = sh;
+            least = cost;
+            bn = w;
+        }
+    }
+    return best;
 }
 
 template <bool FP16>
@@ -467,11 +577,16 @@ cudaError_t launch_tiles(const AdapterParams &p, const OpsDevice &dev, cudaStrea
         const cudaError_t e = launch_shrink<FP16>(mx, ma, p, dev, st);
         if (e != cudaSuccess) return e;
     }
-    // the widest tile that still gives every SM one
-    const long long mt = (p.M + TM - 1) / TM;
-    if (mt * ((p.N + 255) / 256) >= dev.sms) return launch_linear<256, FP16>(mx, p, dev, st);
-    if (mt * ((p.N + 127) / 128) >= dev.sms) return launch_linear<128, FP16>(mx, p, dev, st);
-    return launch_linear<64, FP16>(mx, p, dev, st);
+    int bn = 0;
+    const LinearShape sh = shape_of(p, dev.sms, bn);
+    if (sh.tiles == 0) return cudaErrorInvalidValue;
+    switch (bn) {
+        case 256: return launch_linear<256, FP16>(mx, p, sh, dev, st);
+        case 224: return launch_linear<224, FP16>(mx, p, sh, dev, st);
+        case 192: return launch_linear<192, FP16>(mx, p, sh, dev, st);
+        case 160: return launch_linear<160, FP16>(mx, p, sh, dev, st);
+        default: return launch_linear<128, FP16>(mx, p, sh, dev, st);
+    }
 }
 
 }  // namespace

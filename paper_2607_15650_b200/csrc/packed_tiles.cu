@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                    const __grid_constant__ CUtensorMap tmap_v, const TileParams p) {
     using C = Cfg<D>;
-    constexpr int MMA_UNROLL = 4, OUT_UNROLL = 1;
+    constexpr int OUT_UNROLL = 1;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_flag;
@@ -334,55 +334,58 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         reg_dealloc<REGS_OTHER>();
         if (warp == TMA_WARP) {
             // -------------------------------------------------------- TMA producer
-            if (lane == 0) {
-                prefetch_tensormap(&tmap_q);
-                prefetch_tensormap(&tmap_k);
-                prefetch_tensormap(&tmap_v);
-                uint32_t st = 0, ph = 0, q_ph = 0;
-                bool ok = true;
-                auto load_q = [&](const Cursor &it) {
+            // (This warp and the MMA warps run their loops as whole warps and one elected lane issues: what the instructions take then
+            // stays in uniform registers.)
+            uint32_t st = 0, ph = 0, q_ph = 0;
+            bool ok = true;
+            auto load_q = [&](const Cursor &it) {
 #pragma unroll 1
-                    for (int q = 0; q < NQ; ++q) {
-                        ok = ok && wait(bars.q_empty + 8 * q, q_ph ^ 1u);
-                        if (!ok) return;
+                for (int q = 0; q < NQ; ++q) {
+                    ok = ok && wait_all(bars.q_empty + 8 * q, q_ph ^ 1u);
+                    if (!ok) return;
+                    if (elect_lane()) {
                         mbar_arrive_expect_tx(bars.q_full + 8 * q, C::TILE_BYTES);
 #pragma unroll
                         for (int hf = 0; hf < C::NHALF; ++hf)
                             tma_load_4d(q_smem + q * C::TILE_BYTES + hf * C::HALF_BYTES, &tmap_q, bars.q_full + 8 * q, hf * 64,
                                         it.h * p.mq.mul_h, it.row0 + q * TILE, it.b * p.mq.mul_b);
                     }
-                    q_ph ^= 1u;
-                };
-                auto load_kv = [&](const Cursor &it, bool is_k) {
-                    ok = ok && wait(bars.kv_empty + 8 * st, ph ^ 1u);
-                    if (!ok) return;
-                    // V with keys that do not count for all rows lands on a barrier of its own; the mending warp passes it on
-                    const uint32_t bar = (!is_k && it.mended(p, it.key0()) ? bars.kv_raw : bars.kv_full) + 8 * st;
+                    __syncwarp();
+                }
+                q_ph ^= 1u;
+            };
+            auto load_kv = [&](const Cursor &it, bool is_k) {
+                ok = ok && wait_all(bars.kv_empty + 8 * st, ph ^ 1u);
+                if (!ok) return;
+                // V with keys that do not count for all rows lands on a barrier of its own; the mending warp passes it on
+                const uint32_t bar = (!is_k && it.mended(p, it.key0()) ? bars.kv_raw : bars.kv_full) + 8 * st;
+                const int hk = p.c.rep == 1 ? it.h : it.h / p.c.rep;
+                const int h = hk * (is_k ? p.mk.mul_h : p.mv.mul_h), b = it.b * (is_k ? p.mk.mul_b : p.mv.mul_b);
+                if (elect_lane()) {
                     mbar_arrive_expect_tx(bar, C::TILE_BYTES);
-                    const int hk = p.c.rep == 1 ? it.h : it.h / p.c.rep;
-                    const int h = hk * (is_k ? p.mk.mul_h : p.mv.mul_h), b = it.b * (is_k ? p.mk.mul_b : p.mv.mul_b);
 #pragma unroll
                     for (int hf = 0; hf < C::NHALF; ++hf)
                         tma_load_4d(kv_smem + st * C::TILE_BYTES + hf * C::HALF_BYTES, is_k ? &tmap_k : &tmap_v, bar, hf * 64, h, it.key0(), b);
-                    if (++st == C::STAGES) { st = 0; ph ^= 1u; }
-                };
-                Cursor nxt; nxt.first_item(p);
-                nxt.skip_empty(p);
-                Cursor cur = nxt;
-                bool have = false;   // a tile whose V is still to be loaded
-#pragma unroll 1
-                while (ok && (have || nxt.valid)) {
-#pragma unroll 1
-                    for (int v = 0; v < 2; ++v)   // K of the next tile, V of this one
-                        if (v ? have : nxt.valid) load_kv(v ? cur : nxt, v == 0);
-                    // (after this V: nothing that Q's place waits for is behind it)
-                    if (nxt.valid && nxt.t == 0) load_q(nxt);
-                    cur = nxt;
-                    have = nxt.valid;
-                    if (have) nxt.advance(p);
                 }
-                if (!ok) give_up(abort_ptr, p.c.status);
+                __syncwarp();
+                if (++st == C::STAGES) { st = 0; ph ^= 1u; }
+            };
+            Cursor nxt; nxt.first_item(p);
+            nxt.skip_empty(p);
+            Cursor cur = nxt;
+            bool have = false;   // a tile whose V is still to be loaded
+#pragma unroll 1
+            while (ok && (have || nxt.valid)) {
+#pragma unroll 1
+                for (int v = 0; v < 2; ++v)   // K of the next tile, V of this one
+                    if (v ? have : nxt.valid) load_kv(v ? cur : nxt, v == 0);
+                // (after this V: nothing that Q's place waits for is behind it)
+                if (nxt.valid && nxt.t == 0) load_q(nxt);
+                cur = nxt;
+                have = nxt.valid;
+                if (have) nxt.advance(p);
             }
+            if (!ok && lane == 0) give_up(abort_ptr, p.c.status);
         } else if (warp == MEND_WARP) {
             // -------------------------------------------------------- V's rows that do not count for all; bias tables
             uint32_t raw_ph = 0;   // parity of every stage's kv_raw (one bit each)
@@ -461,7 +464,6 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             if (!ok && lane == 0) give_up(abort_ptr, p.c.status);
         } else {
             // -------------------------------------------------------- MMA issuer of query tile mq
-            const bool leader = (lane == 0);
             const int mq = warp - MMA_WARP;
             const uint64_t qdesc = make_smem_desc_sw128(q_smem + mq * C::TILE_BYTES, 16, 1024);
             const uint64_t kdesc0 = make_smem_desc_sw128(kv_smem, 16, 1024);
@@ -470,10 +472,10 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             auto issue_qk = [&](uint32_t st) {
                 constexpr uint32_t IDESC_QK = make_idesc_bf16_f32(128, TILE, false, FP16);
                 const uint64_t b0 = kdesc0 + (uint64_t)((st * C::TILE_BYTES) >> 4);
-#pragma unroll MMA_UNROLL
+#pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) {
                     const uint32_t koff = ((kk / 4) * C::HALF_BYTES + (kk % 4) * 32) >> 4;
-                    if (leader) mma_ss(tmem_base + C::S_COL, qdesc + koff, b0 + koff, IDESC_QK, kk > 0 ? 1u : 0u);
+                    mma_ss(tmem_base + C::S_COL, qdesc + koff, b0 + koff, IDESC_QK, kk > 0 ? 1u : 0u);
                 }
             };
             // O (+)= P V
@@ -481,9 +483,9 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                 constexpr uint32_t IDESC_PV = make_idesc_bf16_f32(128, D, true, FP16);
                 const uint64_t b0 = vdesc0 + (uint64_t)((st * C::TILE_BYTES) >> 4);
                 const uint32_t d = tmem_base + C::O_COL + mq * D, a = tmem_base + C::P_COL + mq * C::P_STRIDE;
-#pragma unroll MMA_UNROLL
+#pragma unroll
                 for (int kk = 0; kk < TILE / 16; ++kk)
-                    if (leader) mma_ts(d, a + kk * 8, b0 + (uint64_t)((kk * 2048) >> 4), IDESC_PV, (accumulate || kk > 0) ? 1u : 0u);
+                    mma_ts(d, a + kk * 8, b0 + (uint64_t)((kk * 2048) >> 4), IDESC_PV, (accumulate || kk > 0) ? 1u : 0u);
             };
             // The one place for S is used by the tiles in turn, tile 0 first: a phase of s_free is one read of S.
             const uint32_t s_turn = mq ? 0u : 1u;
@@ -512,12 +514,13 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                         ok = __all_sync(0xFFFFFFFFu, r) != 0;
                         if (!ok) break;
                         tc_fence_after();
-                        issue_qk(st);
-                        if (leader) {
+                        if (elect_lane()) {
+                            issue_qk(st);
                             tc_commit(bars.s_full + 8 * mq);
                             tc_commit(bars.kv_empty + 8 * st);
                             if (within ? k + 2 == tiles : next_single) tc_commit(bars.q_empty + 8 * mq);   // its item's last Q K^T
                         }
+                        __syncwarp();
                     }
                     st = stv;
                     ph = phv;
@@ -533,12 +536,13 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                     }
                     if (!ok) break;
                     tc_fence_after();
-                    issue_pv(stv, k > 0);
-                    if (leader) {
+                    if (elect_lane()) {
+                        issue_pv(stv, k > 0);
                         tc_commit(bars.pv_done + 8 * mq);
                         if (!within) tc_commit(bars.o_full + 8 * mq);
                         tc_commit(bars.kv_empty + 8 * stv);
                     }
+                    __syncwarp();
                     t_phase ^= 1u;
                     if (++st == C::STAGES) { st = 0; ph ^= 1u; }
                 }
@@ -549,7 +553,7 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                     nxt.advance(p);
                 }
             }
-            if (!ok && leader) give_up(abort_ptr, p.c.status);
+            if (!ok && lane == 0) give_up(abort_ptr, p.c.status);
         }
     } else {
         reg_alloc<REGS_SOFTMAX>();

@@ -15,15 +15,32 @@ __device__ __forceinline__ uint32_t timer_lo_ns() {
     asm volatile("mov.u32 %0, %%globaltimer_lo;" : "=r"(t));
     return t;
 }
-// False when the wait ran out or another role of the CTA gave up.
+// False when the wait ran out or another role of the CTA gave up.  (The timer is read rarely: that takes some 100 cycles.)
 __device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, const volatile int *abort_flag) {
-    if (mbar_try_wait(bar, parity)) return true;
-    const uint32_t since = timer_lo_ns();
-    uint32_t n = 0;
+    uint32_t n = 0, since = 0;
 #pragma unroll 1
-    while (!mbar_try_wait(bar, parity))
-        if ((++n & 0x3Fu) == 0u && (*abort_flag || timer_lo_ns() - since > TILE_WAIT_NS)) return false;
+    while (!mbar_try_wait(bar, parity)) {
+        if ((++n & 0x3Fu) != 0u) continue;
+        const uint32_t now = timer_lo_ns();
+        if (n == 64u) since = now;
+        if (*abort_flag || now - since > TILE_WAIT_NS) return false;
+    }
     return true;
+}
+// The same for a whole warp, which leaves it together.
+__device__ __forceinline__ bool wait_all_lanes(uint32_t bar, uint32_t parity, const volatile int *abort_flag) {
+    return __all_sync(0xFFFFFFFFu, wait_or_abort(bar, parity, abort_flag)) != 0;
+}
+__device__ __forceinline__ bool elect_lane() {
+    uint32_t is;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+    return is != 0;
+}
+// The same, one lane asks.
+__device__ __forceinline__ bool wait_or_abort_warp(uint32_t bar, uint32_t parity, const volatile int *abort_flag) {
+    int ok = 1;
+    if ((threadIdx.x & 31) == 0) ok = wait_or_abort(bar, parity, abort_flag);
+    return __shfl_sync(0xFFFFFFFFu, ok, 0) != 0;
 }
 // A role whose wait ran out: the others leave their loops, and the host learns of it.
 __device__ __forceinline__ void give_up(volatile int *abort_flag, int32_t *status) {
@@ -45,6 +62,63 @@ __device__ __forceinline__ void tma_load_2d(uint32_t smem_dst, const CUtensorMap
 __device__ __forceinline__ void tma_load_3d(uint32_t smem_dst, const CUtensorMap *tm, uint32_t bar, int c0, int c1, int c2) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                  ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+
+// ---- pairs of CTAs (cta_group::2): the even one issues MMAs over both's shared memory, each holds its own 128 rows of D
+__device__ __forceinline__ uint32_t rank_in_cluster() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void sync_cluster() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The address, in the cluster's window, of what stands at `smem_addr` in the CTA of that rank.
+__device__ __forceinline__ uint32_t at_rank(uint32_t smem_addr, uint32_t rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// Loads into this CTA's shared memory whose bytes count on the pair's barrier (an address in the cluster's window).
+__device__ __forceinline__ void tma_pair_2d(uint32_t smem_dst, const CUtensorMap *tm, uint32_t cluster_bar, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(cluster_bar), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void tma_pair_3d(uint32_t smem_dst, const CUtensorMap *tm, uint32_t cluster_bar, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(cluster_bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t smem_result_slot, uint32_t ncols) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_result_slot), "r"(ncols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t ncols) {
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// D += A B for the pair's rows whose bit of `off` is 0; the others keep what they have.
+__device__ __forceinline__ void mma_pair_rows(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, const uint32_t (&off)[8]) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, 1, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, {%4, %5, %6, %7, %8, %9, %10, %11}, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(off[0]), "r"(off[1]), "r"(off[2]), "r"(off[3]), "r"(off[4]), "r"(off[5]),
+          "r"(off[6]), "r"(off[7])
+        : "memory");
+}
+// Arrive on the barrier at this place in both CTAs of the pair (`pair`: their bits among the cluster's) once this thread's MMAs are done.
+__device__ __forceinline__ void commit_pair(uint32_t bar, uint16_t pair) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(pair) : "memory");
 }
 
 // D += A B for the rows (TMEM lanes) whose bit of `off` is 0; the others keep what they have.
