@@ -40,33 +40,38 @@ __device__ __forceinline__ float dot8(uint4 a, uint4 b, float acc) {
     return acc;
 }
 
-// t[m][j] = s_a A_a[j] . x[m]: a warp per (m, j).
+// t[m][j] = s_a A_a[j] . x[m]: four warps per (m, j), two values of j per block.
+constexpr int DOT_WARPS = 4;
 template <bool FP16>
 __global__ void __launch_bounds__(ROWS_THREADS) shrink_rows_kernel(const AdapterParams p) {
+    __shared__ float sums[ROWS_WARPS];
     let_next_start();
-    const int m = blockIdx.y, j = blockIdx.x * ROWS_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (j >= p.rank) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, m = blockIdx.y, j = blockIdx.x * (ROWS_WARPS / DOT_WARPS) + warp / DOT_WARPS;
     const int a = adapter_of_row(p, m);
-    if (a < 0) return;
+    if (a < 0) return;   // (alike for the whole block)
     const uint16_t *x = p.x + m * p.xs, *row = p.a + ((long long)a * p.rank + j) * p.K;
-    float acc[4] = {};
-    int k = lane * 8;
-    for (; k + 3 * 256 < p.K; k += 4 * 256) {
-        uint4 u[4], v[4];
+    constexpr int STEP = DOT_WARPS * 256, AHEAD = 5;
+    float acc[AHEAD] = {};
+    for (int k = (warp % DOT_WARPS * 32 + lane) * 8; k < p.K; k += AHEAD * STEP) {
+        uint4 u[AHEAD], v[AHEAD];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            u[i] = __ldg(reinterpret_cast<const uint4 *>(row + k + i * 256));
-            v[i] = __ldg(reinterpret_cast<const uint4 *>(x + k + i * 256));
+        for (int i = 0; i < AHEAD; ++i) {
+            const bool in = k + i * STEP < p.K;
+            u[i] = in ? __ldg(reinterpret_cast<const uint4 *>(row + k + i * STEP)) : make_uint4(0, 0, 0, 0);
+            v[i] = in ? __ldg(reinterpret_cast<const uint4 *>(x + k + i * STEP)) : make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = dot8<FP16>(u[i], v[i], acc[i]);
+        for (int i = 0; i < AHEAD; ++i) acc[i] = dot8<FP16>(u[i], v[i], acc[i]);
     }
-    for (; k < p.K; k += 256)
-        acc[0] = dot8<FP16>(__ldg(reinterpret_cast<const uint4 *>(row + k)), __ldg(reinterpret_cast<const uint4 *>(x + k)), acc[0]);
-    float sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+    float sum = ((acc[0] + acc[1]) + (acc[2] + acc[3])) + acc[4];
 #pragma unroll
     for (int i = 16; i > 0; i >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, i);
-    if (lane == 0) static_cast<float *>(p.t)[(long long)m * p.rank16 + j] = sum * (p.scales ? __ldg(p.scales + a) : 1.0f);
+    if (lane == 0) sums[warp] = sum;
+    __syncthreads();
+    if (warp % DOT_WARPS == 0 && lane == 0) {
+        sum = (sums[warp] + sums[warp + 1]) + (sums[warp + 2] + sums[warp + 3]);
+        static_cast<float *>(p.t)[(long long)m * p.rank16 + j] = sum * (p.scales ? __ldg(p.scales + a) : 1.0f);
+    }
 }
 
 template <bool FP16>
@@ -79,86 +84,99 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// NT: columns of 8 rows of x; blockIdx.y takes 8 NT rows each.
+// NT: columns of 8 rows of x.  With adapters the block has four warps more, which make B t while the others read W.
+constexpr int MORE_WARPS = 4;
 template <bool FP16, int NT>
-__global__ void __launch_bounds__(ROWS_THREADS) adapter_rows_kernel(const AdapterParams p) {
-    __shared__ float part[ROWS_WARPS][8 * NT][17];   // (a column of padding: the lanes' rows fall on different banks)
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 8 * NT;
-    const int steps = (p.K + CHUNK - 1) / CHUNK;
-    const int from = steps * warp / ROWS_WARPS * CHUNK + 8 * t, to = min(steps * (warp + 1) / ROWS_WARPS * CHUNK, p.K);
-    const bool low = n0 + g < p.N, high = n0 + g + 8 < p.N;
-    const uint16_t *w0 = p.w + (low ? (n0 + g) * p.ws : 0), *w1 = p.w + (high ? (n0 + g + 8) * p.ws : 0);
-    const uint16_t *xr[NT];
-    bool live[NT];
+__global__ void __launch_bounds__(ROWS_THREADS + MORE_WARPS * 32) adapter_rows_kernel(const AdapterParams p) {
+    __shared__ float part[ROWS_WARPS + 1][8 * NT][17];   // (a column of padding: the lanes' rows fall on different banks)
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n0 = blockIdx.x * 16;
+    if (warp < ROWS_WARPS) {
+        const int g = lane >> 2, t = lane & 3;
+        const int steps = (p.K + CHUNK - 1) / CHUNK;
+        const int from = steps * warp / ROWS_WARPS * CHUNK + 8 * t, to = min(steps * (warp + 1) / ROWS_WARPS * CHUNK, p.K);
+        const bool low = n0 + g < p.N, high = n0 + g + 8 < p.N;
+        const uint16_t *w0 = p.w + (low ? (n0 + g) * p.ws : 0), *w1 = p.w + (high ? (n0 + g + 8) * p.ws : 0);
+        const uint16_t *xr[NT];
+        bool live[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        live[n] = m0 + 8 * n + g < p.M;
-        xr[n] = p.x + (live[n] ? (m0 + 8 * n + g) * p.xs : 0);
-    }
-    float acc[NT][4] = {};
-    const uint4 none = make_uint4(0, 0, 0, 0);
-    for (int k = from; k - 8 * t < to; k += BATCH * CHUNK) {
-        uint4 u[BATCH], v[BATCH], x[BATCH][NT];
+        for (int n = 0; n < NT; ++n) {
+            live[n] = 8 * n + g < p.M;
+            xr[n] = p.x + (live[n] ? (8 * n + g) * p.xs : 0);
+        }
+        float acc[NT][4] = {};
+        const uint4 none = make_uint4(0, 0, 0, 0);
+        for (int k = from; k - 8 * t < to; k += BATCH * CHUNK) {
+            uint4 u[BATCH], v[BATCH], x[BATCH][NT];
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            const int at = k + i * CHUNK;
-            const bool in = at < to;
-            u[i] = in && low ? __ldcs(reinterpret_cast<const uint4 *>(w0 + at)) : none;
-            v[i] = in && high ? __ldcs(reinterpret_cast<const uint4 *>(w1 + at)) : none;
+            for (int i = 0; i < BATCH; ++i) {
+                const int at = k + i * CHUNK;
+                const bool in = at < to;
+                u[i] = in && low ? __ldcs(reinterpret_cast<const uint4 *>(w0 + at)) : none;
+                v[i] = in && high ? __ldcs(reinterpret_cast<const uint4 *>(w1 + at)) : none;
+            }
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) x[i][n] = k + i * CHUNK < to && live[n] ? __ldg(reinterpret_cast<const uint4 *>(xr[n] + k + i * CHUNK)) : none;
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    mma_16816<FP16>(acc[n], u[i].x, v[i].x, u[i].y, v[i].y, x[i][n].x, x[i][n].y);
+                    mma_16816<FP16>(acc[n], u[i].z, v[i].z, u[i].w, v[i].w, x[i][n].z, x[i][n].w);
+                }
         }
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) x[i][n] = k + i * CHUNK < to && live[n] ? __ldg(reinterpret_cast<const uint4 *>(xr[n] + k + i * CHUNK)) : none;
+            for (int e = 0; e < 4; ++e) part[warp][8 * n + 2 * t + (e & 1)][g + 8 * (e >> 1)] = acc[n][e];
+    } else {
+        // B t: a warp has two rows of x at a time, half of its lanes a row's 16 columns each
+        const int n = n0 + (lane & 15);
+        int a[2 * NT];
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i)
+        for (int i = 0; i < 2 * NT; ++i) a[i] = 4 * i + warp - ROWS_WARPS < p.M ? adapter_of_row(p, 4 * i + warp - ROWS_WARPS) : -1;
+        // (B's rows on their way before t is there)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                mma_16816<FP16>(acc[n], u[i].x, v[i].x, u[i].y, v[i].y, x[i][n].x, x[i][n].y);
-                mma_16816<FP16>(acc[n], u[i].z, v[i].z, u[i].w, v[i].w, x[i][n].z, x[i][n].w);
+        for (int i = 0; i < 2 * NT; ++i)
+            if (a[i] >= 0 && n < p.N) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.b + ((long long)a[i] * p.N + n) * p.rank + (lane >> 4) * (p.rank / 16 * 8)));
+        wait_for_previous();
+        // lanes 0-15 and 16-31: the even and odd pieces of 8 of the rank
+#pragma unroll
+        for (int i = 0; i < 2 * NT; ++i) {
+            const int m = 4 * i + warp - ROWS_WARPS;
+            float sum = 0.f;
+            if (a[i] >= 0 && n < p.N) {
+                const uint16_t *b = p.b + ((long long)a[i] * p.N + n) * p.rank;
+                const float *tr = static_cast<const float *>(p.t) + (long long)m * p.rank16;
+#pragma unroll 4
+                for (int j = 8 * (lane >> 4); j < p.rank; j += 16) {
+                    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(b + j));
+                    // (t was written beside this kernel: from L2)
+                    const float4 t0 = __ldcg(reinterpret_cast<const float4 *>(tr + j)), t1 = __ldcg(reinterpret_cast<const float4 *>(tr + j + 4));
+                    float2 q = widen<FP16>(v.x);
+                    sum = fmaf(q.x, t0.x, sum); sum = fmaf(q.y, t0.y, sum);
+                    q = widen<FP16>(v.y);
+                    sum = fmaf(q.x, t0.z, sum); sum = fmaf(q.y, t0.w, sum);
+                    q = widen<FP16>(v.z);
+                    sum = fmaf(q.x, t1.x, sum); sum = fmaf(q.y, t1.y, sum);
+                    q = widen<FP16>(v.w);
+                    sum = fmaf(q.x, t1.z, sum); sum = fmaf(q.y, t1.w, sum);
+                }
             }
+            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 16);
+            if (lane < 16) part[ROWS_WARPS][m][lane] = sum;
+        }
     }
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) part[warp][8 * n + 2 * t + (e & 1)][g + 8 * (e >> 1)] = acc[n][e];
     __syncthreads();
-    // two threads a value of y: half of the warps' sums and half of the rank's pieces each
-    const int half = threadIdx.x & 1;
-    bool waited = false;
 #pragma unroll 1
-    for (int o = threadIdx.x >> 1; o < 128 * NT; o += ROWS_THREADS / 2) {
-        const int n = n0 + (o & 15), c = o >> 4, m = m0 + c;
+    for (int o = threadIdx.x; o < 128 * NT; o += blockDim.x) {
+        const int n = n0 + (o & 15), m = o >> 4;
+        if (m >= p.M || n >= p.N) continue;
         float sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < ROWS_WARPS / 2; ++w) sum += part[half * (ROWS_WARPS / 2) + w][c][o & 15];
-        const bool valid = m < p.M && n < p.N;
-        const int a = valid && p.segments > 0 ? adapter_of_row(p, m) : -1;
-        if (p.segments > 0 && !waited) {
-            wait_for_previous();
-            waited = true;
-        }
-        if (a >= 0) {
-            const uint16_t *b = p.b + ((long long)a * p.N + n) * p.rank;
-            const float *tr = static_cast<const float *>(p.t) + (long long)m * p.rank16;
-#pragma unroll 2
-            for (int j = 8 * half; j < p.rank; j += 16) {
-                const uint4 v = __ldg(reinterpret_cast<const uint4 *>(b + j));
-                // (t was written beside this kernel: from L2)
-                const float4 t0 = __ldcg(reinterpret_cast<const float4 *>(tr + j)), t1 = __ldcg(reinterpret_cast<const float4 *>(tr + j + 4));
-                float2 q = widen<FP16>(v.x);
-                sum = fmaf(q.x, t0.x, sum); sum = fmaf(q.y, t0.y, sum);
-                q = widen<FP16>(v.y);
-                sum = fmaf(q.x, t0.z, sum); sum = fmaf(q.y, t0.w, sum);
-                q = widen<FP16>(v.z);
-                sum = fmaf(q.x, t1.x, sum); sum = fmaf(q.y, t1.y, sum);
-                q = widen<FP16>(v.w);
-                sum = fmaf(q.x, t1.z, sum); sum = fmaf(q.y, t1.w, sum);
-            }
-        }
-        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
-        if (!valid || half) continue;
+        for (int w = 0; w < ROWS_WARPS; ++w) sum += part[w][m][o & 15];
+        if (p.segments) sum += part[ROWS_WARPS][m][o & 15];
         if (p.bias) sum += p.bias_fp32 ? __ldg(static_cast<const float *>(p.bias) + n)
                                        : widen<FP16>(__ldg(static_cast<const uint16_t *>(p.bias) + n)).x;
         p.y[m * p.ys + n] = (uint16_t)pack_half2<FP16>(sum, 0.f);
@@ -168,8 +186,8 @@ __global__ void __launch_bounds__(ROWS_THREADS) adapter_rows_kernel(const Adapte
 template <bool FP16, int NT>
 cudaError_t launch_rows(const AdapterParams &p, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((p.N + 15) / 16), (unsigned)((p.M + 8 * NT - 1) / (8 * NT)));
-    cfg.blockDim = dim3(ROWS_THREADS);
+    cfg.gridDim = dim3((unsigned)((p.N + 15) / 16));
+    cfg.blockDim = dim3(ROWS_THREADS + (p.segments > 0 ? MORE_WARPS * 32 : 0));
     cfg.stream = st;
     cudaLaunchAttribute attr = {};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -181,7 +199,7 @@ cudaError_t launch_rows(const AdapterParams &p, cudaStream_t st) {
 template <bool FP16>
 cudaError_t launch_rows(const AdapterParams &p, cudaStream_t st) {
     if (p.segments > 0) {
-        shrink_rows_kernel<FP16><<<dim3((unsigned)((p.rank + ROWS_WARPS - 1) / ROWS_WARPS), (unsigned)p.M), ROWS_THREADS, 0, st>>>(p);
+        shrink_rows_kernel<FP16><<<dim3((unsigned)(p.rank * DOT_WARPS / ROWS_WARPS), (unsigned)p.M), ROWS_THREADS, 0, st>>>(p);
         const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }

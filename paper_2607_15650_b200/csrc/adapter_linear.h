@@ -19,34 +19,73 @@ struct AdapterParams {
 };
 
 __device__ __forceinline__ int border_of(const AdapterParams &p, int s) { return min(max(__ldg(p.starts + s), 0), p.M); }
-// The first segment that ends behind `row` (p.segments: none).
-__device__ __forceinline__ int first_segment(const AdapterParams &p, int row) {
-    int lo = 0, hi = p.segments;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (border_of(p, mid + 1) > row) hi = mid;
-        else lo = mid + 1;
-    }
-    return lo;
-}
 // Its adapter, or -1 (an index that is none of the adapters' counts as none).
 __device__ __forceinline__ int adapter_of(const AdapterParams &p, int s) {
     const int a = __ldg(p.which + s);
     return a >= 0 && a < p.adapters ? a : -1;
 }
-// The adapter of a row, or -1.
-__device__ __forceinline__ int adapter_of_row(const AdapterParams &p, int row) {
-    const int s = first_segment(p, row);
-    return s < p.segments && border_of(p, s) <= row ? adapter_of(p, s) : -1;
+// Segments are looked at 32 at a time by a whole warp, a lane each: one round of loads instead of a chain.
+
+// How many segments there are before the first that ends behind `row`, in steps of 32 (borders do not decrease).
+__device__ __forceinline__ int segments_before(const AdapterParams &p, int row) {
+    int lo = 0, hi = (p.segments + 31) / 32;   // of the steps
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (border_of(p, 32 * mid) <= row) lo = mid;
+        else hi = mid;
+    }
+    return 32 * lo;
 }
-// A segment's rows within [row0, row1) that have an adapter.
+// A segment's rows within [row0, row1) that have an adapter; adapter -1: none.
 struct Piece { int from, to, adapter; };
 __device__ __forceinline__ Piece piece_of(const AdapterParams &p, int s, int row0, int row1) {
-    Piece r;
+    Piece r = {row1, row1, -1};
+    if (s >= p.segments) return r;
+    r.adapter = adapter_of(p, s);
     r.from = max(border_of(p, s), row0);
     r.to = min(border_of(p, s + 1), row1);
-    r.adapter = r.from < r.to ? adapter_of(p, s) : -1;
+    if (r.from >= r.to) r.adapter = -1;
     return r;
+}
+// The pieces of rows [row0, row1), one after another, alike for all lanes.  `first` may be asked for long before the others.
+struct Pieces {
+    int s;            // the segment of lane 0
+    Piece mine;
+    __device__ __forceinline__ void first(const AdapterParams &p, int row0, int row1) {
+        s = p.segments ? segments_before(p, row0) : 0;
+        mine = piece_of(p, s + (int)(threadIdx.x & 31), row0, row1);
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(const AdapterParams &p, int row0, int row1, F &&f) {
+#pragma unroll 1
+        while (true) {
+            uint32_t on = __ballot_sync(0xFFFFFFFFu, mine.adapter >= 0);
+#pragma unroll 1
+            for (; on != 0u; on &= on - 1u) {
+                const int i = __ffs(on) - 1;
+                Piece q;
+                q.from = __shfl_sync(0xFFFFFFFFu, mine.from, i);
+                q.to = __shfl_sync(0xFFFFFFFFu, mine.to, i);
+                q.adapter = __shfl_sync(0xFFFFFFFFu, mine.adapter, i);
+                if (!f(q)) return;
+            }
+            s += 32;
+            if (s >= p.segments || border_of(p, s) >= row1) return;
+            mine = piece_of(p, s + (int)(threadIdx.x & 31), row0, row1);
+        }
+    }
+};
+// The adapter of a row, or -1; a whole warp asks.
+__device__ __forceinline__ int adapter_of_row(const AdapterParams &p, int row) {
+    const int s = segments_before(p, row) + (int)(threadIdx.x & 31);
+    bool in = false;
+    int a = -1;
+    if (s < p.segments) {
+        a = adapter_of(p, s);
+        in = border_of(p, s) <= row && row < border_of(p, s + 1);
+    }
+    const uint32_t on = __ballot_sync(0xFFFFFFFFu, in);
+    return on ? __shfl_sync(0xFFFFFFFFu, a, __ffs(on) - 1) : -1;
 }
 
 // Few rows: the weights' rows are read once by mma.sync.

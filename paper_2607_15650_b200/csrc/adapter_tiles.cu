@@ -37,14 +37,16 @@ shrink_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     let_next_start();
     // this cluster's pair: the last segment that begins before the end of its tile on the staircase
     const int pair = blockIdx.x / sh.splits, part = blockIdx.x - pair * sh.splits;
-    int lo = 0, hi = p.segments;
-    while (lo < hi) {   // segments below lo: border + 128 s < 128 (pair + 1)
+    const long long beyond = (long long)TM * (pair + 1);
+    int lo = 0, hi = (p.segments + 31) / 32;   // in steps of 32 segments, then a lane each (every warp by itself)
+    while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if ((long long)border_of(p, mid) + (long long)TM * mid < (long long)TM * (pair + 1)) lo = mid + 1;
+        if (border_of(p, 32 * mid) + (long long)TM * 32 * mid < beyond) lo = mid;
         else hi = mid;
     }
-    const int s = lo - 1, tile = pair - s;
-    if (s < 0 || (long long)tile * TM >= p.M) return;   // (alike for the whole cluster)
+    lo = 32 * lo + (threadIdx.x & 31);
+    const int s = (lo & ~31) + __popc(__ballot_sync(0xFFFFFFFFu, lo < p.segments && border_of(p, min(lo, p.segments)) + (long long)TM * lo < beyond)) - 1, tile = pair - s;
+    if (s < 0 || tile < 0 || (long long)tile * TM >= p.M) return;   // (alike for the whole cluster)
     const int row0 = tile * TM;
     const Piece piece = piece_of(p, s, row0, min(row0 + TM, p.M));
     if (piece.adapter < 0) return;
@@ -284,13 +286,12 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             int mi, ni;
             tile_at(sh, w, mi, ni);
             const int row0 = mi * PM, row1 = min(row0 + PM, p.M), row = row0 + (int)half * TM, col = ni * BN + (int)half * (BN / 2);
+            Pieces pieces;
+            if (p.segments && part == 0) pieces.first(p, row0, row1);
 #pragma unroll 1
             for (int k = k_from; k < k_to && ok; k += ATOMS * BK) stage(&map_x, &map_w, k, min(k + ATOMS * BK, k_to), row, col, -1);
-            if (part != 0) continue;
-#pragma unroll 1
-            for (int s = p.segments ? first_segment(p, row0) : 0; s < p.segments && border_of(p, s) < row1 && ok; ++s) {
-                const Piece piece = piece_of(p, s, row0, row1);
-                if (piece.adapter < 0) continue;
+            if (!p.segments || part != 0) continue;
+            pieces.each(p, row0, row1, [&](const Piece &piece) {
                 if (!t_ready) {
                     wait_for_previous();
                     asm volatile("fence.proxy.async.global;" ::: "memory");
@@ -298,7 +299,8 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 }
 #pragma unroll 1
                 for (int k = 0; k < p.rank16 && ok; k += ATOMS * BK) stage(&map_t, &map_b, k, min(k + ATOMS * BK, p.rank16), row, col, piece.adapter);
-            }
+                return ok;
+            });
         }
         if (!ok) give_up(abort_ptr, p.status);
         if (p.segments && !t_ready) wait_for_previous();   // (no launch behind this one starts before the shrink kernel's end)
@@ -312,6 +314,9 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             for (int w = pair; w < sh.tiles && ok; w += pairs, ++n) {
                 int mi, ni;
                 tile_at(sh, w, mi, ni);
+                const int row0 = mi * PM, row1 = min(row0 + PM, p.M);
+                Pieces pieces;
+                if (p.segments && part == 0) pieces.first(p, row0, row1);
                 const uint32_t acc = n & 1u, d = tmem + acc * C::COLS;
                 ok = wait_all_lanes(acc_empty + 8 * acc, ((n >> 1) & 1u) ^ 1u, abort_ptr);
                 if (!ok) break;
@@ -335,11 +340,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                     __syncwarp();
                     if (++st == C::STAGES) { st = 0; ph ^= 1u; }
                 }
-                const int row0 = mi * PM, row1 = min(row0 + PM, p.M);
-#pragma unroll 1
-                for (int s = p.segments && part == 0 ? first_segment(p, row0) : p.segments; s < p.segments && border_of(p, s) < row1 && ok; ++s) {
-                    const Piece piece = piece_of(p, s, row0, row1);
-                    if (piece.adapter < 0) continue;
+                if (ok && p.segments && part == 0) pieces.each(p, row0, row1, [&](const Piece &piece) {
                     uint32_t off[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -349,7 +350,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
 #pragma unroll 1
                     for (int k = 0; k < p.rank16; k += ATOMS * BK) {
                         ok = wait_all_lanes(full + 8 * st, ph, abort_ptr);
-                        if (!ok) break;
+                        if (!ok) return false;
                         tc_fence_after();
                         const uint64_t ad = make_smem_desc_sw128(base + st * C::STAGE, 16, 1024), bd = make_smem_desc_sw128(base + st * C::STAGE + A_BYTES, 16, 1024);
                         if (elect_lane()) {
@@ -363,7 +364,8 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                         __syncwarp();
                         if (++st == C::STAGES) { st = 0; ph ^= 1u; }
                     }
-                }
+                    return true;
+                });
                 if (ok && elect_lane()) commit_pair(acc_full + 8 * acc, both);
                 __syncwarp();
             }
