@@ -230,6 +230,8 @@ def _load_ops():
     spec = importlib.util.spec_from_file_location("_ditango_ops", OPS_PATH)
     ops = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(ops)
+    if ops.torch_version != torch.__version__.split("+")[0]:
+        raise ImportError(f"{OPS_PATH} is built for torch {ops.torch_version}: run `python -m paper_2607_15650_b200.build --force`")
 
     def on_device(index, name, args, kw):
         with torch.cuda.device(index):
@@ -240,7 +242,7 @@ def _load_ops():
 
     ops._bind(tuple(C.cast(getattr(L, n), C.c_void_p).value for n in _OPS),
               (torch.bfloat16, torch.float16, torch.float32, torch.float64, torch.int32, torch.uint8, torch.bool, torch.float8_e4m3fn),
-              (torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, on_device, raise_status))
+              (on_device, raise_status))
     globals().update({n: getattr(ops, n) for n in _OPS}, _norm_rows=ops._norm_rows)
 
 

@@ -5,10 +5,12 @@
 nvcc cross-compiles without a GPU.  The library links the static CUDA runtime and resolves the
 one driver entry point it needs (tensor-map encoding) at run time, so it has no link-time
 dependency on libcuda.  The Python entry points of the context-free operators are a module of
-their own, which needs a C compiler and Python's headers; without those the library is built alone.
+their own, which needs a C and C++ compiler and Python's and torch's headers; without the compiler or Python's headers the library is
+built alone.
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import shlex
 import shutil
@@ -26,7 +28,7 @@ SOURCES = ["api.cu", "attn_states.cu", "state_merge.cu", "plan.cu", "planner.cu"
 HEADERS = ["dt_internal.h", "ops.h", "cross_attn.h", "adapter_linear.h", "packed_attn.h", "tile_wait.cuh", "ptx_sm100.cuh", os.path.join("..", "..", "include", "ditango.h")]
 # Python entry points of the context-free operators, for this interpreter
 OPS_LIB = os.path.join(HERE, "_ditango_ops" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
-OPS_SOURCE = "ops_py.c"
+OPS_SOURCE, OPS_TENSOR = "ops_py.c", "ops_tensor.cpp"      # (the second against torch's headers)
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 
@@ -38,14 +40,17 @@ def _stale(lib=LIB, files=SOURCES + HEADERS) -> bool:
 
 
 def _build_ops(force: bool) -> None:
-    if not force and not _stale(OPS_LIB, [OPS_SOURCE, HEADERS[-1]]):
+    if not force and not _stale(OPS_LIB, [OPS_SOURCE, OPS_TENSOR, "ops_tensor.h", HEADERS[-1]]):
         return
     cc, include = shlex.split(os.environ.get("CC") or "gcc"), sysconfig.get_paths()["include"]
     if shutil.which(cc[0]) is None or not os.path.exists(os.path.join(include, "Python.h")):
         warnings.warn(f"no Python entry points of the context-free operators: {cc[0]} or {include}/Python.h is missing")
         return
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
     tmp = OPS_LIB + f".tmp{os.getpid()}"
-    subprocess.run([*cc, "-O2", "-std=c11", "-shared", "-fPIC", "-Wall", "-I" + include, "-o", tmp, os.path.join(CSRC, OPS_SOURCE)], check=True)
+    subprocess.run([*cc, "-O2", "-shared", "-fPIC", "-Wall", "-I" + include, "-I" + os.path.join(torch, "include"),
+                    "-I" + os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include"), "-o", tmp, os.path.join(CSRC, OPS_SOURCE),
+                    os.path.join(CSRC, OPS_TENSOR), "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10", "-lstdc++"], check=True)
     os.replace(tmp, OPS_LIB)
 
 

@@ -1,24 +1,12 @@
-/* Python entry points of the context-free operators (dt_rope, dt_add_rmsnorm, dt_cross_attn, dt_adapter_linear, dt_packed_attn): argument marshalling only, in C
- * because on small tensors the marshalling is the call (through ctypes 8 to 11 us of host time a call, this way 5.7 to 6.1, against 3 to 5 us on the GPU).
- * Tensors are looked at through their Python attributes, so nothing here depends on torch's headers; the library's functions
- * are called through the addresses that binding.py hands to _bind. */
-#define PY_SSIZE_T_CLEAN
-#include <Python.h>
-
-#include "../../include/ditango.h"
-
-enum { MAX_DIM = 8 };
-enum { T_BF16 = DT_VALUE_BF16, T_FP16 = DT_VALUE_FP16, T_FP32 = DT_VALUE_FP32, T_FP64, T_I32, T_U8, T_BOOL, T_E4M3, T_COUNT, T_OTHER = -1 };
-
-typedef struct {
-    int64_t shape[MAX_DIM], stride[MAX_DIM];
-    void *ptr;
-    int nd, dtype;
-    long device;
-} Tensor;
+/* Python entry points of the context-free operators (dt_rope, dt_add_rmsnorm, dt_cross_attn, dt_adapter_linear, dt_packed_attn): argument
+ * marshalling only, in C because on small tensors the marshalling is the call: through ctypes 8 to 11 us of host time a call, through
+ * the tensors' Python attributes 5 to 9, this way 4.1 to 6.3 (most of it the launches), against 3 to 6 us on the GPU.
+ * Tensors are looked at through torch's own headers (ops_tensor.cpp), those of other classes through their Python attributes; the
+ * library's functions are called through the addresses that binding.py hands to _bind. */
+#include "ops_tensor.h"
 
 static PyObject *dtypes[T_COUNT];
-static PyObject *raw_stream, *get_device, *on_device, *raise_status;   /* callables of binding.py and torch */
+static PyObject *on_device, *raise_status;   /* callables of binding.py */
 static PyObject *s_shape, *s_stride, *s_data_ptr, *s_dtype, *s_get_device, *s_cuda_stream;
 static dt_status (*f_rope)(const dt_rope_config *, const void *, const int64_t *, void *, const int64_t *, const void *, const int64_t *,
                            void *, const int64_t *, const double *, const int32_t *, const int64_t *, void *);
@@ -47,6 +35,8 @@ static int ints_of(PyObject *seq, int64_t *out) {   /* a tuple's integers; steal
 }
 
 static int look(PyObject *t, Tensor *x) {   /* 0, or -1 with an error set */
+    const int seen = tensor_look(t, x);
+    if (seen != 0) return seen < 0 ? -1 : 0;
     x->nd = ints_of(PyObject_GetAttr(t, s_shape), x->shape);
     if (x->nd < 0) return -1;
     const int n = ints_of(PyObject_CallMethodNoArgs(t, s_stride), x->stride);
@@ -132,28 +122,18 @@ static int take(const char *name, const char *const *names, int count, int requi
     return 0;
 }
 
-/* The stream's pointer, or the tensors' device is not current and `*again` is the call's result on it (NULL: error set). */
+/* The stream's pointer (NULL for `stream`: torch's current one) into *out; 0, or -1 with an error set. */
 static int stream_of(PyObject *stream, long device, void **out) {
-    PyObject *o;
-    if (stream) {
-        o = PyObject_GetAttr(stream, s_cuda_stream);
-    } else {
-        PyObject *i = PyLong_FromLong(device);
-        if (!i) return -1;
-        o = PyObject_CallOneArg(raw_stream, i);
-        Py_DECREF(i);
-    }
+    if (!stream) return torch_current_stream(device, out);
+    PyObject *o = PyObject_GetAttr(stream, s_cuda_stream);
     if (!o) return -1;
     *out = PyLong_AsVoidPtr(o);
     Py_DECREF(o);
     return PyErr_Occurred() ? -1 : 0;
 }
 static int is_current(long device) {   /* 1, 0, or -1 with an error set */
-    PyObject *o = PyObject_CallNoArgs(get_device);
-    if (!o) return -1;
-    const long d = PyLong_AsLong(o);
-    Py_DECREF(o);
-    return PyErr_Occurred() ? -1 : d == device;
+    long d;
+    return torch_current_device(&d) < 0 ? -1 : d == device;
 }
 /* binding.py makes `device` current and calls again with the same arguments */
 static PyObject *call_on(long device, const char *name, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
@@ -518,8 +498,8 @@ static PyObject *py_rows(PyObject *self, PyObject *list) {
 
 static PyObject *py_bind(PyObject *self, PyObject *args) {
     unsigned long long rope, norm, cross, adapter, packed;
-    PyObject *types, *calls[4];
-    if (!PyArg_ParseTuple(args, "(KKKKK)O!(OOOO)", &rope, &norm, &cross, &adapter, &packed, &PyTuple_Type, &types, &calls[0], &calls[1], &calls[2], &calls[3])) return NULL;
+    PyObject *types, *calls[2];
+    if (!PyArg_ParseTuple(args, "(KKKKK)O!(OO)", &rope, &norm, &cross, &adapter, &packed, &PyTuple_Type, &types, &calls[0], &calls[1])) return NULL;
     NEED(PyTuple_GET_SIZE(types) == T_COUNT);
     f_rope = (void *)(uintptr_t)rope;
     f_norm = (void *)(uintptr_t)norm;
@@ -527,10 +507,8 @@ static PyObject *py_bind(PyObject *self, PyObject *args) {
     f_adapter = (void *)(uintptr_t)adapter;
     f_packed = (void *)(uintptr_t)packed;
     for (int i = 0; i < T_COUNT; ++i) Py_XSETREF(dtypes[i], Py_NewRef(PyTuple_GET_ITEM(types, i)));
-    Py_XSETREF(raw_stream, Py_NewRef(calls[0]));
-    Py_XSETREF(get_device, Py_NewRef(calls[1]));
-    Py_XSETREF(on_device, Py_NewRef(calls[2]));
-    Py_XSETREF(raise_status, Py_NewRef(calls[3]));
+    Py_XSETREF(on_device, Py_NewRef(calls[0]));
+    Py_XSETREF(raise_status, Py_NewRef(calls[1]));
     Py_RETURN_NONE;
 }
 
@@ -574,5 +552,7 @@ PyMODINIT_FUNC PyInit__ditango_ops(void) {
     s_get_device = PyUnicode_InternFromString("get_device");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
     if (!s_shape || !s_stride || !s_data_ptr || !s_dtype || !s_get_device || !s_cuda_stream) return NULL;
-    return PyModule_Create(&module);
+    PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "torch_version", tensor_torch_version) < 0) Py_CLEAR(m);
+    return m;
 }

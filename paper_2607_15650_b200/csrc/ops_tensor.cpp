@@ -1,0 +1,82 @@
+// A tensor's pointer, type, device, shape and strides, and the current device and stream, straight from torch: through Python's
+// attributes a tensor costs 0.4 to 0.9 us of host time, as much as a tenth of a small operator's whole call.
+#include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/autograd/python_variable.h>
+#include <torch/headeronly/version.h>
+
+#include <cstdint>
+
+#include "ops_tensor.h"
+
+namespace {
+
+int type_of(c10::ScalarType t) {
+    switch (t) {
+        case c10::ScalarType::BFloat16: return T_BF16;
+        case c10::ScalarType::Half: return T_FP16;
+        case c10::ScalarType::Float: return T_FP32;
+        case c10::ScalarType::Double: return T_FP64;
+        case c10::ScalarType::Int: return T_I32;
+        case c10::ScalarType::Byte: return T_U8;
+        case c10::ScalarType::Bool: return T_BOOL;
+        case c10::ScalarType::Float8_e4m3fn: return T_E4M3;
+        default: return T_OTHER;
+    }
+}
+template <typename F>
+int guarded(F &&f) {   // no C++ exception leaves through C
+    try {
+        return f();
+    } catch (const c10::Error &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what_without_backtrace());
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+        PyErr_SetString(PyExc_RuntimeError, "unknown C++ exception");
+    }
+    return -1;
+}
+
+}  // namespace
+
+const char *const tensor_torch_version = TORCH_VERSION;
+
+extern "C" int tensor_look(PyObject *o, Tensor *x) {
+    if (!THPVariable_CheckExact(o)) return 0;
+    return guarded([&] {
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (t.layout() != c10::kStrided) {
+            PyErr_SetString(PyExc_AssertionError, "a strided tensor is wanted");
+            return -1;
+        }
+        const auto sizes = t.sizes(), strides = t.strides();
+        if (sizes.size() > MAX_DIM || sizes.size() != strides.size()) {
+            PyErr_SetString(PyExc_AssertionError, "a strided tensor of at most 8 dimensions is wanted");
+            return -1;
+        }
+        x->nd = (int)sizes.size();
+        for (int i = 0; i < x->nd; ++i) {
+            x->shape[i] = sizes[i];
+            x->stride[i] = strides[i];
+        }
+        x->dtype = type_of(t.scalar_type());
+        x->device = t.device().is_cuda() ? (long)t.device().index() : -1;
+        x->ptr = t.data_ptr();
+        return 1;
+    });
+}
+
+extern "C" int torch_current_device(long *device) {
+    return guarded([&] {
+        *device = (long)c10::cuda::current_device();
+        return 0;
+    });
+}
+
+extern "C" int torch_current_stream(long device, void **stream) {
+    return guarded([&] {
+        *stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream();
+        return 0;
+    });
+}
