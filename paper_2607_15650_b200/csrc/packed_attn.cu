@@ -438,7 +438,9 @@ extern "C" dt_status dt_packed_attn(const dt_packed_config *cfg, const void *q_d
     if (c.docs > 65536) return ops_fail(DT_ERR_UNSUPPORTED, "more than 65536 documents in a row");
     if (!(c.softmax_scale > 0.f) || !std::isfinite(c.softmax_scale)) return ops_fail(DT_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
     if (!(c.softcap >= 0.f) || !std::isfinite(c.softcap)) return ops_fail(DT_ERR_INVALID_ARG, "softcap must be finite and >= 0");
-    if (c.softcap > 0.f && !std::isfinite(c.softmax_scale / c.softcap)) return ops_fail(DT_ERR_INVALID_ARG, "softmax_scale / softcap must be finite");
+    // (a subnormal one could become 0, and 0 times infinity would stand where a key does not count)
+    if (c.softcap > 0.f && (!std::isnormal(c.softcap) || !std::isnormal(c.softmax_scale / c.softcap)))
+        return ops_fail(DT_ERR_INVALID_ARG, "softcap and softmax_scale / softcap must be normal numbers");
     if (bias_table_dev && bias_slopes_dev) return ops_fail(DT_ERR_INVALID_ARG, "a bias table or slopes, not both");
     if (bias_table_dev && c.bias_far < 0) return ops_fail(DT_ERR_INVALID_ARG, "bad bias_far");
     if (bias_table_dev && c.bias_far > 512) return ops_fail(DT_ERR_UNSUPPORTED, "bias_far exceeds 512");

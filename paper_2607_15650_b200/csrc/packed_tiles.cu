@@ -1,14 +1,15 @@
 // dt_packed_attn for many query rows: softmax in one pass over the keys, in tensor-memory tiles; 256 query rows of one document and
 // head per work item, against the keys that any of them has.
 //
-// One persistent CTA per SM, 16 warps --
+// One CTA per SM at a time, which stays for as many items as it can take over, 16 warps --
 //   warps 0-3 / 4-7  softmax of query tile 0 / 1 (128 rows each, one row per thread)
-//   warp 8           TMA producer: Q of every item, K and V tiles through a ring in the order the MMAs consume them
+//   warp 8           producer: the items; Q of every item, K and V tiles through a ring in the order the MMAs consume them (TMA)
 //   warps 9, 10      MMA issuers of query tile 0 / 1
 //   warp 11          V's rows that do not count for all of an item's rows; the bias table of every item
 //   warps 12-15      epilogue of both query tiles: O from TMEM, divided by the sum, to the caller's tensor
-// -- and TMEM holds S | P0 | P1 | O0 | O1, as in the cross attention's tiles: one place for S that the two tiles use in turn, one
-// stream of tiles over all items of a CTA, the epilogue in warps of its own.
+// -- and TMEM holds S | P0 | P1 | O0 | O1, one place for S that the two tiles use in turn (D = 64: S0 | S1 | ...), one stream of tiles
+// over all items of a CTA, the epilogue in warps of its own.  A query tile leaves out the item's last tiles of keys where none of its
+// rows has any of them (causal), and all where it has no rows.
 //
 // Masks: a row's keys are an interval that begins where the document does, and so do the tiles; so only tiles that end behind the
 // first row's end are masked, by comparing a column's number with the row's (other tiles do nothing for it).  V of such a tile: rows
@@ -16,8 +17,11 @@
 // be: what of it is not finite is zeroed, so that 0 times it is 0 where it does not count, and added to O in the epilogue where it
 // does (never, in earnest).
 //
-// Capped logits: tanh(y) = y P(y^2), P of degree 6 fitted to 1.2e-7 on [0, 1] and evaluated on the FMA pipe in pairs, where all of a warp's
-// rows stay below the cap in a tile; 1 - 2 / (1 + e^2y) with its two further MUFU operations a logit otherwise.
+// Capped logits: tanh(y) = y P(y^2), evaluated on the FMA pipe in pairs, where all of a warp's rows stay below 0.9 of the cap in a tile;
+// 1 - 2 / (1 + e^2y) with its two further MUFU operations a logit otherwise.  The maximum is taken of the products, so that the polynomial
+// (FMA pipe) of some columns runs beside the exponentials (MUFU) of others.  What runs in earnest is one path: with a second polynomial for
+// some tiles, warps waited for instructions three times as long as they issued them.
+// Slopes: beyond the diagonal's tiles a bias is linear in the column: eight values per row and a step for every eight columns.
 // Bias table: the head's 2 far + 1 values in shared memory with the last ones repeated on both sides, so that a tile near the
 // diagonal reads it without clamping (a thread's columns are neighbours in it, and so are a warp's rows); a tile beyond `far` adds
 // one value.
@@ -46,6 +50,9 @@ constexpr int TABLE_BYTES = (2 * FAR_MOST + 1 + 2 * TABLE_PAD + 3) / 4 * 16;
 // A broken item's number is marked for the epilogue in one of so many places: a V tile that has landed is at most three items ahead of
 // the one whose P V is under way, and that one at most two ahead of the epilogue.
 constexpr int MARKS = 8;
+constexpr int TANH_BYTES = 64;                             // the pairs of capped_near
+constexpr int SLOTS = 4;                                   // items that the producer may be ahead of the slowest role
+constexpr int READERS = THREADS / 32 - 1;                  // warps that read an item
 
 template <int D>
 struct Cfg {
@@ -57,10 +64,12 @@ struct Cfg {
     static constexpr int KV_BYTES = STAGES * TILE_BYTES;
     static constexpr int OUT_BYTES = TILE * 128;              // epilogue staging: 4 warps x [32 rows x 128 bytes]
     static constexpr int ML_BYTES = NQ * TILE * 8;            // (maximum, sum) of every row
-    static constexpr int NBARS = 3 * STAGES + 10 * NQ + 5;
-    static constexpr int SMEM_BYTES = 1024 /*alignment slack*/ + Q_BYTES + KV_BYTES + OUT_BYTES + ML_BYTES + 2 * TABLE_BYTES + MARKS * 4 + NBARS * 8;
+    static constexpr int NBARS = 3 * STAGES + 12 * NQ + 2 * SLOTS + 1;
+    static constexpr int SMEM_BYTES = 1024 /*alignment slack*/ + Q_BYTES + KV_BYTES + OUT_BYTES + ML_BYTES + 2 * TABLE_BYTES + MARKS * 4 + SLOTS * 48 + 16 + TANH_BYTES + NBARS * 8;
     static_assert(SMEM_BYTES + 64 <= 227 * 1024, "beyond the shared memory of a CTA");
-    static constexpr int S_COL = 0, P_COL = 128, P_STRIDE = 64, O_COL = 256;
+    // D = 64 has room for a place for S of each query tile; D = 128 has one that the two use in turn
+    static constexpr int S_PLACES = D == 64 ? 2 : 1;
+    static constexpr int S_COL = 0, P_COL = 128 * S_PLACES, P_STRIDE = 64, O_COL = P_COL + NQ * P_STRIDE;
     static_assert(O_COL + NQ * D <= 512, "beyond the tensor memory of an SM");
 };
 
@@ -68,8 +77,10 @@ struct Bars {
     uint32_t kv_full, kv_empty, kv_raw;                                // + 8*stage; raw: landed, rows still to be mended
     uint32_t q_full, q_empty;                                          // + 8*q
     uint32_t s_full, p_full, o_full, o_free, pv_done, ml_full, s_req;  // + 8*q
-    uint32_t s_free;
+    uint32_t s_free;                                                   // + 8*q where S has two places
     uint32_t tab_full, tab_empty;                                      // + 8*(item & 1)
+    uint32_t item_full, item_empty;                                    // + 8*slot
+    uint32_t asked;                                                    // the next block's number is here
 };
 
 // Tensor maps' coordinates: a dimension of one entry, or one that repeats (stride 0), has one entry in the map too.
@@ -81,45 +92,68 @@ struct TileParams {
     int items;               // B * blocks * H
 };
 
-// The stream of a CTA's tiles: item after item, those without rows left out.  K and V are loaded (and consumed) in the order
-// K_0, K_1, V_0, K_2, V_1, ..., K_n, V_{n-1}, ..., V_last, across items.  Heads run fastest, so that neighbours share K and V in L2
-// where heads are grouped; blocks run from the last, so that causal rows with many keys come first.
-struct Cursor {
-    int w, h, b;
-    Doc doc;
-    int row0, first_end;     // first row; the end of its keys (of the document's and the row's own)
-    int tiles, t;
-    bool valid;
-    __device__ __forceinline__ void look(const TileParams &p) {
-#pragma unroll 1
-        for (;; w += gridDim.x) {
-            valid = w < p.items;
-            tiles = t = 0;
-            if (!valid) return;
-            const int u = w / p.c.H;
-            h = w - u * p.c.H;
-            b = u / p.blocks;
-            if (block_at(p.c, b, p.blocks - 1 - (u - b * p.blocks), ITEM_ROWS, doc, row0)) break;
-        }
-        first_end = keys_end(p.c, doc, row0);
-        tiles = (keys_end(p.c, doc, min(row0 + ITEM_ROWS, doc.q1) - 1) - doc.k0 + TILE - 1) / TILE;
-    }
-    __device__ __forceinline__ void first_item(const TileParams &p) { w = blockIdx.x; look(p); }
-    __device__ __forceinline__ void next_item(const TileParams &p) { w += gridDim.x; look(p); }
-    __device__ __forceinline__ int key0() const { return doc.k0 + t * TILE; }
-    __device__ __forceinline__ void skip_empty(const TileParams &p) {
-#pragma unroll 1
-        while (valid && tiles == 0) next_item(p);
-    }
-    __device__ __forceinline__ void advance(const TileParams &p) {
-        if (++t < tiles) return;
-        next_item(p);
-        skip_empty(p);
-    }
+// The stream of a CTA's tiles goes over its items, K and V in the order K_0, K_1, V_0, K_2, V_1, ..., K_n, V_{n-1}, ..., V_last, across items.
+// A CTA begins with the block of its own number; the next ones it takes over from CTAs of the grid that have not started
+// (clusterlaunchcontrol), a little before it needs them.  So the SMs stay busy whatever the items' lengths, and the launch has a CTA
+// per block.  Heads run fastest, so that neighbours share K and V in L2 where heads are grouped; blocks run from the last, so that causal
+// rows with many keys come first.
+// The producer looks an item up and leaves it in shared memory for the other roles.
+struct Item {
+    int tiles[NQ];           // of keys, for each query tile: the item's first ones; 0: it has no rows or no keys
+    int b, h, row0, q1;      // first row; the end of the document's
+    int k0, k1, shift, prefix_end;
+    int first_end;           // the end of the first row's keys
+    int state;               // 1: an item, 0: there is none any more
+    __device__ __forceinline__ int all() const { return max(tiles[0], tiles[1]); }
+    __device__ __forceinline__ Doc doc() const { return {0, q1, k0, k1, shift, prefix_end}; }
     // Whether the tile of keys from `key` holds keys in memory that do not count for all rows (behind Lk there are zeros: the tensor
     // map ends there).
-    __device__ __forceinline__ bool mended(const TileParams &p, int key) const { return first_end < min(key + TILE, p.c.Lk); }
+    __device__ __forceinline__ bool mended(const PackedParams &p, int key) const { return first_end < min(key + TILE, p.Lk); }
 };
+__device__ __forceinline__ void store_item(uint32_t at, const Item &i) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(i.tiles[0]), "r"(i.tiles[1]), "r"(i.b), "r"(i.h) : "memory");
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + 16), "r"(i.row0), "r"(i.q1), "r"(i.k0), "r"(i.k1) : "memory");
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + 32), "r"(i.shift), "r"(i.prefix_end), "r"(i.first_end), "r"(i.state) : "memory");
+}
+__device__ __forceinline__ void load_item(uint32_t at, Item &i) {
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(i.tiles[0]), "=r"(i.tiles[1]), "=r"(i.b), "=r"(i.h) : "r"(at) : "memory");
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(i.row0), "=r"(i.q1), "=r"(i.k0), "=r"(i.k1) : "r"(at + 16) : "memory");
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(i.shift), "=r"(i.prefix_end), "=r"(i.first_end), "=r"(i.state) : "r"(at + 32) : "memory");
+}
+// Block number w as an item; false: it has no rows.
+__device__ __forceinline__ bool item_of(const TileParams &p, int w, Item &it) {
+    const int u = w / p.c.H;
+    it.h = w - u * p.c.H;
+    it.b = u / p.blocks;
+    Doc doc;
+    if (!block_at(p.c, it.b, p.blocks - 1 - (u - it.b * p.blocks), ITEM_ROWS, doc, it.row0)) return false;
+    it.q1 = doc.q1; it.k0 = doc.k0; it.k1 = doc.k1; it.shift = doc.shift; it.prefix_end = doc.prefix_end;
+    it.first_end = keys_end(p.c, doc, it.row0);
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {   // (a row's keys end no earlier than those of the row before)
+        const int from = it.row0 + q * TILE;
+        it.tiles[q] = from < doc.q1 ? (keys_end(p.c, doc, min(from + TILE, doc.q1) - 1) - doc.k0 + TILE - 1) / TILE : 0;
+    }
+    it.state = 1;
+    return true;
+}
+// Ask for the number of a block that no CTA has begun (one thread; 16 bytes to `dst`, counted on `bar`).
+__device__ __forceinline__ void ask_block(uint32_t dst, uint32_t bar) {
+    mbar_arrive_expect_tx(bar, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(dst), "r"(bar) : "memory");
+}
+// The answer: the block's number, or -1: all have begun (then none may be asked for any more).
+__device__ __forceinline__ int block_answer(uint32_t src) {
+    int w;
+    asm volatile(
+        "{\n\t.reg .b128 r;\n\t.reg .pred p;\n\t"
+        "ld.shared.b128 r, [%1];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+        "mov.b32 %0, -1;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, r;\n\t}"
+        : "=&r"(w) : "r"(src) : "memory");
+    return w;
+}
 
 // O (this thread's row, D fp32 columns) times alpha, in place.  Out of line: it runs once in many tiles.
 template <int D>
@@ -165,14 +199,24 @@ __device__ __noinline__ void add_broken(uint32_t o_tmem, const uint16_t *v, long
     tmem_wait_st();
 }
 
-// tanh(y) / y as a polynomial in y^2 (interpolated at the Chebyshev nodes of [0, 1]): |error of tanh| < 1.2e-7 for |y| <= 1
-__device__ __forceinline__ float2 tanh_over_y(float2 z) {
-    float2 r = __ffma2_rn(make_float2(0.001038025097f, 0.001038025097f), z, make_float2(-0.006194324834f, -0.006194324834f));
-    r = __ffma2_rn(r, z, make_float2(0.02027970829f, 0.02027970829f));
-    r = __ffma2_rn(r, z, make_float2(-0.05345164637f, -0.05345164637f));
-    r = __ffma2_rn(r, z, make_float2(0.1332507615f, 0.1332507615f));
-    r = __ffma2_rn(r, z, make_float2(-0.3333282798f, -0.3333282798f));
-    return __ffma2_rn(r, z, make_float2(0.9999999486f, 0.9999999486f));
+// tanh(y) / y as a polynomial in z = y^2, 1 at 0 and elsewhere fitted so that tanh's largest error on |y| <= 0.9 is least: 1.5e-7 in fp32.
+// Odd degree with a negative leading term: +infinity comes out as -infinity, which is how keys that do not count are left out.
+constexpr float TANH_REACH = 0.9f;
+constexpr int TANH_WORDS = 7;   // scale / cap, and the coefficients times the cap in base 2
+__device__ __forceinline__ float tanh_word(const PackedParams &p, int i) {
+    constexpr float C[] = {0.f, -0.0035873405f, 0.01780440898f, -0.05235944574f, 0.1330328763f, -0.3333134449f, 1.f};
+    return i == 0 ? p.cap_in : p.cap_log2 * C[i];
+}
+// A pair of products as capped logits in base 2 plus `add`, within TANH_REACH of the cap; or anywhere, by exponential and division.
+__device__ __forceinline__ float2 capped_near(const float2 (&c)[TANH_WORDS], float2 x, float2 add) {
+    const float2 y = __fmul2_rn(x, c[0]), z = __fmul2_rn(y, y);
+    float2 r = c[1];
+#pragma unroll
+    for (int i = 2; i < TANH_WORDS; ++i) r = __ffma2_rn(r, z, c[i]);
+    return __ffma2_rn(y, r, add);
+}
+__device__ __forceinline__ float2 capped_any(const PackedParams &p, float2 x) {
+    return make_float2(capped(x.x * p.cap_in, p.cap_log2), capped(x.y * p.cap_in, p.cap_log2));
 }
 
 template <int D, bool FP16, bool CAP, int BIAS>
@@ -193,7 +237,9 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     const uint32_t tab_smem = ml_smem + C::ML_BYTES;
     const uint32_t mark_smem = tab_smem + 2 * TABLE_BYTES;
     Bars bars;
-    bars.kv_full = mark_smem + MARKS * 4;
+    const uint32_t item_smem = mark_smem + MARKS * 4, answer_smem = item_smem + SLOTS * 48;
+    const uint32_t tanh_smem = answer_smem + 16;
+    bars.kv_full = tanh_smem + TANH_BYTES;
     bars.kv_empty = bars.kv_full + 8 * C::STAGES;
     bars.kv_raw = bars.kv_empty + 8 * C::STAGES;
     bars.q_full = bars.kv_raw + 8 * C::STAGES;
@@ -208,6 +254,9 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     bars.tab_full = bars.s_req + 8 * NQ;
     bars.tab_empty = bars.tab_full + 16;
     bars.s_free = bars.tab_empty + 16;   // one place for S: one barrier, used by both tiles in turn
+    bars.item_full = bars.s_free + 16;
+    bars.item_empty = bars.item_full + 8 * SLOTS;
+    bars.asked = bars.item_empty + 8 * SLOTS;
 
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     volatile int *abort_ptr = &abort_flag;
@@ -235,7 +284,14 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             mbar_init(bars.tab_full + 8 * q, 1);
             mbar_init(bars.tab_empty + 8 * q, SOFTMAX_THREADS);
         }
-        mbar_init(bars.s_free, 128);
+        for (int i = 0; i < 2; ++i) mbar_init(bars.s_free + 8 * i, 4);   // a lane of each warp
+        for (int i = 0; i < SLOTS; ++i) {
+            mbar_init(bars.item_full + 8 * i, 1);
+            mbar_init(bars.item_empty + 8 * i, READERS);
+        }
+        mbar_init(bars.asked, 1);
+        if constexpr (CAP)
+            for (int i = 0; i < 2 * TANH_WORDS; ++i) asm volatile("st.shared.f32 [%0], %1;" ::"r"(tanh_smem + i * 4), "f"(tanh_word(p.c, i / 2)) : "memory");
         for (int i = 0; i < MARKS; ++i) asm volatile("st.shared.b32 [%0], %1;" ::"r"(mark_smem + i * 4), "r"(0) : "memory");
         fence_mbar_init();
     }
@@ -248,6 +304,17 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     tc_fence_after();
     const uint32_t tmem_base = tmem_base_slot;
 
+    // The next item of the stream, for a warp that reads them one after another; false: a wait ran out.
+    uint32_t slot = 0, slot_ph = 0;
+    auto next_item = [&](Item &it) {
+        if (!wait_all(bars.item_full + 8 * slot, slot_ph)) return false;
+        load_item(item_smem + 48 * slot, it);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars.item_empty + 8 * slot);
+        if (++slot == SLOTS) { slot = 0; slot_ph ^= 1u; }
+        return true;
+    };
+
     if (warp >= OUT_WARP) {
         reg_dealloc<REGS_OUT>();
         // ------------------------------------------------------------ epilogue of both query tiles
@@ -255,29 +322,33 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         const uint32_t lane_addr = ((uint32_t)((warp % 4) * 32)) << 16;
         const uint32_t stage = out_smem + (warp % 4) * 4096, my_row = stage + lane * 128;
         const int piece = lane & 7;
-        uint32_t phase = 0, item = 0;
+        uint32_t phase[NQ] = {0, 0}, item = 0;
         bool ok = true;
-        Cursor it; it.first_item(p);
+        Item it;
 #pragma unroll 1
-        for (; it.valid && ok; it.next_item(p)) {
+        while (ok) {
+            ok = next_item(it);
+            if (!ok || it.state == 0) break;
 #pragma unroll 1
             for (int q = 0; q < NQ && ok; ++q) {
                 const int q_row = it.row0 + q * TILE + row_in_tile;
-                const bool row_valid = q_row < it.doc.q1;
+                if (q_row - row_in_tile >= it.q1) break;
+                const bool row_valid = q_row < it.q1;
                 const long long lse_at = ((long long)it.b * p.c.H + it.h) * p.c.Lq + q_row;
                 uint16_t *gbase = p.c.out + it.b * p.c.os[0] + (long long)(q_row - lane) * p.c.os[1] + it.h * p.c.os[2];   // row 0 of this warp
                 float m = -INFINITY, l = 0.f;
-                const bool keys = it.tiles > 0;   // (no tile of an item without keys ever ran: O is not read)
+                const bool keys = it.tiles[q] > 0;   // (no tile of rows without keys ever ran: O is not read)
                 const uint32_t o_tmem = tmem_base + lane_addr + C::O_COL + q * D;
                 if (keys) {
-                    ok = wait_all(bars.ml_full + 8 * q, phase) && wait_all(bars.o_full + 8 * q, phase);
+                    ok = wait_all(bars.ml_full + 8 * q, phase[q]) && wait_all(bars.o_full + 8 * q, phase[q]);
+                    phase[q] ^= 1u;
                     if (!ok) break;
                     tc_fence_after();
                     asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(m), "=f"(l) : "r"(ml_smem + (q * TILE + row_in_tile) * 8) : "memory");
                     uint32_t mark;
                     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(mark) : "r"(mark_smem + (item % MARKS) * 4) : "memory");
                     if (mark == item + 1) {
-                        const int from = max(it.first_end, it.doc.k0), to = keys_end(p.c, it.doc, min(q_row, it.doc.q1 - 1));
+                        const int from = max(it.first_end, it.k0), to = keys_end(p.c, it.doc(), min(q_row, it.q1 - 1));
                         add_broken<D, FP16>(o_tmem, p.c.v + it.b * p.c.vs[0] + it.h / p.c.rep * p.c.vs[2], p.c.vs[1], from, to);
                     }
                 }
@@ -285,7 +356,7 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                 if (row_valid && p.c.lse != nullptr) p.c.lse[lse_at] = l == 0.f ? -INFINITY : LN2 * (m + log2f(l));
                 // Rows leave through warp-private shared memory: 128 bytes of every row at a time (swizzled), read back so
                 // that 8 lanes hold the 128 contiguous bytes of one row.
-                const int rows_left = it.doc.q1 - (q_row - lane);   // valid rows of this warp's 32
+                const int rows_left = it.q1 - (q_row - lane);   // valid rows of this warp's 32
 #pragma unroll OUT_UNROLL
                 for (int c0 = 0; c0 < D; c0 += 64) {
 #pragma unroll OUT_UNROLL
@@ -324,10 +395,7 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                     __syncwarp();
                 }
             }
-            if (it.tiles > 0) {
-                phase ^= 1u;
-                ++item;
-            }
+            if (it.all() > 0) ++item;
         }
         if (!ok && lane == 0) give_up(abort_ptr, p.c.status);
     } else if (warp >= TMA_WARP) {
@@ -336,12 +404,53 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             // -------------------------------------------------------- TMA producer
             // (This warp and the MMA warps run their loops as whole warps and one elected lane issues: what the instructions take then
             // stays in uniform registers.)
-            uint32_t st = 0, ph = 0, q_ph = 0;
-            bool ok = true;
-            auto load_q = [&](const Cursor &it) {
+            uint32_t st = 0, ph = 0, q_ph[NQ] = {0, 0}, answer_ph = 0;
+            bool ok = true, asked = false, over = false;   // over: all blocks have begun
+            auto ask = [&]() {
+                if (asked || over) return;
+                if (elect_lane()) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the answer before has been read)
+                    ask_block(answer_smem, bars.asked);
+                }
+                __syncwarp();
+                asked = true;
+            };
+            bool first = true;
+            auto publish = [&](const Item &it) {
+                ok = wait_all(bars.item_empty + 8 * slot, slot_ph ^ 1u);
+                if (!ok) return;
+                if (lane == 0) {
+                    store_item(item_smem + 48 * slot, it);
+                    mbar_arrive(bars.item_full + 8 * slot);
+                }
+                __syncwarp();
+                if (++slot == SLOTS) { slot = 0; slot_ph ^= 1u; }
+            };
+            // The next item with keys, after those without for the epilogue alone; `state` 0: none.
+            auto produce = [&](Item &it) {
 #pragma unroll 1
+                do {
+                    int w = blockIdx.x;
+                    if (!first) {
+                        ask();
+                        ok = wait_all(bars.asked, answer_ph);
+                        if (!ok) return;
+                        answer_ph ^= 1u;
+                        w = block_answer(answer_smem);
+                        asked = false;
+                        __syncwarp();
+                    }
+                    first = false;
+                    over = w < 0;
+                    it = Item{};
+                    if (over || item_of(p, w, it)) publish(it);
+                } while (ok && !over && it.all() == 0);
+            };
+            auto load_q = [&](const Item &it) {
+#pragma unroll
                 for (int q = 0; q < NQ; ++q) {
-                    ok = ok && wait_all(bars.q_empty + 8 * q, q_ph ^ 1u);
+                    if (it.tiles[q] == 0) continue;
+                    ok = ok && wait_all(bars.q_empty + 8 * q, q_ph[q] ^ 1u);
                     if (!ok) return;
                     if (elect_lane()) {
                         mbar_arrive_expect_tx(bars.q_full + 8 * q, C::TILE_BYTES);
@@ -351,79 +460,102 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                                         it.h * p.mq.mul_h, it.row0 + q * TILE, it.b * p.mq.mul_b);
                     }
                     __syncwarp();
+                    q_ph[q] ^= 1u;
                 }
-                q_ph ^= 1u;
             };
-            auto load_kv = [&](const Cursor &it, bool is_k) {
+            auto load_kv = [&](const Item &it, int key, bool is_k) {
                 ok = ok && wait_all(bars.kv_empty + 8 * st, ph ^ 1u);
                 if (!ok) return;
                 // V with keys that do not count for all rows lands on a barrier of its own; the mending warp passes it on
-                const uint32_t bar = (!is_k && it.mended(p, it.key0()) ? bars.kv_raw : bars.kv_full) + 8 * st;
+                const uint32_t bar = (!is_k && it.mended(p.c, key) ? bars.kv_raw : bars.kv_full) + 8 * st;
                 const int hk = p.c.rep == 1 ? it.h : it.h / p.c.rep;
                 const int h = hk * (is_k ? p.mk.mul_h : p.mv.mul_h), b = it.b * (is_k ? p.mk.mul_b : p.mv.mul_b);
                 if (elect_lane()) {
                     mbar_arrive_expect_tx(bar, C::TILE_BYTES);
 #pragma unroll
                     for (int hf = 0; hf < C::NHALF; ++hf)
-                        tma_load_4d(kv_smem + st * C::TILE_BYTES + hf * C::HALF_BYTES, is_k ? &tmap_k : &tmap_v, bar, hf * 64, h, it.key0(), b);
+                        tma_load_4d(kv_smem + st * C::TILE_BYTES + hf * C::HALF_BYTES, is_k ? &tmap_k : &tmap_v, bar, hf * 64, h, key, b);
                 }
                 __syncwarp();
                 if (++st == C::STAGES) { st = 0; ph ^= 1u; }
             };
-            Cursor nxt; nxt.first_item(p);
-            nxt.skip_empty(p);
-            Cursor cur = nxt;
-            bool have = false;   // a tile whose V is still to be loaded
+            Item cur, nxt;
+            produce(nxt);
+            if (ok && nxt.state != 0) {   // (the other items' first K precedes the last V of the item before)
+                load_kv(nxt, nxt.k0, true);
+                load_q(nxt);
+            }
 #pragma unroll 1
-            while (ok && (have || nxt.valid)) {
-#pragma unroll 1
-                for (int v = 0; v < 2; ++v)   // K of the next tile, V of this one
-                    if (v ? have : nxt.valid) load_kv(v ? cur : nxt, v == 0);
-                // (after this V: nothing that Q's place waits for is behind it)
-                if (nxt.valid && nxt.t == 0) load_q(nxt);
+            while (ok && nxt.state != 0) {
                 cur = nxt;
-                have = nxt.valid;
-                if (have) nxt.advance(p);
+                const int n = cur.all();
+#pragma unroll 1
+                for (int t = 0; t < n && ok; ++t) {
+                    if (t + 2 >= n) ask();   // (so late, because a block taken is one that no other SM can begin)
+                    if (t + 1 < n) {
+                        load_kv(cur, cur.k0 + (t + 1) * TILE, true);
+                        load_kv(cur, cur.k0 + t * TILE, false);
+                    } else {
+                        produce(nxt);
+                        if (nxt.state != 0) load_kv(nxt, nxt.k0, true);
+                        if (ok && nxt.state != 0 && nxt.all() <= 2) ask();
+                        load_kv(cur, cur.k0 + t * TILE, false);
+                        // (after this V: nothing that Q's place waits for is behind it)
+                        if (nxt.state != 0) load_q(nxt);
+                    }
+                }
             }
             if (!ok && lane == 0) give_up(abort_ptr, p.c.status);
+            if (!ok && asked) wait_all_lanes(bars.asked, answer_ph, abort_ptr);   // (an answer under way comes within microseconds; see settle_if)
         } else if (warp == MEND_WARP) {
             // -------------------------------------------------------- V's rows that do not count for all; bias tables
             uint32_t raw_ph = 0;   // parity of every stage's kv_raw (one bit each)
             bool ok = true;
             // the head's table for item number n into place n & 1, once the softmax is done with item n - 2
-            auto fill_table = [&](const Cursor &it, uint32_t n) {
+            auto fill_table = [&](const Item &it, uint32_t n) {
                 if constexpr (BIAS == BIAS_TABLE) {
                     ok = ok && wait_all(bars.tab_empty + 8 * (n & 1u), ((n >> 1) & 1u) ^ 1u);
                     if (!ok) return;
                     const float *src = p.c.table + (long long)it.h * (2 * p.c.far + 1);
                     const uint32_t dst = tab_smem + (n & 1u) * TABLE_BYTES;
-                    const int count = 2 * p.c.far + 1 + 2 * TABLE_PAD;
-#pragma unroll 4
+                    const int count = 2 * p.c.far + 1;
+#pragma unroll 9
                     for (int i = lane; i < count; i += 32)
-                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(dst + i * 4), "f"(__ldg(src + min(max(i - TABLE_PAD, 0), 2 * p.c.far)) * LOG2E) : "memory");
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(dst + (TABLE_PAD + i) * 4), "f"(__ldg(src + i) * LOG2E) : "memory");
+                    const float low = __ldg(src) * LOG2E, high = __ldg(src + count - 1) * LOG2E;
+#pragma unroll 4
+                    for (int i = lane; i < TABLE_PAD; i += 32) {
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(dst + i * 4), "f"(low) : "memory");
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(dst + (TABLE_PAD + count + i) * 4), "f"(high) : "memory");
+                    }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bars.tab_full + 8 * (n & 1u));
                 }
             };
-            Cursor it; it.first_item(p);
-            it.skip_empty(p);
+            auto next_keys = [&](Item &it) {   // the next item with keys
+                do ok = next_item(it);
+                while (ok && it.state != 0 && it.all() == 0);
+            };
+            Item cur, nxt;
             uint32_t place = 0, n = 0;   // K/V tiles of the stream so far; items
-            if (it.valid) fill_table(it, 0);
+            next_keys(nxt);
+            if (ok && nxt.state != 0) fill_table(nxt, 0);
 #pragma unroll 1
-            while (it.valid && ok) {
-                const Cursor cur = it;
-                it.next_item(p);
-                it.skip_empty(p);
-                if (BIAS == BIAS_TABLE && it.valid) fill_table(it, n + 1);
-                if (!ok) break;
+            while (ok && nxt.state != 0) {
+                cur = nxt;
                 // V of tile t is number 2 t + 2 of the item's K and V tiles in the stream's order (the last, which the next item's first
                 // K precedes, likewise; with no next item it is number 2 t + 1), counted from the item's first K
-                const int last = cur.tiles - 1;
+                const int last = cur.all() - 1;
 #pragma unroll 1
-                for (int t = max(0, (cur.first_end - cur.doc.k0) / TILE); t <= last && ok; ++t) {
-                    const int key0 = cur.doc.k0 + t * TILE;
-                    if (!cur.mended(p, key0)) continue;
-                    const uint32_t st = (place + 2 * t + 1 + (t < last || it.valid ? 1u : 0u)) % C::STAGES;
+                for (int t = min(max(0, (cur.first_end - cur.k0) / TILE), last); t <= last && ok; ++t) {
+                    if (t == last) {
+                        next_keys(nxt);
+                        if (ok && nxt.state != 0) fill_table(nxt, n + 1);
+                        if (!ok) break;
+                    }
+                    const int key0 = cur.k0 + t * TILE;
+                    if (!cur.mended(p.c, key0)) continue;
+                    const uint32_t st = (place + 2 * t + 1 + (t < last || nxt.state != 0 ? 1u : 0u)) % C::STAGES;
                     ok = wait_all(bars.kv_raw + 8 * st, (raw_ph >> st) & 1u);
                     if (!ok) break;
                     raw_ph ^= 1u << st;
@@ -433,7 +565,7 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                         const int r = 32 * i + lane, key = key0 + r;
                         if (key < cur.first_end || key >= p.c.Lk) continue;   // (behind Lk there are zeros already: the tensor map ends there)
                         const uint32_t row = kv_smem + st * C::TILE_BYTES + r * 128;
-                        const bool none = key >= cur.doc.k1;
+                        const bool none = key >= cur.k1;
 #pragma unroll 2
                         for (int c = 0; c < C::NHALF * 8; ++c) {   // (pieces in a lane's own order: the rows' banks coincide)
                             const uint32_t a = row + (c >> 3) * C::HALF_BYTES + (((c + lane) & 7) << 4);
@@ -458,7 +590,7 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bars.kv_full + 8 * st);
                 }
-                place += 2 * cur.tiles;
+                place += 2 * (last + 1);
                 ++n;
             }
             if (!ok && lane == 0) give_up(abort_ptr, p.c.status);
@@ -475,7 +607,7 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) {
                     const uint32_t koff = ((kk / 4) * C::HALF_BYTES + (kk % 4) * 32) >> 4;
-                    mma_ss(tmem_base + C::S_COL, qdesc + koff, b0 + koff, IDESC_QK, kk > 0 ? 1u : 0u);
+                    mma_ss(tmem_base + C::S_COL + (C::S_PLACES == 2 ? mq * 128 : 0), qdesc + koff, b0 + koff, IDESC_QK, kk > 0 ? 1u : 0u);
                 }
             };
             // O (+)= P V
@@ -487,38 +619,59 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                 for (int kk = 0; kk < TILE / 16; ++kk)
                     mma_ts(d, a + kk * 8, b0 + (uint64_t)((kk * 2048) >> 4), IDESC_PV, (accumulate || kk > 0) ? 1u : 0u);
             };
-            // The one place for S is used by the tiles in turn, tile 0 first: a phase of s_free is one read of S.
-            const uint32_t s_turn = mq ? 0u : 1u;
-            uint32_t st = 0, ph = 0, q_phase = 0, of_phase = 0, t_phase = 0;   // place: K/V tiles of the stream so far
+            // One place for S is used by the tiles in turn, tile 0 first: a phase of s_free is one read of S, and a query tile that does
+            // not want the item's tile of keys passes its turn on.  Two places: a phase of the tile's own s_free is one read.
+            const uint32_t s_free = bars.s_free + (C::S_PLACES == 2 ? 8 * mq : 0);
+            uint32_t s_turn = C::S_PLACES == 2 || mq == 0 ? 1u : 0u;
+            uint32_t st = 0, ph = 0, q_phase = 0, of_phase = 0, t_phase = 0;   // st, ph: the stream's next K/V tile
             bool ok = true;
-            Cursor nxt; nxt.first_item(p);
-            nxt.skip_empty(p);
-            int tiles = 1;                                // of the current item; before the first: a step without a P V
+            Item it;
+            auto next_keys = [&]() {   // the next item with keys
+                do ok = next_item(it);
+                while (ok && it.state != 0 && it.all() == 0);
+            };
+            next_keys();
+            int tiles = 1, mine = 0;                      // of the current item; before the first: a step without a P V
             bool have = false;
 #pragma unroll 1
-            while (ok && (have || nxt.valid)) {
-                const bool next_item = nxt.valid, next_single = nxt.tiles == 1;
+            while (ok && (have || it.state != 0)) {
 #pragma unroll 1
                 for (int k = 0; k < tiles; ++k) {
-                    const bool within = k + 1 < tiles, more = within || next_item;
+                    const bool within = k + 1 < tiles;
+                    if (have && !within) {   // (the producer has left it there before it loaded this item's last tiles)
+                        next_keys();
+                        if (!ok) break;
+                    }
+                    const bool more = within || it.state != 0;
+                    const int next_mine = mq == 0 ? it.tiles[0] : it.tiles[1];
                     uint32_t stv = st, phv = ph;   // V of this tile
                     if (more && ++stv == C::STAGES) { stv = 0; phv ^= 1u; }
-                    if (have) ok = wait_all(bars.s_req + 8 * mq, t_phase);   // the softmax will be ready for its next S shortly
+                    if (C::S_PLACES == 1 && k < mine) ok = wait_all(bars.s_req + 8 * mq, t_phase);   // the softmax will be ready for its next S shortly
                     if (!ok) break;
                     if (more) {   // the next tile's Q K^T first: the softmax waits for it
-                        bool r = wait(bars.kv_full + 8 * st, ph) && wait(bars.s_free, s_turn);
-                        if (!within) {
+                        const bool use = within ? k + 1 < mine : next_mine > 0;
+                        bool r = wait(bars.kv_full + 8 * st, ph);
+                        if (use || C::S_PLACES == 1) {
+                            r = r && wait(s_free, s_turn);
+                            if (C::S_PLACES == 2) s_turn ^= 1u;
+                        }
+                        if (!within && use) {
                             r = r && wait(bars.q_full + 8 * mq, q_phase);
                             q_phase ^= 1u;
                         }
                         ok = __all_sync(0xFFFFFFFFu, r) != 0;
                         if (!ok) break;
                         tc_fence_after();
-                        if (elect_lane()) {
-                            issue_qk(st);
-                            tc_commit(bars.s_full + 8 * mq);
-                            tc_commit(bars.kv_empty + 8 * st);
-                            if (within ? k + 2 == tiles : next_single) tc_commit(bars.q_empty + 8 * mq);   // its item's last Q K^T
+                        if (use) {
+                            if (elect_lane()) {
+                                issue_qk(st);
+                                tc_commit(bars.s_full + 8 * mq);
+                                tc_commit(bars.kv_empty + 8 * st);
+                                if (within ? k + 2 == mine : next_mine == 1) tc_commit(bars.q_empty + 8 * mq);   // its item's last Q K^T
+                            }
+                        } else {
+                            if (C::S_PLACES == 1 && lane < 4) mbar_arrive(s_free);
+                            if (lane == 0) mbar_arrive(bars.kv_empty + 8 * st);
                         }
                         __syncwarp();
                     }
@@ -527,8 +680,9 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                     if (!have) break;
                     // V has landed (and is mended), P is stored, and the epilogue of the item before has drained O
                     {
-                        bool r = wait(bars.kv_full + 8 * stv, phv) && wait(bars.p_full + 8 * mq, t_phase);
-                        if (k == 0) {
+                        bool r = wait(bars.kv_full + 8 * stv, phv);
+                        if (k < mine) r = r && wait(bars.p_full + 8 * mq, t_phase);
+                        if (k == 0 && mine > 0) {
                             r = r && wait(bars.o_free + 8 * mq, of_phase ^ 1u);
                             of_phase ^= 1u;
                         }
@@ -536,22 +690,23 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                     }
                     if (!ok) break;
                     tc_fence_after();
-                    if (elect_lane()) {
-                        issue_pv(stv, k > 0);
-                        tc_commit(bars.pv_done + 8 * mq);
-                        if (!within) tc_commit(bars.o_full + 8 * mq);
-                        tc_commit(bars.kv_empty + 8 * stv);
+                    if (k < mine) {
+                        if (elect_lane()) {
+                            issue_pv(stv, k > 0);
+                            tc_commit(bars.pv_done + 8 * mq);
+                            if (k + 1 == mine) tc_commit(bars.o_full + 8 * mq);
+                            tc_commit(bars.kv_empty + 8 * stv);
+                        }
+                        t_phase ^= 1u;
+                    } else if (lane == 0) {
+                        mbar_arrive(bars.kv_empty + 8 * stv);
                     }
                     __syncwarp();
-                    t_phase ^= 1u;
                     if (++st == C::STAGES) { st = 0; ph ^= 1u; }
                 }
-                have = next_item;
-                if (have) {   // (the item after is looked up while this one's first tiles run)
-                    tiles = nxt.tiles;
-                    nxt.t = tiles - 1;
-                    nxt.advance(p);
-                }
+                have = it.state != 0;
+                tiles = it.all();
+                mine = mq == 0 ? it.tiles[0] : it.tiles[1];
             }
             if (!ok && lane == 0) give_up(abort_ptr, p.c.status);
         }
@@ -561,28 +716,43 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         const int q = warp / 4;
         const int row_in_tile = (warp % 4) * 32 + lane;
         const uint32_t lane_addr = ((uint32_t)((warp % 4) * 32)) << 16;
-        const uint32_t s_tmem = tmem_base + lane_addr + C::S_COL;
+        const uint32_t s_tmem = tmem_base + lane_addr + C::S_COL + (C::S_PLACES == 2 ? q * 128 : 0);
+        const uint32_t s_free = bars.s_free + (C::S_PLACES == 2 ? 8 * q : 0);
         const uint32_t p_tmem = tmem_base + lane_addr + C::P_COL + q * C::P_STRIDE;
         const uint32_t o_tmem = tmem_base + lane_addr + C::O_COL + q * D;
-        uint32_t s_phase = 0, pv_phase = 0, p_items = 0;   // p_items: items handed to the epilogue
+        uint32_t s_phase = 0, pv_phase = 0, p_items = 0, tables = 0;   // p_items: items handed to the epilogue; tables: items with keys
+        // (from shared memory, so that they stay in registers: as literals they are moved there again for every use)
+        float2 cap_c[TANH_WORDS];
+        if constexpr (CAP) {
+#pragma unroll
+            for (int i = 0; i < TANH_WORDS; ++i) asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(cap_c[i].x), "=f"(cap_c[i].y) : "r"(tanh_smem + i * 8) : "memory");
+        }
         bool ok = true, p_stored = false;   // p_stored: P's columns hold an earlier tile's P, which its P V may still read
-        Cursor it; it.first_item(p);
-        it.skip_empty(p);
 #pragma unroll 1
-        while (it.valid && ok) {
+        while (ok) {
+            int tiles, end, place, head;
+            {
+                Item it;
+                ok = next_item(it);
+                if (!ok || it.state == 0) break;
+                if (it.all() == 0) continue;
+                tiles = q == 0 ? it.tiles[0] : it.tiles[1];
+                const int row = it.row0 + q * TILE + row_in_tile;
+                end = keys_end(p.c, it.doc(), min(row, it.q1 - 1)) - it.k0;   // keys of this row
+                place = row + it.shift - it.k0;                              // of the row, among the document's keys
+                head = it.h;
+            }
             float m_used = -INFINITY, l_sum = 0.f;
-            const int row = it.row0 + q * TILE + row_in_tile;
-            const int end = keys_end(p.c, it.doc, min(row, it.doc.q1 - 1)) - it.doc.k0;   // keys of this row
-            const int place = row + it.doc.shift - it.doc.k0, tile_place = place - row_in_tile;   // of the row, of the tile's first
+            const int tile_place = place - row_in_tile;   // of the tile's first row
             float slope = 0.f;
-            if constexpr (BIAS == BIAS_SLOPES) slope = __ldg(p.c.slopes + it.h) * LOG2E;
+            if constexpr (BIAS == BIAS_SLOPES) slope = __ldg(p.c.slopes + head) * LOG2E;
             uint32_t tab = 0;   // of distance 0
             if constexpr (BIAS == BIAS_TABLE) {
-                tab = tab_smem + (p_items & 1u) * TABLE_BYTES + (p.c.far + TABLE_PAD) * 4;
-                ok = wait_all(bars.tab_full + 8 * (p_items & 1u), (p_items >> 1) & 1u);
+                tab = tab_smem + (tables & 1u) * TABLE_BYTES + (p.c.far + TABLE_PAD) * 4;
+                ok = wait_all(bars.tab_full + 8 * (tables & 1u), (tables >> 1) & 1u);
             }
 #pragma unroll 1
-            for (int t = 0; t < it.tiles; ++t) {
+            for (int t = 0; t < tiles; ++t) {
                 ok = ok && wait_all(bars.s_full + 8 * q, s_phase);
                 if (!ok) break;
                 s_phase ^= 1u;
@@ -594,74 +764,100 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                 tmem_ld_x32(s_tmem + 96, s[3]);
                 tmem_wait_ld();
                 tc_fence_before();
-                mbar_arrive(bars.s_free);   // S has been read: the next Q K^T may overwrite it
+                __syncwarp();
+                if (lane == 0) mbar_arrive(s_free);   // S has been read: the next Q K^T may overwrite it
                 auto sv = [&](int c) -> uint32_t & { return s[c >> 5][c & 31]; };
-                // ---- logits in base 2, where the products are not them up to a factor
+                auto pair = [&](int c) { return make_float2(__uint_as_float(sv(c)), __uint_as_float(sv(c + 1))); };
+                auto put = [&](int c, float2 x) {
+                    sv(c) = __float_as_uint(x.x);
+                    sv(c + 1) = __float_as_uint(x.y);
+                };
+                // The logit of column c, in base 2, is what s holds times `factor`, plus `add`, plus c / 8 times `step8` (slopes); or, if
+                // `fused`, what s holds capped.
+                float factor = p.c.scale_log2, add = 0.f, step8 = 0.f;
+                bool fused = false;
+                const int here = end - t * TILE;
+                const bool masked = __any_sync(0xFFFFFFFFu, here < TILE);   // some key does not count for some row
+                auto mask = [&](uint32_t value) {
+#pragma unroll
+                    for (int c = 0; c < 128; ++c)
+                        if (c >= here) sv(c) = value;
+                };
+                auto largest = [&](auto &&of) {   // four chains of three-input max; NaN is left out
+                    float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int c = 0; c < 128; c += 2) mx4[(c >> 1) & 3] = fmax3(mx4[(c >> 1) & 3], of(__uint_as_float(sv(c))), of(__uint_as_float(sv(c + 1))));
+                    return fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+                };
+                float m_tile;
                 if constexpr (CAP) {
-                    float top4[4] = {0.f, 0.f, 0.f, 0.f};
+                    if (masked) mask(0x7FFFFFFFu);   // NaN
+                    const bool near = __all_sync(0xFFFFFFFFu, !(largest([](float x) { return fabsf(x); }) * p.c.cap_in > TANH_REACH)) != 0;
+                    if (BIAS == BIAS_NONE && near) {
+                        // tanh does not change the order, so that the maximum is known before any logit is capped
+                        m_tile = capped(largest([](float x) { return x; }) * p.c.cap_in, p.c.cap_log2);
+                        if (masked) mask(0x7F800000u);   // (+infinity: see capped_near)
+                        fused = true;
+                    } else if (near) {
 #pragma unroll
-                    for (int c = 0; c < 128; c += 8)
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) top4[u] = fmax3(top4[u], fabsf(__uint_as_float(sv(c + 2 * u))), fabsf(__uint_as_float(sv(c + 2 * u + 1))));
-                    const float y_top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * p.c.cap_in;
-                    if (__all_sync(0xFFFFFFFFu, y_top <= 1.0f)) {
-                        const float2 in2 = make_float2(p.c.cap_in, p.c.cap_in), sc2 = make_float2(p.c.scale_log2, p.c.scale_log2);
-#pragma unroll
-                        for (int c = 0; c < 128; c += 2) {
-                            const float2 x = make_float2(__uint_as_float(sv(c)), __uint_as_float(sv(c + 1))), y = __fmul2_rn(x, in2);
-                            const float2 r = __fmul2_rn(__fmul2_rn(x, sc2), tanh_over_y(__fmul2_rn(y, y)));
-                            sv(c) = __float_as_uint(r.x);
-                            sv(c + 1) = __float_as_uint(r.y);
-                        }
+                        for (int c = 0; c < 128; c += 2) put(c, capped_near(cap_c, pair(c), make_float2(0.f, 0.f)));
                     } else {
 #pragma unroll
-                        for (int c = 0; c < 128; ++c) sv(c) = __float_as_uint(capped(__uint_as_float(sv(c)) * p.c.cap_in, p.c.cap_log2));
+                        for (int c = 0; c < 128; c += 2) put(c, capped_any(p.c, pair(c)));
                     }
+                    factor = 1.f;
                 }
-                constexpr bool IN_BASE_2 = CAP || BIAS != BIAS_NONE;
-                const float unit = CAP ? 1.0f : p.c.scale_log2;
                 if constexpr (BIAS == BIAS_TABLE) {
                     const int d0 = t * TILE - tile_place;   // of the tile's first key and row
                     if (d0 - (TILE - 1) > p.c.far || d0 + (TILE - 1) < -p.c.far) {   // one value for all
-                        float add;
                         asm volatile("ld.shared.f32 %0, [%1];" : "=f"(add) : "r"(tab + (d0 > 0 ? p.c.far : -p.c.far) * 4));
-                        const float2 add2 = make_float2(add, add), u2 = make_float2(unit, unit);
-#pragma unroll
-                        for (int c = 0; c < 128; c += 2) {
-                            const float2 x = __ffma2_rn(make_float2(__uint_as_float(sv(c)), __uint_as_float(sv(c + 1))), u2, add2);
-                            sv(c) = __float_as_uint(x.x);
-                            sv(c + 1) = __float_as_uint(x.y);
-                        }
                     } else {
                         const uint32_t at = tab + (t * TILE - place) * 4;
 #pragma unroll
                         for (int c = 0; c < 128; ++c) {
-                            float add;
-                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(add) : "r"(at + 4 * c));   // (volatile: behind the wait for the table)
-                            sv(c) = __float_as_uint(fmaf(__uint_as_float(sv(c)), unit, add));
+                            float bias;
+                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(bias) : "r"(at + 4 * c));   // (volatile: behind the wait for the table)
+                            sv(c) = __float_as_uint(fmaf(__uint_as_float(sv(c)), factor, bias));
                         }
+                        factor = 1.f;
                     }
                 }
                 if constexpr (BIAS == BIAS_SLOPES) {
                     const float d = (float)(t * TILE - place);
+                    const int d0 = t * TILE - tile_place;
+                    if (d0 + (TILE - 1) <= 0 || d0 >= TILE - 1) {   // all keys before all rows, or behind: linear in c, eight values and a step
+                        const float by = d0 > 0 ? -slope : slope;
+                        float2 b8[4];
 #pragma unroll
-                    for (int c = 0; c < 128; ++c) sv(c) = __float_as_uint(fmaf(-slope, fabsf(d + (float)c), __uint_as_float(sv(c)) * unit));
+                        for (int u = 0; u < 4; ++u) b8[u] = make_float2(by * (float)(2 * u), by * (float)(2 * u + 1));
+                        const float2 f2 = make_float2(factor, factor);
+#pragma unroll
+                        for (int c = 0; c < 128; c += 2) put(c, __ffma2_rn(pair(c), f2, b8[(c >> 1) & 3]));
+                        add = by * d;
+                        step8 = by * 8.f;
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 128; ++c) sv(c) = __float_as_uint(fmaf(-slope, fabsf(d + (float)c), __uint_as_float(sv(c)) * factor));
+                    }
+                    factor = 1.f;
                 }
-                // ---- keys that do not count for this row
-                const int here = end - t * TILE;
-                if (__any_sync(0xFFFFFFFFu, here < TILE)) {
+                if (!fused) {
+                    if (masked) mask(0xFF800000u);   // -infinity
+                    if constexpr (BIAS == BIAS_SLOPES) {
+                        m_tile = -INFINITY;
 #pragma unroll
-                    for (int c = 0; c < 128; ++c)
-                        if (c >= here) sv(c) = 0xFF800000u;
+                        for (int c = 0; c < 128; c += 8) {
+                            float m8 = fmaxf(__uint_as_float(sv(c)), __uint_as_float(sv(c + 1)));
+#pragma unroll
+                            for (int u = 1; u < 4; ++u) m8 = fmax3(m8, __uint_as_float(sv(c + 2 * u)), __uint_as_float(sv(c + 2 * u + 1)));
+                            m_tile = fmaxf(m_tile, fmaf(step8, (float)(c / 8), m8));
+                        }
+                        m_tile += add;
+                    } else {
+                        m_tile = largest([](float x) { return x; });
+                        m_tile = BIAS == BIAS_TABLE ? fmaf(m_tile, factor, add) : m_tile * factor;
+                    }
                 }
-                float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};   // four chains of three-input max
-#pragma unroll
-                for (int c = 0; c < 128; c += 8) {
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) mx4[u] = fmax3(mx4[u], __uint_as_float(sv(c + 2 * u)), __uint_as_float(sv(c + 2 * u + 1)));
-                }
-                const float factor = IN_BASE_2 ? 1.0f : p.c.scale_log2;
-                const float m_tile = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * factor;
                 bool p_place_free = !p_stored;
                 if (t == 0) {
                     m_used = packed_reference<FP16>(p.c, m_tile);
@@ -680,22 +876,30 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                     scale_o<D>(o_tmem, alpha);
                 }
                 const float m_ref = m_used == -INFINITY ? 0.f : m_used;   // no key so far: every P is 0
-                const float2 sc2 = make_float2(factor, factor), nm2 = make_float2(-m_ref, -m_ref);
+                const float nm = add - m_ref;
                 float2 rs4[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                 uint32_t pk2[2][32];   // P as packed 16-bit pairs (even key in the low half)
-                auto exps = [&](int part) {   // 32 keys
+                auto exps_of = [&](int part, auto &&logits) {   // 32 keys
 #pragma unroll
                     for (int c = part * 32; c < part * 32 + 32; c += 2) {
-                        const float2 x2 = make_float2(__uint_as_float(sv(c)), __uint_as_float(sv(c + 1)));
-                        const float2 x = IN_BASE_2 ? __fadd2_rn(x2, nm2) : __ffma2_rn(x2, sc2, nm2);
+                        const float2 x = logits(c);
                         const float2 pp = make_float2(ex2_approx(x.x), ex2_approx(x.y));
                         rs4[(c >> 1) & 3] = __fadd2_rn(rs4[(c >> 1) & 3], pp);
                         pk2[c >> 6][(c >> 1) & 31] = pack_p<FP16>(pp.x, pp.y);
                     }
                 };
+                auto exps = [&](int part) {
+                    if constexpr (BIAS == BIAS_SLOPES) {
+                        exps_of(part, [&](int c) { const float n = fmaf(step8, (float)(c / 8), nm); return __fadd2_rn(pair(c), make_float2(n, n)); });
+                    } else {
+                        const float2 nm2 = make_float2(nm, nm), f2 = make_float2(factor, factor);
+                        if (fused) exps_of(part, [&](int c) { return capped_near(cap_c, pair(c), nm2); });
+                        else exps_of(part, [&](int c) { return __ffma2_rn(pair(c), f2, nm2); });
+                    }
+                };
                 exps(0);
                 exps(1);
-                mbar_arrive(bars.s_req + 8 * q);   // half of the exponentials are done: ask for the next S
+                if (C::S_PLACES == 1) mbar_arrive(bars.s_req + 8 * q);   // half of the exponentials are done: ask for the next S
                 exps(2);
                 exps(3);
                 if (!p_place_free) {   // the P V of the tile before (of this item or the last) is done with P's columns
@@ -714,16 +918,18 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                 mbar_arrive(bars.p_full + 8 * q);
             }
             if (!ok) break;
-            if constexpr (BIAS == BIAS_TABLE) mbar_arrive(bars.tab_empty + 8 * (p_items & 1u));
+            if constexpr (BIAS == BIAS_TABLE) {
+                mbar_arrive(bars.tab_empty + 8 * (tables & 1u));
+                ++tables;
+            }
+            if (tiles == 0) continue;
             // (m, l) for the epilogue, once it has read the item before's: it hands O back behind that, and with more than one tile
             // P V of the second has waited for it.  Without this wait ml_full could complete twice before the epilogue looks.
-            if (p_items > 0 && it.tiles == 1) ok = wait_all(bars.o_free + 8 * q, (p_items - 1) & 1u);
+            if (p_items > 0 && tiles == 1) ok = wait_all(bars.o_free + 8 * q, (p_items - 1) & 1u);
             if (!ok) break;
             ++p_items;
             asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(ml_smem + (q * TILE + row_in_tile) * 8), "f"(m_used), "f"(l_sum) : "memory");
             mbar_arrive(bars.ml_full + 8 * q);
-            it.t = it.tiles - 1;
-            it.advance(p);
         }
         if (!ok && lane == 0) give_up(abort_ptr, p.c.status);
     }
@@ -780,7 +986,7 @@ cudaError_t launch_packed_tiles(const PackedParams &c, int D, bool fp16, const O
     const long long items = (long long)c.B * c.H * p.blocks;
     if (items > 0x3FFFFFFF) return cudaErrorInvalidValue;
     p.items = (int)items;
-    const int grid = p.items < dev.sms ? p.items : dev.sms;
+    const int grid = p.items;
     CUtensorMap tq, tk, tv;
     if (!encode(dev.encode_tiled, &tq, &p.mq, c.q, c.qs, c.B, c.Lq, c.H, D, fp16) ||
         !encode(dev.encode_tiled, &tk, &p.mk, c.k, c.ks, c.B, c.Lk, c.Hkv, D, fp16) ||
