@@ -84,6 +84,62 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// t for the tiles where the rows are not very many: 16 rows x 16 of the rank per block, for each pair of (16 rows, segment that it meets),
+// found on a staircase as in adapter_tiles.cu.  K is split over the warps as above.  Small blocks without tensor memory fit an SM beside a CTA
+// of the projection, which so begins with W at once: 64 rows through 5120 x 5120 with adapters of rank 16 took 27.7 us with the kernel of
+// tensor-memory tiles, 19.7 without adapters.
+template <bool FP16>
+__global__ void __launch_bounds__(ROWS_THREADS) shrink_blocks_kernel(const AdapterParams p) {
+    __shared__ float part[ROWS_WARPS][16][17];
+    let_next_start();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, j0 = blockIdx.y * 16;
+    int s, tile;
+    if (!pair_at(p, blockIdx.x, 16, s, tile)) return;   // (alike for the whole block)
+    const int row0 = tile * 16;
+    const Piece piece = piece_of(p, s, row0, min(row0 + 16, p.M));
+    if (piece.adapter < 0) return;
+    const int steps = (p.K + CHUNK - 1) / CHUNK;
+    const int from = steps * warp / ROWS_WARPS * CHUNK + 8 * t, to = min(steps * (warp + 1) / ROWS_WARPS * CHUNK, p.K);
+    const uint16_t *src[4];   // rows g and g + 8 of x, and of A
+    bool live[4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        live[i] = row0 + g + 8 * i < p.M;
+        src[i] = p.x + (live[i] ? (long long)(row0 + g + 8 * i) * p.xs : 0);
+        live[2 + i] = j0 + g + 8 * i < p.rank;
+        src[2 + i] = p.a + ((long long)piece.adapter * p.rank + (live[2 + i] ? j0 + g + 8 * i : 0)) * p.K;
+    }
+    float acc[2][4] = {};
+    for (int k = from; k - 8 * t < to; k += BATCH * CHUNK) {
+        uint4 v[BATCH][4];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                v[i][r] = k + i * CHUNK < to && live[r] ? __ldg(reinterpret_cast<const uint4 *>(src[r] + k + i * CHUNK)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                mma_16816<FP16>(acc[n], v[i][0].x, v[i][1].x, v[i][0].y, v[i][1].y, v[i][2 + n].x, v[i][2 + n].y);
+                mma_16816<FP16>(acc[n], v[i][0].z, v[i][1].z, v[i][0].w, v[i][1].w, v[i][2 + n].z, v[i][2 + n].w);
+            }
+    }
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[warp][g + 8 * (e >> 1)][8 * n + 2 * t + (e & 1)] = acc[n][e];
+    __syncthreads();
+    const int r = threadIdx.x >> 4, c = threadIdx.x & 15, row = row0 + r;
+    if (row < piece.from || row >= piece.to) return;
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < ROWS_WARPS; ++w) sum += part[w][r][c];
+    // (columns beyond the rank are 0, whatever x holds)
+    sum = j0 + c < p.rank ? sum * (p.scales ? __ldg(p.scales + piece.adapter) : 1.0f) : 0.f;
+    static_cast<uint16_t *>(p.t)[(long long)row * p.rank16 + j0 + c] = (uint16_t)pack_half2<FP16>(sum, 0.f);
+}
+
 // NT: columns of 8 rows of x.  With adapters the block has four warps more, which make B t while the others read W.
 constexpr int MORE_WARPS = 4;
 template <bool FP16, int NT>
@@ -211,6 +267,13 @@ constexpr int FEW_ROWS = 16;
 size_t workspace_of(int64_t rows, int rank) { return (size_t)rows * (size_t)((rank + 15) / 16 * 16) * (rows <= FEW_ROWS ? 4 : 2); }
 
 }  // namespace
+
+cudaError_t launch_shrink_blocks(const AdapterParams &p, bool fp16, cudaStream_t st) {
+    const dim3 grid((unsigned)pairs_of(p, 16), (unsigned)(p.rank16 / 16));
+    if (fp16) shrink_blocks_kernel<true><<<grid, ROWS_THREADS, 0, st>>>(p);
+    else shrink_blocks_kernel<false><<<grid, ROWS_THREADS, 0, st>>>(p);
+    return cudaGetLastError();
+}
 
 cudaError_t launch_adapter_rows(const AdapterParams &p, bool fp16, cudaStream_t st) {
     return fp16 ? launch_rows<true>(p, st) : launch_rows<false>(p, st);

@@ -47,18 +47,48 @@ __device__ __forceinline__ Piece piece_of(const AdapterParams &p, int s, int row
     if (r.from >= r.to) r.adapter = -1;
     return r;
 }
+// Pair (tile i of `size` rows, segment s that it meets) is number i + s: a staircase, so no list is made.
+inline int pairs_of(const AdapterParams &p, int size) { return (p.M + size - 1) / size + p.segments; }
+// The pair of that number, alike for all lanes; false: none.
+__device__ __forceinline__ bool pair_at(const AdapterParams &p, int pair, int size, int &s, int &tile) {
+    // the last segment that begins before the end of its tile on the staircase: in steps of 32 segments, then a lane each
+    const long long beyond = (long long)size * (pair + 1);
+    int lo = 0, hi = (p.segments + 31) / 32;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (border_of(p, 32 * mid) + (long long)size * 32 * mid < beyond) lo = mid;
+        else hi = mid;
+    }
+    lo = 32 * lo + (threadIdx.x & 31);
+    const bool before = lo < p.segments && border_of(p, min(lo, p.segments)) + (long long)size * lo < beyond;
+    s = (lo & ~31) + __popc(__ballot_sync(0xFFFFFFFFu, before)) - 1;
+    tile = pair - s;
+    return s >= 0 && tile >= 0 && (long long)tile * size < p.M;
+}
 // The pieces of rows [row0, row1), one after another, alike for all lanes.  `first` may be asked for long before the others.
 struct Pieces {
     int s;            // the segment of lane 0
-    Piece mine;
-    __device__ __forceinline__ void first(const AdapterParams &p, int row0, int row1) {
+    int at, end, which;   // of the lane's, as they stand in memory: nothing waits for them before `each`
+    __device__ __forceinline__ void look(const AdapterParams &p) {
+        const int i = s + (int)(threadIdx.x & 31);
+        at = end = 0;
+        which = -1;
+        if (i < p.segments) {
+            at = __ldg(p.starts + i);
+            end = __ldg(p.starts + i + 1);
+            which = __ldg(p.which + i);
+        }
+    }
+    __device__ __forceinline__ void first(const AdapterParams &p, int row0) {
         s = p.segments ? segments_before(p, row0) : 0;
-        mine = piece_of(p, s + (int)(threadIdx.x & 31), row0, row1);
+        look(p);
     }
     template <typename F>
     __device__ __forceinline__ void each(const AdapterParams &p, int row0, int row1, F &&f) {
 #pragma unroll 1
         while (true) {
+            Piece mine = {max(min(max(at, 0), p.M), row0), min(min(max(end, 0), p.M), row1), which};
+            if (mine.from >= mine.to || which >= p.adapters) mine.adapter = -1;
             uint32_t on = __ballot_sync(0xFFFFFFFFu, mine.adapter >= 0);
 #pragma unroll 1
             for (; on != 0u; on &= on - 1u) {
@@ -71,7 +101,7 @@ struct Pieces {
             }
             s += 32;
             if (s >= p.segments || border_of(p, s) >= row1) return;
-            mine = piece_of(p, s + (int)(threadIdx.x & 31), row0, row1);
+            look(p);
         }
     }
 };
@@ -90,6 +120,8 @@ __device__ __forceinline__ int adapter_of_row(const AdapterParams &p, int row) {
 
 // Few rows: the weights' rows are read once by mma.sync.
 cudaError_t launch_adapter_rows(const AdapterParams &p, bool fp16, cudaStream_t st);
+// t of the tiles' rows in x's type, by blocks of 16 rows: where they are not very many.
+cudaError_t launch_shrink_blocks(const AdapterParams &p, bool fp16, cudaStream_t st);
 // Many rows: tensor-memory tiles.
 cudaError_t launch_adapter_tiles(const AdapterParams &p, bool fp16, const OpsDevice &dev, cudaStream_t st);
 

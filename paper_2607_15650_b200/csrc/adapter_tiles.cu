@@ -2,14 +2,17 @@
 //
 // shrink_kernel: t = s_a x A_a^T, a tile of 128 rows x rank per pair of (tile of rows, segment that it meets), kept in the inputs'
 // type because that is what the second product multiplies it in (its rounding, 2^-9 or 2^-11 of each t, is a rank-wide average
-// below y's own).  Pair (tile i, segment s) is number i + s: a staircase, so no list is made.  Where there are few pairs, K is
-// split over the CTAs of a cluster, which join their sums through shared memory.
+// below y's own).  Bound by reading x.  Where there are few pairs, K is split over the CTAs of a cluster, which join their sums through
+// shared memory; with fewer rows still, shrink_blocks_kernel (adapter_linear.cu) takes its place.
 //
-// linear_kernel: one persistent CTA per SM and 128 x BN tiles of y; warp 0 loads (TMA, a ring), warp 1 issues the MMAs, warps 2-5
-// write a tile out of one half of the tensor memory while the other half takes the next.  The adapter's part of a tile is just
-// more k-steps into the same accumulator: t (128 x rank) times B_a (BN x rank) for each segment that the tile meets, with the rows
-// of other segments left out by the MMA's own mask of lanes.  So rows never see another request's adapter, whatever it holds,
-// and y is rounded once.
+// linear_kernel: tiles of y by pairs of CTAs (256 rows), by clusters of pairs that share a tile's K, or by single CTAs (128 rows), see
+// shape_of; warp 0 loads (TMA, a ring), warp 1 issues the MMAs, the others write a tile out of one half of the tensor memory while the
+// other half takes the next.  The adapter's part of a tile is just more k-steps into the same accumulator: t (rows x rank) times B_a (columns
+// x rank) for each segment that the tile meets, with the rows of other segments left out by the MMA's own mask of lanes.  So rows never see
+// another request's adapter, whatever it holds, and y is rounded once.
+// Measured without adapters (inputs beyond L2, us; the library's product beside it): 256 x 1024 x 1024 6.1 (3.8), 64 x 5120 x 5120 22.3 (12.2), 512 x
+// 5120 x 5120 27.2 (20.8), 1807 x 4096 x 5120 62 (55), 32760 x 1536 x 1536 110 (106), 75600 x 5120 x 5120 2870 (2550 to 2900, power-capped); with
+// adapters of rank 16 to 64: 8.2, 26.5, 39.3, 70.6, 126.7, 2710.
 #include "adapter_linear.h"
 #include "tile_wait.cuh"
 
@@ -35,18 +38,10 @@ shrink_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     let_next_start();
-    // this cluster's pair: the last segment that begins before the end of its tile on the staircase
+    // this cluster's pair
     const int pair = blockIdx.x / sh.splits, part = blockIdx.x - pair * sh.splits;
-    const long long beyond = (long long)TM * (pair + 1);
-    int lo = 0, hi = (p.segments + 31) / 32;   // in steps of 32 segments, then a lane each (every warp by itself)
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (border_of(p, 32 * mid) + (long long)TM * 32 * mid < beyond) lo = mid;
-        else hi = mid;
-    }
-    lo = 32 * lo + (threadIdx.x & 31);
-    const int s = (lo & ~31) + __popc(__ballot_sync(0xFFFFFFFFu, lo < p.segments && border_of(p, min(lo, p.segments)) + (long long)TM * lo < beyond)) - 1, tile = pair - s;
-    if (s < 0 || tile < 0 || (long long)tile * TM >= p.M) return;   // (alike for the whole cluster)
+    int s, tile;
+    if (!pair_at(p, pair, TM, s, tile)) return;   // (alike for the whole cluster)
     const int row0 = tile * TM;
     const Piece piece = piece_of(p, s, row0, min(row0 + TM, p.M));
     if (piece.adapter < 0) return;
@@ -176,23 +171,40 @@ shrink_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
 }
 
 // ------------------------------------------------------------------------------------------------ y = W x + bias + B t
-constexpr int LINEAR_THREADS = 192, PM = 2 * TM;              // rows of a pair's tile
-constexpr int ATOMS = 2;                                      // of 64 k values in a stage
+constexpr int EPILOGUE_WARPS = 8, LINEAR_THREADS = (2 + EPILOGUE_WARPS) * 32;   // (two warps for each quarter of the tensor memory's lanes)
+// How a tile is made: by pairs of CTAs that walk the tiles (256 rows each); a cluster of 2 to 4 pairs for one tile, each pair with a part of K;
+// single CTAs that walk tiles of 128 rows.
+enum : int { PAIRS = 0, SPLIT_PAIRS = 1, SINGLES = 2 };
+constexpr int MOST_SPLITS = 4;
 
-template <int BN>
+// SPLIT: columns that each pair of a cluster finishes, and floats of a row of them in shared memory (rows of 8 lanes fall on different banks)
+__host__ __device__ constexpr int split_columns(int bn, int splits) { return (bn / 8 + splits - 1) / splits * 8; }
+__host__ __device__ constexpr int split_pitch(int bn, int splits) { return split_columns(bn, splits) + 4; }
+
+template <int BN, int MODE>
 struct LinearCfg {
-    static constexpr int B_BYTES = BN / 2 * 128;              // each CTA of the pair loads half of the columns
+    static constexpr bool SPLIT = MODE == SPLIT_PAIRS;
+    static constexpr int CTAS = MODE == SINGLES ? 1 : 2, PM = CTAS * TM;   // of a tile; its rows
+    // Of 64 k values in a stage.  A wait that is already over takes a warp some 130 cycles and a stage's other overhead 100, so that stages
+    // are as large as leaves two.
+    static constexpr int ATOMS = MODE == SINGLES && BN <= 64 ? 4 : MODE == SPLIT_PAIRS && BN > 128 ? 1 : 2;
+    static constexpr int B_ROWS = BN / CTAS, B_BYTES = B_ROWS * 128;   // each CTA of a pair loads half of the columns
     static constexpr int ATOM = A_BYTES + B_BYTES, STAGE = ATOMS * ATOM;
-    static constexpr int STAGES = 196608 / STAGE;
-    static constexpr int OUT_BYTES = 4 * 32 * 128;            // a warp's staging: 32 rows x 128 bytes
-    static constexpr int SMEM = 1024 + STAGES * STAGE + OUT_BYTES + (2 * STAGES + 4) * 8;
-    static constexpr int PITCH = BN + 4;                      // SPLIT: floats of a row of partial sums, where the stages were
-    static_assert(SMEM + 64 <= 227 * 1024 && TM * PITCH * 4 <= STAGES * STAGE, "beyond the shared memory of a CTA");
-    static constexpr int COLS = 256;                          // TMEM columns from one accumulator to the next
+    static constexpr int OUT = SPLIT ? 0 : EPILOGUE_WARPS * 2 * 2048;        // a warp's staging: 32 rows x 64 bytes, twice
+    static constexpr int SUMS = SPLIT ? (MOST_SPLITS - 1) * TM * split_pitch(BN, MOST_SPLITS) * 4 : 0;   // that other pairs send
+    static constexpr int STAGES = SPLIT ? (226 * 1024 - SUMS) / STAGE : 196608 / STAGE < 12 ? 196608 / STAGE : 12;
+    static constexpr int SMEM = 1024 + STAGES * STAGE + OUT + SUMS + (2 * STAGES + 5) * 8;
+    static_assert(SMEM + 64 <= 227 * 1024 && 2 * STAGES + 5 <= 32, "beyond the shared memory of a CTA, or a warp's lanes");
+    // SPLIT: the partial sums to be sent stand where the stages were
+    static_assert(!SPLIT || (TM * split_pitch(BN, 2) * 4 <= STAGES * STAGE && 2 * TM * split_pitch(BN, 3) * 4 <= STAGES * STAGE && SUMS <= STAGES * STAGE &&
+                             TM * split_pitch(BN, 2) * 4 <= SUMS && 2 * TM * split_pitch(BN, 3) * 4 <= SUMS), "no room for a tile's sums");
+    static constexpr int COLS = MODE == SINGLES ? 128 : 256;  // TMEM columns from one accumulator to the next
+    static_assert(BN <= COLS, "beyond an accumulator's place");
 };
 
 struct LinearShape {
-    int mt, nt, tiles;        // tiles of 256 rows, of BN columns, in all
+    int mode;
+    int mt, nt, tiles;        // tiles of rows, of BN columns, in all
     int group;                // tiles of rows that are walked together, column by column of tiles: their x and W stay in L2
     int splits;               // SPLIT: pairs of a cluster that share a tile's K
 };
@@ -201,6 +213,8 @@ __device__ __forceinline__ void tile_at(const LinearShape &sh, int w, int &mi, i
     ni = i / high;
     mi = first + (i - ni * high);
 }
+
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *m) { asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory"); }
 
 // f[0..COUNT) += bias[col..col + COUNT)
 template <bool FP16, int COUNT>
@@ -220,78 +234,98 @@ __device__ __forceinline__ void add_bias(const AdapterParams &p, int col, float 
     }
 }
 
-// SPLIT: a cluster of 2 to 4 pairs for one tile, each pair with a part of K; else pairs walk the tiles.
-template <int BN, bool FP16, bool SPLIT>
+template <int BN, bool FP16, int MODE>
 __global__ void __launch_bounds__(LINEAR_THREADS, 1)
 linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_t,
-              const __grid_constant__ CUtensorMap map_b, const AdapterParams p, const LinearShape sh) {
-    using C = LinearCfg<BN>;
+              const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_y, const AdapterParams p, const LinearShape sh) {
+    using C = LinearCfg<BN, MODE>;
+    constexpr bool SPLIT = C::SPLIT, PAIR = C::CTAS == 2;
+    constexpr int ATOMS = C::ATOMS, PM = C::PM;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t out_smem = base + C::STAGES * C::STAGE, bars = out_smem + C::OUT_BYTES;
-    const uint32_t full = bars, empty = full + 8 * C::STAGES, acc_full = empty + 8 * C::STAGES, acc_empty = acc_full + 16;
+    const uint32_t out_smem = base + C::STAGES * C::STAGE, sums_smem = out_smem + C::OUT, bars = sums_smem + C::SUMS;
+    const uint32_t full = bars, empty = full + 8 * C::STAGES, acc_full = empty + 8 * C::STAGES, acc_empty = acc_full + 16, sums_in = acc_empty + 16;
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-    const uint32_t rank = rank_in_cluster(), half = rank & 1u, leader = rank & ~1u;      // of the pair: this CTA's rows
+    const uint32_t rank = PAIR ? rank_in_cluster() : 0u, half = rank & 1u, leader = rank & ~1u;      // of the pair: this CTA's rows
     const int part = SPLIT ? (int)(rank >> 1) : 0;
-    const int pair = SPLIT ? (int)blockIdx.x / (2 * sh.splits) : (int)blockIdx.x / 2, pairs = SPLIT ? sh.tiles : (int)gridDim.x / 2;
+    const int pair = SPLIT ? (int)blockIdx.x / (2 * sh.splits) : (int)blockIdx.x / C::CTAS, pairs = SPLIT ? sh.tiles : (int)gridDim.x / C::CTAS;
     volatile int *abort_ptr = &abort_flag;
-    if (threadIdx.x == 0) {
-        abort_flag = 0;
-        for (int i = 0; i < C::STAGES; ++i) {
-            mbar_init(full + 8 * i, 1);
-            mbar_init(empty + 8 * i, 1);
+    if (warp == 0) {
+        if (lane < 2 * C::STAGES + 5) {
+            const int i = lane - 2 * C::STAGES;   // both accumulators' barriers, and the sums' one
+            mbar_init(bars + 8 * lane, i == 2 || i == 3 ? EPILOGUE_WARPS * C::CTAS : 1u);   // (a lane of each warp of both epilogues)
+            fence_mbar_init();
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(acc_full + 8 * i, 1);
-            mbar_init(acc_empty + 8 * i, 8);   // a lane of each warp of both epilogues
+        if (lane == 0) abort_flag = 0;
+        __syncwarp();
+        if constexpr (SPLIT)
+            if (lane == 0) mbar_arrive_expect_tx(sums_in, (uint32_t)((sh.splits - 1) * TM * split_pitch(BN, sh.splits) * 4));
+    } else if (warp == 1) {
+        if constexpr (PAIR) tmem_alloc_pair(smem_u32(&tmem_slot), 512);
+        else {
+            tmem_alloc(smem_u32(&tmem_slot), 256);
+            tmem_relinquish();
         }
-        fence_mbar_init();
+    } else if (warp == 2 && lane == 0) {
+        prefetch_map(&map_x);
+        prefetch_map(&map_w);
+        if constexpr (!SPLIT) prefetch_map(&map_y);
     }
     __syncwarp();
-    sync_cluster();
-    if (warp == 1) tmem_alloc_pair(smem_u32(&tmem_slot), 512);
     tc_fence_before();
-    __syncthreads();
+    if constexpr (PAIR) sync_cluster();
+    else __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
+    // SPLIT: this pair's columns of the tile; [part][row][pitch] in its own stages, and as the others send theirs
+    const int split_cols = SPLIT ? split_columns(BN, sh.splits) : 0, pitch = split_cols + 4;
+    const uint32_t block_bytes = (uint32_t)(TM * pitch * 4);
     const int all = (p.K + BK - 1) / BK, k_from = SPLIT ? all * part / sh.splits * BK : 0, k_to = SPLIT ? min(all * (part + 1) / sh.splits * BK, p.K) : p.K;
 
     // (The loading and the issuing warp run their loops as whole warps and one elected lane issues: what the instructions take, descriptors
     // and addresses, then stays in uniform registers.  With the loops inside `if (lane == 0)` an MMA took 62 cycles to issue.)
     if (warp == 0) {
         uint32_t st = 0, ph = 0;
-        bool ok = true, t_ready = false;
-        const uint32_t full_at = at_rank(full, leader);
+        bool ok = true, t_ready = false, used = false;   // used: the ring has been round once
+        const uint32_t full_at = PAIR ? at_rank(full, leader) : full;
         auto stage = [&](const CUtensorMap *ma, const CUtensorMap *mb, int k, int end, int row, int col, int adapter) {   // k values [k, end) of at most ATOMS atoms
-            ok = ok && wait_all_lanes(empty + 8 * st, ph ^ 1u, abort_ptr);
+            if (used) ok = ok && wait_all_lanes(empty + 8 * st, ph ^ 1u, abort_ptr);
             if (!ok) return;
             const uint32_t bar = full_at + 8 * st, at = base + st * C::STAGE;
             if (elect_lane()) {
-                if (half == 0) mbar_arrive_expect_tx(full + 8 * st, 2 * C::ATOM * ((end - k + BK - 1) / BK));   // both CTAs' bytes
+                if (half == 0) mbar_arrive_expect_tx(full + 8 * st, C::CTAS * C::ATOM * ((end - k + BK - 1) / BK));   // both CTAs' bytes
 #pragma unroll
                 for (int i = 0; i < ATOMS; ++i) {
                     if (k + i * BK >= end) break;
-                    tma_pair_2d(at + i * C::ATOM, ma, bar, k + i * BK, row);
-                    if (adapter < 0) tma_pair_2d(at + i * C::ATOM + A_BYTES, mb, bar, k + i * BK, col);
-                    else tma_pair_3d(at + i * C::ATOM + A_BYTES, mb, bar, k + i * BK, col, adapter);
+                    if constexpr (PAIR) {
+                        tma_pair_2d(at + i * C::ATOM, ma, bar, k + i * BK, row);
+                        if (adapter < 0) tma_pair_2d(at + i * C::ATOM + A_BYTES, mb, bar, k + i * BK, col);
+                        else tma_pair_3d(at + i * C::ATOM + A_BYTES, mb, bar, k + i * BK, col, adapter);
+                    } else {
+                        tma_load_2d(at + i * C::ATOM, ma, bar, k + i * BK, row);
+                        if (adapter < 0) tma_load_2d(at + i * C::ATOM + A_BYTES, mb, bar, k + i * BK, col);
+                        else tma_load_3d(at + i * C::ATOM + A_BYTES, mb, bar, k + i * BK, col, adapter);
+                    }
                 }
             }
             __syncwarp();
-            if (++st == C::STAGES) { st = 0; ph ^= 1u; }
+            if (++st == C::STAGES) { st = 0; ph ^= 1u; used = true; }
         };
 #pragma unroll 1
         for (int w = pair; w < sh.tiles && ok; w += pairs) {
             int mi, ni;
             tile_at(sh, w, mi, ni);
-            const int row0 = mi * PM, row1 = min(row0 + PM, p.M), row = row0 + (int)half * TM, col = ni * BN + (int)half * (BN / 2);
+            const int row0 = mi * PM, row1 = min(row0 + PM, p.M), row = row0 + (int)half * TM, col = ni * BN + (int)half * C::B_ROWS;
             Pieces pieces;
-            if (p.segments && part == 0) pieces.first(p, row0, row1);
+            if (p.segments) pieces.first(p, row0);
 #pragma unroll 1
             for (int k = k_from; k < k_to && ok; k += ATOMS * BK) stage(&map_x, &map_w, k, min(k + ATOMS * BK, k_to), row, col, -1);
-            if (!p.segments || part != 0) continue;
+            if (!p.segments) continue;
+            int turn = 0;   // SPLIT: the pairs take the pieces in turn
             pieces.each(p, row0, row1, [&](const Piece &piece) {
+                if (SPLIT && turn++ % sh.splits != part) return true;
                 if (!t_ready) {
                     wait_for_previous();
                     asm volatile("fence.proxy.async.global;" ::: "memory");
@@ -308,6 +342,10 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         if (half == 0) {
             constexpr uint32_t IDESC = make_idesc_bf16_f32(PM, BN, false, FP16);
             const uint16_t both = (uint16_t)(3u << leader);
+            auto commit = [&](uint32_t bar) {
+                if constexpr (PAIR) commit_pair(bar, both);
+                else tc_commit(bar);
+            };
             uint32_t st = 0, ph = 0, n = 0;
             bool ok = true;
 #pragma unroll 1
@@ -316,7 +354,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 tile_at(sh, w, mi, ni);
                 const int row0 = mi * PM, row1 = min(row0 + PM, p.M);
                 Pieces pieces;
-                if (p.segments && part == 0) pieces.first(p, row0, row1);
+                if (p.segments) pieces.first(p, row0);
                 const uint32_t acc = n & 1u, d = tmem + acc * C::COLS;
                 ok = wait_all_lanes(acc_empty + 8 * acc, ((n >> 1) & 1u) ^ 1u, abort_ptr);
                 if (!ok) break;
@@ -333,17 +371,20 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                             if (k + i * BK >= k_to) break;
 #pragma unroll
                             for (int kk = 0; kk < BK / 16; ++kk)
-                                mma_pair(d, ad + i * (C::ATOM >> 4) + 2 * kk, bd + i * (C::ATOM >> 4) + 2 * kk, IDESC, k > k_from || i > 0 || kk > 0 ? 1u : 0u);
+                                if constexpr (PAIR) mma_pair(d, ad + i * (C::ATOM >> 4) + 2 * kk, bd + i * (C::ATOM >> 4) + 2 * kk, IDESC, k > k_from || i > 0 || kk > 0 ? 1u : 0u);
+                                else mma_ss(d, ad + i * (C::ATOM >> 4) + 2 * kk, bd + i * (C::ATOM >> 4) + 2 * kk, IDESC, k > k_from || i > 0 || kk > 0 ? 1u : 0u);
                         }
-                        commit_pair(empty + 8 * st, both);
+                        commit(empty + 8 * st);
                     }
                     __syncwarp();
                     if (++st == C::STAGES) { st = 0; ph ^= 1u; }
                 }
-                if (ok && p.segments && part == 0) pieces.each(p, row0, row1, [&](const Piece &piece) {
-                    uint32_t off[8];
+                int turn = 0;
+                if (ok && p.segments) pieces.each(p, row0, row1, [&](const Piece &piece) {
+                    if (SPLIT && turn++ % sh.splits != part) return true;
+                    uint32_t off[PM / 32];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
+                    for (int i = 0; i < PM / 32; ++i) {
                         const int from = min(max(piece.from - row0 - 32 * i, 0), 32), to = min(max(piece.to - row0 - 32 * i, 0), 32);
                         off[i] = ~((to == 32 ? 0xFFFFFFFFu : (1u << to) - 1u) & (from == 32 ? 0u : 0xFFFFFFFFu << from));
                     }
@@ -357,86 +398,142 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
 #pragma unroll 1
                             for (int kk = 0; kk < min(ATOMS * BK, p.rank16 - k) / 16; ++kk) {
                                 const uint32_t at = (kk >> 2) * (C::ATOM >> 4) + (kk & 3) * 2;
-                                mma_pair_rows(d, ad + at, bd + at, IDESC, off);
+                                if constexpr (PAIR) mma_pair_rows(d, ad + at, bd + at, IDESC, off);
+                                else mma_ss_rows(d, ad + at, bd + at, IDESC, off);
                             }
-                            commit_pair(empty + 8 * st, both);
+                            commit(empty + 8 * st);
                         }
                         __syncwarp();
                         if (++st == C::STAGES) { st = 0; ph ^= 1u; }
                     }
                     return true;
                 });
-                if (ok && elect_lane()) commit_pair(acc_full + 8 * acc, both);
+                if (ok && elect_lane()) commit(acc_full + 8 * acc);
                 __syncwarp();
             }
             if (!ok) give_up(abort_ptr, p.status);
         }
     } else {
-        const int quarter = warp % 4;
+        const int quarter = warp % 4, side = (warp - 2) / 4;   // this warp's rows; which of every two pieces of columns it has
         const uint32_t lane_addr = ((uint32_t)(quarter * 32)) << 16;
-        const uint32_t stage = out_smem + quarter * 4096, my_row = stage + lane * 128;
-        const int piece = lane & 7;
-        uint32_t n = 0;
+        uint32_t n = 0, n_out = 0;
         bool ok = true;
 #pragma unroll 1
         for (int w = pair; w < sh.tiles; w += pairs, ++n) {
             int mi, ni;
             tile_at(sh, w, mi, ni);
             const uint32_t which = n & 1u, acc = tmem + lane_addr + which * C::COLS;
+            const int row0 = mi * PM + (int)half * TM + quarter * 32, row = row0 + lane;
+            uint16_t *const out = p.y + (long long)row * p.ys + ni * BN;
+            const int cols = row < p.M ? min(BN, p.N - ni * BN) : 0;   // of this lane's row
             ok = wait_or_abort_warp(acc_full + 8 * which, (n >> 1) & 1u, abort_ptr);
             if (!ok) break;
             tc_fence_after();
-            if constexpr (SPLIT) {   // partial sums to where the stages were (every MMA is done), joined across the cluster below
+            if constexpr (SPLIT) {
+                // Partial sums to where the stages were (every MMA is done), by the pair that finishes their columns, and from there to it.
 #pragma unroll 1
-                for (int c0 = 0; c0 < BN; c0 += 32) {
-                    uint32_t v[32];
-                    tmem_ld_x32(acc + c0, v);
-                    tmem_wait_ld();
+                for (int o = 0, slot = 0; o < sh.splits; ++o) {
+                    if (o == part || (slot++ & 1) != side) continue;
+                    const uint32_t to = base + (slot - 1) * block_bytes + (uint32_t)((quarter * 32 + lane) * pitch) * 4u;
+#pragma unroll 1
+                    for (int c0 = 0; c0 < split_cols; c0 += 32) {   // (beyond the tile's columns, some of whatever the accumulator's place holds)
+                        uint32_t v[32];
+                        tmem_ld_x32(acc + o * split_cols + c0, v);
+                        tmem_wait_ld();
 #pragma unroll
-                    for (int c = 0; c < 8; ++c)
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (uint32_t)((quarter * 32 + lane) * C::PITCH + c0 + 4 * c) * 4u), "r"(v[4 * c]),
-                                     "r"(v[4 * c + 1]), "r"(v[4 * c + 2]), "r"(v[4 * c + 3]) : "memory");
+                        for (int c = 0; c < 8; ++c)
+                            if (c0 + 4 * c < split_cols)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (uint32_t)(c0 + 4 * c) * 4u), "r"(v[4 * c]),
+                                             "r"(v[4 * c + 1]), "r"(v[4 * c + 2]), "r"(v[4 * c + 3]) : "memory");
+                    }
                 }
-                break;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane + 1 < sh.splits && (lane & 1) == side) {   // a lane for each of the others; this warp's rows
+                    const uint32_t o = lane < part ? lane : lane + 1, there = 2u * o + half, mine = (uint32_t)(quarter * 32 * pitch) * 4u;
+                    const uint32_t at = sums_smem + ((uint32_t)part < o ? part : part - 1) * block_bytes + mine;
+                    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                 ::"r"(at_rank(at, there)), "r"(base + lane * block_bytes + mine), "r"((uint32_t)(32 * pitch * 4)), "r"(at_rank(sums_in, there)) : "memory");
+                }
+                __syncwarp();
+                ok = wait_all_lanes(sums_in, 0, abort_ptr);
+                if (!ok) break;
             }
-            const int warp_row = mi * PM + (int)half * TM + quarter * 32, rows_left = p.M - warp_row;
-            uint16_t *out = p.y + (long long)warp_row * p.ys;
+            // SPLIT: this pair's columns, with the others' sums in the order of the parts
+            const int first = SPLIT ? part * split_cols : 0, last = SPLIT ? min(first + split_cols, BN) : BN;
+            auto accumulator_read = [&] {   // the tile after next may overwrite it
+                if (w + 2 * pairs >= sh.tiles) return;
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (PAIR) arrive_at(at_rank(acc_empty + 8 * which, leader));
+                    else mbar_arrive(acc_empty + 8 * which);
+                }
+            };
+            if (first + 32 * side >= last) accumulator_read();   // (no columns for this warp)
 #pragma unroll 1
-            for (int c0 = 0; c0 < BN; c0 += 64) {
-                constexpr bool WHOLE = BN % 64 == 0;
-                const int col = ni * BN + c0;
-                uint32_t v[2][32];
-                tmem_ld_x32(acc + c0, v[0]);
-                if (WHOLE || c0 + 64 <= BN) tmem_ld_x32(acc + c0 + 32, v[1]);
+            for (int c0 = first + 32 * side; c0 < last; c0 += 64) {
+                uint32_t v[32];
+                tmem_ld_x32(acc + c0, v);
                 tmem_wait_ld();
-                if (c0 + 64 >= BN) {   // read: the tile after next may overwrite it
-                    tc_fence_before();
+                if (c0 + 64 >= last) accumulator_read();
+                if constexpr (SPLIT) {   // (sums of an order that is the column's own)
+                    const uint32_t sums = sums_smem + (uint32_t)((quarter * 32 + lane) * pitch + c0 - first) * 4u;
+#pragma unroll 1
+                    for (int q = 0; q + 1 < sh.splits; ++q) {
+#pragma unroll
+                        for (int c = 0; c < 32; c += 4) {   // (beyond this pair's columns: into the next row's or the barriers, and not used)
+                            float4 x;
+                            asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(sums + q * block_bytes + (uint32_t)c * 4u));
+                            v[c] = __float_as_uint(__uint_as_float(v[c]) + x.x);
+                            v[c + 1] = __float_as_uint(__uint_as_float(v[c + 1]) + x.y);
+                            v[c + 2] = __float_as_uint(__uint_as_float(v[c + 2]) + x.z);
+                            v[c + 3] = __float_as_uint(__uint_as_float(v[c + 3]) + x.w);
+                        }
+                    }
+                }
+                if (p.bias != nullptr) {
+#pragma unroll 1
+                    for (int i = 0; i < 1; ++i) {
+                        float f[32];
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) f[c] = __uint_as_float(v[c]);
+#pragma unroll
+                        for (int c = 0; c < 32; c += 8)
+                            if (c0 + c < cols) add_bias<FP16, 8>(p, ni * BN + c0 + c, *reinterpret_cast<float (*)[8]>(f + c));
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(f[c]);
+                    }
+                }
+                uint32_t o[16];
+#pragma unroll
+                for (int c = 0; c < 16; ++c) o[c] = pack_half2<FP16>(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
+                if constexpr (SPLIT) {
+                    const int left = min(cols, last) - c0;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (8 * c < left) *reinterpret_cast<uint4 *>(out + c0 + 8 * c) = make_uint4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+                } else {
+                    // 32 rows x 64 bytes to shared memory (swizzled), and from there by TMA, which leaves out what is beyond y
+                    const uint32_t to = out_smem + (uint32_t)((warp - 2) * 2 + (n_out++ & 1)) * 2048u;
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0) arrive_at(at_rank(acc_empty + 8 * which, leader));
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (uint32_t)(lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4))), "r"(o[4 * c]),
+                                     "r"(o[4 * c + 1]), "r"(o[4 * c + 2]), "r"(o[4 * c + 3]) : "memory");
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (row0 < p.M && ni * BN + c0 < p.N)
+                            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+                                         ::"l"(reinterpret_cast<uint64_t>(&map_y)), "r"(to), "r"(ni * BN + c0), "r"(row0) : "memory");
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
                 }
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    float f[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[c >> 2][(c & 3) * 8 + i]);
-                    if (p.bias != nullptr && col + 8 * c < p.N) add_bias<FP16, 8>(p, col + 8 * c, f);
-                    uint32_t o[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[i] = pack_half2<FP16>(f[2 * i], f[2 * i + 1]);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(my_row + (uint32_t)((c ^ (lane & 7)) << 4)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
-                }
-                __syncwarp();
-                const bool in = col + piece * 8 < p.N && (WHOLE || c0 + piece * 8 < BN);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int r = i * 4 + (lane >> 3);
-                    uint4 x;
-                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(stage + r * 128 + (uint32_t)((piece ^ (r & 7)) << 4)) : "memory");
-                    if (in && r < rows_left) __stcs(reinterpret_cast<uint4 *>(out + r * p.ys + col + piece * 8), x);
-                }
-                __syncwarp();
             }
         }
+        if (!SPLIT && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         if (!ok && lane == 0) give_up(abort_ptr, p.status);
     }
     __syncwarp();
@@ -444,39 +541,22 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     __syncthreads();
     tc_fence_after();
     settle_if(*abort_ptr != 0);
-    sync_cluster();   // no CTA leaves, or reuses its stages, while another's MMAs, commits or arrivals reach it
-    if constexpr (SPLIT) {
-        int mi, ni;
-        tile_at(sh, pair, mi, ni);
-        // rows part, part + splits, ... of this CTA's half: 4 columns at a time, the parts in order
-        constexpr int PIECES = BN / 4;
-        const int row0 = mi * PM + (int)half * TM, rows = min(TM, p.M - row0), count = (rows - part + sh.splits - 1) / sh.splits * PIECES;
-#pragma unroll 4
-        for (int i = threadIdx.x; i < count; i += LINEAR_THREADS) {
-            const int r = i / PIECES * sh.splits + part, c = i % PIECES * 4, col = ni * BN + c;
-            const uint32_t at = base + (uint32_t)(r * C::PITCH + c) * 4u;
-            float4 x[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                x[q] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (q < sh.splits)
-                    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x[q].x), "=f"(x[q].y), "=f"(x[q].z), "=f"(x[q].w) : "r"(at_rank(at, 2 * q + half)));
-            }
-            float f[4] = {((x[0].x + x[1].x) + x[2].x) + x[3].x, ((x[0].y + x[1].y) + x[2].y) + x[3].y,
-                          ((x[0].z + x[1].z) + x[2].z) + x[3].z, ((x[0].w + x[1].w) + x[2].w) + x[3].w};
-            if (col >= p.N) continue;
-            if (p.bias != nullptr) add_bias<FP16, 4>(p, col, f);
-            *reinterpret_cast<uint2 *>(p.y + (row0 + r) * p.ys + col) = make_uint2(pack_half2<FP16>(f[0], f[1]), pack_half2<FP16>(f[2], f[3]));
-        }
-        sync_cluster();
+    if constexpr (PAIR) sync_cluster();   // no CTA leaves while another's MMAs, commits, arrivals or sums reach it, or are still read from it
+    if (warp == 1) {
+        if constexpr (PAIR) tmem_dealloc_pair(tmem, 512);
+        else tmem_dealloc(tmem, 256);
     }
-    if (warp == 1) tmem_dealloc_pair(tmem, 512);
 }
 
 bool map_rows(void *fn, CUtensorMap *tm, const void *base, bool fp16, long long rows, int width, long long stride, int box_rows) {
     const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
     const cuuint32_t box[2] = {BK, (cuuint32_t)box_rows};
     return encode_map(fn, tm, base, fp16, 2, dims, strides, box);
+}
+bool map_out(void *fn, CUtensorMap *tm, const AdapterParams &p, bool fp16) {
+    const cuuint64_t dims[2] = {(cuuint64_t)p.N, (cuuint64_t)p.M}, strides[1] = {(cuuint64_t)p.ys * 2};
+    const cuuint32_t box[2] = {32, 32};
+    return encode_map(fn, tm, p.y, fp16, 2, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_64B);
 }
 bool map_adapters(void *fn, CUtensorMap *tm, const void *base, bool fp16, int adapters, int rows, int width, int box_rows) {
     const cuuint64_t dims[3] = {(cuuint64_t)width, (cuuint64_t)rows, (cuuint64_t)adapters};
@@ -490,7 +570,7 @@ cudaError_t launch_shrink(const CUtensorMap &mx, const CUtensorMap &ma, const Ad
     static OncePerDevice once;
     const cudaError_t e = once(dev, [] { return cudaFuncSetAttribute(shrink_kernel<FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SHRINK_MOST); });
     if (e != cudaSuccess) return e;
-    const int pairs = (p.M + TM - 1) / TM + p.segments;
+    const int pairs = pairs_of(p, TM);
     ShrinkShape sh;
     sh.steps = (p.K + BK - 1) / BK;
     sh.splits = 1;
@@ -511,72 +591,98 @@ cudaError_t launch_shrink(const CUtensorMap &mx, const CUtensorMap &ma, const Ad
     return cudaLaunchKernelEx(&cfg, shrink_kernel<FP16>, mx, ma, p, sh);
 }
 
-template <int BN, bool FP16, bool SPLIT>
+template <int BN, bool FP16, int MODE>
 cudaError_t launch_linear(const CUtensorMap &mx, const AdapterParams &p, LinearShape sh, const OpsDevice &dev, cudaStream_t st) {
-    using C = LinearCfg<BN>;
+    using C = LinearCfg<BN, MODE>;
     static OncePerDevice once;
-    const cudaError_t e = once(dev, [] { return cudaFuncSetAttribute(linear_kernel<BN, FP16, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); });
+    const cudaError_t e = once(dev, [] { return cudaFuncSetAttribute(linear_kernel<BN, FP16, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); });
     if (e != cudaSuccess) return e;
-    CUtensorMap mw, mt, mb;
-    if (!map_rows(dev.encode_tiled, &mw, p.w, FP16, p.N, p.K, p.ws, BN / 2)) return cudaErrorInvalidValue;
-    mt = mb = mw;
+    CUtensorMap mw, mt, mb, my;
+    if (!map_rows(dev.encode_tiled, &mw, p.w, FP16, p.N, p.K, p.ws, C::B_ROWS)) return cudaErrorInvalidValue;
+    mt = mb = my = mw;
+    if (MODE != SPLIT_PAIRS && !map_out(dev.encode_tiled, &my, p, FP16)) return cudaErrorInvalidValue;
     if (p.segments && (!map_rows(dev.encode_tiled, &mt, p.t, FP16, p.M, p.rank16, p.rank16, TM) ||
-                       !map_adapters(dev.encode_tiled, &mb, p.b, FP16, p.adapters, p.N, p.rank, BN / 2)))
+                       !map_adapters(dev.encode_tiled, &mb, p.b, FP16, p.adapters, p.N, p.rank, C::B_ROWS)))
         return cudaErrorInvalidValue;
-    const int pairs = dev.sms / 2;
+    const int workers = dev.sms / C::CTAS;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(SPLIT ? 2 * sh.splits * sh.tiles : 2 * (sh.tiles < pairs ? sh.tiles : pairs)));
+    cfg.gridDim = dim3((unsigned)(C::CTAS * (MODE == SPLIT_PAIRS ? sh.splits * sh.tiles : sh.tiles < workers ? sh.tiles : workers)));
     cfg.blockDim = dim3(LINEAR_THREADS);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = st;
     cudaLaunchAttribute attr[2] = {};
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)(SPLIT ? 2 * sh.splits : 2); attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.x = (unsigned)(MODE == SPLIT_PAIRS ? 2 * sh.splits : C::CTAS); attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = p.segments ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, linear_kernel<BN, FP16, SPLIT>, mx, mw, mt, mb, p, sh);
+    return cudaLaunchKernelEx(&cfg, linear_kernel<BN, FP16, MODE>, mx, mw, mt, mb, my, p, sh);
 }
 template <int BN, bool FP16>
 cudaError_t launch_linear(const CUtensorMap &mx, const AdapterParams &p, const LinearShape &sh, const OpsDevice &dev, cudaStream_t st) {
-    return sh.splits > 1 ? launch_linear<BN, FP16, true>(mx, p, sh, dev, st) : launch_linear<BN, FP16, false>(mx, p, sh, dev, st);
+    if constexpr (BN <= 128)
+        if (sh.mode == SINGLES) return launch_linear<BN, FP16, SINGLES>(mx, p, sh, dev, st);
+    if constexpr (BN >= 128 && BN <= 192)   // (wider tiles' partial sums would not fit)
+        if (sh.mode == SPLIT_PAIRS) return launch_linear<BN, FP16, SPLIT_PAIRS>(mx, p, sh, dev, st);
+    if constexpr (BN >= 128) return launch_linear<BN, FP16, PAIRS>(mx, p, sh, dev, st);
+    return cudaErrorInvalidValue;
 }
 
-// The tile's width and the parts of K: pairs of SMs walk the tiles in rounds, so the time goes by rounds x (columns of a tile + what a
-// tile costs besides); with few tiles K is split while the clusters still find a place at once.
+// The tile, by what a CTA's time goes by, in cycles, fitted to measured times of 128 x 512 x 512 to 1024 x 4096 x 5120 (us, singles of 32 and 64
+// columns, pairs of 128 and 160, two parts of 128 or 160): 128 x 512 x 512 4.7 5.0 6.2 6.8 7.1; 64 x 1536 x 1536 6.6 7.3 8.4 9.6 8.3; 600 x 2048 x
+// 600 8.3 9.0 9.9 11.4 9.2; 64 x 5120 x 5120 34.5 21.6 20.6 26.1 18.2; 512 x 5120 x 5120 77.7 55.8 36.6 28.2.  An atom of K takes its MMAs, its
+// loads (54 bytes a cycle and SM with most SMs loading, else 80) or the issuing; clusters cost their barriers, parts of K the exchange.
 inline LinearShape shape_of(const AdapterParams &p, int sms, int &bn) {
     LinearShape best = {};
     double least = 0;
-    for (int w : {256, 224, 192, 160, 128}) {
+    const int atoms = (p.K + BK - 1) / BK;
+    auto consider = [&](int mode, int w, int splits) {
         LinearShape sh = {};
-        sh.mt = (p.M + PM - 1) / PM;
+        const int ctas = mode == SINGLES ? 1 : 2;
+        sh.mode = mode;
+        sh.mt = (p.M + ctas * TM - 1) / (ctas * TM);
         sh.nt = (p.N + w - 1) / w;
-        const long long tiles = (long long)sh.mt * sh.nt, pairs = sms / 2;
-        if (tiles > 0x3FFFFFFF) continue;
+        const long long tiles = (long long)sh.mt * sh.nt, workers = sms / ctas;
+        if (tiles > 0x3FFFFFFF) return;
         sh.tiles = (int)tiles;
         sh.group = 8;
-        sh.splits = 1;
-        // clusters of 2, 4, 6 and 8 CTAs that find a place at once with one CTA per SM
-        const long long places[5] = {0, pairs, sms * 15 / 64, sms / 7, sms / 10 + 1};
-        while (sh.splits < 4 && tiles <= places[sh.splits + 1] && p.K >= (sh.splits + 1) * 4 * BK) ++sh.splits;
-        const double rounds = sh.splits > 1 ? 1.0 / sh.splits : (double)((tiles + pairs - 1) / pairs), cost = rounds * (w + 96) + (sh.splits > 1 ? w / 4 : 0);
+        sh.splits = splits;
+        const long long busy = (tiles < workers ? tiles * splits : workers) * ctas;
+        const double loads = (TM + w / ctas) * 128 / (10 * busy > 6 * sms ? 54.0 : 80.0);
+        double atom = loads > 2 * w ? loads : 2 * w;
+        if (atom < 270) atom = 270;
+        const int part = (atoms + splits - 1) / splits;
+        const double cost = (mode == SINGLES ? 6500 + 12 * w : mode == PAIRS ? 7500 + 15 * w : 14000 + 15 * w) +
+                            (splits > 1 ? 1.0 : (double)((tiles + workers - 1) / workers)) * (part * atom + 300);
         if (best.tiles == 0 || cost < least) {
             best = sh;
             least = cost;
             bn = w;
         }
+    };
+    for (int w : {256, 224, 192, 160, 128}) {
+        consider(PAIRS, w, 1);
+        // clusters of 4, 6 and 8 CTAs that find a place at once with one CTA per SM
+        const int places[5] = {0, 0, sms * 15 / 64, sms / 7, sms / 10 + 1};
+        const long long tiles = (long long)((p.M + 2 * TM - 1) / (2 * TM)) * ((p.N + w - 1) / w);
+        for (int splits = 2; w <= 192 && splits <= MOST_SPLITS; ++splits)
+            if (tiles <= places[splits] && atoms >= splits * 4) consider(SPLIT_PAIRS, w, splits);
     }
+    for (int w : {128, 64, 32}) consider(SINGLES, w, 1);
     return best;
 }
 
+constexpr int BLOCKS_PER_SM = 4;
 template <bool FP16>
 cudaError_t launch_tiles(const AdapterParams &p, const OpsDevice &dev, cudaStream_t st) {
     CUtensorMap mx, ma;
     if (!map_rows(dev.encode_tiled, &mx, p.x, FP16, p.M, p.K, p.xs, TM)) return cudaErrorInvalidValue;
     if (p.segments) {
         if (!map_adapters(dev.encode_tiled, &ma, p.a, FP16, p.adapters, p.rank, p.K, p.rank16)) return cudaErrorInvalidValue;
-        const cudaError_t e = launch_shrink<FP16>(mx, ma, p, dev, st);
+        // blocks of 16 rows that all find a place at once, beside the projection's CTAs; beyond that they would read x too often
+        const bool blocks = (long long)pairs_of(p, 16) * (p.rank16 / 16) <= BLOCKS_PER_SM * dev.sms;
+        const cudaError_t e = blocks ? launch_shrink_blocks(p, FP16, st) : launch_shrink<FP16>(mx, ma, p, dev, st);
         if (e != cudaSuccess) return e;
     }
     int bn = 0;
@@ -587,7 +693,9 @@ cudaError_t launch_tiles(const AdapterParams &p, const OpsDevice &dev, cudaStrea
         case 224: return launch_linear<224, FP16>(mx, p, sh, dev, st);
         case 192: return launch_linear<192, FP16>(mx, p, sh, dev, st);
         case 160: return launch_linear<160, FP16>(mx, p, sh, dev, st);
-        default: return launch_linear<128, FP16>(mx, p, sh, dev, st);
+        case 128: return launch_linear<128, FP16>(mx, p, sh, dev, st);
+        case 64: return launch_linear<64, FP16>(mx, p, sh, dev, st);
+        default: return launch_linear<32, FP16>(mx, p, sh, dev, st);
     }
 }
 

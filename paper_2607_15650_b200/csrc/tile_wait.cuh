@@ -139,14 +139,14 @@ typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, 
                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// 16-bit values as a tensor map of `rank` dimensions, innermost first, `strides` in bytes (those of dimensions 1 and on); 128-byte
-// swizzle, boxes of 64 values; what lies outside reads as zero.
+// 16-bit values as a tensor map of `rank` dimensions, innermost first, `strides` in bytes (those of dimensions 1 and on); boxes of 64
+// values with the 128-byte swizzle, or of another's width; what lies outside reads as zero.
 inline bool encode_map(void *fn, CUtensorMap *tm, const void *base, bool fp16, int rank, const cuuint64_t *dims, const cuuint64_t *strides,
-                       const cuuint32_t *box) {
+                       const cuuint32_t *box, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
     const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
     return reinterpret_cast<EncodeTiled>(fn)(tm, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank,
                                              const_cast<void *>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                             swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
