@@ -37,6 +37,7 @@ shrink_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
+    wait_for_previous();
     let_next_start();
     // this cluster's pair
     const int pair = blockIdx.x / sh.splits, part = blockIdx.x - pair * sh.splits;
@@ -279,6 +280,8 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     else __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
+    if (p.segments == 0) wait_for_previous();   // (else the launch before is t's kernel, which has waited)
+    let_next_start();
     // SPLIT: this pair's columns of the tile; [part][row][pitch] in its own stages, and as the others send theirs
     const int split_cols = SPLIT ? split_columns(BN, sh.splits) : 0, pitch = split_cols + 4;
     const uint32_t block_bytes = (uint32_t)(TM * pitch * 4);
@@ -583,11 +586,13 @@ cudaError_t launch_shrink(const CUtensorMap &mx, const CUtensorMap &ma, const Ad
     cfg.blockDim = dim3(SHRINK_THREADS);
     cfg.dynamicSmemBytes = sh.smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr = {};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = (unsigned)sh.splits; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    cudaLaunchAttribute attr[2] = {};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)sh.splits; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, shrink_kernel<FP16>, mx, ma, p, sh);
 }
 
@@ -616,7 +621,7 @@ cudaError_t launch_linear(const CUtensorMap &mx, const AdapterParams &p, LinearS
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = p.segments ? 2 : 1;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, linear_kernel<BN, FP16, MODE>, mx, mw, mt, mb, my, p, sh);
 }
 template <int BN, bool FP16>

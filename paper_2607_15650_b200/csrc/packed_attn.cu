@@ -17,12 +17,13 @@
 #include <cmath>
 
 #include "packed_attn.h"
+#include "tile_wait.cuh"
 
 namespace dt {
 namespace {
 
 // ------------------------------------------------------------------------------------------------ few rows
-constexpr int FEW_KEYS = 16, FEW_WARPS = 4, FEW_THREADS = FEW_WARPS * 32;
+constexpr int FEW_KEYS = 16, FEW_WARPS = 4, FEW_THREADS = FEW_WARPS * 32;   // at most: blocks for few keys have fewer warps
 constexpr int FEW_STATES = FEW_WARPS + 1;   // one per warp, and one of the keys that only some of the rows have
 
 template <bool FP16>
@@ -46,8 +47,10 @@ struct FewCfg {
     static constexpr int ROW = D * 2, TILE = FEW_KEYS * ROW, STAGE = 2 * TILE;   // bytes: a key's row, K of a chunk, K and V
     static constexpr int MAX_STAGES = D == 128 ? 3 : 6;
     static constexpr int PITCH = D + 4;                                           // floats of a row of O
-    static constexpr int STATES = FEW_STATES * ROWS * (PITCH + 2) * 4 + ROWS * 8;
-    static int smem(int stages) { return FEW_WARPS * stages * STAGE > STATES ? FEW_WARPS * stages * STAGE : STATES; }
+    static int smem(int warps, int stages) {
+        const int ring = warps * stages * STAGE, states = (warps + 1) * ROWS * (PITCH + 2) * 4 + ROWS * 8;
+        return ring > states ? ring : states;
+    }
 };
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool here) {   // zeros where there is nothing to read
@@ -101,7 +104,9 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) packed_few_kernel(const Packed
     constexpr int FEW_ROWS = 8 * NT;
     using C = FewCfg<D, FEW_ROWS>;
     extern __shared__ __align__(128) uint8_t smem_raw[];
-    const int splits = shape.splits, stages = shape.stages;
+    wait_for_previous();
+    let_next_start();
+    const int splits = shape.splits, stages = shape.stages, warps = blockDim.x >> 5;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int split = splits > 1 ? (int)cluster_rank() : 0;
     const int b = blockIdx.y / p.Hkv, hk = blockIdx.y - b * p.Hkv;
@@ -115,7 +120,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) packed_few_kernel(const Packed
     const int len = keys_end(p, doc, l0) - doc.k0;
     auto token_of = [&](int r) { return l0 + r / heads; };
     auto head_of = [&](int r) { return hk * p.rep + h0 + r % heads; };
-    const int step = splits * FEW_WARPS * FEW_KEYS, first = (split * FEW_WARPS + warp) * FEW_KEYS;
+    const int step = splits * warps * FEW_KEYS, first = (split * warps + warp) * FEW_KEYS;
     const uint32_t ring = smem_u32(smem_raw) + warp * stages * C::STAGE;
 
     // Chunk of keys -> ring stage.  16-byte piece c of row r lies at c ^ (r & 7): the fragments' reads meet no bank twice.
@@ -249,8 +254,8 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) packed_few_kernel(const Packed
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();   // the rings are done with: the states take their place
     float *const so = reinterpret_cast<float *>(smem_raw);                       // [warp][row][PITCH]
-    float *const sm = so + FEW_STATES * FEW_ROWS * C::PITCH, *const sl = sm + FEW_STATES * FEW_ROWS;   // [warp][row]
-    float *const cm = sl + FEW_STATES * FEW_ROWS, *const cl = cm + FEW_ROWS;      // the block's joined state (O in so's first)
+    float *const sm = so + (warps + 1) * FEW_ROWS * C::PITCH, *const sl = sm + (warps + 1) * FEW_ROWS;   // [warp][row]
+    float *const cm = sl + (warps + 1) * FEW_ROWS, *const cl = cm + FEW_ROWS;      // the block's joined state (O in so's first)
     // this warp's state
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -275,9 +280,9 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) packed_few_kernel(const Packed
         }
     // Causal rows of several tokens: the keys behind the first token's end, fewer than there are tokens, row by row and in fp32, so that
     // a key has no effect on the rows it does not count for (in a product of all rows, 0 times its V would be NaN if that is).
-    const int states = p.causal && shape.tokens > 1 ? FEW_STATES : FEW_WARPS;
-    if (states > FEW_WARPS) {
-        for (int r = warp; r < live; r += FEW_WARPS) {
+    const int states = p.causal && shape.tokens > 1 ? warps + 1 : warps;
+    if (states > warps) {
+        for (int r = warp; r < live; r += warps) {
             const int l = token_of(r), h = head_of(r), end = split == 0 ? keys_end(p, doc, l) - doc.k0 : len;
             const RowBias bias = row_bias<BIAS>(p, h, l + doc.shift - doc.k0);
             const uint16_t *qr = p.q + b * p.qs[0] + l * p.qs[1] + h * p.qs[2], *kr0 = p.k + b * p.ks[0] + hk * p.ks[2], *vr0 = p.v + b * p.vs[0] + hk * p.vs[2];
@@ -287,8 +292,8 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) packed_few_kernel(const Packed
                 qv[i] = value<FP16>(qr[lane + 32 * i]);
                 acc[i] = 0.f;
             }
-#pragma unroll 1
-            for (int key = len; key < end; ++key) {
+#pragma unroll 4
+            for (int key = len; key < end; ++key) {   // (several keys' loads at once)
                 float s = 0.f, vv[D / 32];
 #pragma unroll
                 for (int i = 0; i < D / 32; ++i) {
@@ -305,16 +310,16 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) packed_few_kernel(const Packed
                 for (int i = 0; i < D / 32; ++i) acc[i] = fmaf(acc[i], alpha, pr * vv[i]);
             }
             if (lane == 0) {
-                sm[FEW_WARPS * FEW_ROWS + r] = top;
-                sl[FEW_WARPS * FEW_ROWS + r] = sum;
+                sm[warps * FEW_ROWS + r] = top;
+                sl[warps * FEW_ROWS + r] = sum;
             }
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) so[(FEW_WARPS * FEW_ROWS + r) * C::PITCH + lane + 32 * i] = acc[i];
+            for (int i = 0; i < D / 32; ++i) so[(warps * FEW_ROWS + r) * C::PITCH + lane + 32 * i] = acc[i];
         }
     }
     __syncthreads();
     // join the block's warps, 4 values of a row at a time, into the first warp's place
-    for (int i = threadIdx.x; i < live * (D / 4); i += FEW_THREADS) {
+    for (int i = threadIdx.x; i < live * (D / 4); i += blockDim.x) {
         const int r = i / (D / 4), c = i - r * (D / 4);
         float top = -INFINITY;
 #pragma unroll
@@ -341,7 +346,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) packed_few_kernel(const Packed
     else __syncthreads();
     // join the cluster's blocks: groups of 4 values (row, 4 values) shared out over the blocks
     const uint32_t m_addr = smem_u32(cm), l_addr = smem_u32(cl), o_addr = smem_u32(so);
-    for (int i = split * FEW_THREADS + threadIdx.x; i < live * (D / 4); i += splits * FEW_THREADS) {
+    for (int i = split * blockDim.x + threadIdx.x; i < live * (D / 4); i += splits * blockDim.x) {
         const int r = i / (D / 4), c = i - r * (D / 4);
         float top = -INFINITY;
         for (int s = 0; s < splits; ++s) top = fmaxf(top, splits > 1 ? ld_cluster(m_addr + 4 * r, s) : cm[r]);
@@ -378,7 +383,7 @@ cudaError_t launch_few(const PackedParams &p, const OpsDevice &dev, cudaStream_t
     using C = FewCfg<D, 8 * NT>;
     static OncePerDevice once;
     const cudaError_t e = once(dev, [] {
-        return cudaFuncSetAttribute(packed_few_kernel<D, FP16, NT, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem(C::MAX_STAGES));
+        return cudaFuncSetAttribute(packed_few_kernel<D, FP16, NT, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem(FEW_WARPS, C::MAX_STAGES));
     });
     if (e != cudaSuccess) return e;
     FewShape sh;
@@ -388,22 +393,28 @@ cudaError_t launch_few(const PackedParams &p, const OpsDevice &dev, cudaStream_t
     // (with borders, up to as many blocks as there are documents have no rows)
     const long long groups = (p.q_starts ? (long long)((p.Lq + sh.tokens - 1) / sh.tokens) * sh.head_blocks : units) * p.B * p.Hkv;
     // Split the keys while that still gives every warp a chunk of its own and the blocks fit the GPU at once (2 per SM).
+    // Many small documents: with one warp 12 blocks fit an SM instead of 3 (12 of them in 14 tokens, 40 heads, 3 rows: 12 us instead of 26);
+    // where the blocks find a place at once, more warps are the faster ones (3 in 5 tokens, 8 heads, 3 rows: 8 us instead of 12).
+    const bool few_blocks = units * p.B * p.Hkv <= 2LL * dev.sms;
+    const int warps = few_blocks || p.Lk > 4 * FEW_KEYS ? FEW_WARPS : p.Lk > 2 * FEW_KEYS ? 2 : 1;
     int splits = 1;
-    while (splits < 8 && groups * splits * 2 <= 2LL * dev.sms && splits * FEW_WARPS * FEW_KEYS < p.Lk) splits *= 2;
-    const int chunks = (p.Lk + splits * FEW_WARPS * FEW_KEYS - 1) / (splits * FEW_WARPS * FEW_KEYS);   // of a warp
+    while (splits < 8 && groups * splits * 2 <= 2LL * dev.sms && splits * warps * FEW_KEYS < p.Lk && warps == FEW_WARPS) splits *= 2;
+    const int chunks = (p.Lk + splits * warps * FEW_KEYS - 1) / (splits * warps * FEW_KEYS);   // of a warp
     sh.splits = splits;
     sh.stages = chunks >= C::MAX_STAGES ? C::MAX_STAGES : chunks >= 3 ? 3 : 2;
     if (units * splits > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(units * splits), (unsigned)(p.B * p.Hkv));
-    cfg.blockDim = dim3(FEW_THREADS);
-    cfg.dynamicSmemBytes = C::smem(sh.stages);
+    cfg.blockDim = dim3((unsigned)(warps * 32));
+    cfg.dynamicSmemBytes = C::smem(warps, sh.stages);
     cfg.stream = st;
-    cudaLaunchAttribute attr = {};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = (unsigned)splits; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = splits > 1 ? 1 : 0;
+    cudaLaunchAttribute attr[2] = {};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // (starts beside the end of the launch before and waits for it)
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)splits; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = splits > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, packed_few_kernel<D, FP16, NT, CAP, BIAS>, p, sh);
 }
 template <int D, bool FP16, int NT>

@@ -303,6 +303,8 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = tmem_base_slot;
+    wait_for_previous();
+    let_next_start();
 
     // The next item of the stream, for a warp that reads them one after another; false: a wait ran out.
     uint32_t slot = 0, slot_ph = 0;
@@ -966,8 +968,17 @@ cudaError_t launch(int grid, const CUtensorMap &tq, const CUtensorMap &tk, const
         return cudaFuncSetAttribute(packed_tile_kernel<D, FP16, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::SMEM_BYTES);
     });
     if (e != cudaSuccess) return e;
-    packed_tile_kernel<D, FP16, CAP, BIAS><<<grid, THREADS, Cfg<D>::SMEM_BYTES, st>>>(tq, tk, tv, p);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = Cfg<D>::SMEM_BYTES;
+    cfg.stream = st;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;   // (starts beside the end of the launch before and waits for it)
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, packed_tile_kernel<D, FP16, CAP, BIAS>, tq, tk, tv, p);
 }
 template <int D, bool FP16>
 cudaError_t launch(int grid, const CUtensorMap &tq, const CUtensorMap &tk, const CUtensorMap &tv, const TileParams &p, const OpsDevice &dev, cudaStream_t st) {
