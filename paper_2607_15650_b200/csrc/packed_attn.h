@@ -51,20 +51,31 @@ __device__ __forceinline__ int keys_end(const PackedParams &p, const Doc &d, int
 // q0_d / size + d + j of its row of the batch: ceil(n / size) <= (q0 + n) / size - q0 / size + 1, so no two have the same number, and
 // Lq / size + docs numbers are enough.  No list is made; some numbers have no rows.
 __host__ __device__ inline int blocks_of(int Lq, int docs, int size, bool borders) { return borders ? Lq / size + docs : (Lq + size - 1) / size; }
-// The document and first row of block `u` of row b of the batch; false: no rows.
+// The document and first row of block `u` of row b of the batch, alike for a whole warp, which asks together; false: no rows.  32 documents
+// are looked at at once, a lane each: one round of loads instead of a chain.
 __device__ __forceinline__ bool block_at(const PackedParams &p, int b, int u, int size, Doc &doc, int &row0) {
-    int d = 0;
     if (p.q_starts != nullptr) {   // the last document whose number is not beyond u
         const int32_t *at = p.q_starts + (long long)b * (p.docs + 1);
-        int hi = p.docs;
-        while (hi - d > 1) {
-            const int mid = (d + hi) >> 1;
-            if (clamped(at + mid, p.Lq) / size + mid <= u) d = mid;
+        int lo = 0, hi = (p.docs + 31) / 32;   // of the steps
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (clamped(at + 32 * mid, p.Lq) / size + 32 * mid <= u) lo = mid;
             else hi = mid;
         }
-        u -= clamped(at + d, p.Lq) / size + d;
+        const int d = min(32 * lo + (int)(threadIdx.x & 31), p.docs - 1);
+        const Doc mine = doc_of(p, b, d);
+        const int number = mine.q0 / size + d;
+        const int from = max(__popc(__ballot_sync(0xFFFFFFFFu, number <= u && 32 * lo + (int)(threadIdx.x & 31) < p.docs)) - 1, 0);
+        doc.q0 = __shfl_sync(0xFFFFFFFFu, mine.q0, from);
+        doc.q1 = __shfl_sync(0xFFFFFFFFu, mine.q1, from);
+        doc.k0 = __shfl_sync(0xFFFFFFFFu, mine.k0, from);
+        doc.k1 = __shfl_sync(0xFFFFFFFFu, mine.k1, from);
+        doc.prefix_end = __shfl_sync(0xFFFFFFFFu, mine.prefix_end, from);
+        doc.shift = doc.k1 - doc.q1;
+        u -= __shfl_sync(0xFFFFFFFFu, number, from);
+    } else {
+        doc = doc_of(p, b, 0);
     }
-    doc = doc_of(p, b, d);
     if (u < 0 || u > (doc.q1 - doc.q0) / size) return false;
     row0 = doc.q0 + u * size;
     return row0 < doc.q1;
