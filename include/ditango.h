@@ -442,7 +442,8 @@ dt_status dt_cross_attn(const dt_cross_config *cfg, const void *q_dev, const int
 /* ------------------------------------------------------------------------------------------------------------------
  * Operators for several requests packed into one batch: their rows stand behind one another, and int32 borders on the device say
  * where each begins.  As above: no context, nothing is allocated, stream-ordered, capturable, no atomics.  Borders do not decrease
- * (those outside the rows are clamped). */
+ * (those outside the rows are clamped).  Launches are programmatic: each begins beside the end of the launch before in its stream, waits
+ * for that one's end before it looks at memory, and lets the next begin likewise if that asks for it. */
 
 /* A projection that all rows share, with a low-rank adapter per segment of rows:
  *     y[m] = W x[m] + bias + scales[a] B_a (A_a x[m]),   a = adapters_of[s] for starts[s] <= m < starts[s + 1].
@@ -491,7 +492,7 @@ typedef struct {
     int32_t dtype;                    /* DT_VALUE_BF16 or DT_VALUE_FP16 */
     int32_t B, Lq, Lk, H, H_kv, D;
     int32_t docs, causal, bias_far;
-    float softmax_scale, softcap;     /* softcap 0: none */
+    float softmax_scale, softcap;     /* softcap 0: none; else softcap and softmax_scale / softcap are normal numbers */
 } dt_packed_config;
 dt_status dt_packed_attn(const dt_packed_config *cfg, const void *q_dev, const int64_t q_strides_blhd[4], const void *k_dev,
                          const int64_t k_strides_blhd[4], const void *v_dev, const int64_t v_strides_blhd[4], const int32_t *q_starts_dev,
