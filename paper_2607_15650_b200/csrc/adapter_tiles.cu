@@ -10,9 +10,9 @@
 // other half takes the next.  The adapter's part of a tile is just more k-steps into the same accumulator: t (rows x rank) times B_a (columns
 // x rank) for each segment that the tile meets, with the rows of other segments left out by the MMA's own mask of lanes.  So rows never see
 // another request's adapter, whatever it holds, and y is rounded once.
-// Measured without adapters (inputs beyond L2, us; the library's product beside it): 256 x 1024 x 1024 6.1 (3.8), 64 x 5120 x 5120 22.3 (12.2), 512 x
-// 5120 x 5120 27.2 (20.8), 1807 x 4096 x 5120 62 (55), 32760 x 1536 x 1536 110 (106), 75600 x 5120 x 5120 2870 (2550 to 2900, power-capped); with
-// adapters of rank 16 to 64: 8.2, 26.5, 39.3, 70.6, 126.7, 2710.
+// Measured without adapters (inputs beyond L2, us; the library's product beside it): 256 x 1024 x 1024 5.3 (3.7), 64 x 5120 x 5120 21.2 (12.0), 512 x
+// 5120 x 5120 26.2 (20.5), 1807 x 4096 x 5120 60 (54), 32760 x 1536 x 1536 107 (104), 75600 x 5120 x 5120 2720 to 2940 (2550 to 2900, power-capped); with
+// adapters of rank 16 to 64: 8.2, 26.5, 30.2, 70, 125, 2590 to 2670.
 #include "adapter_linear.h"
 #include "tile_wait.cuh"
 
@@ -191,11 +191,12 @@ struct LinearCfg {
     static constexpr int ATOMS = MODE == SINGLES && BN <= 64 ? 4 : MODE == SPLIT_PAIRS && BN > 128 ? 1 : 2;
     static constexpr int B_ROWS = BN / CTAS, B_BYTES = B_ROWS * 128;   // each CTA of a pair loads half of the columns
     static constexpr int ATOM = A_BYTES + B_BYTES, STAGE = ATOMS * ATOM;
-    static constexpr int OUT = SPLIT ? 0 : EPILOGUE_WARPS * 2 * 2048;        // a warp's staging: 32 rows x 64 bytes, twice
+    static constexpr int OUT = SPLIT ? 0 : EPILOGUE_WARPS * 2048;            // a warp's staging: 32 rows x 64 bytes
     static constexpr int SUMS = SPLIT ? (MOST_SPLITS - 1) * TM * split_pitch(BN, MOST_SPLITS) * 4 : 0;   // that other pairs send
-    static constexpr int STAGES = SPLIT ? (226 * 1024 - SUMS) / STAGE : 196608 / STAGE < 12 ? 196608 / STAGE : 12;
+    static constexpr int STAGES = SPLIT ? (215 * 1024 - SUMS) / STAGE : 196608 / STAGE < 12 ? 196608 / STAGE : 12;
     static constexpr int SMEM = 1024 + STAGES * STAGE + OUT + SUMS + (2 * STAGES + 5) * 8;
-    static_assert(SMEM + 64 <= 227 * 1024 && 2 * STAGES + 5 <= 32, "beyond the shared memory of a CTA, or a warp's lanes");
+    static_assert(SMEM + 64 <= 216 * 1024 + 512 &&   // (a block of shrink_blocks_kernel finds a place beside it)
+                   2 * STAGES + 5 <= 32, "beyond the shared memory of a CTA, or a warp's lanes");
     // SPLIT: the partial sums to be sent stand where the stages were
     static_assert(!SPLIT || (TM * split_pitch(BN, 2) * 4 <= STAGES * STAGE && 2 * TM * split_pitch(BN, 3) * 4 <= STAGES * STAGE && SUMS <= STAGES * STAGE &&
                              TM * split_pitch(BN, 2) * 4 <= SUMS && 2 * TM * split_pitch(BN, 3) * 4 <= SUMS), "no room for a tile's sums");
@@ -419,7 +420,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     } else {
         const int quarter = warp % 4, side = (warp - 2) / 4;   // this warp's rows; which of every two pieces of columns it has
         const uint32_t lane_addr = ((uint32_t)(quarter * 32)) << 16;
-        uint32_t n = 0, n_out = 0;
+        uint32_t n = 0;
         bool ok = true;
 #pragma unroll 1
         for (int w = pair; w < sh.tiles; w += pairs, ++n) {
@@ -518,8 +519,8 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                         if (8 * c < left) *reinterpret_cast<uint4 *>(out + c0 + 8 * c) = make_uint4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
                 } else {
                     // 32 rows x 64 bytes to shared memory (swizzled), and from there by TMA, which leaves out what is beyond y
-                    const uint32_t to = out_smem + (uint32_t)((warp - 2) * 2 + (n_out++ & 1)) * 2048u;
-                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                    const uint32_t to = out_smem + (uint32_t)(warp - 2) * 2048u;
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     __syncwarp();
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
@@ -678,14 +679,15 @@ inline LinearShape shape_of(const AdapterParams &p, int sms, int &bn) {
     return best;
 }
 
-constexpr int BLOCKS_PER_SM = 4;
+constexpr int BLOCKS_PER_SM = 2;
 template <bool FP16>
 cudaError_t launch_tiles(const AdapterParams &p, const OpsDevice &dev, cudaStream_t st) {
     CUtensorMap mx, ma;
     if (!map_rows(dev.encode_tiled, &mx, p.x, FP16, p.M, p.K, p.xs, TM)) return cudaErrorInvalidValue;
     if (p.segments) {
         if (!map_adapters(dev.encode_tiled, &ma, p.a, FP16, p.adapters, p.rank, p.K, p.rank16)) return cudaErrorInvalidValue;
-        // blocks of 16 rows that all find a place at once, beside the projection's CTAs; beyond that they would read x too often
+        // blocks of 16 rows that all find a place at once, beside the projection's CTAs; beyond that they read A and x too often (4096 x 4096 x
+        // 4096 of rank 32, 524 blocks: 116 us, with tensor-memory tiles 103)
         const bool blocks = (long long)pairs_of(p, 16) * (p.rank16 / 16) <= BLOCKS_PER_SM * dev.sms;
         const cudaError_t e = blocks ? launch_shrink_blocks(p, FP16, st) : launch_shrink<FP16>(mx, ma, p, dev, st);
         if (e != cudaSuccess) return e;
