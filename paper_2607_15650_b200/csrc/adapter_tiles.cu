@@ -497,16 +497,15 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                     }
                 }
                 if (p.bias != nullptr) {
-#pragma unroll 1
-                    for (int i = 0; i < 1; ++i) {
-                        float f[32];
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) f[c] = __uint_as_float(v[c]);
+                    for (int c = 0; c < 32; c += 8) {
+                        if (c0 + c >= cols) continue;
+                        float f[8];
 #pragma unroll
-                        for (int c = 0; c < 32; c += 8)
-                            if (c0 + c < cols) add_bias<FP16, 8>(p, ni * BN + c0 + c, *reinterpret_cast<float (*)[8]>(f + c));
+                        for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[c + i]);
+                        add_bias<FP16, 8>(p, ni * BN + c0 + c, f);
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(f[c]);
+                        for (int i = 0; i < 8; ++i) v[c + i] = __float_as_uint(f[i]);
                     }
                 }
                 uint32_t o[16];
