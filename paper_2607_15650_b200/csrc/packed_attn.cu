@@ -23,8 +23,8 @@ namespace dt {
 namespace {
 
 // ------------------------------------------------------------------------------------------------ few rows
-constexpr int FEW_KEYS = 16, FEW_WARPS = 4, FEW_THREADS = FEW_WARPS * 32;   // at most: blocks for few keys have fewer warps
-constexpr int FEW_STATES = FEW_WARPS + 1;   // one per warp, and one of the keys that only some of the rows have
+constexpr int FEW_KEYS = 16, FEW_WARPS = 4, MOST_WARPS = 8, FEW_THREADS = MOST_WARPS * 32;   // (blocks for few keys have one or two)
+constexpr int FEW_STATES = MOST_WARPS + 1;   // one per warp, and one of the keys that only some of the rows have
 
 template <bool FP16>
 __device__ __forceinline__ float value(uint16_t v) {
@@ -100,7 +100,7 @@ __device__ __forceinline__ float logit(const PackedParams &p, float s, const Row
 }
 
 template <int D, bool FP16, int NT, bool CAP, int BIAS>
-__global__ void __launch_bounds__(FEW_THREADS, 2) packed_few_kernel(const PackedParams p, const FewShape shape) {
+__global__ void __launch_bounds__(FEW_THREADS, 1) packed_few_kernel(const PackedParams p, const FewShape shape) {
     constexpr int FEW_ROWS = 8 * NT;
     using C = FewCfg<D, FEW_ROWS>;
     extern __shared__ __align__(128) uint8_t smem_raw[];
@@ -383,7 +383,7 @@ cudaError_t launch_few(const PackedParams &p, const OpsDevice &dev, cudaStream_t
     using C = FewCfg<D, 8 * NT>;
     static OncePerDevice once;
     const cudaError_t e = once(dev, [] {
-        return cudaFuncSetAttribute(packed_few_kernel<D, FP16, NT, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem(FEW_WARPS, C::MAX_STAGES));
+        return cudaFuncSetAttribute(packed_few_kernel<D, FP16, NT, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem(MOST_WARPS, C::MAX_STAGES));
     });
     if (e != cudaSuccess) return e;
     FewShape sh;
@@ -396,9 +396,20 @@ cudaError_t launch_few(const PackedParams &p, const OpsDevice &dev, cudaStream_t
     // Many small documents: with one warp 12 blocks fit an SM instead of 3 (12 of them in 14 tokens, 40 heads, 3 rows: 12 us instead of 26);
     // where the blocks find a place at once, more warps are the faster ones (3 in 5 tokens, 8 heads, 3 rows: 8 us instead of 12).
     const bool few_blocks = units * p.B * p.Hkv <= 2LL * dev.sms;
-    const int warps = few_blocks || p.Lk > 4 * FEW_KEYS ? FEW_WARPS : p.Lk > 2 * FEW_KEYS ? 2 : 1;
+    int warps = few_blocks || p.Lk > 4 * FEW_KEYS ? FEW_WARPS : p.Lk > 2 * FEW_KEYS ? 2 : 1;
     int splits = 1;
     while (splits < 8 && groups * splits * 2 <= 2LL * dev.sms && splits * warps * FEW_KEYS < p.Lk && warps == FEW_WARPS) splits *= 2;
+    // Few clusters of many keys: a warp's chunk (16 keys) is a chain of 1300 cycles, so what counts is warps.  Blocks of eight leave an SM to one,
+    // so of these clusters only so many find a place at once; one more, and its time comes on top.
+    const int sms = dev.sms, places[9] = {0, 0, sms / 2, 0, sms * 15 / 64, 0, sms / 7, 0, sms / 10 + 1};
+    for (int size = 8; size >= 2 && warps == FEW_WARPS; size -= 2) {
+        if (groups > places[size]) continue;
+        if (size * MOST_WARPS > splits * FEW_WARPS && p.Lk >= 4 * size * MOST_WARPS * FEW_KEYS) {
+            splits = size;
+            warps = MOST_WARPS;
+        }
+        break;
+    }
     const int chunks = (p.Lk + splits * warps * FEW_KEYS - 1) / (splits * warps * FEW_KEYS);   // of a warp
     sh.splits = splits;
     sh.stages = chunks >= C::MAX_STAGES ? C::MAX_STAGES : chunks >= 3 ? 3 : 2;

@@ -192,3 +192,20 @@ def test_many_small_documents():
             o, l, tol, tol_l, _ = ref.attention(q, k, v, 0.1, [[(a, b, a, b, 0) for a, b in zip(at, at[1:])]] * 3, causal=causal, softcap=5.0)
             check(out, o, tol, (L, n, causal))
             check(lse, l, tol_l, (L, n, causal))
+
+
+@pytest.mark.parametrize("B,H,Hk,D", [(1, 2, 1, 64), (2, 8, 4, 128), (2, 40, 8, 64), (3, 20, 5, 128), (1, 20, 20, 128), (5, 8, 8, 64)])
+def test_few_tokens_of_few_heads_behind_many_keys(B, H, Hk, D):
+    """Clusters of every size and both numbers of warps, with lengths that leave some of them without keys."""
+    L = 9001
+    k, v = rnd((B, L, Hk, D), 1, BF16), rnd((B, L, Hk, D), 2, BF16)
+    lens = [L, 40, 5000, 0, 8192][:B]
+    for Lq in (1, 3):
+        q = rnd((B, Lq, H, D), 3 + Lq, BF16, 2.0)
+        for kw in (dict(), dict(softcap=20.0), dict(bias_slopes=2.0 ** -torch.arange(1.0, H + 1, device="cuda"))):
+            out, lse = torch.empty_like(q), torch.empty((B, H, Lq), device="cuda")
+            dt.dt_packed_attn(q, k, v, out, D ** -0.5, causal=True, key_lens=ints(lens), lse_out=lse, **kw)
+            extra = dict(softcap=kw.get("softcap", 0.0), slopes=kw.get("bias_slopes"))
+            o, l, tol, tol_l, _ = ref.attention(q, k, v, D ** -0.5, [[(0, Lq, 0, n, 0)] for n in lens], causal=True, **extra)
+            check(out, o, tol, (Lq, lens, "out"))
+            check(lse, l, tol_l, (Lq, lens, "lse"))
