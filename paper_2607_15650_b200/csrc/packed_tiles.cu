@@ -26,7 +26,7 @@
 // diagonal reads it without clamping (a thread's columns are neighbours in it, and so are a warp's rows); a tile beyond `far` adds
 // one value.
 //
-// Measured (us on the GPU, TFLOP/s in brackets): 4441 x 4441 of 2 x 32 heads of 128 365 (1280), with a cap 569 (820); 17550 causal of 40 heads with slopes in fp16
+// Measured (us on the GPU, TFLOP/s in brackets): sequences of 4441 and 2961 of 32 heads of 128 365 (1280), with a cap 569 (820); 17550 causal of 40 heads with slopes in fp16
 // 2980 (1058); three documents in 32760 of 12 heads 2070 (1340); 2048 of 64 heads of 64 103 (640), in 32 documents 47.
 //
 // Every wait on an mbarrier is bounded; on expiry the CTA records STATUS_WAIT_TIMEOUT, leaves its loops, lets what is under way
