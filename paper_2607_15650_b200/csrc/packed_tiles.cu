@@ -4,6 +4,7 @@
 // One CTA per SM at a time, which stays for as many items as it can take over, 16 warps --
 //   warps 0-3 / 4-7  softmax of query tile 0 / 1 (128 rows each, one row per thread)
 //   warp 8           producer: the items; Q of every item, K and V tiles through a ring in the order the MMAs consume them (TMA)
+//                    (and OUT and LSE of blocks without keys, which are no items)
 //   warps 9, 10      MMA issuers of query tile 0 / 1
 //   warp 11          V's rows that do not count for all of an item's rows; the bias table of every item
 //   warps 12-15      epilogue of both query tiles: O from TMEM, divided by the sum, to the caller's tensor
@@ -54,7 +55,10 @@ constexpr int TABLE_BYTES = (2 * FAR_MOST + 1 + 2 * TABLE_PAD + 3) / 4 * 16;
 // the one whose P V is under way, and that one at most two ahead of the epilogue.
 constexpr int MARKS = 8;
 constexpr int TANH_BYTES = 64;                             // the pairs of capped_near
-constexpr int SLOTS = 4;                                   // items that the producer may be ahead of the slowest role
+// Items that the producer may be ahead of the slowest role.  It publishes one item (or the end) ahead of the last V of the item before,
+// which the epilogue still waits for: what is published there may never need a place that the epilogue has yet to hand back, so
+// blocks without keys, of which any number may come in a row, do not pass through here.
+constexpr int SLOTS = 4;
 constexpr int READERS = THREADS / 32 - 1;                  // warps that read an item
 
 template <int D>
@@ -100,9 +104,9 @@ struct TileParams {
 // (clusterlaunchcontrol), a little before it needs them.  So the SMs stay busy whatever the items' lengths, and the launch has a CTA
 // per block.  Heads run fastest, so that neighbours share K and V in L2 where heads are grouped; blocks run from the last, so that causal
 // rows with many keys come first.
-// The producer looks an item up and leaves it in shared memory for the other roles.
+// The producer looks an item up and leaves it in shared memory for the other roles; rows of a block without keys it writes itself.
 struct Item {
-    int tiles[NQ];           // of keys, for each query tile: the item's first ones; 0: it has no rows or no keys
+    int tiles[NQ];           // of keys, for each query tile: the item's first ones; 0: it has no rows or no keys (not both of them)
     int b, h, row0, q1;      // first row; the end of the document's
     int k0, k1, shift, prefix_end;
     int first_end;           // the end of the first row's keys
@@ -400,7 +404,7 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                     __syncwarp();
                 }
             }
-            if (it.all() > 0) ++item;
+            ++item;
         }
         if (!ok && lane == 0) give_up(abort_ptr, p.c.status);
     } else if (warp >= TMA_WARP) {
@@ -431,7 +435,18 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                 __syncwarp();
                 if (++slot == SLOTS) { slot = 0; slot_ph ^= 1u; }
             };
-            // The next item with keys, after those without for the epilogue alone; `state` 0: none.
+            // OUT = 0 and LSE = -infinity for the rows of a block without keys.
+            auto write_none = [&](const Item &it) {
+                constexpr int PIECES = D / 8, ROWS = 32 / PIECES;   // 16-byte pieces of a row; rows a pass of the warp takes
+                const int to = min(it.row0 + ITEM_ROWS, it.q1);
+                uint16_t *const out = p.c.out + it.b * p.c.os[0] + it.h * p.c.os[2] + lane % PIECES * 8;
+#pragma unroll 4
+                for (int row = it.row0 + lane / PIECES; row < to; row += ROWS) __stcs(reinterpret_cast<uint4 *>(out + row * p.c.os[1]), make_uint4(0u, 0u, 0u, 0u));
+                if (p.c.lse == nullptr) return;
+                float *const lse = p.c.lse + ((long long)it.b * p.c.H + it.h) * p.c.Lq;
+                for (int row = it.row0 + lane; row < to; row += 32) lse[row] = -INFINITY;
+            };
+            // The next item with keys; `state` 0: none.
             auto produce = [&](Item &it) {
 #pragma unroll 1
                 do {
@@ -448,8 +463,11 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                     first = false;
                     over = w < 0;
                     it = Item{};
-                    if (over || item_of(p, w, it)) publish(it);
-                } while (ok && !over && it.all() == 0);
+                    if (over || !item_of(p, w, it) || it.all() > 0) continue;
+                    ask();   // (the next number comes while this block's rows are written)
+                    write_none(it);
+                } while (!over && it.all() == 0);
+                publish(it);
             };
             auto load_q = [&](const Item &it) {
 #pragma unroll
@@ -537,13 +555,9 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                     if (lane == 0) mbar_arrive(bars.tab_full + 8 * (n & 1u));
                 }
             };
-            auto next_keys = [&](Item &it) {   // the next item with keys
-                do ok = next_item(it);
-                while (ok && it.state != 0 && it.all() == 0);
-            };
             Item cur, nxt;
             uint32_t place = 0, n = 0;   // K/V tiles of the stream so far; items
-            next_keys(nxt);
+            ok = next_item(nxt);
             if (ok && nxt.state != 0) fill_table(nxt, 0);
 #pragma unroll 1
             while (ok && nxt.state != 0) {
@@ -554,7 +568,7 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 #pragma unroll 1
                 for (int t = min(max(0, (cur.first_end - cur.k0) / TILE), last); t <= last && ok; ++t) {
                     if (t == last) {
-                        next_keys(nxt);
+                        ok = next_item(nxt);
                         if (ok && nxt.state != 0) fill_table(nxt, n + 1);
                         if (!ok) break;
                     }
@@ -631,11 +645,7 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             uint32_t st = 0, ph = 0, q_phase = 0, of_phase = 0, t_phase = 0;   // st, ph: the stream's next K/V tile
             bool ok = true;
             Item it;
-            auto next_keys = [&]() {   // the next item with keys
-                do ok = next_item(it);
-                while (ok && it.state != 0 && it.all() == 0);
-            };
-            next_keys();
+            ok = next_item(it);
             int tiles = 1, mine = 0;                      // of the current item; before the first: a step without a P V
             bool have = false;
 #pragma unroll 1
@@ -644,7 +654,7 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                 for (int k = 0; k < tiles; ++k) {
                     const bool within = k + 1 < tiles;
                     if (have && !within) {   // (the producer has left it there before it loaded this item's last tiles)
-                        next_keys();
+                        ok = next_item(it);
                         if (!ok) break;
                     }
                     const bool more = within || it.state != 0;
@@ -725,7 +735,7 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         const uint32_t s_free = bars.s_free + (C::S_PLACES == 2 ? 8 * q : 0);
         const uint32_t p_tmem = tmem_base + lane_addr + C::P_COL + q * C::P_STRIDE;
         const uint32_t o_tmem = tmem_base + lane_addr + C::O_COL + q * D;
-        uint32_t s_phase = 0, pv_phase = 0, p_items = 0, tables = 0;   // p_items: items handed to the epilogue; tables: items with keys
+        uint32_t s_phase = 0, pv_phase = 0, p_items = 0, tables = 0;   // p_items: items handed to the epilogue; tables: items
         // (from shared memory, so that they stay in registers: as literals they are moved there again for every use)
         float2 cap_c[TANH_WORDS];
         if constexpr (CAP) {
@@ -740,7 +750,6 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                 Item it;
                 ok = next_item(it);
                 if (!ok || it.state == 0) break;
-                if (it.all() == 0) continue;
                 tiles = q == 0 ? it.tiles[0] : it.tiles[1];
                 const int row = it.row0 + q * TILE + row_in_tile;
                 end = keys_end(p.c, it.doc(), min(row, it.q1 - 1)) - it.k0;   // keys of this row

@@ -323,3 +323,59 @@ def test_many_items_of_every_length():
     L = at[-1] + 5
     for kind in (dict(), dict(far=100, causal=True), dict(softcap=6.0, causal=True)):
         Case(1, L, L, 8, 4, 64, BF16, borders=[(at, at)], seed=1, **kind).check()
+
+
+NO_KEYS = [dict(D=64), dict(D=128), dict(D=64, far=128), dict(D=128, far=20), dict(D=128, slopes=True), dict(D=64, softcap=6.0)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("kind", NO_KEYS)
+def test_many_blocks_without_keys_behind_blocks_with_keys(kind, dtype):
+    """Many times as many blocks of 256 rows as there are SMs, most of them without keys, so that a CTA takes over several of those in
+    a row behind one with keys: OUT = 0 and LSE = -inf there."""
+    # a padded batch one of whose requests has no keys; and with the blocks without keys first and last
+    for keys in ([300, 0], [0, 300, 0]):
+        B = len(keys)
+        Case(B, 4096, 300, 64, 64, dtype=dtype, lens=(None, keys), seed=1, **kind).check("padded")
+    # a long causal sequence over few keys, the blocks with keys first
+    Case(1, 9001, 300, 40, 8, dtype=dtype, causal=True, seed=2, **kind).check("causal")
+    # latents beside prompts, some of which are empty
+    q = [0, 1500, 3100, 3100, 5200, 5201, 7000, 9000, 10500, 12000]
+    k = [0, 130, 130, 130, 130, 130, 430, 430, 430, 600]
+    for causal in (False, True):
+        Case(1, 12100, 600, 40, 40, dtype=dtype, borders=[(q, k)], causal=causal, lse=causal, seed=3, **kind).check("prompts")
+
+
+def test_blocks_without_keys_in_the_place_of_q():
+    """Rows of a view are written and nothing beside them."""
+    L, H = 5000, 40
+    qkv = rnd((2, L + 3, 3 * H, 64), 1, BF16)
+    before = qkv.clone()
+    q, k, v = (qkv[:, :L, i * H:(i + 1) * H] for i in range(3))
+    c = Case(2, L, L, H, H, 64, BF16, lens=([L, L - 5], [700, 0]), seed=1)
+    c.q, c.k, c.v = (t.clone() for t in (q, k, v))
+    dt.dt_packed_attn(q, k, v, q, c.scale, lse_out=c.lse, **c.kw)
+    dt.dt_poll_ops()
+    assert torch.equal(qkv[:, L:], before[:, L:]) and torch.equal(qkv[:, :, H:], before[:, :, H:]) and torch.equal(q[1, L - 5:], before[1, L - 5:L, :H])
+    c.out = q.clone()
+    c.out[1, L - 5:] = 7
+    c.check("in place", call=False)
+
+
+def test_blocks_without_keys_replayed():
+    """Captured, with lengths that change between the replays."""
+    L = 4096
+    c = Case(2, L, 400, 64, 64, 64, FP16, lens=([L, L], [400, 0]), seed=4)
+    c.call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.call()
+    for keys in ([400, 0], [0, 17], [0, 0], [1, 400]):
+        c.kw["key_lens"].copy_(ints(keys))
+        c.docs = [[(0, L, 0, n, 0)] for n in keys]
+        c.out.fill_(7)
+        c.lse.fill_(7)
+        g.replay()
+        dt.dt_poll_ops()
+        c.check(keys, call=False)
