@@ -479,7 +479,8 @@ dt_status dt_adapter_linear(const dt_adapter_config *cfg, const void *x_dev, con
  *     LSE_i = log sum_j exp(x_ij),   OUT_i = sum_j exp(x_ij - LSE_i) v_j
  * over the document's keys j; causal: those with j <= p_i, and the document's first prefix_lens[b][d] keys.  A row without keys has
  * OUT = 0 and LSE = -inf; rows of q in no document are left as they were.  What stands in K and V at keys that do not count for a
- * row (other documents', later ones, padding; NaN and infinities too) has no effect on it.
+ * row (other documents', later ones, padding; NaN and infinities too) has no effect on it.  A capped logit is within 2^-20 of itself,
+ * however large the cap; with a cap, a row's last bits may depend on whether other rows' logits come near it.
  *   q, out          device [B, Lq, H, D]; out may be q (same strides), out's rows may not overlap
  *   k, v            device [B, Lk, H_kv, D], strides of their own; query head h reads key head h / (H / H_kv)
  *   q_starts, k_starts        device, int32 [B][docs + 1], or both NULL with docs = 0

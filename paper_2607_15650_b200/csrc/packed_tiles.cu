@@ -19,7 +19,7 @@
 // does (never, in earnest).
 //
 // Capped logits: tanh(y) = y P(y^2), evaluated on the FMA pipe in pairs, where all of a warp's rows stay below 0.9 of the cap in a tile;
-// 1 - 2 / (1 + e^2y) with its two further MUFU operations a logit otherwise.  The maximum is taken of the products, so that the polynomial
+// otherwise that or, with two further MUFU operations a logit, 1 - 2 / (1 + e^2y), by each logit's place.  The maximum is taken of the products, so that the polynomial
 // (FMA pipe) of some columns runs beside the exponentials (MUFU) of others.  What runs in earnest is one path: with a second polynomial for
 // some tiles, warps waited for instructions three times as long as they issued them.
 // Slopes: beyond the diagonal's tiles a bias is linear in the column: eight values per row and a step for every eight columns.
@@ -206,15 +206,10 @@ __device__ __noinline__ void add_broken(uint32_t o_tmem, const uint16_t *v, long
     tmem_wait_st();
 }
 
-// tanh(y) / y as a polynomial in z = y^2, 1 at 0 and elsewhere fitted so that tanh's largest error on |y| <= 0.9 is least: 1.5e-7 in fp32.
-// Odd degree with a negative leading term: +infinity comes out as -infinity, which is how keys that do not count are left out.
-constexpr float TANH_REACH = 0.9f;
-constexpr int TANH_WORDS = 7;   // scale / cap, and the coefficients times the cap in base 2
-__device__ __forceinline__ float tanh_word(const PackedParams &p, int i) {
-    constexpr float C[] = {0.f, -0.0035873405f, 0.01780440898f, -0.05235944574f, 0.1330328763f, -0.3333134449f, 1.f};
-    return i == 0 ? p.cap_in : p.cap_log2 * C[i];
-}
-// A pair of products as capped logits in base 2 plus `add`, within TANH_REACH of the cap; or anywhere, by exponential and division.
+constexpr int TANH_WORDS = TANH_DEGREE + 2;   // scale / cap, and the coefficients times the cap in base 2
+__device__ __forceinline__ float tanh_word(const PackedParams &p, int i) { return i == 0 ? p.cap_in : p.cap_log2 * tanh_coefficient(i - 1); }
+// A pair of products as capped logits in base 2 plus `add`, within TANH_REACH of the cap; or anywhere, where each goes its own way.
+// (The leading term of the polynomial's odd degree is negative, so that +infinity comes out as -infinity: keys that do not count are left out that way.)
 __device__ __forceinline__ float2 capped_near(const float2 (&c)[TANH_WORDS], float2 x, float2 add) {
     const float2 y = __fmul2_rn(x, c[0]), z = __fmul2_rn(y, y);
     float2 r = c[1];
@@ -222,8 +217,9 @@ __device__ __forceinline__ float2 capped_near(const float2 (&c)[TANH_WORDS], flo
     for (int i = 2; i < TANH_WORDS; ++i) r = __ffma2_rn(r, z, c[i]);
     return __ffma2_rn(y, r, add);
 }
-__device__ __forceinline__ float2 capped_any(const PackedParams &p, float2 x) {
-    return make_float2(capped(x.x * p.cap_in, p.cap_log2), capped(x.y * p.cap_in, p.cap_log2));
+__device__ __forceinline__ float2 capped_any(const PackedParams &p, const float2 (&c)[TANH_WORDS], float2 x) {
+    const float2 y = __fmul2_rn(x, c[0]), near = capped_near(c, x, make_float2(0.f, 0.f));
+    return make_float2(fabsf(y.x) <= TANH_REACH ? near.x : capped_far(y.x, p.cap_log2), fabsf(y.y) <= TANH_REACH ? near.y : capped_far(y.y, p.cap_log2));
 }
 
 template <int D, bool FP16, bool CAP, int BIAS>
@@ -817,7 +813,7 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                         for (int c = 0; c < 128; c += 2) put(c, capped_near(cap_c, pair(c), make_float2(0.f, 0.f)));
                     } else {
 #pragma unroll
-                        for (int c = 0; c < 128; c += 2) put(c, capped_any(p.c, pair(c)));
+                        for (int c = 0; c < 128; c += 2) put(c, capped_any(p.c, cap_c, pair(c)));
                     }
                     factor = 1.f;
                 }

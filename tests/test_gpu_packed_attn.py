@@ -379,3 +379,32 @@ def test_blocks_without_keys_replayed():
         g.replay()
         dt.dt_poll_ops()
         c.check(keys, call=False)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("L,H,D", [(1, 2, 128), (3, 8, 64), (300, 40, 64), (300, 40, 128)])
+@pytest.mark.parametrize("cap", [1e4, 1e6, 1e9, 1e20])
+def test_caps_far_above_the_logits(cap, L, H, D, dtype):
+    """A capped logit is off by a part of itself (2^-20), not of the cap; also beside a row whose logits come near the cap."""
+    q, k, v = rnd((1, L, H, D), 1, dtype, 1.5), rnd((1, 600, H, D), 2, dtype, 1.5), rnd((1, 600, H, D), 3, dtype)
+    scale, docs = 4 * D ** -0.5, [[(0, L, 0, 600, 0)]]
+    table = rnd((H, 65), 4, FP32)
+    for kw, extra in ((dict(), dict()), (dict(bias_table=table), dict(table=table))):
+        o, l, _, _, _ = ref.attention(q, k, v, scale, docs, softcap=cap, **extra)
+        # (so far below the cap the weights are those without one, and so is what the other roundings may do)
+        _, _, tol, tol_l, _ = ref.attention(q, k, v, scale, docs, **extra)
+        x = torch.einsum("blhd,bkhd->bhlk", q.double(), k.double()).abs().amax(-1) * scale
+        tol_l = tol_l + 2.0 ** -20 * x
+        tol = tol + 2 * 2.0 ** -20 * x.transpose(1, 2)[..., None] * v.double().abs().amax()
+        out, lse = torch.empty_like(q), torch.empty((1, H, L), device="cuda")
+        dt.dt_packed_attn(q, k, v, out, scale, softcap=cap, lse_out=lse, **kw)
+        check(out, o, tol, "out")
+        check(lse, l, tol_l, "lse")
+        if cap == 1e4 and L > 1:
+            near = q.clone()
+            near[0, 1] = (near[0, 1].double() * (cap / x[0, :, 1, None])).to(dtype)
+            dt.dt_packed_attn(near, k, v, out, scale, softcap=cap, lse_out=lse, **kw)
+            rest = [i for i in range(L) if i != 1]
+            check(out[:, rest], o[:, rest], tol[:, rest], "out beside")
+            check(lse[:, :, rest], l[:, :, rest], tol_l[:, :, rest], "lse beside")
+            assert torch.isfinite(out).all() and torch.isfinite(lse).all()
