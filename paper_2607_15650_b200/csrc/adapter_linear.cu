@@ -15,7 +15,6 @@
 #include <cmath>
 
 #include "adapter_linear.h"
-#include "tile_wait.cuh"
 
 namespace dt {
 namespace {
@@ -48,7 +47,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) shrink_rows_kernel(const Adapter
     wait_for_previous();
     let_next_start();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, m = blockIdx.y, j = blockIdx.x * (ROWS_WARPS / DOT_WARPS) + warp / DOT_WARPS;
-    const int a = adapter_of_row(p, m);
+    const int a = adapter_of_row<true>(p, m);
     if (a < 0) return;   // (alike for the whole block)
     const uint16_t *x = p.x + m * p.xs, *row = p.a + ((long long)a * p.rank + j) * p.K;
     constexpr int STEP = DOT_WARPS * 256, AHEAD = 5;
@@ -58,8 +57,8 @@ __global__ void __launch_bounds__(ROWS_THREADS) shrink_rows_kernel(const Adapter
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             const bool in = k + i * STEP < p.K;
-            u[i] = in ? __ldg(reinterpret_cast<const uint4 *>(row + k + i * STEP)) : make_uint4(0, 0, 0, 0);
-            v[i] = in ? __ldg(reinterpret_cast<const uint4 *>(x + k + i * STEP)) : make_uint4(0, 0, 0, 0);
+            u[i] = in ? *reinterpret_cast<const uint4 *>(row + k + i * STEP) : make_uint4(0, 0, 0, 0);
+            v[i] = in ? *reinterpret_cast<const uint4 *>(x + k + i * STEP) : make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) acc[i] = dot8<FP16>(u[i], v[i], acc[i]);
@@ -71,7 +70,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) shrink_rows_kernel(const Adapter
     __syncthreads();
     if (warp % DOT_WARPS == 0 && lane == 0) {
         sum = (sums[warp] + sums[warp + 1]) + (sums[warp + 2] + sums[warp + 3]);
-        static_cast<float *>(p.t)[(long long)m * p.rank16 + j] = sum * (p.scales ? __ldg(p.scales + a) : 1.0f);
+        static_cast<float *>(p.t)[(long long)m * p.rank16 + j] = sum * (p.scales ? p.scales[a] : 1.0f);
     }
 }
 
@@ -118,7 +117,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) shrink_blocks_kernel(const Adapt
         for (int i = 0; i < BATCH; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                v[i][r] = k + i * CHUNK < to && live[r] ? __ldg(reinterpret_cast<const uint4 *>(src[r] + k + i * CHUNK)) : make_uint4(0, 0, 0, 0);
+                v[i][r] = k + i * CHUNK < to && live[r] ? *reinterpret_cast<const uint4 *>(src[r] + k + i * CHUNK) : make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < BATCH; ++i)
 #pragma unroll
@@ -138,7 +137,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) shrink_blocks_kernel(const Adapt
 #pragma unroll
     for (int w = 0; w < ROWS_WARPS; ++w) sum += part[w][r][c];
     // (columns beyond the rank are 0, whatever x holds)
-    sum = j0 + c < p.rank ? sum * (p.scales ? __ldg(p.scales + piece.adapter) : 1.0f) : 0.f;
+    sum = j0 + c < p.rank ? sum * (p.scales ? p.scales[piece.adapter] : 1.0f) : 0.f;
     static_cast<uint16_t *>(p.t)[(long long)row * p.rank16 + j0 + c] = (uint16_t)pack_half2<FP16>(sum, 0.f);
 }
 
@@ -171,13 +170,13 @@ __global__ void __launch_bounds__(ROWS_THREADS + MORE_WARPS * 32) adapter_rows_k
             for (int i = 0; i < BATCH; ++i) {
                 const int at = k + i * CHUNK;
                 const bool in = at < to;
-                u[i] = in && low ? __ldcs(reinterpret_cast<const uint4 *>(w0 + at)) : none;
-                v[i] = in && high ? __ldcs(reinterpret_cast<const uint4 *>(w1 + at)) : none;
+                u[i] = in && low ? load_once(reinterpret_cast<const uint4 *>(w0 + at)) : none;
+                v[i] = in && high ? load_once(reinterpret_cast<const uint4 *>(w1 + at)) : none;
             }
 #pragma unroll
             for (int i = 0; i < BATCH; ++i)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) x[i][n] = k + i * CHUNK < to && live[n] ? __ldg(reinterpret_cast<const uint4 *>(xr[n] + k + i * CHUNK)) : none;
+                for (int n = 0; n < NT; ++n) x[i][n] = k + i * CHUNK < to && live[n] ? load_shared_by_blocks(reinterpret_cast<const uint4 *>(xr[n] + k + i * CHUNK)) : none;
 #pragma unroll
             for (int i = 0; i < BATCH; ++i)
 #pragma unroll
@@ -195,15 +194,16 @@ __global__ void __launch_bounds__(ROWS_THREADS + MORE_WARPS * 32) adapter_rows_k
         const int n = n0 + (lane & 15);
         int a[2 * NT];
 #pragma unroll
-        for (int i = 0; i < 2 * NT; ++i) a[i] = 4 * i + warp - ROWS_WARPS < p.M ? adapter_of_row(p, 4 * i + warp - ROWS_WARPS) : -1;
+        for (int i = 0; i < 2 * NT; ++i) a[i] = 4 * i + warp - ROWS_WARPS < p.M ? adapter_of_row<false>(p, 4 * i + warp - ROWS_WARPS) : -1;
         // (B's rows on their way before t is there)
 #pragma unroll
         for (int i = 0; i < 2 * NT; ++i)
             if (a[i] >= 0 && n < p.N) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.b + ((long long)a[i] * p.N + n) * p.rank + (lane >> 4) * (p.rank / 16 * 8)));
         wait_for_previous();
         // lanes 0-15 and 16-31: the even and odd pieces of 8 of the rank
+        float sums[2 * NT];
 #pragma unroll
-        for (int i = 0; i < 2 * NT; ++i) {
+        for (int i = 0; i < 2 * NT; ++i) {   // (all rows' loads ahead of the first shuffle)
             const int m = 4 * i + warp - ROWS_WARPS;
             float sum = 0.f;
             if (a[i] >= 0 && n < p.N) {
@@ -211,9 +211,8 @@ __global__ void __launch_bounds__(ROWS_THREADS + MORE_WARPS * 32) adapter_rows_k
                 const float *tr = static_cast<const float *>(p.t) + (long long)m * p.rank16;
 #pragma unroll 4
                 for (int j = 8 * (lane >> 4); j < p.rank; j += 16) {
-                    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(b + j));
-                    // (t was written beside this kernel: from L2)
-                    const float4 t0 = __ldcg(reinterpret_cast<const float4 *>(tr + j)), t1 = __ldcg(reinterpret_cast<const float4 *>(tr + j + 4));
+                    const uint4 v = *reinterpret_cast<const uint4 *>(b + j);
+                    const float4 t0 = *reinterpret_cast<const float4 *>(tr + j), t1 = *reinterpret_cast<const float4 *>(tr + j + 4);
                     float2 q = widen<FP16>(v.x);
                     sum = fmaf(q.x, t0.x, sum); sum = fmaf(q.y, t0.y, sum);
                     q = widen<FP16>(v.y);
@@ -224,8 +223,12 @@ __global__ void __launch_bounds__(ROWS_THREADS + MORE_WARPS * 32) adapter_rows_k
                     sum = fmaf(q.x, t1.z, sum); sum = fmaf(q.y, t1.w, sum);
                 }
             }
-            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 16);
-            if (lane < 16) part[ROWS_WARPS][m][lane] = sum;
+            sums[i] = sum;
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * NT; ++i) {
+            sums[i] += __shfl_xor_sync(0xFFFFFFFFu, sums[i], 16);
+            if (lane < 16) part[ROWS_WARPS][4 * i + warp - ROWS_WARPS][lane] = sums[i];
         }
     }
     __syncthreads();
@@ -237,8 +240,8 @@ __global__ void __launch_bounds__(ROWS_THREADS + MORE_WARPS * 32) adapter_rows_k
 #pragma unroll
         for (int w = 0; w < ROWS_WARPS; ++w) sum += part[w][m][o & 15];
         if (p.segments) sum += part[ROWS_WARPS][m][o & 15];
-        if (p.bias) sum += p.bias_fp32 ? __ldg(static_cast<const float *>(p.bias) + n)
-                                       : widen<FP16>(__ldg(static_cast<const uint16_t *>(p.bias) + n)).x;
+        if (p.bias) sum += p.bias_fp32 ? load_l2(static_cast<const float *>(p.bias) + n)
+                                       : widen<FP16>(load_l2(static_cast<const uint16_t *>(p.bias) + n)).x;
         p.y[m * p.ys + n] = (uint16_t)pack_half2<FP16>(sum, 0.f);
     }
 }

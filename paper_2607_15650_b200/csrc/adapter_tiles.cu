@@ -14,7 +14,6 @@
 // 5120 x 5120 26.2 (20.5), 1807 x 4096 x 5120 60 (54), 32760 x 1536 x 1536 107 (104), 75600 x 5120 x 5120 2720 to 2940 (2550 to 2900, power-capped); with
 // adapters of rank 16 to 64: 8.2, 26.5, 30.2, 70, 125, 2590 to 2670.
 #include "adapter_linear.h"
-#include "tile_wait.cuh"
 
 namespace dt {
 namespace {
@@ -103,7 +102,7 @@ shrink_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         if (!ok) give_up(abort_ptr, p.status);
     }
     __syncwarp();
-    const float scale = p.scales ? __ldg(p.scales + piece.adapter) : 1.0f;
+    const float scale = p.scales ? p.scales[piece.adapter] : 1.0f;
     uint16_t *t = static_cast<uint16_t *>(p.t);
     float *sums = reinterpret_cast<float *>(smem_raw + (base - smem_u32(smem_raw)));   // SPLIT: [row][rank16 + 4]
     const int pitch = p.rank16 + 4;
@@ -218,16 +217,16 @@ __device__ __forceinline__ void tile_at(const LinearShape &sh, int w, int &mi, i
 
 __device__ __forceinline__ void prefetch_map(const CUtensorMap *m) { asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory"); }
 
-// f[0..COUNT) += bias[col..col + COUNT)
+// f[0..COUNT) += bias[col..col + COUNT), behind the kernel's own wait for the launch before
 template <bool FP16, int COUNT>
 __device__ __forceinline__ void add_bias(const AdapterParams &p, int col, float (&f)[COUNT]) {
     if (p.bias_fp32) {
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) f[i] += __ldg(static_cast<const float *>(p.bias) + col + i);
+        for (int i = 0; i < COUNT; ++i) f[i] += static_cast<const float *>(p.bias)[col + i];
     } else {
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
-            const uint32_t h = __ldg(static_cast<const uint16_t *>(p.bias) + col + i);
+            const uint32_t h = static_cast<const uint16_t *>(p.bias)[col + i];
             float b;
             if constexpr (FP16) asm("{\n\t.reg .b16 h;\n\tcvt.u16.u32 h, %1;\n\tcvt.f32.f16 %0, h;\n\t}" : "=f"(b) : "r"(h));
             else b = __uint_as_float(h << 16);
@@ -418,6 +417,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             if (!ok) give_up(abort_ptr, p.status);
         }
     } else {
+        if (p.bias != nullptr) wait_for_previous();   // (t is made by the time that the first tile is)
         const int quarter = warp % 4, side = (warp - 2) / 4;   // this warp's rows; which of every two pieces of columns it has
         const uint32_t lane_addr = ((uint32_t)(quarter * 32)) << 16;
         uint32_t n = 0;

@@ -89,7 +89,7 @@ struct RowBias {
 template <int BIAS>
 __device__ __forceinline__ RowBias row_bias(const PackedParams &p, int head, int place) {
     RowBias r = {place, 0.f, nullptr};
-    if constexpr (BIAS == BIAS_SLOPES) r.slope_log2 = __ldg(p.slopes + head) * LOG2E;
+    if constexpr (BIAS == BIAS_SLOPES) r.slope_log2 = p.slopes[head] * LOG2E;
     if constexpr (BIAS == BIAS_TABLE) r.table = p.table + (long long)head * (2 * p.far + 1) + p.far;
     return r;
 }
@@ -98,7 +98,7 @@ template <bool CAP, int BIAS>
 __device__ __forceinline__ float logit(const PackedParams &p, float s, const RowBias &r, int key) {
     float x = CAP ? capped(s * p.cap_in, p.cap_log2) : s * p.scale_log2;
     if constexpr (BIAS == BIAS_SLOPES) x = fmaf(-r.slope_log2, fabsf((float)(key - r.place)), x);
-    if constexpr (BIAS == BIAS_TABLE) x = fmaf(__ldg(r.table + min(max(key - r.place, -p.far), p.far)), LOG2E, x);
+    if constexpr (BIAS == BIAS_TABLE) x = fmaf(r.table[min(max(key - r.place, -p.far), p.far)], LOG2E, x);
     return x;
 }
 

@@ -23,7 +23,7 @@ struct PackedParams {
 
 // A document: its queries and keys, the key at which query i stands (i + shift), the end of its prefix.
 struct Doc { int q0, q1, k0, k1, shift, prefix_end; };
-__device__ __forceinline__ int clamped(const int32_t *at, int most) { return min(max(__ldg(at), 0), most); }
+__device__ __forceinline__ int clamped(const int32_t *at, int most) { return min(max(*at, 0), most); }
 __device__ __forceinline__ Doc doc_of(const PackedParams &p, int b, int d) {
     Doc r;
     if (p.q_starts != nullptr) {

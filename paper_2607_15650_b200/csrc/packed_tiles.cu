@@ -196,7 +196,7 @@ __device__ __noinline__ void add_broken(uint32_t o_tmem, const uint16_t *v, long
         for (int key = from; key < to; ++key) {
 #pragma unroll
             for (int c = 0; c < 32; ++c) {
-                const float x = value_of<FP16>(__ldg(v + key * stride + c0 + c));
+                const float x = value_of<FP16>(v[key * stride + c0 + c]);
                 if (!(fabsf(x) < INFINITY)) o[c] = __float_as_uint(__uint_as_float(o[c]) + x);
             }
         }
@@ -540,8 +540,8 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                     const int count = 2 * p.c.far + 1;
 #pragma unroll 9
                     for (int i = lane; i < count; i += 32)
-                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(dst + (TABLE_PAD + i) * 4), "f"(__ldg(src + i) * LOG2E) : "memory");
-                    const float low = __ldg(src) * LOG2E, high = __ldg(src + count - 1) * LOG2E;
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(dst + (TABLE_PAD + i) * 4), "f"(src[i] * LOG2E) : "memory");
+                    const float low = src[0] * LOG2E, high = src[count - 1] * LOG2E;
 #pragma unroll 4
                     for (int i = lane; i < TABLE_PAD; i += 32) {
                         asm volatile("st.shared.f32 [%0], %1;" ::"r"(dst + i * 4), "f"(low) : "memory");
@@ -755,7 +755,7 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             float m_used = -INFINITY, l_sum = 0.f;
             const int tile_place = place - row_in_tile;   // of the tile's first row
             float slope = 0.f;
-            if constexpr (BIAS == BIAS_SLOPES) slope = __ldg(p.c.slopes + head) * LOG2E;
+            if constexpr (BIAS == BIAS_SLOPES) slope = p.c.slopes[head] * LOG2E;
             uint32_t tab = 0;   // of distance 0
             if constexpr (BIAS == BIAS_TABLE) {
                 tab = tab_smem + (tables & 1u) * TABLE_BYTES + (p.c.far + TABLE_PAD) * 4;

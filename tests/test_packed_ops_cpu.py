@@ -2,6 +2,8 @@
 device, the entry points look at their tensors.  No GPU needed."""
 import ctypes as C
 import math
+import os
+import re
 
 import pytest
 import torch
@@ -120,3 +122,17 @@ def test_tensors_of_other_classes_are_seen_alike(lib):
     want = dt._norm_rows([base])
     assert want == (4, 4, [(240, 40)])
     assert dt._norm_rows([base.as_subclass(Sub)]) == want and dt._norm_rows([torch.nn.Parameter(base)]) == want
+
+
+def test_kernels_that_begin_early_promise_nothing_about_what_they_read():
+    """A kernel that is resident while the launch before may still write reads nothing by ld.global.nc (__ldg), and by no cached-load
+    intrinsic that the compiler may move ahead of the wait."""
+    csrc = os.path.join(os.path.dirname(build.__file__), "csrc")
+    early = set()
+    for f in sorted(os.listdir(csrc)):
+        if f.endswith((".cu", ".cuh", ".h")):
+            text = re.sub(r"//.*", "", open(os.path.join(csrc, f)).read())
+            if re.search(r"wait_for_previous\(\)|AdapterParams|PackedParams", text):
+                early.add(f)
+                assert not re.search(r"\b__ld(g|cg|cs|ca|lu|cv)\s*\(|ld\.global\.nc|__restrict__", text), f
+    assert early >= {"adapter_linear.cu", "adapter_linear.h", "adapter_tiles.cu", "packed_attn.cu", "packed_attn.h", "packed_tiles.cu", "tile_wait.cuh"}
