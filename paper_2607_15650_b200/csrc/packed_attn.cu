@@ -518,7 +518,7 @@ extern "C" dt_status dt_packed_attn(const dt_packed_config *cfg, const void *q_d
     const long long items = (long long)c.B * c.H * ((c.Lq + 255) / 256);
     const long long steps = (items + dev->sms - 1) / dev->sms * tiles;
     cudaError_t e;
-    if (c.Lk > 0 && few_blocks * tiles > steps * (c.D == 64 ? 290 : 200)) e = launch_packed_tiles(p, c.D, fp16, *dev, st);
+    if (c.Lk > 0 && few_blocks * tiles > steps * (c.D == 64 ? 290 : 200) && tile_blocks(p) <= MOST_TILE_BLOCKS) e = launch_packed_tiles(p, c.D, fp16, *dev, st);
     else e = c.D == 64 ? (fp16 ? launch_few<64, true>(p, *dev, st) : launch_few<64, false>(p, *dev, st))
                        : (fp16 ? launch_few<128, true>(p, *dev, st) : launch_few<128, false>(p, *dev, st));
     return e == cudaSuccess ? DT_OK : ops_fail_cuda(e, "packed-attention launch");

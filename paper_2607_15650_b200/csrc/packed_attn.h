@@ -104,7 +104,11 @@ __device__ __forceinline__ float capped(float y, float cap_log2) {
 template <bool FP16>
 __device__ __forceinline__ float packed_reference(const PackedParams &p, float top) { return FP16 ? top - p.ref_below : top; }
 
-// Many query rows (Lk > 0): tensor-memory tiles.
+// Many query rows (Lk > 0): tensor-memory tiles, for up to MOST_TILE_BLOCKS numbers of blocks of TILE_BLOCK rows in all.  A CTA that meets
+// numbers without rows goes through them one by one, while its other warps' bounded waits run: 2^24 of them take 148 CTAs 140 ms (the few-row kernel 3 ms).
+constexpr int TILE_BLOCK = 256;
+constexpr long long MOST_TILE_BLOCKS = 1 << 24;
+inline long long tile_blocks(const PackedParams &p) { return (long long)p.B * p.H * blocks_of(p.Lq, p.docs, TILE_BLOCK, p.q_starts != nullptr); }
 cudaError_t launch_packed_tiles(const PackedParams &p, int D, bool fp16, const OpsDevice &dev, cudaStream_t st);
 
 }  // namespace dt

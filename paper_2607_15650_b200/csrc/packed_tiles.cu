@@ -41,6 +41,7 @@ namespace dt {
 namespace {
 
 constexpr int NQ = 2, TILE = 128, ITEM_ROWS = NQ * TILE;   // query tiles in flight; rows of a query tile, keys of a K/V tile
+static_assert(ITEM_ROWS == TILE_BLOCK, "a block's rows");
 constexpr int SOFTMAX_THREADS = NQ * 128;
 constexpr int TMA_WARP = SOFTMAX_THREADS / 32, MMA_WARP = TMA_WARP + 1, MEND_WARP = TMA_WARP + 3, OUT_WARP = TMA_WARP + 4;
 constexpr int THREADS = SOFTMAX_THREADS + 256;
@@ -96,7 +97,6 @@ struct TileParams {
     PackedParams c;
     MapCoord mq, mk, mv;
     int blocks;              // numbers of blocks of 256 rows in a row of the batch
-    int items;               // B * blocks * H
 };
 
 // The stream of a CTA's tiles goes over its items, K and V in the order K_0, K_1, V_0, K_2, V_1, ..., K_n, V_{n-1}, ..., V_last, across items.
@@ -1002,10 +1002,7 @@ cudaError_t launch_packed_tiles(const PackedParams &c, int D, bool fp16, const O
     TileParams p = {};
     p.c = c;
     p.blocks = blocks_of(c.Lq, c.docs, ITEM_ROWS, c.q_starts != nullptr);
-    const long long items = (long long)c.B * c.H * p.blocks;
-    if (items > 0x3FFFFFFF) return cudaErrorInvalidValue;
-    p.items = (int)items;
-    const int grid = p.items;
+    const int grid = (int)tile_blocks(c);
     CUtensorMap tq, tk, tv;
     if (!encode(dev.encode_tiled, &tq, &p.mq, c.q, c.qs, c.B, c.Lq, c.H, D, fp16) ||
         !encode(dev.encode_tiled, &tk, &p.mk, c.k, c.ks, c.B, c.Lk, c.Hkv, D, fp16) ||

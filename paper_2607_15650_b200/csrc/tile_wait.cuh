@@ -7,7 +7,7 @@
 
 namespace dt {
 
-// No wait of these kernels is for more than one item's loads and MMAs; well within the 4.3 s after which the timer's low word wraps.
+// No wait of these kernels is for more than one item's loads and MMAs, or the look-up of the next one (see MOST_TILE_BLOCKS); well within the 4.3 s after which the timer's low word wraps.
 constexpr uint32_t TILE_WAIT_NS = 3500000000u;
 
 __device__ __forceinline__ uint32_t timer_lo_ns() {

@@ -408,3 +408,21 @@ def test_caps_far_above_the_logits(cap, L, H, D, dtype):
             check(out[:, rest], o[:, rest], tol[:, rest], "out beside")
             check(lse[:, :, rest], l[:, :, rest], tol_l[:, :, rest], "lse beside")
             assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+
+
+def test_very_many_documents_of_very_many_heads():
+    """Nearly all of them without rows: as many numbers of blocks of 256 rows as tiles go through, and more, which few-row blocks take."""
+    docs = 65535
+    for H, Hk, Lq in ((256, 256, 512), (8192, 512, 64), (16384, 1024, 64)):
+        at = [0] * 3 + [Lq // 3] * (docs - 5) + [Lq // 2] * 2 + [Lq - 1]
+        assert len(at) == docs + 1
+        q, k, v = rnd((1, Lq, H, 64), 1, BF16, 1.3), rnd((1, Lq, Hk, 64), 2, BF16, 1.3), rnd((1, Lq, Hk, 64), 3, BF16)
+        out, lse = torch.full_like(q, 7), torch.full((1, H, Lq), 7.0, device="cuda")
+        dt.dt_packed_attn(q, k, v, out, 0.125, q_starts=ints([at]), k_starts=ints([at]), lse_out=lse)
+        dt.dt_poll_ops()
+        heads = torch.arange(0, H, max(1, H // 32), device="cuda")      # of 32 heads
+        some = [[(a, b, a, b, 0) for a, b in zip(at, at[1:]) if b > a]]
+        o, l, tol, tol_l, rows = ref.attention(q[:, :, heads], k[:, :, heads // (H // Hk)], v[:, :, heads // (H // Hk)], 0.125, some)
+        check(out[:, :, heads][rows], o[rows], tol[rows], "out")
+        check(lse[:, heads][:, :, rows[0]], l[:, :, rows[0]], tol_l[:, :, rows[0]], "lse")
+        assert (out[:, Lq - 1:] == 7).all() and (lse[:, :, Lq - 1:] == 7).all()
