@@ -226,12 +226,12 @@ _OPS = ("dt_rope", "dt_add_rmsnorm", "dt_cross_attn", "dt_adapter_linear", "dt_p
 def _load_ops():
     L = lib()
     if not os.path.exists(OPS_PATH):
-        raise ImportError(f"{OPS_PATH} is missing: run `python -m paper_2607_15650_b200.build` (a C compiler and Python's headers)")
+        raise ImportError(f"{OPS_PATH} is missing: run `python -m paper_2607_15650_b200.build` (a C and C++ compiler, Python's and torch's headers)")
     spec = importlib.util.spec_from_file_location("_ditango_ops", OPS_PATH)
     ops = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(ops)
-    if ops.torch_version != torch.__version__.split("+")[0]:
-        raise ImportError(f"{OPS_PATH} is built for torch {ops.torch_version}: run `python -m paper_2607_15650_b200.build --force`")
+    if ops.torch_version != str(torch.__version__):
+        raise ImportError(f"{OPS_PATH} is built for torch {ops.torch_version}, not {torch.__version__}: run `python -m paper_2607_15650_b200.build`")
 
     def on_device(index, name, args, kw):
         with torch.cuda.device(index):

@@ -5,13 +5,14 @@
 nvcc cross-compiles without a GPU.  The library links the static CUDA runtime and resolves the
 one driver entry point it needs (tensor-map encoding) at run time, so it has no link-time
 dependency on libcuda.  The Python entry points of the context-free operators are a module of
-their own, which needs a C and C++ compiler and Python's and torch's headers; without the compiler or Python's headers the library is
-built alone.
+their own, which needs a C and C++ compiler and Python's and torch's headers (with CUDA); without one of them the library is built
+alone.  It is built for one torch, and anew when that is another.
 """
 from __future__ import annotations
 
 import importlib.util
 import os
+import re
 import shlex
 import shutil
 import subprocess
@@ -29,6 +30,7 @@ HEADERS = ["dt_internal.h", "ops.h", "cross_attn.h", "adapter_linear.h", "packed
 # Python entry points of the context-free operators, for this interpreter
 OPS_LIB = os.path.join(HERE, "_ditango_ops" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 OPS_SOURCE, OPS_TENSOR = "ops_py.c", "ops_tensor.cpp"      # (the second against torch's headers)
+OPS_LIBS = ("torch_python", "torch_cpu", "c10_cuda", "c10")       # of torch
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 
@@ -39,19 +41,53 @@ def _stale(lib=LIB, files=SOURCES + HEADERS) -> bool:
     return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in files)
 
 
+def _torch():
+    """(torch's folder, its whole version), without importing it; (None, None) where there is none."""
+    spec = importlib.util.find_spec("torch")
+    for folder in (spec.submodule_search_locations or [] if spec else []):
+        at = os.path.join(folder, "version.py")
+        if os.path.exists(at):
+            with open(at) as f:
+                found = re.search(r"^__version__\s*=\s*['\"]([^'\"]+)", f.read(), re.M)
+            if found:
+                return folder, found[1]
+    return None, None
+
+
+def _built_for():
+    """The version of torch that the module of Python entry points is built for, as left beside it; None where there is none."""
+    try:
+        with open(OPS_LIB + ".torch") as f:
+            return f.read()
+    except OSError:
+        return None
+
+
 def _build_ops(force: bool) -> None:
-    if not force and not _stale(OPS_LIB, [OPS_SOURCE, OPS_TENSOR, "ops_tensor.h", HEADERS[-1]]):
+    torch, version = _torch()
+    if not force and _built_for() == version and not _stale(OPS_LIB, [OPS_SOURCE, OPS_TENSOR, "ops_tensor.h", HEADERS[-1]]):
         return
     cc, include = shlex.split(os.environ.get("CC") or "gcc"), sysconfig.get_paths()["include"]
-    if shutil.which(cc[0]) is None or not os.path.exists(os.path.join(include, "Python.h")):
-        warnings.warn(f"no Python entry points of the context-free operators: {cc[0]} or {include}/Python.h is missing")
+    cuda = os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include")
+    missing = [] if shutil.which(cc[0]) else [cc[0]]
+    needed = [os.path.join(include, "Python.h")]
+    if torch is None:
+        missing.append("torch")
+    else:
+        needed += [os.path.join(torch, "include", *f.split("/")) for f in ("torch/csrc/autograd/python_variable.h", "c10/cuda/CUDAStream.h")]
+        needed += [os.path.join(torch, "lib", f"lib{n}.so") for n in OPS_LIBS] + [os.path.join(cuda, "cuda_runtime_api.h")]
+    missing += [f for f in needed if not os.path.exists(f)]
+    if missing:
+        warnings.warn(f"no Python entry points of the context-free operators: {', '.join(missing)} missing")
         return
-    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
     tmp = OPS_LIB + f".tmp{os.getpid()}"
-    subprocess.run([*cc, "-O2", "-shared", "-fPIC", "-Wall", "-I" + include, "-I" + os.path.join(torch, "include"),
-                    "-I" + os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include"), "-o", tmp, os.path.join(CSRC, OPS_SOURCE),
-                    os.path.join(CSRC, OPS_TENSOR), "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10", "-lstdc++"], check=True)
+    subprocess.run([*cc, "-O2", "-shared", "-fPIC", "-Wall", "-I" + include, "-I" + os.path.join(torch, "include"), "-I" + cuda,
+                    f'-DBUILT_FOR_TORCH="{version}"', "-o", tmp, os.path.join(CSRC, OPS_SOURCE), os.path.join(CSRC, OPS_TENSOR),
+                    "-L" + os.path.join(torch, "lib"), *("-l" + n for n in OPS_LIBS), "-lstdc++"], check=True)
     os.replace(tmp, OPS_LIB)
+    with open(tmp, "w") as f:
+        f.write(version)
+    os.replace(tmp, OPS_LIB + ".torch")
 
 
 def _build_lib(force: bool, verbose: bool) -> None:

@@ -3,7 +3,6 @@
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
-#include <torch/headeronly/version.h>
 
 #include <cstdint>
 
@@ -40,7 +39,7 @@ int guarded(F &&f) {   // no C++ exception leaves through C
 
 }  // namespace
 
-const char *const tensor_torch_version = TORCH_VERSION;
+const char *const tensor_torch_version = BUILT_FOR_TORCH;
 
 extern "C" int tensor_look(PyObject *o, Tensor *x) {
     if (!THPVariable_CheckExact(o)) return 0;

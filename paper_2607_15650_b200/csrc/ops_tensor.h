@@ -19,7 +19,7 @@ typedef struct {
 #ifdef __cplusplus
 extern "C" {
 #endif
-extern const char *const tensor_torch_version;   /* that of the headers */
+extern const char *const tensor_torch_version;   /* the whole one, of the headers */
 /* 1; 0: not of torch's own class (its Python attributes count); -1 with an error set */
 int tensor_look(PyObject *o, Tensor *x);
 /* 0, or -1 with an error set */
