@@ -805,7 +805,8 @@ packed_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
                     const bool near = __all_sync(0xFFFFFFFFu, !(largest([](float x) { return fabsf(x); }) * p.c.cap_in > TANH_REACH)) != 0;
                     if (BIAS == BIAS_NONE && near) {
                         // tanh does not change the order, so that the maximum is known before any logit is capped
-                        m_tile = capped(largest([](float x) { return x; }) * p.c.cap_in, p.c.cap_log2);
+                        m_tile = largest([](float x) { return x; });
+                        m_tile = m_tile == -INFINITY ? -p.c.cap_log2 : capped_near(cap_c, make_float2(m_tile, m_tile), make_float2(0.f, 0.f)).x;   // (-infinity: no key counts)
                         if (masked) mask(0x7F800000u);   // (+infinity: see capped_near)
                         fused = true;
                     } else if (near) {
