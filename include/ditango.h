@@ -457,7 +457,8 @@ dt_status dt_cross_attn(const dt_cross_config *cfg, const void *q_dev, const int
  *   scales_dev      device, fp32 [adapters], or NULL: 1
  *   starts_dev, adapters_of_dev   device, int32 [segments + 1] and [segments]
  *   workspace_dev   device, dt_adapter_workspace_bytes(rows, rank) bytes of any content; calls that share one are ordered, and so are
- *                   replays of graphs that do
+ *                   replays of graphs that do.  (Up to 16 rows want twice as much each: a workspace for all calls of up to n rows holds
+ *                   the larger of n rows' bytes and of min(n, 16)'s)
  * Without segments or adapters the last six are not looked at.  One launch for the projection and one, beside it, for the adapters.
  * Limits: K, N multiples of 8, at most 2^20; rank a multiple of 8, 8 to 128; rows up to 2^30, adapters 65535, segments 2^20. */
 typedef struct {

@@ -276,7 +276,8 @@ def dt_rope_grid_freqs(dims, base=10000.0):
 
 
 def dt_adapter_workspace_bytes(rows, rank):
-    """Bytes of the workspace that dt_adapter_linear wants for so many rows and adapters of that rank."""
+    """Bytes of the workspace that dt_adapter_linear wants for so many rows and adapters of that rank (up to 16 rows want twice as much
+    each: for all calls of up to n rows, the larger of n's and min(n, 16)'s)."""
     n = C.c_size_t()
     s = lib().dt_adapter_workspace_bytes(int(rows), int(rank), C.byref(n))
     if s != DT_OK:

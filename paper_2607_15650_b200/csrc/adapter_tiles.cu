@@ -1,8 +1,8 @@
 // dt_adapter_linear for many rows: tensor-memory tiles.
 //
 // shrink_kernel: t = s_a x A_a^T, a tile of 128 rows x rank per pair of (tile of rows, segment that it meets), kept in the inputs'
-// type because that is what the second product multiplies it in (its rounding, 2^-9 or 2^-11 of each t, is a rank-wide average
-// below y's own).  Bound by reading x.  Where there are few pairs, K is split over the CTAs of a cluster, which join their sums through
+// type because that is what the second product multiplies it in (its rounding, 2^-8 or 2^-11 of each t at most, is averaged over the
+// rank, and no larger than y's own).  Bound by reading x.  Where there are few pairs, K is split over the CTAs of a cluster, which join their sums through
 // shared memory; with fewer rows still, shrink_blocks_kernel (adapter_linear.cu) takes its place.
 //
 // linear_kernel: tiles of y by pairs of CTAs (256 rows), by clusters of pairs that share a tile's K, or by single CTAs (128 rows), see

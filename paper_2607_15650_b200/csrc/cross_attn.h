@@ -26,7 +26,7 @@ struct CrossParams {
 // maximum, and anew when a logit exceeds it by more than P_TOP: P <= 2^P_TOP, finite in both types.
 template <bool FP16>
 constexpr float P_TOP = FP16 ? 15.0f : 8.0f;
-// bf16 has fp32's range: every P is rounded by half a step (2^-9), and the reference stands at the maximum.  fp16's normal range
+// bf16 has fp32's range: every P is rounded by half a step (2^-8 at most), and the reference stands at the maximum.  fp16's normal range
 // ends at 2^-14, and a P under 2^-25 is zero though the sum counts it: with the reference at the maximum, 2^20 keys of
 // 2^-25.4 of the largest weight each lost their 2 % of OUT altogether.  So fp16's reference stands lower: keys down to
 // 2^-(14 + ref_below) of the largest weight are rounded by half a step (2^-11), and smaller ones are off by 2^-(25 + ref_below) of
