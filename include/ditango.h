@@ -494,7 +494,7 @@ typedef struct {
     int32_t dtype;                    /* DT_VALUE_BF16 or DT_VALUE_FP16 */
     int32_t B, Lq, Lk, H, H_kv, D;
     int32_t docs, causal, bias_far;
-    float softmax_scale, softcap;     /* softcap 0: none; else softcap and softmax_scale / softcap are normal numbers */
+    float softmax_scale, softcap;     /* up to 2^127; softcap 0: none; else softcap and softmax_scale / softcap are normal numbers */
 } dt_packed_config;
 dt_status dt_packed_attn(const dt_packed_config *cfg, const void *q_dev, const int64_t q_strides_blhd[4], const void *k_dev,
                          const int64_t k_strides_blhd[4], const void *v_dev, const int64_t v_strides_blhd[4], const int32_t *q_starts_dev,

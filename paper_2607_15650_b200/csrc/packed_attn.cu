@@ -463,6 +463,8 @@ extern "C" dt_status dt_packed_attn(const dt_packed_config *cfg, const void *q_d
     if (c.docs > 65536) return ops_fail(DT_ERR_UNSUPPORTED, "more than 65536 documents in a row");
     if (!(c.softmax_scale > 0.f) || !std::isfinite(c.softmax_scale)) return ops_fail(DT_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
     if (!(c.softcap >= 0.f) || !std::isfinite(c.softcap)) return ops_fail(DT_ERR_INVALID_ARG, "softcap must be finite and >= 0");
+    if (!std::isfinite(c.softmax_scale * LOG2E) || !std::isfinite(c.softcap * LOG2E))
+        return ops_fail(DT_ERR_INVALID_ARG, "softmax_scale and softcap must be finite in base 2 (at most 2^127)");
     // (a subnormal one could become 0, and 0 times infinity would stand where a key does not count)
     if (c.softcap > 0.f && (!std::isnormal(c.softcap) || !std::isnormal(c.softmax_scale / c.softcap)))
         return ops_fail(DT_ERR_INVALID_ARG, "softcap and softmax_scale / softcap must be normal numbers");

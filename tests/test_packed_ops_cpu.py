@@ -136,3 +136,13 @@ def test_kernels_that_begin_early_promise_nothing_about_what_they_read():
                 early.add(f)
                 assert not re.search(r"\b__ld(g|cg|cs|ca|lu|cv)\s*\(|ld\.global\.nc|__restrict__", text), f
     assert early >= {"adapter_linear.cu", "adapter_linear.h", "adapter_tiles.cu", "packed_attn.cu", "packed_attn.h", "packed_tiles.cu", "tile_wait.cuh"}
+
+
+@pytest.mark.parametrize("kw", [dict(softmax_scale=3e38), dict(softmax_scale=3.4e38, softcap=3.4e38), dict(softmax_scale=100.0, softcap=3e38)])
+def test_scales_and_caps_that_base_2_does_not_hold_are_refused(lib, kw):
+    """Logits are kept in base 2, where a factor beyond 2^127.5 is infinite and every row would be NaN."""
+    assert packed_call(lib, **kw) == INV
+    assert b"base 2" in lib.dt_last_error(None)
+    ok = {k: 2.0 ** 127 for k in kw}
+    ok["Lq"] = 0
+    assert packed_call(lib, **ok) == dt.DT_OK
